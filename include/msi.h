@@ -445,6 +445,142 @@ msi_status msi_residual_init(const uint16_t *x0_bf16, float *h, uint16_t *x_bf16
 msi_status msi_residual_add(const float *out, float *h, uint16_t *x_bf16, uint32_t rows, uint32_t cols,
                             void *stream);
 
+/* ---- Attention block of a stacked layer: projections, a bounded cache of
+ * keys and values in 8 bits, the attention that reads it and the eviction that
+ * keeps it bounded.  These calls need no plan.  They run asynchronously on
+ * `stream`, on the current HIP device, which must be the one that holds the
+ * arrays; they allocate nothing, keep nothing between calls and can be
+ * captured into a graph.  Calls on different streams are independent as long
+ * as they share no workspace and no pages that one of them writes. */
+
+typedef enum { MSI_F32 = 0, MSI_BF16 = 1 } msi_dtype;
+typedef enum { MSI_ACT_NONE = 0, MSI_ACT_SILU = 1, MSI_ACT_GELU = 2, MSI_ACT_GELU_TANH = 3 } msi_activation;
+
+/* out[m, n] = act(sum_k x[m, k] w[n, k] + bias[n]) + residual[m, n].  GELU is
+ * z Phi(z); GELU_TANH its form with tanh.  Sums, bias, activation and the
+ * residual's addition in fp32, one rounding on the way out.  Strides are
+ * elements from one row to the next; k is contiguous. */
+typedef struct {
+    const void *x;               /* [M, K] bf16, x_stride >= K, a multiple of 8       */
+    const void *w;               /* [N, K] bf16, row-major                             */
+    const float *bias;           /* [N], or NULL                                       */
+    const void *residual;        /* [M, N] in residual_dtype, or NULL; may be `out`    */
+    void *out;                   /* [M, N] in out_dtype                                */
+    uint32_t M, N, K;            /* K a multiple of 8, 8 <= K <= 2^21; M or N may be 0 */
+    uint32_t activation;         /* msi_activation                                     */
+    uint32_t residual_dtype, out_dtype;   /* msi_dtype                                 */
+    uint64_t x_stride, residual_stride, out_stride;
+} msi_linear_args;
+
+/* Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+msi_status msi_linear(const msi_linear_args *args, void *stream);
+
+/* The cache of one layer: a pool of pages with stable addresses, each 64
+ * tokens of every head, handed to sequences by the caller's page tables.  Page
+ * p, head h: 64 rows of K codes, then 64 rows of V codes, one byte an element;
+ * value = scale * code, one fp32 scale for the block's K and one for its V.
+ * Codes are OCP e4m3 (no NaN codes) or int8 in -127 .. 127.  `mass` holds each
+ * token's accumulated attention weight, by head. */
+#define MSI_KV_BLOCK 64u
+typedef enum { MSI_KV_E4M3 = 0, MSI_KV_INT8 = 1 } msi_kv_format;
+typedef struct {
+    uint32_t format;             /* msi_kv_format                                      */
+    uint32_t n_pages;            /* >= 1                                               */
+    uint32_t n_heads;            /* heads of K and V, 1 .. 256                         */
+    uint32_t head_dim;           /* 64, 128 or 256                                     */
+    void *data;                  /* [n_pages, n_heads, 2, 64, head_dim] bytes          */
+    float *scales;               /* [n_pages, n_heads, 2]: K, V                        */
+    float *mass;                 /* [n_pages, n_heads, 64], or NULL                    */
+} msi_kv_cache;
+
+/* The sequences of one call.  Sequence i has lens[i] tokens in the pages
+ * table[i, 0], table[i, 1], ... and brings the call's rows cu_rows[i] ..
+ * cu_rows[i + 1] - 1 (n of them), which stand for its last n tokens.  The
+ * arrays are on the device and read by the kernels; the host's bounds size the
+ * launches.  A sequence whose numbers break a bound is left out, with its rows
+ * of the output unwritten, and raises MSI_KV_BAD_LENGTH; a page index outside
+ * the pool raises MSI_KV_BAD_PAGE, nothing is written there, and its tokens count as absent
+ * (zeros when read).  Status words: a caller-owned device word (or NULL) into which the kernels OR what they
+ * met; the caller clears it. */
+#define MSI_KV_BAD_PAGE 1u
+#define MSI_KV_NONFINITE 2u      /* an appended element is infinite (stored as the largest code) or NaN (stored as 0) */
+#define MSI_KV_BAD_LENGTH 4u
+typedef struct {
+    uint32_t n_seqs;             /* <= 65535                                           */
+    uint32_t max_blocks;         /* row length of table                                */
+    uint32_t n_rows;             /* rows of the call's row arrays                      */
+    uint32_t max_rows;           /* bound of one sequence's rows                       */
+    uint32_t max_len;            /* bound of lens, <= 64 * max_blocks                  */
+    uint32_t reserved;
+    const int32_t *table;        /* [n_seqs, max_blocks]                               */
+    const int32_t *lens;         /* [n_seqs]                                           */
+    const int32_t *cu_rows;      /* [n_seqs + 1] ascending from 0                      */
+} msi_kv_seqs;
+
+/* Write the last n tokens of every sequence (lens already counts them): k and
+ * v are [n_rows, n_heads, head_dim] bf16, strides in elements from row to row,
+ * multiples of 8.  A block's scale is the least power of two s >= 2^-64 with
+ * |x| <= 448 s (e4m3) or 127 s (int8) over its new finite elements, or the scale it had if it held
+ * tokens and that is larger; codes are x / s rounded to nearest, ties to even; codes the block held move to a
+ * grown scale the same way.  The new tokens' mass becomes 0.  Bytes after the
+ * last token stay as they were.  No page may be written for two sequences by
+ * one call.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,
+                         uint64_t k_stride, uint64_t v_stride, uint32_t *status, void *stream);
+
+/* The last n tokens of every sequence as bf16: code * scale, exact for scales
+ * that msi_kv_append or msi_kv_evict wrote.  Arguments as msi_kv_append's. */
+msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void *k, void *v, uint64_t k_stride,
+                       uint64_t v_stride, uint32_t *status, void *stream);
+
+/* Attention of the rows over their sequences: row r of n sees the tokens up to
+ * its own, t <= len - n + r; query head a reads head a / (n_q_heads / n_heads).
+ * out = softmax(scale q k^T) v, zero for a row that sees no token (n > len is
+ * allowed here).  With mass_rows > 0, mass[t] = mass_decay * mass[t] + the sum
+ * of the probabilities that the sequence's last mass_rows rows and the head's
+ * query heads give token t, for every token (with mass_decay 0 the old value
+ * is not read).  Sums are taken in a fixed order: equal calls give equal
+ * bits.  `out` must not overlap q. */
+typedef struct {
+    const void *q;               /* [n_rows, n_q_heads, head_dim] bf16                 */
+    void *out;                   /* the same shape, bf16                               */
+    uint64_t q_stride, out_stride;   /* elements from row to row, multiples of 8       */
+    uint32_t n_q_heads;          /* a multiple of the cache's n_heads                  */
+    float scale;
+    uint32_t mass_rows;          /* 0: mass is neither read nor written                */
+    float mass_decay;
+    void *workspace;             /* msi_kv_attention_workspace bytes (NULL if 0)       */
+    uint64_t workspace_bytes;
+    uint32_t *status;
+} msi_kv_attention_args;
+
+/* Errors: MSI_E_INVALID_ARG, MSI_E_NOMEM (workspace), MSI_E_DEVICE.  The
+ * workspace's size follows from the host's bounds; its contents are scratch. */
+msi_status msi_kv_attention_workspace(const msi_kv_cache *cache, const msi_kv_seqs *seqs, uint32_t n_q_heads,
+                                      uint32_t mass_rows, uint64_t *bytes);
+msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_attention_args *args,
+                            void *stream);
+
+/* Cut every sequence back to at most `budget` tokens a head: its first `sinks`
+ * and last `recent` tokens, and of the others those with the largest mass
+ * (equal ones from the lowest index on; NaN below everything), in ascending
+ * order.  Heads keep tokens of their own.  The kept tokens go to the pages of
+ * dst_table [n_seqs, dst_blocks], which no sequence of the call may hold, with
+ * their mass, coded again by blocks of 64 as an append to empty pages would; new_lens[i] =
+ * min(lens[i], budget); keep [n_seqs, n_heads, budget] gets the kept indices, then -1.  A sequence
+ * within its budget is copied whole.  cu_rows is not read.  Tokens of a page outside the pool are kept last, as
+ * zeros.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+typedef struct {
+    uint32_t budget;             /* >= 1                                               */
+    uint32_t sinks, recent;      /* sinks + recent <= budget                           */
+    uint32_t dst_blocks;         /* 64 * dst_blocks >= min(budget, max_len)            */
+    const int32_t *dst_table;
+    int32_t *new_lens;           /* [n_seqs], not lens itself                          */
+    int32_t *keep;               /* [n_seqs, n_heads, budget]                          */
+    uint32_t *status;
+} msi_kv_evict_args;
+msi_status msi_kv_evict(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_evict_args *args, void *stream);
+
 /* Source-service counters (plans with a source; zeros otherwise). */
 typedef struct {
     uint64_t reads_issued, reads_completed, reads_failed;

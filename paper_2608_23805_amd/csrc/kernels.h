@@ -9,8 +9,12 @@
 #include <utility>
 
 #include "common.h"
+#include "kv_common.h"
 
 namespace msi {
+
+// Sets the calling thread's msi_last_error and returns `status` (msi_abi.hip).
+int32_t abi_error(int32_t status, const char *text);
 
 // Per-launch telemetry: while `stop` is set, kernels launched through
 // launch_k carry HIP events that the runtime records at the first kernel's
@@ -271,5 +275,56 @@ hipError_t launch_set_gens(uint32_t *gen_dev, const GenBatch &b, hipStream_t s);
 hipError_t launch_residual(const uint16_t *x0, const float *out, float *h, uint16_t *x, int rows, int cols,
                            hipStream_t s);
 hipError_t launch_clear_word(uint32_t *word, hipStream_t s);
+
+// ---- projection with its epilogue (linear.hip)
+constexpr int LINEAR_NONE = 0, LINEAR_SILU = 1, LINEAR_GELU = 2, LINEAR_GELU_TANH = 3;
+struct LinearArgs {
+    const uint16_t *x, *w;       // [M, K] with x_stride elements from row to row, [N, K]
+    const float *bias;           // [N] or null
+    const float *res_f32;        // one of these, or neither
+    const uint16_t *res_bf16;
+    float *out_f32;              // one of these
+    uint16_t *out_bf16;
+    int64_t x_stride, res_stride, out_stride;
+    int M, N, K;
+    bool vec4;                   // four features of a row may be read and written together
+};
+hipError_t launch_linear(const LinearArgs &A, int act, hipStream_t st);
+
+// ---- paged 8-bit cache of keys and values (kv_cache.hip); strides in elements, fmt KV_E4M3 or KV_INT8
+hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,
+                            int64_t k_stride, int64_t v_stride, uint32_t *status, hipStream_t st);
+hipError_t launch_kv_read(const KvCache &c, int fmt, const KvSeqs &s, uint16_t *k, uint16_t *v, int64_t k_stride,
+                          int64_t v_stride, uint32_t *status, hipStream_t st);
+hipError_t launch_kv_evict(const KvCache &c, int fmt, const KvSeqs &s, const int32_t *dst_table, int dst_blocks,
+                           int32_t *new_lens, int32_t *keep, int budget, int sinks, int recent, uint32_t *status,
+                           hipStream_t st);
+
+// ---- attention over the cache (kv_attention.hip)
+struct AttentionCut {
+    bool few;                    // at most 32 packed rows a sequence and head
+    int tile_rows, tiles;        // packed rows of a workgroup, workgroups along them
+    int chunk, splits;           // blocks of a workgroup, workgroups along the cache
+    size_t part_ml, part_o, scores, bytes;   // workspace offsets and size
+};
+AttentionCut attention_cut(int S, int H, int G, int D, int max_rows, int max_len, bool mass);
+struct AttentionLaunch {
+    KvCache c;
+    KvSeqs s;
+    const uint16_t *q;
+    uint16_t *out;
+    int64_t q_stride, out_stride;   // elements from one row to the next
+    int G;                       // query heads of a cache head
+    float scale_log2;            // scale * log2(e): scores are powers of two
+    int chunk, n_splits, part_rows;
+    float *part_ml, *part_o;     // [S, H, splits, part_rows, 2 | D] maxima and sums, unnormalised outputs
+    float *scores;               // [S, score_blocks, H, score_rows, 64], or null
+    int score_blocks, score_rows;
+    float *lse;                  // [n_rows, H G] log2 of the rows' sums (many rows), or null
+    int mass_rows;
+    float decay;
+    uint32_t *status;
+};
+hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st);
 
 }  // namespace msi

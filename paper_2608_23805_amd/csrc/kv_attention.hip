@@ -1,0 +1,874 @@
+// kv_attention.hip -- attention over the paged 8-bit cache, gfx950.
+//
+// For a query row of sequence i at position len - n + r of its tokens, head a
+// of the G query heads that share cache head h:
+//     s_t = scale * q . k_t      over the tokens t <= len - n + r,
+//     p = softmax(s),  out = sum_t p_t v_t,
+// and, where the tokens' weights are kept, mass_t = decay * mass_t + the sum of
+// p_t over the last mass_rows rows and the G heads.
+//
+// Rows of one cache head are packed (row, head of the group) so that every byte
+// of the cache that a workgroup reads serves all of them.  One pass over the
+// cache with a running maximum and sum per row.  Products are transposed:
+// S^T = K Q^T and O^T = V^T P^T, so that the scores of a query row stay in one
+// lane column, and the token order of an MFMA's reduction is the one in which
+// the scores already lie, so P never moves between lanes.  Codes become bf16
+// exactly; the block's K scale multiplies the fp32 scores and its V scale the
+// probabilities.  Probabilities are rounded to bf16 for the second product
+// (at most 2^-9 relative each, the same as the output's own rounding); their
+// sum, the maxima, the scores and all accumulators are fp32.
+#include <algorithm>
+
+#include "kernels.h"
+#include "kv_device.h"
+
+namespace msi {
+
+namespace {
+
+// Eight codes as bf16 (exact).
+template <int FMT>
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b)
+{
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t w = i ? b : a;
+        if constexpr (FMT == KV_INT8) {
+            const f32x4 f = kv_unpack4<FMT>(w);
+            typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+            r[2 * i] = __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(f[0]), static_cast<__bf16>(f[1])});
+            r[2 * i + 1] = __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(f[2]), static_cast<__bf16>(f[3])});
+        } else {
+            r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+            r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+        }
+    }
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16_hw(float lo, float hi)
+{
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+    return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
+}
+
+// 4 x 4 bytes transposed: byte d of word t becomes byte t of word d.
+__device__ __forceinline__ void transpose4(const uint32_t (&in)[4], uint32_t (&out)[4])
+{
+    const uint32_t a = __builtin_amdgcn_perm(in[1], in[0], 0x05010400u);   // t0d0 t1d0 t0d1 t1d1
+    const uint32_t b = __builtin_amdgcn_perm(in[1], in[0], 0x07030602u);   // t0d2 t1d2 t0d3 t1d3
+    const uint32_t c = __builtin_amdgcn_perm(in[3], in[2], 0x05010400u);
+    const uint32_t d = __builtin_amdgcn_perm(in[3], in[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+template <typename Op>
+__device__ __forceinline__ float across16(float v, Op op)      // over the lanes l % 16 equal
+{
+    const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(s16[0]), __uint_as_float(s16[1]));
+    const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
+}
+
+__device__ __forceinline__ float vmax(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float vsum(float a, float b) { return a + b; }
+
+// Rows are numbered row * G + head of the group within a sequence and cache head.
+__device__ __forceinline__ int row_limit(const KvSeq &q, int token_row) { return q.len - q.n + token_row + 1; }
+
+// ---------------------------------------------------------------- few rows
+//
+// Up to 16 RT packed rows (single tokens, drafted tokens): bound by reading the
+// cache.  No LDS on the way: the wavefront's loads are the MFMA operands.  A
+// workgroup of four wavefronts takes `chunk` blocks of a sequence's cache, the
+// wavefronts every fourth one; their results meet in LDS, and those of several
+// chunks in the join kernel.
+//
+// K: lane (i, j) = (lane % 16, lane / 16) reads 16 bytes 16 j of each 64-byte
+// piece of token 16 g + i; the elements of a reduction step of 32 are in the
+// order 64 (c / 2) + 16 j + 8 (c % 2) + 0..7, and the queries are read in the same.
+// V: lane (i, j) reads D / 16 bytes from i D / 16 of the eight tokens
+// 32 u + 4 j + 0..3 and 32 u + 16 + 4 j + 0..3, whose scores it holds, and
+// transposes them in registers to eight tokens of each of its D / 16 elements.
+template <int FMT, int D, int RT>
+struct FewRows {
+    static constexpr int TOK = D == 256 ? 32 : KV_BLOCK;    // tokens of a step
+    static constexpr int STEPS = KV_BLOCK / TOK;            // steps of a block
+    static constexpr int GT = TOK / 16;                     // groups of 16 tokens
+    static constexpr int KL = D / 64;                       // 16-byte loads of a K row per lane
+    static constexpr int W = D / 16;                        // V bytes per lane and token
+    static constexpr int VW = W / 4;                        // words
+    static constexpr int OS = D + 4;                        // LDS row stride of the outputs (words)
+
+    struct Codes {
+        u32x4 k[GT][KL];
+        uint32_t v[GT / 2][8][VW];
+    };
+
+    static __device__ __forceinline__ void load_k(u32x4 (&k)[GT][KL], const uint8_t *block, int step)
+    {
+        const int lane = threadIdx.x & 63;
+        const uint8_t *p = block + (step * TOK + (lane & 15)) * D + 16 * (lane >> 4);
+#pragma unroll
+        for (int g = 0; g < GT; ++g)
+#pragma unroll
+            for (int l = 0; l < KL; ++l)
+                k[g][l] = load_stream16(p + 16 * g * D + 64 * l);
+    }
+
+    static __device__ __forceinline__ void load_v(uint32_t (&v)[GT / 2][8][VW], const uint8_t *block, int step)
+    {
+        const int lane = threadIdx.x & 63;
+        const uint8_t *p = block + KV_BLOCK * D + (step * TOK + 4 * (lane >> 4)) * D + (lane & 15) * W;
+#pragma unroll
+        for (int u = 0; u < GT / 2; ++u)
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const uint8_t *a = p + (32 * u + (t < 4 ? t : 12 + t)) * D;
+                typedef __attribute__((ext_vector_type(VW))) uint32_t vec;
+                const vec w = __builtin_nontemporal_load(reinterpret_cast<const vec *>(a));
+                if constexpr (VW == 1) {
+                    v[u][t][0] = w[0];
+                } else {
+#pragma unroll
+                    for (int x = 0; x < VW; ++x)
+                        v[u][t][x] = w[x];
+                }
+            }
+    }
+};
+
+template <int FMT, int D, int RT>
+__global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
+{
+    using F = FewRows<FMT, D, RT>;
+    constexpr int TOK = F::TOK, GT = F::GT, W = F::W, VW = F::VW, OS = F::OS;
+    __shared__ __attribute__((aligned(16))) float olds[4][16][OS];
+    __shared__ float ml[4][RT][16][2];
+
+    const int i = blockIdx.z, split = blockIdx.x;
+    const int h = int(blockIdx.y) % A.c.H, tile = int(blockIdx.y) / A.c.H;
+    const KvSeq q = kv_seq(A.s, i, false);
+    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+        kv_raise(A.status, KV_BAD_LENGTH);
+    const int rows = q.n * A.G, r0 = tile * 16 * RT;
+    if (r0 >= rows)
+        return;
+    const int b0 = split * A.chunk, b1 = min(b0 + A.chunk, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+    const bool direct = A.n_splits == 1;
+    if (b0 >= b1 && !direct)
+        return;                                              // the join goes by the length too
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, j = lane >> 4;
+
+    // page of the l-th block of this wavefront in lane l
+    int pages = -1;
+    if (b0 + wave + 4 * lane < b1)
+        pages = A.s.table[int64_t(i) * A.s.max_blocks + b0 + wave + 4 * lane];
+    const bool known = kv_page_ok(pages, A.c.n_pages);
+    if (b0 + wave + 4 * lane < b1 && !known)
+        kv_raise(A.status, KV_BAD_PAGE);
+    if (!known)
+        pages = -1;
+
+    bf16x8 qf[RT][D / 32];
+    int limit[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int r = r0 + 16 * x + col, rc = min(r, rows - 1);
+        const int tr = rc / A.G, hd = rc - tr * A.G;
+        limit[x] = r < rows ? row_limit(q, tr) : 0;
+        const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+            qf[x][c] = *reinterpret_cast<const bf16x8 *>(src + 64 * (c / 2) + 16 * j + 8 * (c % 2));
+    }
+
+    f32x4 acc[RT][W];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        m[x] = -INFINITY;
+        l[x] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < W; ++c)
+            acc[x][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int nb = b1 - b0 > wave ? (b1 - b0 - wave + 3) / 4 : 0;      // blocks of this wavefront
+    const int steps = nb * F::STEPS;
+    auto block_at = [&](int s) {
+        const int page = __builtin_amdgcn_readlane(pages, s / F::STEPS);
+        return A.c.data + kv_offset(max(page, 0), h, A.c.H, D);
+    };
+    auto scales_at = [&](int s) {
+        const int page = __builtin_amdgcn_readlane(pages, s / F::STEPS);
+        return *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(max(page, 0)) * A.c.H + h) * 2);
+    };
+    typename F::Codes cur;
+    float2 sc{1.0f, 1.0f};
+    if (steps > 0) {
+        sc = scales_at(0);
+        F::load_k(cur.k, block_at(0), 0);
+        F::load_v(cur.v, block_at(0), 0);
+    }
+    for (int s = 0; s < steps; ++s) {
+        const int blk = b0 + wave + 4 * (s / F::STEPS);
+        const bool here = __builtin_amdgcn_readlane(pages, s / F::STEPS) >= 0;
+        const int t0 = blk * KV_BLOCK + (s % F::STEPS) * TOK;
+        const int s1 = min(s + 1, steps - 1);
+        const uint8_t *next = block_at(s1);
+        const float2 sc_next = scales_at(s1);
+
+        // ---- scores of TOK tokens (rows of S^T) and 16 RT rows (columns)
+        f32x4 sv[RT][GT];
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+                sv[x][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                const bf16x8 kf = codes_bf16<FMT>(cur.k[g][c / 2][2 * (c % 2)], cur.k[g][c / 2][2 * (c % 2) + 1]);
+#pragma unroll
+                for (int x = 0; x < RT; ++x)
+                    sv[x][g] = mfma16(kf, qf[x][c], sv[x][g]);
+            }
+        }
+        F::load_k(cur.k, next, s1 % F::STEPS);                 // (the last step reads its own block again)
+
+        const float ks = sc.x * A.scale_log2;
+        const bool tail = !here || t0 + TOK > q.len;
+        if (tail) {                                            // bytes past the last token may be anything
+#pragma unroll
+            for (int u = 0; u < GT / 2; ++u)
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    const int tok = t0 + 32 * u + 4 * j + (t < 4 ? t : 12 + t);
+#pragma unroll
+                    for (int w = 0; w < VW; ++w)
+                        cur.v[u][t][w] = here && tok < q.len ? cur.v[u][t][w] : 0u;
+                }
+        }
+        bf16x8 pf[RT][GT / 2];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            float top = -INFINITY;
+            // every row sees the whole step unless the step reaches past the first row's limit
+            const bool masked = !here || t0 + TOK > q.len - q.n + 1 || r0 + 16 * (x + 1) > rows;
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float z = sv[x][g][r] * ks;
+                    if (masked)
+                        z = here && t0 + 16 * g + 4 * j + r < limit[x] ? z : -INFINITY;
+                    sv[x][g][r] = z;
+                    top = fmaxf(top, z);
+                }
+            if (A.scores && r0 + 16 * x + col < rows) {
+                float *dst = A.scores + (((int64_t(i) * A.score_blocks + blk) * A.c.H + h) * A.score_rows + r0 + 16 * x + col) *
+                                            KV_BLOCK + (s % F::STEPS) * TOK + 4 * j;
+#pragma unroll
+                for (int g = 0; g < GT; ++g)
+                    *reinterpret_cast<f32x4 *>(dst + 16 * g) = sv[x][g];
+            }
+            top = across16(top, vmax);
+            const float m1 = fmaxf(m[x], top);
+            const float ref = m1 == -INFINITY ? 0.0f : m1;
+            if (__any(m1 != m[x])) {
+                const float a = __builtin_amdgcn_exp2f(m[x] - ref);
+                l[x] *= a;
+#pragma unroll
+                for (int c = 0; c < W; ++c)
+                    acc[x][c] *= a;
+                m[x] = m1;
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(sv[x][g][r] - ref);
+                    sum += p;
+                    sv[x][g][r] = p == 0.0f ? 0.0f : p * sc.y;
+                }
+            l[x] += sum;
+#pragma unroll
+            for (int u = 0; u < GT / 2; ++u)
+                pf[x][u] = __builtin_bit_cast(
+                    bf16x8, u32x4{pack_bf16_hw(sv[x][2 * u][0], sv[x][2 * u][1]), pack_bf16_hw(sv[x][2 * u][2], sv[x][2 * u][3]),
+                                  pack_bf16_hw(sv[x][2 * u + 1][0], sv[x][2 * u + 1][1]),
+                                  pack_bf16_hw(sv[x][2 * u + 1][2], sv[x][2 * u + 1][3])});
+        }
+        // ---- O^T: lane (i, j) holds elements i D / 16 + c of the eight tokens
+#pragma unroll
+        for (int u = 0; u < GT / 2; ++u)
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+                uint32_t lo[4], hi[4];
+                const uint32_t a[4] = {cur.v[u][0][w], cur.v[u][1][w], cur.v[u][2][w], cur.v[u][3][w]};
+                const uint32_t b[4] = {cur.v[u][4][w], cur.v[u][5][w], cur.v[u][6][w], cur.v[u][7][w]};
+                transpose4(a, lo);
+                transpose4(b, hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bf16x8 vf = codes_bf16<FMT>(lo[e], hi[e]);
+#pragma unroll
+                    for (int x = 0; x < RT; ++x)
+                        acc[x][4 * w + e] = mfma16(vf, pf[x][u], acc[x][4 * w + e]);
+                }
+            }
+        F::load_v(cur.v, next, s1 % F::STEPS);
+        sc = sc_next;
+    }
+
+    // ---- the four wavefronts' results: lane (col, j) holds elements (4 j + r) W + c of row col
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const float lx = across16(l[x], vsum);
+        if (j == 0) {
+            ml[wave][x][col][0] = m[x];
+            ml[wave][x][col][1] = lx;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        if (x)
+            __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < W; c += 4)
+                *reinterpret_cast<f32x4 *>(&olds[wave][col][(4 * j + r) * W + c]) =
+                    f32x4{acc[x][c][r], acc[x][c + 1][r], acc[x][c + 2][r], acc[x][c + 3][r]};
+        __syncthreads();
+        // thread: row tid / 16, elements tid % 16 * 4 + 64 k
+        const int row = tid >> 4, r = r0 + 16 * x + row;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            mx = fmaxf(mx, ml[w][x][row][0]);
+        const float ref = mx == -INFINITY ? 0.0f : mx;
+        float a[4], sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            a[w] = __builtin_amdgcn_exp2f(ml[w][x][row][0] - ref);
+            sum += a[w] * ml[w][x][row][1];
+        }
+        if (r < rows) {
+            const int tr = r / A.G, hd = r - tr * A.G;
+            const int64_t part = ((int64_t(i) * A.c.H + h) * A.n_splits + split) * A.part_rows + r;
+            if ((tid & 15) == 0 && A.part_ml) {
+                A.part_ml[2 * part] = mx;
+                A.part_ml[2 * part + 1] = sum;
+            }
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int k = 0; k < D / 64; ++k) {
+                const int e = (tid & 15) * 4 + 64 * k;
+                f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    o += a[w] * *reinterpret_cast<const f32x4 *>(&olds[w][row][e]);
+                if (direct) {
+                    uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + e;
+                    *reinterpret_cast<uint2 *>(dst) =
+                        make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+                } else {
+                    *reinterpret_cast<f32x4 *>(A.part_o + part * D + e) = o;
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- many rows
+//
+// A workgroup of four wavefronts owns 128 packed rows, 32 a wavefront, and
+// walks the cache in steps of 64 tokens: K [64, D] and V^T [D, 64] go to LDS
+// as bf16 (converted once for all four wavefronts), v_mfma_f32_32x32x16_bf16
+// for both products.  V^T is stored in the order in which a lane holds the
+// scores: slot 8 (2 u + hf) + r of 16-token group u is token
+// 16 u + 4 hf + r (r < 4) or 16 u + 4 + 4 hf + r.
+template <int D>
+struct ManyRows {
+    static constexpr int TOK = KV_BLOCK;
+    static constexpr int KS = D * 2 + 16;                 // LDS row strides (bytes)
+    static constexpr int VS = TOK * 2 + 16;
+    static constexpr int KBYTES = TOK * KS, VBYTES = D * VS;
+    static constexpr int ROWS = 128;
+};
+
+template <int FMT, int D>
+__device__ __forceinline__ void stage_k(uint8_t *lds, const uint8_t *block)
+{
+    using M = ManyRows<D>;
+    // 16 codes per thread and pass
+    constexpr int CPR = D / 16, PASSES = KV_BLOCK * CPR / 256;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int idx = p * 256 + threadIdx.x, t = idx / CPR, c = idx % CPR;
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(block + t * D + c * 16);
+        bf16x8 *dst = reinterpret_cast<bf16x8 *>(lds + t * M::KS + c * 32);
+        dst[0] = codes_bf16<FMT>(w[0], w[1]);
+        dst[1] = codes_bf16<FMT>(w[2], w[3]);
+    }
+}
+
+template <int FMT, int D>
+__device__ __forceinline__ void stage_v(uint8_t *lds, const uint8_t *block, int valid)
+{
+    using M = ManyRows<D>;
+    // thread: four elements 4 e.. of the eight tokens of one slot group
+    constexpr int EQ = D / 4, PASSES = (EQ * 8 + 255) / 256;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int idx = p * 256 + threadIdx.x, e = idx % EQ, sg = idx / EQ, u = sg >> 1, hf = sg & 1;
+        if (EQ * 8 % 256 && sg >= 8)
+            break;
+        uint32_t w[2][4];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int t = 16 * u + 4 * hf + (x < 4 ? x : 4 + x);
+            const uint32_t c = *reinterpret_cast<const uint32_t *>(block + t * D + 4 * e);
+            w[x >> 2][x & 3] = t < valid ? c : 0u;
+        }
+        uint32_t lo[4], hi[4];
+        transpose4(w[0], lo);
+        transpose4(w[1], hi);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<bf16x8 *>(lds + (4 * e + x) * M::VS + sg * 16) = codes_bf16<FMT>(lo[x], hi[x]);
+    }
+}
+
+__device__ __forceinline__ float across32(float v, float (*op)(float, float))
+{
+    const auto s32 = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return op(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
+}
+
+// Query fragments of 32 rows from r0 on: lane (col, hf) = (lane % 32, lane / 32), elements 16 c + 8 hf + 0..7.
+template <int D>
+__device__ __forceinline__ void load_q32(bf16x8 (&qf)[D / 16], const AttentionLaunch &A, const KvSeq &q, int h, int r0,
+                                         int rows)
+{
+    const int lane = threadIdx.x & 63;
+    const int rc = min(r0 + (lane & 31), rows - 1), tr = rc / A.G, hd = rc - tr * A.G;
+    const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+        qf[c] = *reinterpret_cast<const bf16x8 *>(src + 16 * c);
+}
+
+// S^T of 64 tokens and 32 rows: sv[b][v] is token 32 b + 8 (v / 4) + 4 hf + v % 4 of row col.
+template <int D>
+__device__ __forceinline__ void scores32(f32x16 (&sv)[2], const uint8_t *lds, const bf16x8 (&qf)[D / 16])
+{
+    using M = ManyRows<D>;
+    const int lane = threadIdx.x & 63;
+    const uint8_t *kp = lds + (lane & 31) * M::KS + 16 * (lane >> 5);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            sv[b][v] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            sv[b] = mfma32(*reinterpret_cast<const bf16x8 *>(kp + 32 * b * M::KS + 32 * c), qf[c], sv[b]);
+    }
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(AttentionLaunch A)
+{
+    using M = ManyRows<D>;
+    __shared__ __attribute__((aligned(16))) uint8_t kl[M::KBYTES];
+    __shared__ __attribute__((aligned(16))) uint8_t vl[M::VBYTES];
+    const int i = blockIdx.z, split = int(blockIdx.y) % A.n_splits, h = int(blockIdx.y) / A.n_splits;
+    const KvSeq q = kv_seq(A.s, i, false);
+    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+        kv_raise(A.status, KV_BAD_LENGTH);
+    const int rows = q.n * A.G, r0 = int(blockIdx.x) * M::ROWS;
+    if (r0 >= rows)
+        return;
+    const bool direct = A.n_splits == 1;
+    const int len_blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
+    if (split * A.chunk >= len_blocks && !direct)
+        return;
+    // blocks up to the last row's limit
+    const int last = min(r0 + M::ROWS, rows) - 1;
+    const int most = max(row_limit(q, last / A.G), 0);
+    const int b0 = split * A.chunk, b1 = min(b0 + A.chunk, (most + KV_BLOCK - 1) / KV_BLOCK);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, hf = lane >> 5;
+    const int w0 = r0 + 32 * wave;                          // this wavefront's rows
+    const bool idle = w0 >= rows;
+    const int r = w0 + col;
+    const int limit = r < rows ? row_limit(q, r / A.G) : 0;
+    const int least = idle ? 0 : row_limit(q, w0 / A.G);    // the first row's limit: blocks below it need no mask
+    const int wave_most = idle ? 0 : row_limit(q, min(w0 + 31, rows - 1) / A.G);
+
+    bf16x8 qf[D / 16];
+    load_q32<D>(qf, A, q, h, w0, rows);
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            acc[c][v] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    for (int b = b0; b < b1; ++b) {
+        const int page0 = __builtin_amdgcn_readfirstlane(A.s.table[int64_t(i) * A.s.max_blocks + b]);
+        const bool here = kv_page_ok(page0, A.c.n_pages);
+        const int page = here ? page0 : 0;
+        if (!here && tid == 0)
+            kv_raise(A.status, KV_BAD_PAGE);
+        const uint8_t *block = A.c.data + kv_offset(page, h, A.c.H, D);
+        __syncthreads();
+        stage_k<FMT, D>(kl, block);
+        stage_v<FMT, D>(vl, block + KV_BLOCK * D, here ? q.len - b * KV_BLOCK : 0);
+        __syncthreads();
+        const int t0 = b * KV_BLOCK;
+        if (!here || t0 >= wave_most)
+            continue;
+        const float2 sc = *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(page) * A.c.H + h) * 2);
+        f32x16 sv[2];
+        scores32<D>(sv, kl, qf);
+        const float ks = sc.x * A.scale_log2;
+        float top = -INFINITY;
+        const bool masked = t0 + KV_BLOCK > least || w0 + 32 > rows;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                float z = sv[x][v] * ks;
+                if (masked)
+                    z = t0 + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? z : -INFINITY;
+                sv[x][v] = z;
+                top = fmaxf(top, z);
+            }
+        top = across32(top, vmax);
+        const float m1 = fmaxf(m, top);
+        const float ref = m1 == -INFINITY ? 0.0f : m1;
+        if (__any(m1 != m)) {
+            const float a = __builtin_amdgcn_exp2f(m - ref);
+            l *= a;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                acc[c] *= a;
+            m = m1;
+        }
+        bf16x8 pf[4];
+        float sum = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float p = __builtin_amdgcn_exp2f(sv[x][v] - ref);
+                sum += p;
+                sv[x][v] = p == 0.0f ? 0.0f : p * sc.y;
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                pf[2 * x + u] = __builtin_bit_cast(
+                    bf16x8, u32x4{pack_bf16_hw(sv[x][8 * u], sv[x][8 * u + 1]), pack_bf16_hw(sv[x][8 * u + 2], sv[x][8 * u + 3]),
+                                  pack_bf16_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
+        }
+        l += sum;
+        const uint8_t *vp = vl + col * M::VS + 16 * hf;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                acc[c] = mfma32(*reinterpret_cast<const bf16x8 *>(vp + 32 * c * M::VS + 32 * u), pf[u], acc[c]);
+    }
+
+    // ---- lane (col, hf) holds elements 32 c + 8 (v / 4) + 4 hf + v % 4 of its row
+    l = across32(l, vsum);
+    if (r >= rows)
+        return;
+    const int tr = r / A.G, hd = r - tr * A.G;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (direct) {
+        uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + 4 * hf;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4)
+                *reinterpret_cast<uint2 *>(dst + 32 * c + 2 * v) =
+                    make_uint2(pack_bf16x2(acc[c][v] * inv, acc[c][v + 1] * inv),
+                               pack_bf16x2(acc[c][v + 2] * inv, acc[c][v + 3] * inv));
+        if (A.lse && hf == 0)
+            A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
+    } else {
+        const int64_t part = ((int64_t(i) * A.c.H + h) * A.n_splits + split) * A.part_rows + r;
+        if (hf == 0) {
+            A.part_ml[2 * part] = m;
+            A.part_ml[2 * part + 1] = l;
+        }
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4)
+                *reinterpret_cast<f32x4 *>(A.part_o + part * D + 32 * c + 2 * v + 4 * hf) =
+                    f32x4{acc[c][v], acc[c][v + 1], acc[c][v + 2], acc[c][v + 3]};
+    }
+}
+
+// ---------------------------------------------------------------- join
+//
+// Maximum and sum of a row over the chunks' results, by one wavefront (lanes
+// take every 64th chunk; the sums meet in a fixed tree).
+__device__ __forceinline__ float2 join_ml(const AttentionLaunch &A, int64_t first, int n)
+{
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY;
+    for (int s = lane; s < n; s += 64)
+        m = fmaxf(m, A.part_ml[2 * (first + int64_t(s) * A.part_rows)]);
+    m = wave_max(m);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    for (int s = lane; s < n; s += 64) {
+        const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * (first + int64_t(s) * A.part_rows));
+        l += __builtin_amdgcn_exp2f(x.x - ref) * x.y;
+    }
+    return make_float2(m, wave_sum(l));
+}
+
+// One workgroup of 256 threads per (packed row, head, sequence): its D elements over the chunks.
+__global__ void __launch_bounds__(256) kv_join_kernel(AttentionLaunch A)
+{
+    __shared__ float part[4][256];
+    const int i = blockIdx.z, h = blockIdx.y, r = blockIdx.x;
+    const KvSeq q = kv_seq(A.s, i, false);
+    if (r >= q.n * A.G)
+        return;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int D = A.c.D;
+    const int n = ((q.len + KV_BLOCK - 1) / KV_BLOCK + A.chunk - 1) / A.chunk;
+    const int64_t first = (int64_t(i) * A.c.H + h) * A.n_splits * A.part_rows + r;
+    const float2 ml = join_ml(A, first, n);
+    const float ref = ml.x == -INFINITY ? 0.0f : ml.x;
+    // wavefront w takes the chunks w, w + 4, ...; lane l the elements 4 l .. 4 l + 3
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+    if (4 * lane < D)
+        for (int s = wave; s < n; s += 4) {
+            const int64_t p = first + int64_t(s) * A.part_rows;
+            o += __builtin_amdgcn_exp2f(A.part_ml[2 * p] - ref) * *reinterpret_cast<const f32x4 *>(A.part_o + p * D + 4 * lane);
+        }
+    *reinterpret_cast<f32x4 *>(&part[wave][4 * lane]) = o;
+    __syncthreads();
+    const int tr = r / A.G, hd = r - tr * A.G;
+    if (tid < D) {
+        const float sum = ((part[0][tid] + part[1][tid]) + part[2][tid]) + part[3][tid];
+        A.out[(int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + tid] =
+            f32_to_bf16(ml.y == 0.0f ? 0.0f : sum / ml.y);
+    }
+    if (A.lse && tid == 0)
+        A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = ml.y == 0.0f ? INFINITY : ml.x + log2f(ml.y);
+}
+
+// ---------------------------------------------------------------- weights
+//
+// From the scores that the few-rows kernel left: one wavefront per block,
+// lane = token.  A row without a token it sees has no weights (its log-sum is
+// +infinity).
+constexpr int MASS_BLOCKS = 16;              // blocks of a workgroup
+
+__global__ void __launch_bounds__(256) kv_mass_scores_kernel(AttentionLaunch A)
+{
+    extern __shared__ float lse[];           // [rows that count]
+    const int i = blockIdx.z, h = blockIdx.y;
+    const KvSeq q = kv_seq(A.s, i, false);
+    const int blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
+    const int b0 = int(blockIdx.x) * MASS_BLOCKS;
+    if (b0 >= blocks)
+        return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int rows = q.n * A.G, from = max(q.n - A.mass_rows, 0) * A.G;
+    const int n = (blocks + A.chunk - 1) / A.chunk;
+    for (int r = from + wave; r < rows; r += 4) {
+        const float2 ml = join_ml(A, (int64_t(i) * A.c.H + h) * A.n_splits * A.part_rows + r, n);
+        if (lane == 0)
+            lse[r - from] = ml.y == 0.0f ? INFINITY : ml.x + log2f(ml.y);
+    }
+    __syncthreads();
+    for (int b = b0 + wave; b < min(b0 + MASS_BLOCKS, blocks); b += 4) {
+        const int page = A.s.table[int64_t(i) * A.s.max_blocks + b];
+        if (!kv_page_ok(page, A.c.n_pages))
+            continue;
+        const float *src = A.scores + ((int64_t(i) * A.score_blocks + b) * A.c.H + h) * A.score_rows * KV_BLOCK + lane;
+        float w = 0.0f;
+        for (int r = from; r < rows; ++r)
+            w += __builtin_amdgcn_exp2f(src[r * KV_BLOCK] - lse[r - from]);
+        if (b * KV_BLOCK + lane < q.len) {
+            float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + lane;
+            *dst = A.decay != 0.0f ? fmaf(A.decay, *dst, w) : w;
+        }
+    }
+}
+
+// For many rows the scores are computed again from K: one workgroup per
+// block, its wavefronts take every fourth group of 32 rows.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
+{
+    using M = ManyRows<D>;
+    __shared__ __attribute__((aligned(16))) uint8_t kl[M::KBYTES];
+    __shared__ float part[4][KV_BLOCK];
+    const int i = blockIdx.z, h = blockIdx.y, b = blockIdx.x;
+    const KvSeq q = kv_seq(A.s, i, false);
+    if (b * KV_BLOCK >= q.len)
+        return;
+    const int page = __builtin_amdgcn_readfirstlane(A.s.table[int64_t(i) * A.s.max_blocks + b]);
+    if (!kv_page_ok(page, A.c.n_pages))
+        return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int col = lane & 31, hf = lane >> 5;
+    stage_k<FMT, D>(kl, A.c.data + kv_offset(page, h, A.c.H, D));
+    __syncthreads();
+    const float ks = A.c.scales[(int64_t(page) * A.c.H + h) * 2] * A.scale_log2;
+    const int rows = q.n * A.G;
+    // rows below `from` do not count, or do not see the block
+    const int from = max(max(q.n - A.mass_rows, 0), b * KV_BLOCK - (q.len - q.n)) * A.G;
+    f32x16 w[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            w[x][v] = 0.0f;
+    for (int r0 = from + 32 * wave; r0 < rows; r0 += 128) {
+        bf16x8 qf[D / 16];
+        load_q32<D>(qf, A, q, h, r0, rows);
+        f32x16 sv[2];
+        scores32<D>(sv, kl, qf);
+        const int r = r0 + col, rc = min(r, rows - 1), tr = rc / A.G;
+        const int limit = r < rows ? row_limit(q, tr) : 0;
+        const float z0 = A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + rc - tr * A.G];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -z0));
+                w[x][v] += b * KV_BLOCK + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? p : 0.0f;
+            }
+    }
+    // over the 32 columns: four steps within 16 lanes, then the other 16
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            float a = w[x][v];
+            a += __uint_as_float(dpp_move<dpp::QUAD_1032>(__float_as_uint(a)));
+            a += __uint_as_float(dpp_move<dpp::QUAD_2301>(__float_as_uint(a)));
+            a += __uint_as_float(dpp_move<dpp::ROW_HALF_MIRROR>(__float_as_uint(a)));
+            a += __uint_as_float(dpp_move<dpp::ROW_MIRROR>(__float_as_uint(a)));
+            const auto s16 = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(a), false, false);
+            a = __uint_as_float(s16[0]) + __uint_as_float(s16[1]);
+            if (col == 0)
+                part[wave][32 * x + 8 * (v >> 2) + 4 * hf + (v & 3)] = a;
+        }
+    __syncthreads();
+    if (threadIdx.x < KV_BLOCK && b * KV_BLOCK + int(threadIdx.x) < q.len) {
+        const int t = threadIdx.x;
+        const float sum = ((part[0][t] + part[1][t]) + part[2][t]) + part[3][t];
+        float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + t;
+        *dst = A.decay != 0.0f ? fmaf(A.decay, *dst, sum) : sum;
+    }
+}
+
+template <typename F>
+void with_shape(int fmt, int D, F f)
+{
+    auto by_d = [&](auto fm) {
+        if (D == 64)
+            f(fm, std::integral_constant<int, 64>{});
+        else if (D == 128)
+            f(fm, std::integral_constant<int, 128>{});
+        else
+            f(fm, std::integral_constant<int, 256>{});
+    };
+    if (fmt == KV_INT8)
+        by_d(std::integral_constant<int, KV_INT8>{});
+    else
+        by_d(std::integral_constant<int, KV_E4M3>{});
+}
+
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+}  // namespace
+
+// How a call is cut, by its host-side bounds alone: the same cut sizes the
+// workspace and launches the kernels.
+AttentionCut attention_cut(int S, int H, int G, int D, int max_rows, int max_len, bool mass)
+{
+    AttentionCut c{};
+    const int64_t rows = int64_t(max_rows) * G;
+    const int blocks = (max_len + KV_BLOCK - 1) / KV_BLOCK;
+    c.few = rows <= 32;
+    c.tile_rows = c.few ? (rows <= 16 ? 16 : 32) : 128;
+    c.tiles = int((rows + c.tile_rows - 1) / c.tile_rows);
+    // about 2048 workgroups of few rows, 512 of many, none of less than 4 blocks
+    const int64_t units = int64_t(S) * H * c.tiles;
+    const int64_t want = std::max<int64_t>(1, (c.few ? 2048 : 512) / std::max<int64_t>(units, 1));
+    int chunk = int((blocks + want - 1) / want);
+    chunk = std::min(std::max((chunk + 3) / 4 * 4, 4), c.few ? 256 : 1 << 30);
+    c.chunk = chunk;
+    c.splits = std::max(1, (blocks + chunk - 1) / chunk);
+    const bool parts = c.splits > 1 || (mass && c.few);
+    c.part_ml = 0;
+    size_t off = parts ? up256(size_t(S) * H * c.splits * rows * 2 * sizeof(float)) : 0;
+    c.part_o = off;
+    off += c.splits > 1 ? up256(size_t(S) * H * c.splits * rows * D * sizeof(float)) : 0;
+    c.scores = off;
+    off += mass && c.few ? up256(size_t(S) * blocks * H * rows * KV_BLOCK * sizeof(float)) : 0;
+    c.bytes = off;                              // (the log-sums of many rows follow: they go by n_rows)
+    return c;
+}
+
+hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st)
+{
+    const int H = A.c.H, S = A.s.S;
+    const int rows = A.s.max_rows * A.G;
+    if (c.few) {
+        const dim3 grid(c.splits, H * c.tiles, S);
+        with_shape(fmt, A.c.D, [&](auto f, auto d) {
+            if (c.tile_rows == 16)
+                launch_k(kv_few_rows_kernel<decltype(f)::value, decltype(d)::value, 1>, grid, 256, 0, st, A);
+            else
+                launch_k(kv_few_rows_kernel<decltype(f)::value, decltype(d)::value, 2>, grid, 256, 0, st, A);
+        });
+    } else {
+        const dim3 grid(c.tiles, H * c.splits, S);
+        with_shape(fmt, A.c.D, [&](auto f, auto d) {
+            launch_k(kv_many_rows_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, A);
+        });
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && c.splits > 1) {
+        launch_k(kv_join_kernel, dim3(rows, H, S), 256, 0, st, A);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || !A.mass_rows)
+        return e;
+    const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
+    if (blocks == 0)
+        return e;
+    if (c.few)
+        launch_k(kv_mass_scores_kernel, dim3((blocks + MASS_BLOCKS - 1) / MASS_BLOCKS, H, S), 256, size_t(rows) * 4, st, A);
+    else
+        with_shape(fmt, A.c.D, [&](auto f, auto d) {
+            launch_k(kv_mass_rows_kernel<decltype(f)::value, decltype(d)::value>, dim3(blocks, H, S), 256, 0, st, A);
+        });
+    return hipGetLastError();
+}
+
+}  // namespace msi

@@ -1,0 +1,529 @@
+// kv_cache.hip -- writing, reading and cutting back the paged 8-bit cache of
+// keys and values, gfx950.
+//
+// A page holds 64 tokens of every head; (page, head) is K codes [64, D], then
+// V codes [64, D], with one fp32 scale each: value = scale * code.  All three
+// operators move each byte once and are bound by HBM (long calls) or by the
+// launch (single tokens).
+#include <algorithm>
+#include <type_traits>
+
+#include "kernels.h"
+#include "kv_device.h"
+
+namespace msi {
+
+namespace {
+
+// Thread t of 256 owns the D / 8 chunks of 8 elements of a row in turn: chunk
+// t % (D / 8) of rows t / (D / 8) + i * ROWS.  16 bytes of bf16, 8 of codes.
+template <int D>
+struct RowChunks {
+    static constexpr int CPR = D / 8;             // chunks of a row
+    static constexpr int ROWS = 256 / CPR;        // rows of one pass of the workgroup
+    static constexpr int N = KV_BLOCK / ROWS;     // passes over a block
+};
+
+__device__ __forceinline__ void unpack_bf16x8(const u32x4 &w, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+
+// ---------------------------------------------------------------- append
+//
+// One workgroup per (block, head, sequence) that receives rows.  Its new rows
+// of K and V stay in registers between the two passes (largest magnitude, then
+// codes); old rows of the block are touched only if its scale grows.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, const uint16_t *__restrict__ k,
+                                                        const uint16_t *__restrict__ v, int64_t k_stride,
+                                                        int64_t v_stride, uint32_t *status)
+{
+    using R = RowChunks<D>;
+    __shared__ float part[8];
+    const int h = blockIdx.y, i = blockIdx.z;
+    const KvSeq q = kv_seq(s, i, true);
+    if (!q.ok && blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+        kv_raise(status, KV_BAD_LENGTH);
+    const int start = q.len - q.n;                       // position of the first new row
+    const int blk = start / KV_BLOCK + int(blockIdx.x);
+    if (q.n == 0 || blk * KV_BLOCK >= q.len)
+        return;
+    const int page = __builtin_amdgcn_readfirstlane(s.table[int64_t(i) * s.max_blocks + blk]);
+    if (!kv_page_ok(page, c.n_pages)) {
+        if (threadIdx.x == 0)
+            kv_raise(status, KV_BAD_PAGE);
+        return;
+    }
+    const int lo = max(start - blk * KV_BLOCK, 0), hi = min(q.len - blk * KV_BLOCK, KV_BLOCK);   // new rows of the block
+    const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
+    const int64_t src0 = int64_t(q.row0) + (blk * KV_BLOCK - start);       // call's row of the block's row 0
+    u32x4 x[2][R::N];
+#pragma unroll
+    for (int p = 0; p < R::N; ++p) {
+        const int r = r0 + p * R::ROWS;
+        if (r >= lo && r < hi) {
+            x[0][p] = load_stream16(k + (src0 + r) * k_stride + h * D + chunk * 8);
+            x[1][p] = load_stream16(v + (src0 + r) * v_stride + h * D + chunk * 8);
+        } else {
+            x[0][p] = x[1][p] = u32x4{0, 0, 0, 0};
+        }
+    }
+    float *sc = c.scales + (int64_t(page) * c.H + h) * 2;
+    const float was[2] = {lo ? sc[0] : 0.0f, lo ? sc[1] : 0.0f};   // (read before the barriers below, written after)
+    uint32_t flags = 0;
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint32_t m = 0;                                   // largest finite magnitude: bf16 bits order as integers
+#pragma unroll
+        for (int p = 0; p < R::N; ++p)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t a = x[j][p][w] & 0x7FFFu, b = (x[j][p][w] >> 16) & 0x7FFFu;
+                if (a >= 0x7F80u || b >= 0x7F80u)
+                    flags = KV_NONFINITE;
+                m = max(m, max(a >= 0x7F80u ? 0u : a, b >= 0x7F80u ? 0u : b));
+            }
+        top[j] = block_max256(__uint_as_float(m << 16), part + 4 * j);
+    }
+    kv_raise(status, flags);
+    uint8_t *base = c.data + kv_offset(page, h, c.H, D);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float need = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT));
+        const float scale = fmaxf(need, was[j]);
+        uint8_t *dst = base + j * (KV_BLOCK * D);
+        if (lo && scale != was[j]) {                      // the old rows move to the larger scale
+            for (int r = r0; r < lo; r += R::ROWS) {
+                uint2 *o = reinterpret_cast<uint2 *>(dst + r * D + chunk * 8);
+                const uint2 w = *o;
+                const f32x4 a = kv_unpack4<FMT>(w.x), b = kv_unpack4<FMT>(w.y);
+                // (code * was is exact, or rounded once in fp32 where a caller's own scale is no power of two)
+                *o = make_uint2(kv_pack4<FMT>(a[0] * was[j] / scale, a[1] * was[j] / scale, a[2] * was[j] / scale,
+                                              a[3] * was[j] / scale),
+                                kv_pack4<FMT>(b[0] * was[j] / scale, b[1] * was[j] / scale, b[2] * was[j] / scale,
+                                              b[3] * was[j] / scale));
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < R::N; ++p) {
+            const int r = r0 + p * R::ROWS;
+            if (r >= lo && r < hi) {
+                float f[8];
+                unpack_bf16x8(x[j][p], f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    f[e] = f[e] != f[e] ? 0.0f : f[e] / scale;      // NaN is stored as zero, infinities as the largest code
+                *reinterpret_cast<uint2 *>(dst + r * D + chunk * 8) =
+                    make_uint2(kv_pack4<FMT>(f[0], f[1], f[2], f[3]), kv_pack4<FMT>(f[4], f[5], f[6], f[7]));
+            }
+        }
+        if (threadIdx.x == 0)
+            sc[j] = scale;
+    }
+    if (c.mass && int(threadIdx.x) >= lo && int(threadIdx.x) < hi)
+        c.mass[(int64_t(page) * c.H + h) * KV_BLOCK + threadIdx.x] = 0.0f;
+}
+
+// ---------------------------------------------------------------- read
+//
+// The mirror of append: row r of a sequence is its token len - n + r.  Values
+// leave as bf16: exact for scales that are powers of two, as append writes
+// them (a code has at most 8 significant bits), rounded to nearest otherwise.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint16_t *__restrict__ k,
+                                                      uint16_t *__restrict__ v, int64_t k_stride, int64_t v_stride,
+                                                      uint32_t *status)
+{
+    using R = RowChunks<D>;
+    const int h = blockIdx.y, i = blockIdx.z;
+    const KvSeq q = kv_seq(s, i, true);
+    if (!q.ok && blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+        kv_raise(status, KV_BAD_LENGTH);
+    const int start = q.len - q.n;
+    const int blk = start / KV_BLOCK + int(blockIdx.x);
+    if (q.n == 0 || blk * KV_BLOCK >= q.len)
+        return;
+    const int page = __builtin_amdgcn_readfirstlane(s.table[int64_t(i) * s.max_blocks + blk]);
+    const bool ok = kv_page_ok(page, c.n_pages);
+    if (!ok && threadIdx.x == 0)
+        kv_raise(status, KV_BAD_PAGE);
+    const int lo = max(start - blk * KV_BLOCK, 0), hi = min(q.len - blk * KV_BLOCK, KV_BLOCK);
+    const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
+    const int64_t dst0 = int64_t(q.row0) + (blk * KV_BLOCK - start);
+    const uint8_t *base = c.data + kv_offset(ok ? page : 0, h, c.H, D);
+    const float *sc = c.scales + (int64_t(ok ? page : 0) * c.H + h) * 2;
+    uint2 w[2][R::N];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int p = 0; p < R::N; ++p) {
+            const int r = r0 + p * R::ROWS;
+            w[j][p] = make_uint2(0, 0);                    // a bad page reads as zeros
+            if (ok && r >= lo && r < hi)
+                w[j][p] = *reinterpret_cast<const uint2 *>(base + j * (KV_BLOCK * D) + r * D + chunk * 8);
+        }
+    const float scale[2] = {ok ? sc[0] : 0.0f, ok ? sc[1] : 0.0f};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int p = 0; p < R::N; ++p) {
+            const int r = r0 + p * R::ROWS;
+            if (r >= lo && r < hi) {
+                const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * scale[j], b = kv_unpack4<FMT>(w[j][p].y) * scale[j];
+                uint16_t *o = (j ? v + (dst0 + r) * v_stride : k + (dst0 + r) * k_stride) + h * D + chunk * 8;
+                *reinterpret_cast<u32x4 *>(o) = u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                                      pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+            }
+        }
+}
+
+// ---------------------------------------------------------------- evict
+//
+// Selection, one 1024-thread workgroup per (head, sequence): token t of the
+// chunk sits in round t / 1024 of thread t % 1024, so a wavefront's round is 64
+// consecutive tokens and reads one page's weights (256 bytes).  The weight of
+// the last kept token is found by three rounds of histograms over 11, 11 and
+// 10 bits of the order-preserving key; equal weights are kept from the lowest
+// index on, by a prefix count in index order.  Sequences of up to
+// 1024 * ROUNDS tokens keep their keys in registers through all passes; longer
+// ones read them again in chunks of that size.
+constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64, BINS = 2048;
+
+// Order-preserving key of a weight: larger weights have larger keys, -0 is
+// +0, NaN is below everything.
+__device__ __forceinline__ uint32_t mass_key(float m)
+{
+    if (m != m)
+        return 0u;
+    const uint32_t u = __float_as_uint(m == 0.0f ? 0.0f : m);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+template <int ROUNDS>
+__global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, KvSeqs s, int32_t *__restrict__ keep,
+                                                                   int32_t *__restrict__ new_lens, int budget, int sinks,
+                                                                   int recent, uint32_t *status)
+{
+    constexpr int CHUNK = SELECT_THREADS * ROUNDS;
+    __shared__ int hist[BINS];
+    __shared__ int counts[ROUNDS * SELECT_WAVES];
+    __shared__ int part[SELECT_WAVES];
+    __shared__ int found[2];
+    const int h = blockIdx.x, i = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const KvSeq q = kv_seq(s, i, false);
+    if (!q.ok && tid == 0)
+        kv_raise(status, KV_BAD_LENGTH);
+    const int len = q.len, kept = min(len, budget);
+    int32_t *out = keep + (int64_t(i) * c.H + h) * budget;
+    if (h == 0 && tid == 0)
+        new_lens[i] = kept;
+    for (int t = kept + tid; t < budget; t += SELECT_THREADS)
+        out[t] = -1;
+    if (len <= budget) {
+        for (int t = tid; t < len; t += SELECT_THREADS)
+            out[t] = t;
+        return;
+    }
+    const int first = sinks, last = len - recent;          // candidates [first, last); first <= last as sinks + recent <= budget < len
+    const int want = budget - sinks - recent;              // of them to keep
+    const int32_t *table = s.table + int64_t(i) * s.max_blocks;
+    const int chunks = (len + CHUNK - 1) / CHUNK;
+    uint32_t key[ROUNDS];
+    bool bad = false;
+    auto load = [&](int base) {
+        int page[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int t = base + r * SELECT_THREADS + wave * 64;
+            page[r] = t < len ? table[t / KV_BLOCK] : -1;
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int t = base + r * SELECT_THREADS + tid;
+            const bool ok = kv_page_ok(page[r], c.n_pages);
+            bad |= t < len && !ok;
+            key[r] = 0;                                    // (a bad page's tokens go first)
+            if (t < len && ok)
+                key[r] = mass_key(c.mass[(int64_t(page[r]) * c.H + h) * KV_BLOCK + lane]);
+        }
+    };
+    auto candidate = [&](int t) { return t >= first && t < last; };
+
+    // ---- the key of the last kept candidate, and how many equal ones are kept
+    uint32_t prefix = 0, mask = 0;
+    int rest = want;
+    if (chunks == 1)
+        load(0);
+    if (want > 0) {
+        constexpr int SHIFT[3] = {21, 10, 0}, WIDTH[3] = {11, 11, 10};
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const uint32_t digits = (1u << WIDTH[pass]) - 1;
+            for (int b = tid; b < BINS; b += SELECT_THREADS)
+                hist[b] = 0;
+            __syncthreads();
+            for (int ch = 0; ch < chunks; ++ch) {
+                if (chunks > 1)
+                    load(ch * CHUNK);
+#pragma unroll
+                for (int r = 0; r < ROUNDS; ++r) {
+                    const bool in = candidate(ch * CHUNK + r * SELECT_THREADS + tid) && (key[r] & mask) == prefix;
+                    const uint32_t d = (key[r] >> SHIFT[pass]) & digits;
+                    const uint64_t who = __ballot(in);
+                    if (who == 0)
+                        continue;
+                    // one addition where the whole wavefront agrees (all weights zero, or equal)
+                    const int leader = __ffsll((unsigned long long)who) - 1;
+                    const uint32_t d0 = __builtin_amdgcn_readlane(d, leader);
+                    if (__ballot(in && d != d0) == 0) {
+                        if (lane == leader)
+                            atomicAdd(&hist[d0], __popcll(who));
+                    } else if (in) {
+                        atomicAdd(&hist[d], 1);
+                    }
+                }
+            }
+            __syncthreads();
+            // thread t owns bins b, b - 1 counted from the top: find the bin where the running count reaches `rest`
+            const int b = BINS - 1 - 2 * tid;
+            const int n1 = hist[b], n0 = hist[b - 1];
+            const int incl = wave_scan_incl(n1 + n0);
+            if (lane == 63)
+                part[wave] = incl;
+            __syncthreads();
+            int before = incl - (n1 + n0);
+            for (int w = 0; w < wave; ++w)
+                before += part[w];
+            if (before < rest && before + n1 + n0 >= rest) {
+                const bool second = before + n1 < rest;
+                found[0] = second ? b - 1 : b;
+                found[1] = rest - before - (second ? n1 : 0);
+            }
+            __syncthreads();
+            prefix |= uint32_t(found[0]) << SHIFT[pass];
+            mask |= digits << SHIFT[pass];
+            rest = found[1];                               // of the keys with this prefix, so many are kept
+            __syncthreads();
+        }
+    }
+
+    // ---- kept tokens in ascending order: ranks by prefix counts over (round, wavefront)
+    int done_eq = 0, done = 0;                             // equal keys and kept tokens of earlier chunks
+    constexpr int CELLS = ROUNDS * SELECT_WAVES;
+    static_assert(CELLS <= SELECT_THREADS, "one prefix per thread");
+    auto prefix_counts = [&]() {                           // counts[] -> exclusive prefixes; returns the total
+        __syncthreads();
+        const int v = tid < CELLS ? counts[tid] : 0;
+        const int incl = wave_scan_incl(v);
+        if (lane == 63)
+            part[wave] = incl;
+        __syncthreads();
+        int before = incl - v, total = 0;
+        for (int w = 0; w < SELECT_WAVES; ++w) {
+            before += w < wave ? part[w] : 0;
+            total += part[w];
+        }
+        if (tid < CELLS)
+            counts[tid] = before;
+        __syncthreads();
+        return total;
+    };
+    for (int ch = 0; ch < chunks; ++ch) {
+        if (chunks > 1 || want <= 0)
+            load(ch * CHUNK);
+        uint64_t eq[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            eq[r] = __ballot(want > 0 && candidate(ch * CHUNK + r * SELECT_THREADS + tid) && key[r] == prefix);
+            if (lane == 0)
+                counts[r * SELECT_WAVES + wave] = __popcll(eq[r]);
+        }
+        const int n_eq = prefix_counts();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int t = ch * CHUNK + r * SELECT_THREADS + tid;
+            const int rank = done_eq + counts[r * SELECT_WAVES + wave] + __popcll(eq[r] & lanemask_lt(lane));
+            const bool cand = candidate(t);
+            const bool in = t < len && (!cand || (want > 0 && (key[r] > prefix || (key[r] == prefix && rank < rest))));
+            eq[r] = __ballot(in);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (lane == 0)
+                counts[r * SELECT_WAVES + wave] = __popcll(eq[r]);
+        const int n_in = prefix_counts();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            if (eq[r] >> lane & 1)
+                out[done + counts[r * SELECT_WAVES + wave] + __popcll(eq[r] & lanemask_lt(lane))] =
+                    ch * CHUNK + r * SELECT_THREADS + tid;
+        done_eq += n_eq;
+        done += n_in;
+        __syncthreads();
+    }
+    if (bad)
+        kv_raise(status, KV_BAD_PAGE);
+}
+
+// The kept tokens, copied to their new pages: one workgroup per (new block,
+// head, sequence) gathers 64 rows of K and V and codes them again under the
+// block's own scale, as an append of their values to an empty page would.
+template <int FMT, int D>
+__global__ void __launch_bounds__(256) kv_compact_kernel(KvCache c, KvSeqs s, const int32_t *__restrict__ dst_table,
+                                                         int dst_blocks, const int32_t *__restrict__ keep, int budget,
+                                                         uint32_t *status)
+{
+    using R = RowChunks<D>;
+    __shared__ float part[8];
+    __shared__ int row_page[KV_BLOCK], row_slot[KV_BLOCK];
+    const int b = blockIdx.x, h = blockIdx.y, i = blockIdx.z;
+    const KvSeq q = kv_seq(s, i, false);
+    const int n = min(KV_BLOCK, min(q.len, budget) - b * KV_BLOCK);
+    if (n <= 0)
+        return;
+    const int to = __builtin_amdgcn_readfirstlane(dst_table[int64_t(i) * dst_blocks + b]);
+    if (!kv_page_ok(to, c.n_pages)) {
+        if (threadIdx.x == 0)
+            kv_raise(status, KV_BAD_PAGE);
+        return;
+    }
+    if (threadIdx.x < KV_BLOCK) {
+        int page = -1, slot = 0;
+        if (int(threadIdx.x) < n) {
+            const int t = keep[(int64_t(i) * c.H + h) * budget + b * KV_BLOCK + threadIdx.x];
+            page = s.table[int64_t(i) * s.max_blocks + t / KV_BLOCK];
+            slot = t % KV_BLOCK;
+            if (!kv_page_ok(page, c.n_pages))
+                page = -1;
+        }
+        row_page[threadIdx.x] = page;
+        row_slot[threadIdx.x] = slot;
+        if (int(threadIdx.x) < n)
+            c.mass[(int64_t(to) * c.H + h) * KV_BLOCK + threadIdx.x] =
+                page < 0 ? 0.0f : c.mass[(int64_t(page) * c.H + h) * KV_BLOCK + slot];
+    }
+    __syncthreads();
+    const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
+    uint2 w[2][R::N];
+    float sc[2][R::N];
+#pragma unroll
+    for (int p = 0; p < R::N; ++p) {
+        const int r = r0 + p * R::ROWS;
+        const int page = row_page[r];
+        const int64_t at = kv_offset(max(page, 0), h, c.H, D) + row_slot[r] * D + chunk * 8;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w[j][p] = make_uint2(0, 0);
+            sc[j][p] = 0.0f;
+            if (page >= 0) {
+                w[j][p] = *reinterpret_cast<const uint2 *>(c.data + at + j * (KV_BLOCK * D));
+                sc[j][p] = c.scales[(int64_t(page) * c.H + h) * 2 + j];
+            }
+        }
+    }
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float m = 0.0f;
+#pragma unroll
+        for (int p = 0; p < R::N; ++p) {
+            const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * sc[j][p], d = kv_unpack4<FMT>(w[j][p].y) * sc[j][p];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                m = fmaxf(m, fmaxf(fabsf(a[e]), fabsf(d[e])));
+        }
+        top[j] = block_max256(m, part + 4 * j);
+    }
+    uint8_t *base = c.data + kv_offset(to, h, c.H, D);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float scale = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT));
+#pragma unroll
+        for (int p = 0; p < R::N; ++p) {
+            const int r = r0 + p * R::ROWS;
+            if (r < n) {
+                const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * sc[j][p], d = kv_unpack4<FMT>(w[j][p].y) * sc[j][p];
+                *reinterpret_cast<uint2 *>(base + j * (KV_BLOCK * D) + r * D + chunk * 8) =
+                    make_uint2(kv_pack4<FMT>(a[0] / scale, a[1] / scale, a[2] / scale, a[3] / scale),
+                               kv_pack4<FMT>(d[0] / scale, d[1] / scale, d[2] / scale, d[3] / scale));
+            }
+        }
+        if (threadIdx.x == 0)
+            c.scales[(int64_t(to) * c.H + h) * 2 + j] = scale;
+    }
+}
+
+// Calls f with the format and head size as constants.
+template <typename F>
+void with_shape(int fmt, int D, F f)
+{
+    auto by_d = [&](auto fm) {
+        if (D == 64)
+            f(fm, std::integral_constant<int, 64>{});
+        else if (D == 128)
+            f(fm, std::integral_constant<int, 128>{});
+        else
+            f(fm, std::integral_constant<int, 256>{});
+    };
+    if (fmt == KV_INT8)
+        by_d(std::integral_constant<int, KV_INT8>{});
+    else
+        by_d(std::integral_constant<int, KV_E4M3>{});
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,
+                            int64_t k_stride, int64_t v_stride, uint32_t *status, hipStream_t st)
+{
+    // n rows from any position touch at most (n + 126) / 64 blocks
+    const dim3 grid((s.max_rows + 126) / KV_BLOCK, c.H, s.S);
+    with_shape(fmt, c.D, [&](auto f, auto d) {
+        launch_k(kv_append_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, c, s, k, v, k_stride,
+                 v_stride, status);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvCache &c, int fmt, const KvSeqs &s, uint16_t *k, uint16_t *v, int64_t k_stride,
+                          int64_t v_stride, uint32_t *status, hipStream_t st)
+{
+    const dim3 grid((s.max_rows + 126) / KV_BLOCK, c.H, s.S);
+    with_shape(fmt, c.D, [&](auto f, auto d) {
+        launch_k(kv_read_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, c, s, k, v, k_stride,
+                 v_stride, status);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_evict(const KvCache &c, int fmt, const KvSeqs &s, const int32_t *dst_table, int dst_blocks,
+                           int32_t *new_lens, int32_t *keep, int budget, int sinks, int recent, uint32_t *status,
+                           hipStream_t st)
+{
+    const dim3 grid(c.H, s.S);
+    if (s.max_len <= 4 * SELECT_THREADS)
+        launch_k(kv_select_kernel<4>, grid, SELECT_THREADS, 0, st, c, s, keep, new_lens, budget, sinks, recent, status);
+    else if (s.max_len <= 16 * SELECT_THREADS)
+        launch_k(kv_select_kernel<16>, grid, SELECT_THREADS, 0, st, c, s, keep, new_lens, budget, sinks, recent, status);
+    else
+        launch_k(kv_select_kernel<64>, grid, SELECT_THREADS, 0, st, c, s, keep, new_lens, budget, sinks, recent, status);
+    hipError_t e = hipGetLastError();
+    const int blocks = (std::min(budget, s.max_len) + KV_BLOCK - 1) / KV_BLOCK;
+    if (e != hipSuccess || blocks == 0)
+        return e;
+    with_shape(fmt, c.D, [&](auto f, auto d) {
+        launch_k(kv_compact_kernel<decltype(f)::value, decltype(d)::value>, dim3(blocks, c.H, s.S), 256, 0, st, c, s,
+                 dst_table, dst_blocks, static_cast<const int32_t *>(keep), budget, status);
+    });
+    return hipGetLastError();
+}
+
+}  // namespace msi

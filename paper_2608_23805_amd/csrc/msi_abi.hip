@@ -115,6 +115,8 @@ struct FwdBufs {
 
 }  // namespace
 
+int32_t msi::abi_error(int32_t status, const char *text) { return fail(status, text); }
+
 // Scratch of msi_moe_forward_noalloc: the act and y parts of a forward's
 // workspace live here, so that entry point needs no allocation.  Each device
 // the library runs on holds its own copy for the life of the process; host
