@@ -9,32 +9,42 @@ namespace msi {
 
 namespace {
 
-// exact: expf and a true division, erff, tanhf
+// SiLU and the tanh form share z / (1 + e^-u) (u = z, or twice the tanh's
+// argument), with expf and a true division.  GELU takes Phi(-|z|) from erfc by
+// formula 7.1.26 of Abramowitz and Stegun, a polynomial in 1 / (1 + p x) times
+// e^-x^2 with an error under 1.5e-7 of erf, x = |z| / sqrt(2): a quarter of the
+// instructions of erff, and no cancellation for negative z.
 template <int ACT>
 __device__ __forceinline__ float activate(float z)
 {
-    if constexpr (ACT == LINEAR_SILU)
+    if constexpr (ACT == LINEAR_SILU) {
         return silu(z);
-    else if constexpr (ACT == LINEAR_GELU)
-        return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    else if constexpr (ACT == LINEAR_GELU_TANH)
-        return 0.5f * z * (1.0f + tanhf(0.79788456080286536f * (z + 0.044715f * z * z * z)));
-    else
+    } else if constexpr (ACT == LINEAR_GELU_TANH) {
+        return z / (1.0f + expf(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
+    } else if constexpr (ACT == LINEAR_GELU) {
+        const float x = fabsf(z) * 0.70710678118654752f;
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+        float p = fmaf(1.061405429f, t, -1.453152027f);
+        p = fmaf(p, t, 1.421413741f);
+        p = fmaf(p, t, -0.284496736f);
+        p = fmaf(p, t, 0.254829592f);
+        const float q = 0.5f * p * t * __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);
+        return fmaxf(z, 0.0f) - fminf(fabsf(z), 3.0e38f) * q;
+    } else {
         return z;
+    }
 }
 
-// Four consecutive features n .. n + 3 of row m leave together.
+// Features n .. n + 3 of row m leave: act(v + bias) + residual; bias: their
+// four (zero past N).
 template <int ACT>
-__device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f32x4 v)
+__device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f32x4 v, const f32x4 &bias)
 {
-    if (n >= A.N)
-        return;
-    if (A.vec4) {
-        if (A.bias)
-            v += *reinterpret_cast<const f32x4 *>(A.bias + n);
+    v += bias;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = activate<ACT>(v[i]);
+    for (int i = 0; i < 4; ++i)
+        v[i] = activate<ACT>(v[i]);
+    if (A.vec4) {
         if (A.res_f32) {
             v += *reinterpret_cast<const f32x4 *>(A.res_f32 + m * A.res_stride + n);
         } else if (A.res_bf16) {
@@ -46,13 +56,13 @@ __device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f3
             *reinterpret_cast<f32x4 *>(A.out_f32 + m * A.out_stride + n) = v;
         else
             *reinterpret_cast<uint2 *>(A.out_bf16 + m * A.out_stride + n) =
-                make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                make_uint2(pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3]));
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (n + i < A.N) {
-            float z = activate<ACT>(A.bias ? v[i] + A.bias[n + i] : v[i]);
+            float z = v[i];
             if (A.res_f32)
                 z += A.res_f32[m * A.res_stride + n + i];
             else if (A.res_bf16)
@@ -64,132 +74,105 @@ __device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f3
         }
 }
 
-// ---------------------------------------------------------------- few rows
-//
-// Up to 16 MT rows: bound by streaming W.  A workgroup of eight wavefronts
-// owns 16 features; each wavefront an eighth of K (in whole 64-element
-// pieces), so that a CU has many loads in flight however few features there
-// are; the eight sums meet in LDS in a fixed order.
-constexpr int FEW_WAVES = 8;
-
-template <int ACT, int MT>
-__global__ void __launch_bounds__(64 * FEW_WAVES) linear_few_kernel(LinearArgs A)
+__device__ __forceinline__ f32x4 bias4(const LinearArgs &A, int n)
 {
-    __shared__ float sums[FEW_WAVES][MT][16][20];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int col = lane & 15, j = lane >> 4;
-    const int n0 = int(blockIdx.x) * 16;
-    const int K = A.K, pieces = (K + 63) / 64, per = (pieces + FEW_WAVES - 1) / FEW_WAVES;
-    const int p0 = wave * per, p1 = min(p0 + per, pieces);
-    const uint16_t *wr = A.w + int64_t(min(n0 + col, A.N - 1)) * K + 8 * j;
-    const uint16_t *xr[MT];
+    f32x4 b{0.f, 0.f, 0.f, 0.f};
+    if (A.bias)
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-        xr[t] = A.x + int64_t(min(16 * t + col, A.M - 1)) * A.x_stride + 8 * j;
-    f32x4 acc[MT];
+        for (int i = 0; i < 4; ++i)
+            b[i] = n + i < A.N ? A.bias[n + i] : 0.0f;
+    return b;
+}
+
+// A wavefront's block of 16 MB rows x 16 NB features leaves through LDS of its
+// own (`mine`, 16 rows at a time), so that rows are read (residual) and written
+// in runs of 16 NB features and the epilogue's code is small.  Lane (row, group)
+// of an MFMA block holds four consecutive features of one row.
+template <int ACT, int NB, int MB>
+__device__ __forceinline__ void store_block(const LinearArgs &A, float *mine, const f32x4 (&acc)[NB][MB], int m0, int rows,
+                                            int n0)
+{
+    constexpr int W = 16 * NB, LD = W + 4, LPR = W / 4, RPI = 64 / LPR;   // lanes of a row, rows of a pass
+    const int lane = threadIdx.x & 63;
+    const int n = n0 + 4 * (lane % LPR), r0 = lane / LPR;
+    const f32x4 bias = bias4(A, n);
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-        acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const u32x4 zero{0, 0, 0, 0};
-    auto piece = [&](int p, u32x4 (&w)[2], u32x4 (&x)[MT][2]) {
+    for (int q = 0; q < MB; ++q) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const int k = 64 * p + 32 * c;
-            const bool in = k + 8 * j < K;           // K is a multiple of 8
-            w[c] = in ? load_stream16(wr + k) : zero;
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                x[t][c] = in ? *reinterpret_cast<const u32x4 *>(xr[t] + k) : zero;
+        for (int a = 0; a < NB; ++a)
+            *reinterpret_cast<f32x4 *>(mine + (lane & 15) * LD + 16 * a + 4 * (lane >> 4)) = acc[a][q];
+        // (a wavefront's LDS operations are in order; the fences keep the compiler from moving them)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll 2
+        for (int r = r0; r < 16; r += RPI) {
+            const int m = 16 * q + r;
+            if (m < rows && n < A.N)
+                store4<ACT>(A, int64_t(m0) + m, n, *reinterpret_cast<const f32x4 *>(mine + r * LD + 4 * (lane % LPR)), bias);
         }
-    };
-    auto mma = [&](const u32x4 (&w)[2], const u32x4 (&x)[MT][2]) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                acc[t] = mfma16(as_bf16x8(w[c]), as_bf16x8(x[t][c]), acc[t]);
-    };
-    constexpr int U = MT == 1 ? 4 : 2;               // pieces in flight
-    int p = p0;
-    for (; p + U <= p1; p += U) {
-        u32x4 w[U][2], x[U][MT][2];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            piece(p + u, w[u], x[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            mma(w[u], x[u]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     }
-    for (; p < p1; ++p) {
-        u32x4 w[2], x[MT][2];
-        piece(p, w, x);
-        mma(w, x);
-    }
-    // lane (col, j) holds features 4 j .. 4 j + 3 of row col
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        *reinterpret_cast<f32x4 *>(&sums[wave][t][col][4 * j]) = acc[t];
-    __syncthreads();
-    if (wave < MT) {
-        f32x4 v = *reinterpret_cast<const f32x4 *>(&sums[0][wave][col][4 * j]);
-#pragma unroll
-        for (int u = 1; u < FEW_WAVES; ++u)
-            v += *reinterpret_cast<const f32x4 *>(&sums[u][wave][col][4 * j]);
-        const int m = 16 * wave + col;
-        if (m < A.M)
-            store4<ACT>(A, m, n0 + 4 * j, v);
-    }
+}
+
+// Tile t of a launch as (row tile, feature tile): bands of 8 row tiles, down
+// the band before the next feature tile, so that the tiles one XCD works on
+// together (xcd_swizzle gives it a contiguous range) share rows on both sides.
+__device__ __forceinline__ int2 tile_at(int t, int ntm, int ntn)
+{
+    const int band = t / (8 * ntn), in = t - band * 8 * ntn;
+    const int height = min(8, ntm - 8 * band);
+    return make_int2(8 * band + in % height, in / height);
 }
 
 // ---------------------------------------------------------------- tiles
 //
-// BM rows x TN features a workgroup; K in stages of 64 elements copied
-// straight into one of NBUF LDS buffers, NBUF - 1 in flight; WR x WC
-// wavefronts of 16 x 16 x 32 MFMAs with the weights as the A operand, so a lane
-// ends with four consecutive features of a row.  Slot s of stage row r holds
+// BM rows x TN features a workgroup; K in stages of 64 KG elements copied
+// straight into one of NBUF LDS buffers, NBUF - 1 in flight.  KG groups of WR x
+// WC wavefronts each multiply their own 64 elements of a stage (16 x 16 x 32
+// MFMAs with the weights as the A operand, so a lane ends with four
+// consecutive features of a row) and their sums meet in LDS in a fixed order.
+// Without the groups a stage's barrier, copies, fragment reads and few MFMAs
+// follow each other with nothing beside them.  Slot s of stage row r holds
 // 16-byte chunk s ^ ((r / 2) % 8), which spreads a fragment read over the banks.
-template <int BM_, int TN_, int WR_, int WC_, int NBUF_, int WPC_>
+template <int BM_, int TN_, int WR_, int WC_, int KG_, int NBUF_, int WPC_>
 struct LinearShape {
-    static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, NBUF = NBUF_, WPC = WPC_;
-    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
-    static constexpr int BK = 64, ROWB = BK * 2;
-    static constexpr int STAGE = (BM + TN) * ROWB;
+    static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, KG = KG_, NBUF = NBUF_, WPC = WPC_;
+    static constexpr int WAVES = WR * WC * KG, THREADS = 64 * WAVES;
+    static constexpr int ROWB = 128, SLICE = (BM + TN) * ROWB, STAGE = KG * SLICE;
     static constexpr int MB = BM / WR / 16, NB = TN / WC / 16;
-    static constexpr int LA = BM / 8 / WAVES, LB = TN / 8 / WAVES, LPS = LA + LB;
+    static constexpr int LA = KG * BM / 8 / WAVES, LB = KG * TN / 8 / WAVES, LPS = LA + LB;
+    static constexpr int SUMS = (KG - 1) * BM * TN * 4 + WR * WC * 16 * (16 * NB + 4) * 4;   // LDS of the epilogue
     static constexpr size_t LDS = size_t(NBUF) * STAGE;
-    static_assert(BM % (8 * WAVES) == 0 && TN % (8 * WAVES) == 0 && LDS * WPC <= 160 * 1024, "");
+    static_assert(KG * BM % (8 * WAVES) == 0 && KG * TN % (8 * WAVES) == 0 && LDS * WPC <= 160 * 1024, "");
+    static_assert(SUMS <= int(LDS) && LA <= 16 && LB <= 16 && LPS * (NBUF - 2) < 64, "");
 };
-using Tile64 = LinearShape<64, 64, 2, 2, 4, 2>;
-using Tile128 = LinearShape<128, 128, 2, 2, 2, 2>;
-using Tile256 = LinearShape<256, 256, 4, 2, 2, 1>;
 
 template <int ACT, class S>
 __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile_kernel(LinearArgs A)
 {
     constexpr int BM = S::BM, TN = S::TN, NBUF = S::NBUF, WAVES = S::WAVES, ROWB = S::ROWB, STAGE = S::STAGE, MB = S::MB,
-                  NB = S::NB, LA = S::LA, LB = S::LB, LPS = S::LPS;
+                  NB = S::NB, LA = S::LA, LB = S::LB, LPS = S::LPS, KG = S::KG;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
-    const int ntn = (A.N + TN - 1) / TN;
-    const int t = xcd_swizzle(int(blockIdx.x), int(gridDim.x));
-    const int m0 = (t / ntn) * BM, n0 = (t % ntn) * TN;
+    const int2 at = tile_at(xcd_swizzle(int(blockIdx.x), int(gridDim.x)), (A.M + BM - 1) / BM, (A.N + TN - 1) / TN);
+    const int m0 = at.x * BM, n0 = at.y * TN;
     const int K = A.K;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int rl = lane >> 3, sl = lane & 7;
     const int vm = min(BM, A.M - m0), vn = min(TN, A.N - n0);
-    // offsets from the tile's first rows (under 2^31: the caller's strides are bounded)
+    // offsets from the tile's first rows (under 2^31: the caller's strides are bounded); copy c of the workgroup
+    // brings 8 rows of slice c / (BM / 8)
     uint32_t aoff[LA], boff[LB];
     int last = 0;                                 // bit i: A copy i of the last stage lies past K; bit 16 + i: B copy i
-    const int nstage = (K + 63) / 64, tail = K - 64 * (nstage - 1);
+    const int nstage = (K + 64 * KG - 1) / (64 * KG), tail = K - 64 * KG * (nstage - 1);
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        const int r = 8 * (WAVES * i + wave) + rl, ch = sl ^ ((r >> 1) & 7);
+        const int c = WAVES * i + wave, r = 8 * (c % (BM / 8)) + rl, ch = 8 * (c / (BM / 8)) + (sl ^ ((r >> 1) & 7));
         aoff[i] = uint32_t(min(r, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(ch << 4);
         last |= int(8 * ch >= tail) << i;
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        const int r = 8 * (WAVES * i + wave) + rl, ch = sl ^ ((r >> 1) & 7);
+        const int c = WAVES * i + wave, r = 8 * (c % (TN / 8)) + rl, ch = 8 * (c / (TN / 8)) + (sl ^ ((r >> 1) & 7));
         boff[i] = uint32_t(min(r, vn - 1)) * uint32_t(K * 2) + uint32_t(ch << 4);
         last |= int(8 * ch >= tail) << (16 + i);
     }
@@ -197,21 +180,23 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
         const_cast<uint16_t *>(A.x + int64_t(m0) * A.x_stride), 0, 0x7fffffff, ring::RSRC_FLAGS);
     const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.w + int64_t(n0) * K), 0,
                                                                         0x7fffffff, ring::RSRC_FLAGS);
+    // a stage: the slices' A rows (KG BM of them), then their B rows
     auto issue = [&](int stage, int buf) {
         uint8_t *b = lds8 + buf * STAGE;
         // an offset past the buffer's end reads nothing and leaves zeros in LDS
-        const bool edge = stage == nstage - 1 && tail < 64;
+        const bool edge = stage == nstage - 1 && tail < 64 * KG;
+        const uint32_t kb = uint32_t(stage * (KG * ROWB));
 #pragma unroll
         for (int i = 0; i < LB; ++i)
-            dma16_lds(br, b + BM * ROWB + (WAVES * i + wave) * 1024,
-                      edge && (last >> (16 + i) & 1) ? 0x80000000u : boff[i] + uint32_t(stage * ROWB), 0);
+            dma16_lds(br, b + KG * BM * ROWB + (WAVES * i + wave) * 1024,
+                      edge && (last >> (16 + i) & 1) ? 0x80000000u : boff[i] + kb, 0);
 #pragma unroll
         for (int i = 0; i < LA; ++i)
-            dma16_lds(ar, b + (WAVES * i + wave) * 1024,
-                      edge && (last >> i & 1) ? 0x80000000u : aoff[i] + uint32_t(stage * ROWB), 0);
+            dma16_lds(ar, b + (WAVES * i + wave) * 1024, edge && (last >> i & 1) ? 0x80000000u : aoff[i] + kb, 0);
     };
     const int r16 = lane & 15, g = lane >> 4;
-    const int wm = wave / S::WC, wn = wave % S::WC;
+    const int grp = wave / (S::WR * S::WC), wi = wave % (S::WR * S::WC);
+    const int wm = wi / S::WC, wn = wi % S::WC;
     f32x4 acc[NB][MB];
 #pragma unroll
     for (int a = 0; a < NB; ++a)
@@ -219,17 +204,18 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
         for (int q = 0; q < MB; ++q)
             acc[a][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto compute = [&](int buf) {
-        const uint8_t *b = lds8 + buf * STAGE;
+        const uint8_t *xa = lds8 + buf * STAGE + (grp * BM + wm * MB * 16) * ROWB;
+        const uint8_t *wb = lds8 + buf * STAGE + (KG * BM + grp * TN + wn * NB * 16) * ROWB;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const uint32_t fo = uint32_t(r16 * ROWB + (((4 * kb + g) ^ ((r16 >> 1) & 7)) << 4));
             u32x4 fw[NB], fx[MB];
 #pragma unroll
             for (int a = 0; a < NB; ++a)
-                fw[a] = *reinterpret_cast<const u32x4 *>(b + (BM + (wn * NB + a) * 16) * ROWB + fo);
+                fw[a] = *reinterpret_cast<const u32x4 *>(wb + a * 16 * ROWB + fo);
 #pragma unroll
             for (int q = 0; q < MB; ++q)
-                fx[q] = *reinterpret_cast<const u32x4 *>(b + (wm * MB + q) * 16 * ROWB + fo);
+                fx[q] = *reinterpret_cast<const u32x4 *>(xa + q * 16 * ROWB + fo);
 #pragma unroll
             for (int q = 0; q < MB; ++q)
 #pragma unroll
@@ -257,14 +243,143 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
         cur = cur == NBUF - 1 ? 0 : cur + 1;
         nxt = nxt == NBUF - 1 ? 0 : nxt + 1;
     }
-#pragma unroll
-    for (int q = 0; q < MB; ++q) {
-        const int row = (wm * MB + q) * 16 + r16;
-        if (row < vm)
+    __syncthreads();                              // every fragment has been read: LDS changes its use
+    if constexpr (KG > 1) {
+        // groups 1 .. leave their sums, lane by lane; group 0 adds them in order
+        f32x4 *sums = reinterpret_cast<f32x4 *>(lds8 + S::WR * S::WC * 16 * (16 * NB + 4) * 4);
+        constexpr int PER = S::WR * S::WC * MB * NB * 64;
+        if (grp > 0) {
 #pragma unroll
             for (int a = 0; a < NB; ++a)
-                store4<ACT>(A, m0 + row, n0 + (wn * NB + a) * 16 + 4 * g, acc[a][q]);
+#pragma unroll
+                for (int q = 0; q < MB; ++q)
+                    sums[(grp - 1) * PER + ((wi * NB + a) * MB + q) * 64 + lane] = acc[a][q];
+        }
+        __syncthreads();
+        if (grp > 0)
+            return;
+        for (int o = 0; o < KG - 1; ++o)
+#pragma unroll
+            for (int a = 0; a < NB; ++a)
+#pragma unroll
+                for (int q = 0; q < MB; ++q)
+                    acc[a][q] += sums[o * PER + ((wi * NB + a) * MB + q) * 64 + lane];
     }
+    store_block<ACT, NB, MB>(A, reinterpret_cast<float *>(lds8) + wi * 16 * (16 * NB + 4), acc, m0 + wm * MB * 16,
+                             vm - wm * MB * 16, n0 + wn * NB * 16);
+}
+
+// ---------------------------------------------------------------- 256 x 256 tiles
+//
+// Many tiles: bound by the matrix cores.  Eight wavefronts as 4 (rows) x 2
+// (features), each 64 rows x 128 features; K in stages of 32 elements through
+// a ring of four LDS buffers; the fragments of stage s + 1 are read between the
+// MFMAs of stage s.  Every step issues the same copies (those past the last
+// stage read nothing), so every wait is for the same count.
+template <int ACT>
+__global__ void __launch_bounds__(ring::THREADS, 2) linear_ring_kernel(LinearArgs A)
+{
+    using namespace ring;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NBUF * STAGE];
+    const int2 at = tile_at(xcd_swizzle(int(blockIdx.x), int(gridDim.x)), (A.M + TM - 1) / TM, (A.N + TN - 1) / TN);
+    const int m0 = at.x * TM, n0 = at.y * TN;
+    const int K = A.K;
+    const int vm = min(TM, A.M - m0), vn = min(TN, A.N - n0);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    // copy i of this wavefront covers stage rows 16 (i WAVES + wave) + lane / 4; lane % 4 is the 16-byte slot it fills
+    const int rl = lane >> 2, ch = (lane & 3) ^ ring_swz(rl & 15);
+    uint32_t aoff[LA], boff[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i)
+        aoff[i] = uint32_t(min((i * WAVES + wave) * 16 + rl, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(ch << 4);
+#pragma unroll
+    for (int i = 0; i < LB; ++i)
+        boff[i] = uint32_t(min((i * WAVES + wave) * 16 + rl, vn - 1)) * uint32_t(K * 2) + uint32_t(ch << 4);
+    const int nstage = (K + SK - 1) / SK;
+    const bool past = SK * (nstage - 1) + 8 * ch >= K;      // this lane's chunk of the last stage lies past K
+    const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(A.x + int64_t(m0) * A.x_stride), 0, 0x7fffffff, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.w + int64_t(n0) * K), 0,
+                                                                        0x7fffffff, RSRC_FLAGS);
+    auto issue = [&](int stage) {
+        uint8_t *buf = lds + (stage % NBUF) * STAGE;
+        // offsets past the buffers' ends read nothing and leave zeros
+        const uint32_t none = stage >= nstage || (stage == nstage - 1 && past) ? 0x80000000u : 0u;
+        const uint32_t kb = uint32_t(stage * ROWB);
+#pragma unroll
+        for (int i = 0; i < LA; ++i)
+            dma16_lds(ar, buf + (i * WAVES + wave) * 1024, (aoff[i] + kb) | none, 0);
+#pragma unroll
+        for (int i = 0; i < LB; ++i)
+            dma16_lds(br, buf + TM * ROWB + (i * WAVES + wave) * 1024, (boff[i] + kb) | none, 0);
+    };
+    auto sync_stage = [&](auto waitn) {
+        __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(decltype(waitn)::value));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    using W_STEADY = std::integral_constant<int, LPS * (NBUF - 3)>;   // stage s+1 landed, s+2 in flight
+    using W_FIRST = std::integral_constant<int, LPS * (NBUF - 2)>;    // stage 0 landed, 1 and 2 in flight
+    const int wm = wave >> 1, wn = wave & 1;
+    const uint32_t fofs = uint32_t((lane & 15) * ROWB + (((lane >> 4) ^ ring_swz(lane & 15)) << 4));
+    auto wrow = [&](int a) { return wn * 128 + a * 16; };
+
+#pragma unroll
+    for (int s = 0; s < NBUF - 1; ++s)
+        issue(s);
+    sync_stage(W_FIRST{});
+    f32x4 acc[8][4];   // [feature block][row block]
+#pragma unroll
+    for (int a = 0; a < 8; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 fw[2][8], fx[4];
+    {
+        const uint8_t *b0 = lds + fofs;
+#pragma unroll
+        for (int a = 0; a < 8; ++a)
+            fw[0][a] = *reinterpret_cast<const u32x4 *>(b0 + TM * ROWB + wrow(a) * ROWB);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            fx[b] = *reinterpret_cast<const u32x4 *>(b0 + (wm * 64 + b * 16) * ROWB);
+    }
+    // MFMAs of stage s from fw[H] / fx, reading stage s+1's fragments (after the last stage those are never used)
+    auto step = [&](int s, auto h) {
+        constexpr int H = decltype(h)::value;
+        const uint8_t *nb = lds + ((s + 1) % NBUF) * STAGE + fofs;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+#pragma unroll
+            for (int a = 0; a < 8; ++a)
+                acc[a][b] = mfma16(as_bf16x8(fw[H][a]), as_bf16x8(fx[b]), acc[a][b]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                fw[H ^ 1][b * 2 + q] = *reinterpret_cast<const u32x4 *>(nb + TM * ROWB + wrow(b * 2 + q) * ROWB);
+            fx[b] = *reinterpret_cast<const u32x4 *>(nb + (wm * 64 + b * 16) * ROWB);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+    };
+    // (an odd last stage is followed by one of zeros)
+    for (int s = 0; s < nstage; s += 2) {
+        sync_stage(W_STEADY{});
+        issue(s + NBUF - 1);
+        step(s, std::integral_constant<int, 0>{});
+        sync_stage(W_STEADY{});
+        issue(s + NBUF);
+        step(s + 1, std::integral_constant<int, 1>{});
+    }
+    __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));    // the last copies (zeros) have landed,
+    __syncthreads();                              // every fragment has been read: LDS changes its use
+    store_block<ACT, 8, 4>(A, reinterpret_cast<float *>(lds) + wave * 16 * 132, acc, m0 + wm * 64, vm - wm * 64,
+                           n0 + wn * 128);
 }
 
 template <int ACT, class S>
@@ -279,23 +394,34 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t st)
     return hipGetLastError();
 }
 
+// The smallest tiles that give one to every CU at most, since one wave of
+// workgroups lasts as long as a tile does: a stage of 64 K elements takes a CU
+// 0.10 us with tiles of 32 x 32, 0.11 with 32 x 64, 0.19 with 64 x 64, 0.24 with 64 x 128, 0.42
+// with 128 x 128.  [us; 16 rows, K 2048, N 5120: 7.0 / 7.7 / 9.9 / 13.9 / 17.7; 256, 4096, 2048: 14.8 / 12.7 / 16.7
+// / 23.4 / 31.9; 509, 4096, 2048: 26.3 / 22.9 / 18.0 / 23.9 / 31.5; 1000, 1000, 3000: 27.7 / 30.9 / 20.0 / 20.9 / 14.1.]
+// Past that, 128 x 128 tiles two to a CU, about 1.0 us a pair and stage, or
+// 256 x 256 ones, about 1.85 us, whichever fills its rounds better [1024, 2048, 5120: 28.6
+// and 49.3; 4096, 4096, 2048: 63.5 and 88.4; 2048, 2048, 5120: 52.5 and 51.1; 4096, 2048, 8192: 133 and 121].
 template <int ACT>
 hipError_t launch_act(const LinearArgs &A, hipStream_t st)
 {
-    if (A.M <= 32) {
-        const unsigned grid = unsigned((A.N + 15) / 16);
-        if (A.M <= 16)
-            launch_k(linear_few_kernel<ACT, 1>, grid, 64 * FEW_WAVES, 0, st, A);
-        else
-            launch_k(linear_few_kernel<ACT, 2>, grid, 64 * FEW_WAVES, 0, st, A);
-        return hipGetLastError();
-    }
-    auto tiles = [&](int64_t b) { return (A.M + b - 1) / b * ((A.N + b - 1) / b); };
-    if (tiles(256) >= 256)
-        return launch_tile<ACT, Tile256>(A, st);
-    if (tiles(128) >= 256)
-        return launch_tile<ACT, Tile128>(A, st);
-    return launch_tile<ACT, Tile64>(A, st);
+    constexpr int64_t CUS = 256;
+    auto tiles = [&](int64_t m, int64_t n) { return (A.M + m - 1) / m * ((A.N + n - 1) / n); };
+    if (tiles(32, 32) <= CUS)
+        return launch_tile<ACT, LinearShape<32, 32, 2, 2, 2, 4, 2>>(A, st);
+    if (tiles(32, 64) <= CUS)
+        return launch_tile<ACT, LinearShape<32, 64, 1, 2, 4, 3, 1>>(A, st);
+    if (tiles(64, 64) <= CUS)
+        return launch_tile<ACT, LinearShape<64, 64, 2, 2, 2, 4, 1>>(A, st);
+    if (tiles(64, 128) <= CUS)
+        return launch_tile<ACT, LinearShape<64, 128, 2, 2, 2, 3, 1>>(A, st);
+    if (tiles(128, 128) <= CUS)
+        return launch_tile<ACT, LinearShape<128, 128, 4, 4, 1, 3, 1>>(A, st);
+    const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
+    if (37 * ((t256 + CUS - 1) / CUS) > 20 * ((t128 + 2 * CUS - 1) / (2 * CUS)))
+        return launch_tile<ACT, LinearShape<128, 128, 4, 2, 1, 2, 2>>(A, st);
+    launch_k(linear_ring_kernel<ACT>, unsigned(t256), ring::THREADS, 0, st, A);
+    return hipGetLastError();
 }
 
 }  // namespace

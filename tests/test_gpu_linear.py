@@ -65,9 +65,15 @@ def test_in_place(M, kind):
     _case(M, 128, 192, residual=kind, out=kind, inplace=True)
 
 
-@pytest.mark.parametrize("M,K,N", [(2100, 136, 2080), (4096, 64, 4100), (1030, 200, 4097)])
-def test_large_tiles(M, K, N):
+@pytest.mark.parametrize("M,K,N", [
+    (33, 1000, 4095), (70, 392, 5003),                       # 32 x 32, 32 x 64
+    (300, 520, 3000), (511, 136, 2048), (260, 264, 8100),    # 64 x 64, 64 x 128
+    (1000, 200, 3001), (1030, 200, 4097), (2050, 72, 2050),  # 128 x 128, one and two to a CU
+    (4096, 64, 4100), (2100, 136, 8192), (8200, 8, 2049),    # 256 x 256, odd numbers of stages
+])
+def test_every_tile(M, K, N):
     _case(M, K, N, act="silu", residual="bf16", out="bf16")
+    _case(M, K, N, act="none", residual="none", out="f32", pad=8)
 
 
 def test_infinite_activation_arguments():
