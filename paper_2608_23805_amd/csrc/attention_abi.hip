@@ -89,6 +89,8 @@ const char *check_heads(const KvCache &c, const KvSeqs &s, uint32_t n_q_heads)
         return "n_q_heads must be a multiple of n_heads, at most 4096";
     if (uint64_t(s.max_rows) * (n_q_heads / c.H) > MOST)
         return "max_rows times the heads of a group must be at most 2^30";
+    if (uint64_t(s.S) * ((s.max_len + KV_BLOCK - 1) / KV_BLOCK) > MOST)
+        return "n_seqs times the blocks of max_len must be at most 2^30";
     return nullptr;
 }
 
@@ -196,7 +198,7 @@ msi_status msi_kv_attention_workspace(const msi_kv_cache *cache, const msi_kv_se
         return bad(e);
     *bytes = 0;
     if (s.S && s.max_rows) {
-        const AttentionCut cut = attention_cut(s.S, c.H, int(n_q_heads) / c.H, c.D, s.max_rows, s.max_len, mass_rows != 0);
+        const AttentionCut cut = attention_cut(s.S, c.H, int(n_q_heads) / c.H, c.D, c.n_pages, s.max_rows, s.max_len, mass_rows != 0);
         *bytes = cut.bytes + lse_bytes(cut, s, n_q_heads, mass_rows);
     }
     return MSI_OK;
@@ -229,7 +231,7 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     if (a->q == a->out)
         return bad("out must not be q");
     const AttentionCut cut =
-        attention_cut(s.S, c.H, int(a->n_q_heads) / c.H, c.D, s.max_rows, s.max_len, a->mass_rows != 0);
+        attention_cut(s.S, c.H, int(a->n_q_heads) / c.H, c.D, c.n_pages, s.max_rows, s.max_len, a->mass_rows != 0);
     const size_t lse = lse_bytes(cut, s, a->n_q_heads, a->mass_rows), need = cut.bytes + lse;
     if (need && (!a->workspace || a->workspace_bytes < need))
         return abi_error(MSI_E_NOMEM, "workspace smaller than msi_kv_attention_workspace says");
@@ -245,19 +247,20 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     A.out_stride = int64_t(a->out_stride);
     A.G = int(a->n_q_heads) / c.H;
     A.scale_log2 = float(double(a->scale) * 1.4426950408889634);
-    A.chunk = cut.chunk;
-    A.n_splits = cut.splits;
+    A.direct = cut.direct;
+    A.per = cut.per;
     A.part_rows = s.max_rows * A.G;
     if (cut.part_o > cut.part_ml)
         A.part_ml = reinterpret_cast<float *>(ws + cut.part_ml);
-    if (cut.splits > 1)
+    if (!cut.direct)
+        A.plan = reinterpret_cast<int2 *>(ws);
+    if (!cut.direct)
         A.part_o = reinterpret_cast<float *>(ws + cut.part_o);
     if (a->mass_rows && cut.few)
         A.scores = reinterpret_cast<float *>(ws + cut.scores);
+    A.score_blocks = cut.score_blocks;
     if (lse)
         A.lse = reinterpret_cast<float *>(ws + cut.bytes);
-    A.score_blocks = (s.max_len + KV_BLOCK - 1) / KV_BLOCK;
-    A.score_rows = A.part_rows;
     A.mass_rows = int(std::min(a->mass_rows, MOST));
     A.decay = a->mass_decay;
     A.status = a->status;

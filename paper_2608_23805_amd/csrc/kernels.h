@@ -303,11 +303,13 @@ hipError_t launch_kv_evict(const KvCache &c, int fmt, const KvSeqs &s, const int
 // ---- attention over the cache (kv_attention.hip)
 struct AttentionCut {
     bool few;                    // at most 32 packed rows a sequence and head
-    int tile_rows, tiles;        // packed rows of a workgroup, workgroups along them
-    int chunk, splits;           // blocks of a workgroup, workgroups along the cache
+    bool direct;                 // a unit is a whole sequence, results go straight to the output
+    int tile_rows, per;          // packed rows of a workgroup, workgroups (heads, row tiles) of a unit
+    int units;                   // bound of the units
+    int score_blocks;            // blocks of a sequence in the scores, 0: they go by page
     size_t part_ml, part_o, scores, bytes;   // workspace offsets and size
 };
-AttentionCut attention_cut(int S, int H, int G, int D, int max_rows, int max_len, bool mass);
+AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows, int max_len, bool mass);
 struct AttentionLaunch {
     KvCache c;
     KvSeqs s;
@@ -316,10 +318,11 @@ struct AttentionLaunch {
     int64_t q_stride, out_stride;   // elements from one row to the next
     int G;                       // query heads of a cache head
     float scale_log2;            // scale * log2(e): scores are powers of two
-    int chunk, n_splits, part_rows;
-    float *part_ml, *part_o;     // [S, H, splits, part_rows, 2 | D] maxima and sums, unnormalised outputs
-    float *scores;               // [S, score_blocks, H, score_rows, 64], or null
-    int score_blocks, score_rows;
+    int direct, per, part_rows;  // see AttentionCut; part_rows = max_rows * G
+    int2 *plan;                  // [S] first unit and number of units of a sequence that has tokens; null if direct
+    float *part_ml, *part_o;     // [units, H, part_rows, 2 | D] maxima and sums, unnormalised outputs
+    float *scores;               // [S * score_blocks | n_pages, H, part_rows, 64], or null
+    int score_blocks;
     float *lse;                  // [n_rows, H G] log2 of the rows' sums (many rows), or null
     int mass_rows;
     float decay;

@@ -81,13 +81,96 @@ __device__ __forceinline__ float vsum(float a, float b) { return a + b; }
 // Rows are numbered row * G + head of the group within a sequence and cache head.
 __device__ __forceinline__ int row_limit(const KvSeq &q, int token_row) { return q.len - q.n + token_row + 1; }
 
+// ---------------------------------------------------------------- units
+//
+// The caches of a call are cut into units of about equally many blocks, sized
+// on the device from the actual lengths, however ragged the batch is and
+// however loose the host's bounds are. Units
+// are numbered along the sequences, so the workgroups that have work come
+// first, and every wavefront finds its unit by a scan of the lengths (64
+// sequences a step; a few loads for a usual batch).  Where the host already
+// knows that cutting would gain nothing (A.direct), unit i is sequence i whole.
+__device__ __forceinline__ int blocks_of(const KvSeqs &s, int i)      // per lane
+{
+    if (i >= s.S)
+        return 0;
+    const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, false);
+    return q.n ? (q.len + KV_BLOCK - 1) / KV_BLOCK : 0;
+}
+
+struct Unit {
+    int seq, split, n, first;        // the split-th of the n units of sequence seq, which start at number `first`
+};
+
+// Blocks of a unit for `work` blocks in all (times heads and row tiles): one
+// workgroup per CU as long as each has at most 16 blocks, four a wavefront;
+// then units of 16, which hide their start and their partial results' way
+// through memory, until there are 2048 of them (131072 tokens of one sequence, 2 heads
+// of 256: 36 us with 16 blocks, 46 with 4; 48 sequences of up to 16384, 8 heads of 128:
+// 246, 233, 223 and 219 us with 256, 512, 1024 and 2048 workgroups).
+constexpr int LEAST_BLOCKS = 4, ENOUGH_BLOCKS = 16, FILL_WORKGROUPS = 256, MOST_WORKGROUPS = 2048;
+
+__device__ __forceinline__ int unit_chunk(int64_t work)
+{
+    const int64_t fill = (work + FILL_WORKGROUPS - 1) / FILL_WORKGROUPS;
+    if (fill <= ENOUGH_BLOCKS)
+        return max(int(fill), LEAST_BLOCKS);
+    return int(max(int64_t(ENOUGH_BLOCKS), (work + MOST_WORKGROUPS - 1) / MOST_WORKGROUPS));
+}
+
+// The unit numbered `at` (seq = -1: there are not so many).
+__device__ __forceinline__ Unit find_unit(const AttentionLaunch &A, int at)
+{
+    if (A.direct)
+        return Unit{at, 0, 1, at};
+    const int lane = threadIdx.x & 63;
+    const int mine = blocks_of(A.s, lane);
+    int total = mine;
+    for (int base = 64; base < A.s.S; base += 64)
+        total += blocks_of(A.s, base + lane);
+    total = __builtin_amdgcn_readlane(wave_scan_incl(total), 63);
+    const int chunk = unit_chunk(int64_t(total) * A.per);
+    int before = 0;
+    for (int base = 0; base < A.s.S; base += 64) {
+        const int b = base ? blocks_of(A.s, base + lane) : mine;
+        const int n = (b + chunk - 1) / chunk, incl = wave_scan_incl(n);
+        const uint64_t hit = __ballot(at < before + incl);
+        if (hit) {
+            const int l = __ffsll((unsigned long long)hit) - 1;
+            const int nl = __builtin_amdgcn_readlane(n, l), first = before + __builtin_amdgcn_readlane(incl, l) - nl;
+            return Unit{base + l, at - first, nl, first};
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    return Unit{-1, 0, 0, 0};
+}
+
+// Blocks [first, second) of a unit of a sequence of `blocks`.
+__device__ __forceinline__ int2 unit_blocks(const Unit &u, int blocks)
+{
+    return make_int2(int(int64_t(blocks) * u.split / u.n), int(int64_t(blocks) * (u.split + 1) / u.n));
+}
+
+// Index of a packed row's partial result.
+__device__ __forceinline__ int64_t part_index(const AttentionLaunch &A, int unit, int h, int r)
+{
+    return (int64_t(unit) * A.c.H + h) * A.part_rows + r;
+}
+
+// First score of a block: by page where the pool is smaller than the batch's tables.
+__device__ __forceinline__ int64_t score_index(const AttentionLaunch &A, int i, int blk, int page, int h, int row)
+{
+    const int64_t at = A.score_blocks ? int64_t(i) * A.score_blocks + blk : int64_t(page);
+    return ((at * A.c.H + h) * A.part_rows + row) * KV_BLOCK;
+}
+
 // ---------------------------------------------------------------- few rows
 //
 // Up to 16 RT packed rows (single tokens, drafted tokens): bound by reading the
 // cache.  No LDS on the way: the wavefront's loads are the MFMA operands.  A
-// workgroup of four wavefronts takes `chunk` blocks of a sequence's cache, the
-// wavefronts every fourth one; their results meet in LDS, and those of several
-// chunks in the join kernel.
+// workgroup of four wavefronts takes a unit's blocks, the wavefronts every
+// fourth one; their results meet in LDS, and those of a sequence's units in
+// the finish kernel.
 //
 // K: lane (i, j) = (lane % 16, lane / 16) reads 16 bytes 16 j of each 64-byte
 // piece of token 16 g + i; the elements of a reduction step of 32 are in the
@@ -97,7 +180,7 @@ __device__ __forceinline__ int row_limit(const KvSeq &q, int token_row) { return
 // transposes them in registers to eight tokens of each of its D / 16 elements.
 template <int FMT, int D, int RT>
 struct FewRows {
-    static constexpr int TOK = D == 256 ? 32 : KV_BLOCK;    // tokens of a step
+    static constexpr int TOK = D * RT >= 256 ? 32 : KV_BLOCK;    // tokens of a step: what fits the registers
     static constexpr int STEPS = KV_BLOCK / TOK;            // steps of a block
     static constexpr int GT = TOK / 16;                     // groups of 16 tokens
     static constexpr int KL = D / 64;                       // 16-byte loads of a K row per lane
@@ -118,7 +201,7 @@ struct FewRows {
         for (int g = 0; g < GT; ++g)
 #pragma unroll
             for (int l = 0; l < KL; ++l)
-                k[g][l] = load_stream16(p + 16 * g * D + 64 * l);
+                k[g][l] = *reinterpret_cast<const u32x4 *>(p + 16 * g * D + 64 * l);
     }
 
     static __device__ __forceinline__ void load_v(uint32_t (&v)[GT / 2][8][VW], const uint8_t *block, int step)
@@ -131,7 +214,7 @@ struct FewRows {
             for (int t = 0; t < 8; ++t) {
                 const uint8_t *a = p + (32 * u + (t < 4 ? t : 12 + t)) * D;
                 typedef __attribute__((ext_vector_type(VW))) uint32_t vec;
-                const vec w = __builtin_nontemporal_load(reinterpret_cast<const vec *>(a));
+                const vec w = *reinterpret_cast<const vec *>(a);
                 if constexpr (VW == 1) {
                     v[u][t][0] = w[0];
                 } else {
@@ -150,33 +233,42 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
     constexpr int TOK = F::TOK, GT = F::GT, W = F::W, VW = F::VW, OS = F::OS;
     __shared__ __attribute__((aligned(16))) float olds[4][16][OS];
     __shared__ float ml[4][RT][16][2];
+    constexpr bool QLDS = D == 256 && RT == 2;               // two tiles of long queries do not fit the registers
+    __shared__ bf16x8 qlds[QLDS ? RT * (D / 32) * 64 : 1];
 
-    const int i = blockIdx.z, split = blockIdx.x;
-    const int h = int(blockIdx.y) % A.c.H, tile = int(blockIdx.y) / A.c.H;
+    const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
+    if (unit.seq < 0)
+        return;
+    const int i = unit.seq, sub = int(blockIdx.x) % A.per, h = sub % A.c.H, tile = sub / A.c.H;
     const KvSeq q = kv_seq(A.s, i, false);
-    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+    if (!q.ok && sub == 0 && threadIdx.x == 0)
         kv_raise(A.status, KV_BAD_LENGTH);
+    if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
+        A.plan[i] = make_int2(unit.first, unit.n);
     const int rows = q.n * A.G, r0 = tile * 16 * RT;
     if (r0 >= rows)
         return;
-    const int b0 = split * A.chunk, b1 = min(b0 + A.chunk, (q.len + KV_BLOCK - 1) / KV_BLOCK);
-    const bool direct = A.n_splits == 1;
-    if (b0 >= b1 && !direct)
-        return;                                              // the join goes by the length too
+    const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+    const int b0 = range.x, b1 = range.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, j = lane >> 4;
 
-    // page of the l-th block of this wavefront in lane l
-    int pages = -1;
-    if (b0 + wave + 4 * lane < b1)
-        pages = A.s.table[int64_t(i) * A.s.max_blocks + b0 + wave + 4 * lane];
-    const bool known = kv_page_ok(pages, A.c.n_pages);
-    if (b0 + wave + 4 * lane < b1 && !known)
-        kv_raise(A.status, KV_BAD_PAGE);
-    if (!known)
-        pages = -1;
+    // pages of this wavefront's next 64 blocks, one a lane (-1: bad)
+    auto page_list = [&](int k) {
+        const int b = b0 + wave + 4 * (k + lane);
+        int page = -1;
+        if (b < b1) {
+            page = A.s.table[int64_t(i) * A.s.max_blocks + b];
+            if (!kv_page_ok(page, A.c.n_pages)) {
+                kv_raise(A.status, KV_BAD_PAGE);
+                page = -1;
+            }
+        }
+        return page;
+    };
+    int pages = page_list(0);
 
-    bf16x8 qf[RT][D / 32];
+    bf16x8 qf[QLDS ? 1 : RT][QLDS ? 1 : D / 32];
     int limit[RT];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
@@ -185,9 +277,24 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
         limit[x] = r < rows ? row_limit(q, tr) : 0;
         const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c)
-            qf[x][c] = *reinterpret_cast<const bf16x8 *>(src + 64 * (c / 2) + 16 * j + 8 * (c % 2));
+        for (int c = 0; c < D / 32; ++c) {
+            const bf16x8 v = *reinterpret_cast<const bf16x8 *>(src + 64 * (c / 2) + 16 * j + 8 * (c % 2));
+            if constexpr (QLDS) {
+                if (wave == 0)
+                    qlds[(x * (D / 32) + c) * 64 + lane] = v;
+            } else {
+                qf[x][c] = v;
+            }
+        }
     }
+    if constexpr (QLDS)
+        __syncthreads();
+    auto query = [&](int x, int c) {
+        if constexpr (QLDS)
+            return qlds[(x * (D / 32) + c) * 64 + lane];
+        else
+            return qf[x][c];
+    };
 
     f32x4 acc[RT][W];
     float m[RT], l[RT];
@@ -202,28 +309,28 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
 
     const int nb = b1 - b0 > wave ? (b1 - b0 - wave + 3) / 4 : 0;      // blocks of this wavefront
     const int steps = nb * F::STEPS;
-    auto block_at = [&](int s) {
-        const int page = __builtin_amdgcn_readlane(pages, s / F::STEPS);
-        return A.c.data + kv_offset(max(page, 0), h, A.c.H, D);
-    };
-    auto scales_at = [&](int s) {
-        const int page = __builtin_amdgcn_readlane(pages, s / F::STEPS);
+    auto block_at = [&](int page) { return A.c.data + kv_offset(max(page, 0), h, A.c.H, D); };
+    auto scales_at = [&](int page) {
         return *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(max(page, 0)) * A.c.H + h) * 2);
     };
     typename F::Codes cur;
     float2 sc{1.0f, 1.0f};
+    int page = __builtin_amdgcn_readlane(pages, 0);
     if (steps > 0) {
-        sc = scales_at(0);
-        F::load_k(cur.k, block_at(0), 0);
-        F::load_v(cur.v, block_at(0), 0);
+        sc = scales_at(page);
+        F::load_k(cur.k, block_at(page), 0);
+        F::load_v(cur.v, block_at(page), 0);
     }
     for (int s = 0; s < steps; ++s) {
         const int blk = b0 + wave + 4 * (s / F::STEPS);
-        const bool here = __builtin_amdgcn_readlane(pages, s / F::STEPS) >= 0;
+        const bool here = page >= 0;
         const int t0 = blk * KV_BLOCK + (s % F::STEPS) * TOK;
-        const int s1 = min(s + 1, steps - 1);
-        const uint8_t *next = block_at(s1);
-        const float2 sc_next = scales_at(s1);
+        const int s1 = min(s + 1, steps - 1), k1 = s1 / F::STEPS;
+        if (k1 % 64 == 0 && k1 != s / F::STEPS)
+            pages = page_list(k1);
+        const int page1 = __builtin_amdgcn_readlane(pages, k1 % 64);
+        const uint8_t *next = block_at(page1);
+        const float2 sc_next = scales_at(page1);
 
         // ---- scores of TOK tokens (rows of S^T) and 16 RT rows (columns)
         f32x4 sv[RT][GT];
@@ -237,12 +344,12 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
                 const bf16x8 kf = codes_bf16<FMT>(cur.k[g][c / 2][2 * (c % 2)], cur.k[g][c / 2][2 * (c % 2) + 1]);
 #pragma unroll
                 for (int x = 0; x < RT; ++x)
-                    sv[x][g] = mfma16(kf, qf[x][c], sv[x][g]);
+                    sv[x][g] = mfma16(kf, query(x, c), sv[x][g]);
             }
         }
         F::load_k(cur.k, next, s1 % F::STEPS);                 // (the last step reads its own block again)
 
-        const float ks = sc.x * A.scale_log2;
+        const float ks = (here ? sc.x : 0.0f) * A.scale_log2, vs = here ? sc.y : 0.0f;
         const bool tail = !here || t0 + TOK > q.len;
         if (tail) {                                            // bytes past the last token may be anything
 #pragma unroll
@@ -272,11 +379,11 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
                     top = fmaxf(top, z);
                 }
             if (A.scores && r0 + 16 * x + col < rows) {
-                float *dst = A.scores + (((int64_t(i) * A.score_blocks + blk) * A.c.H + h) * A.score_rows + r0 + 16 * x + col) *
-                                            KV_BLOCK + (s % F::STEPS) * TOK + 4 * j;
+                float *dst = A.scores + score_index(A, i, blk, page, h, r0 + 16 * x + col) + (s % F::STEPS) * TOK + 4 * j;
+                if (here || A.score_blocks)
 #pragma unroll
-                for (int g = 0; g < GT; ++g)
-                    *reinterpret_cast<f32x4 *>(dst + 16 * g) = sv[x][g];
+                    for (int g = 0; g < GT; ++g)
+                        *reinterpret_cast<f32x4 *>(dst + 16 * g) = sv[x][g];
             }
             top = across16(top, vmax);
             const float m1 = fmaxf(m[x], top);
@@ -296,7 +403,7 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
                 for (int r = 0; r < 4; ++r) {
                     const float p = __builtin_amdgcn_exp2f(sv[x][g][r] - ref);
                     sum += p;
-                    sv[x][g][r] = p == 0.0f ? 0.0f : p * sc.y;
+                    sv[x][g][r] = p * vs;
                 }
             l[x] += sum;
 #pragma unroll
@@ -326,6 +433,7 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
             }
         F::load_v(cur.v, next, s1 % F::STEPS);
         sc = sc_next;
+        page = page1;
     }
 
     // ---- the four wavefronts' results: lane (col, j) holds elements (4 j + r) W + c of row col
@@ -363,7 +471,7 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
         }
         if (r < rows) {
             const int tr = r / A.G, hd = r - tr * A.G;
-            const int64_t part = ((int64_t(i) * A.c.H + h) * A.n_splits + split) * A.part_rows + r;
+            const int64_t part = part_index(A, unit.first + unit.split, h, r);
             if ((tid & 15) == 0 && A.part_ml) {
                 A.part_ml[2 * part] = mx;
                 A.part_ml[2 * part + 1] = sum;
@@ -376,7 +484,7 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
                     o += a[w] * *reinterpret_cast<const f32x4 *>(&olds[w][row][e]);
-                if (direct) {
+                if (A.direct) {
                     uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + e;
                     *reinterpret_cast<uint2 *>(dst) =
                         make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
@@ -491,21 +599,23 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
     using M = ManyRows<D>;
     __shared__ __attribute__((aligned(16))) uint8_t kl[M::KBYTES];
     __shared__ __attribute__((aligned(16))) uint8_t vl[M::VBYTES];
-    const int i = blockIdx.z, split = int(blockIdx.y) % A.n_splits, h = int(blockIdx.y) / A.n_splits;
-    const KvSeq q = kv_seq(A.s, i, false);
-    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-        kv_raise(A.status, KV_BAD_LENGTH);
-    const int rows = q.n * A.G, r0 = int(blockIdx.x) * M::ROWS;
-    if (r0 >= rows)
+    const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
+    if (unit.seq < 0)
         return;
-    const bool direct = A.n_splits == 1;
-    const int len_blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
-    if (split * A.chunk >= len_blocks && !direct)
+    const int i = unit.seq, sub = int(blockIdx.x) % A.per, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
+    const KvSeq q = kv_seq(A.s, i, false);
+    if (!q.ok && sub == 0 && threadIdx.x == 0)
+        kv_raise(A.status, KV_BAD_LENGTH);
+    if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
+        A.plan[i] = make_int2(unit.first, unit.n);
+    const int rows = q.n * A.G;
+    if (r0 >= rows)
         return;
     // blocks up to the last row's limit
     const int last = min(r0 + M::ROWS, rows) - 1;
     const int most = max(row_limit(q, last / A.G), 0);
-    const int b0 = split * A.chunk, b1 = min(b0 + A.chunk, (most + KV_BLOCK - 1) / KV_BLOCK);
+    const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+    const int b0 = range.x, b1 = min(range.y, (most + KV_BLOCK - 1) / KV_BLOCK);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hf = lane >> 5;
     const int w0 = r0 + 32 * wave;                          // this wavefront's rows
@@ -574,7 +684,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
             for (int v = 0; v < 16; ++v) {
                 const float p = __builtin_amdgcn_exp2f(sv[x][v] - ref);
                 sum += p;
-                sv[x][v] = p == 0.0f ? 0.0f : p * sc.y;
+                sv[x][v] = p * sc.y;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -597,7 +707,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
         return;
     const int tr = r / A.G, hd = r - tr * A.G;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    if (direct) {
+    if (A.direct) {
         uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + 4 * hf;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
@@ -609,7 +719,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
         if (A.lse && hf == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
     } else {
-        const int64_t part = ((int64_t(i) * A.c.H + h) * A.n_splits + split) * A.part_rows + r;
+        const int64_t part = part_index(A, unit.first + unit.split, h, r);
         if (hf == 0) {
             A.part_ml[2 * part] = m;
             A.part_ml[2 * part + 1] = l;
@@ -623,96 +733,126 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
     }
 }
 
-// ---------------------------------------------------------------- join
+// ---------------------------------------------------------------- finish
 //
-// Maximum and sum of a row over the chunks' results, by one wavefront (lanes
-// take every 64th chunk; the sums meet in a fixed tree).
-__device__ __forceinline__ float2 join_ml(const AttentionLaunch &A, int64_t first, int n)
+// log2 of the sum of a row's powers; a row that sees nothing has none: +infinity makes its probabilities zero.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? INFINITY : m + log2f(l); }
+
+// Two (maximum, sum) pairs of a row as one.
+__device__ __forceinline__ void join_pair(float &m, float &l, float m1, float l1)
 {
-    const int lane = threadIdx.x & 63;
-    float m = -INFINITY;
-    for (int s = lane; s < n; s += 64)
-        m = fmaxf(m, A.part_ml[2 * (first + int64_t(s) * A.part_rows)]);
-    m = wave_max(m);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    for (int s = lane; s < n; s += 64) {
-        const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * (first + int64_t(s) * A.part_rows));
-        l += __builtin_amdgcn_exp2f(x.x - ref) * x.y;
-    }
-    return make_float2(m, wave_sum(l));
+    const float top = fmaxf(m, m1), ref = top == -INFINITY ? 0.0f : top;
+    l = __builtin_amdgcn_exp2f(m - ref) * l + __builtin_amdgcn_exp2f(m1 - ref) * l1;
+    m = top;
 }
 
-// One workgroup of 256 threads per (packed row, head, sequence): its D elements over the chunks.
-__global__ void __launch_bounds__(256) kv_join_kernel(AttentionLaunch A)
-{
-    __shared__ float part[4][256];
-    const int i = blockIdx.z, h = blockIdx.y, r = blockIdx.x;
-    const KvSeq q = kv_seq(A.s, i, false);
-    if (r >= q.n * A.G)
-        return;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int D = A.c.D;
-    const int n = ((q.len + KV_BLOCK - 1) / KV_BLOCK + A.chunk - 1) / A.chunk;
-    const int64_t first = (int64_t(i) * A.c.H + h) * A.n_splits * A.part_rows + r;
-    const float2 ml = join_ml(A, first, n);
-    const float ref = ml.x == -INFINITY ? 0.0f : ml.x;
-    // wavefront w takes the chunks w, w + 4, ...; lane l the elements 4 l .. 4 l + 3
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
-    if (4 * lane < D)
-        for (int s = wave; s < n; s += 4) {
-            const int64_t p = first + int64_t(s) * A.part_rows;
-            o += __builtin_amdgcn_exp2f(A.part_ml[2 * p] - ref) * *reinterpret_cast<const f32x4 *>(A.part_o + p * D + 4 * lane);
-        }
-    *reinterpret_cast<f32x4 *>(&part[wave][4 * lane]) = o;
-    __syncthreads();
-    const int tr = r / A.G, hd = r - tr * A.G;
-    if (tid < D) {
-        const float sum = ((part[0][tid] + part[1][tid]) + part[2][tid]) + part[3][tid];
-        A.out[(int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + tid] =
-            f32_to_bf16(ml.y == 0.0f ? 0.0f : sum / ml.y);
-    }
-    if (A.lse && tid == 0)
-        A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = ml.y == 0.0f ? INFINITY : ml.x + log2f(ml.y);
-}
-
-// ---------------------------------------------------------------- weights
-//
-// From the scores that the few-rows kernel left: one wavefront per block,
-// lane = token.  A row without a token it sees has no weights (its log-sum is
-// +infinity).
 constexpr int MASS_BLOCKS = 16;              // blocks of a workgroup
 
-__global__ void __launch_bounds__(256) kv_mass_scores_kernel(AttentionLaunch A)
+// Workgroups [0, join) of a (head, sequence): D / pieces elements of one packed
+// row each, four a lane, the rest of the lanes over the units.  Then, where the
+// few-rows kernel left scores for the weights, one workgroup per MASS_BLOCKS
+// blocks: lane = token, a wavefront's four blocks side by side.  Bound by
+// latency for usual batches, so loads depend on as few others as possible.
+__global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int join, int pieces)
 {
-    extern __shared__ float lse[];           // [rows that count]
+    __shared__ __attribute__((aligned(16))) float part[1024];
+    __shared__ float ml[2][8][32];
     const int i = blockIdx.z, h = blockIdx.y;
     const KvSeq q = kv_seq(A.s, i, false);
-    const int blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
-    const int b0 = int(blockIdx.x) * MASS_BLOCKS;
+    const int2 units = A.plan ? A.plan[i] : make_int2(i, 1);
+    const int rows = q.n * A.G, blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
+    const int first = __builtin_amdgcn_readfirstlane(units.x);
+    const int n = A.plan && blocks == 0 ? 0 : __builtin_amdgcn_readfirstlane(units.y);     // (no unit wrote the plan)
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    if (!q.ok && blockIdx.x == 0 && h == 0 && tid == 0)
+        kv_raise(A.status, KV_BAD_LENGTH);           // (such a sequence has no units)
+    if (int(blockIdx.x) < join) {
+        const int width = A.c.D / pieces, r = int(blockIdx.x) / pieces, e0 = width * (int(blockIdx.x) % pieces);
+        if (r >= rows)
+            return;
+        float m = -INFINITY, l = 0.0f;
+        for (int s = lane; s < n; s += 64) {
+            const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * part_index(A, first + s, h, r));
+            join_pair(m, l, x.x, x.y);
+        }
+        const float top = wave_max(m), ref = top == -INFINITY ? 0.0f : top;
+        l = wave_sum(l * __builtin_amdgcn_exp2f(m - ref));
+        const int lanes = width / 4, groups = 256 / lanes, g = tid / lanes, e = 4 * (tid % lanes);
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = g; s < n; s += groups) {
+            const int64_t p = part_index(A, first + s, h, r);
+            o += __builtin_amdgcn_exp2f(A.part_ml[2 * p] - ref) * *reinterpret_cast<const f32x4 *>(A.part_o + p * A.c.D + e0 + e);
+        }
+        *reinterpret_cast<f32x4 *>(part + g * width + e) = o;
+        __syncthreads();
+        const int tr = r / A.G, hd = r - tr * A.G;
+        if (tid < width) {
+            float sum = 0.0f;
+            for (int k = 0; k < groups; ++k)
+                sum += part[k * width + tid];
+            A.out[(int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * A.c.D + e0 + tid] =
+                f32_to_bf16(l == 0.0f ? 0.0f : sum / l);
+        }
+        if (A.lse && tid == 0 && e0 == 0)
+            A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = log_sum(top, l);
+        return;
+    }
+    const int b0 = (int(blockIdx.x) - join) * MASS_BLOCKS;
     if (b0 >= blocks)
         return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int rows = q.n * A.G, from = max(q.n - A.mass_rows, 0) * A.G;
-    const int n = (blocks + A.chunk - 1) / A.chunk;
-    for (int r = from + wave; r < rows; r += 4) {
-        const float2 ml = join_ml(A, (int64_t(i) * A.c.H + h) * A.n_splits * A.part_rows + r, n);
-        if (lane == 0)
-            lse[r - from] = ml.y == 0.0f ? INFINITY : ml.x + log2f(ml.y);
+    const int from = max(q.n - A.mass_rows, 0) * A.G;
+    constexpr int PER = MASS_BLOCKS / 4;
+    int page[PER];
+    float was[PER], w[PER];
+    const float *src[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int b = b0 + wave + 4 * k;
+        page[k] = b < blocks ? A.s.table[int64_t(i) * A.s.max_blocks + b] : -1;
+        if (!kv_page_ok(page[k], A.c.n_pages))
+            page[k] = -1;
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int b = b0 + wave + 4 * k;
+        src[k] = A.scores + score_index(A, i, page[k] < 0 ? 0 : b, max(page[k], 0), h, 0) + lane;
+        was[k] = w[k] = 0.0f;
+        if (A.decay != 0.0f && page[k] >= 0 && b * KV_BLOCK + lane < q.len)
+            was[k] = A.c.mass[(int64_t(page[k]) * A.c.H + h) * KV_BLOCK + lane];
+    }
+    // the rows' log-sums: eight threads a row (at most 32 rows) over the units, then joined in order
+    {
+        const int r = tid & 31, g = tid >> 5;
+        float m = -INFINITY, l = 0.0f;
+        if (r < rows)
+            for (int u = g; u < n; u += 8) {
+                const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * part_index(A, first + u, h, r));
+                join_pair(m, l, x.x, x.y);
+            }
+        ml[0][g][r] = m;
+        ml[1][g][r] = l;
+        __syncthreads();
+        if (tid < 32) {
+            for (int k = 1; k < 8; ++k)
+                join_pair(m, l, ml[0][k][tid], ml[1][k][tid]);
+            part[tid] = log_sum(m, l);
+        }
     }
     __syncthreads();
-    for (int b = b0 + wave; b < min(b0 + MASS_BLOCKS, blocks); b += 4) {
-        const int page = A.s.table[int64_t(i) * A.s.max_blocks + b];
-        if (!kv_page_ok(page, A.c.n_pages))
-            continue;
-        const float *src = A.scores + ((int64_t(i) * A.score_blocks + b) * A.c.H + h) * A.score_rows * KV_BLOCK + lane;
-        float w = 0.0f;
-        for (int r = from; r < rows; ++r)
-            w += __builtin_amdgcn_exp2f(src[r * KV_BLOCK] - lse[r - from]);
-        if (b * KV_BLOCK + lane < q.len) {
-            float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + lane;
-            *dst = A.decay != 0.0f ? fmaf(A.decay, *dst, w) : w;
-        }
+#pragma unroll 2
+    for (int r = from; r < rows; ++r) {
+        const float z = part[r];
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            w[k] += __builtin_amdgcn_exp2f(src[k][r * KV_BLOCK] - z);
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int b = b0 + wave + 4 * k;
+        if (page[k] >= 0 && b * KV_BLOCK + lane < q.len)
+            A.c.mass[(int64_t(page[k]) * A.c.H + h) * KV_BLOCK + lane] =
+                A.decay != 0.0f ? fmaf(A.decay, was[k], w[k]) : w[k];
     }
 }
 
@@ -808,28 +948,27 @@ size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
 // How a call is cut, by its host-side bounds alone: the same cut sizes the
 // workspace and launches the kernels.
-AttentionCut attention_cut(int S, int H, int G, int D, int max_rows, int max_len, bool mass)
+AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows, int max_len, bool mass)
 {
     AttentionCut c{};
     const int64_t rows = int64_t(max_rows) * G;
     const int blocks = (max_len + KV_BLOCK - 1) / KV_BLOCK;
     c.few = rows <= 32;
     c.tile_rows = c.few ? (rows <= 16 ? 16 : 32) : 128;
-    c.tiles = int((rows + c.tile_rows - 1) / c.tile_rows);
-    // about 2048 workgroups of few rows, 512 of many, none of less than 4 blocks
-    const int64_t units = int64_t(S) * H * c.tiles;
-    const int64_t want = std::max<int64_t>(1, (c.few ? 2048 : 512) / std::max<int64_t>(units, 1));
-    int chunk = int((blocks + want - 1) / want);
-    chunk = std::min(std::max((chunk + 3) / 4 * 4, 4), c.few ? 256 : 1 << 30);
-    c.chunk = chunk;
-    c.splits = std::max(1, (blocks + chunk - 1) / chunk);
-    const bool parts = c.splits > 1 || (mass && c.few);
-    c.part_ml = 0;
-    size_t off = parts ? up256(size_t(S) * H * c.splits * rows * 2 * sizeof(float)) : 0;
+    c.per = int((rows + c.tile_rows - 1) / c.tile_rows) * H;
+    c.direct = blocks <= LEAST_BLOCKS || int64_t(S) * c.per >= (c.few ? 8192 : 256);
+    // sum of ceil(blocks_i / chunk) <= total / chunk + S, and total * per <= chunk * MOST_WORKGROUPS
+    c.units = c.direct ? S : int(std::min<int64_t>(int64_t(S) * ((blocks + LEAST_BLOCKS - 1) / LEAST_BLOCKS),
+                                                   MOST_WORKGROUPS / c.per + S));
+    size_t off = c.direct ? 0 : up256(size_t(S) * sizeof(int2));     // the plan comes first
+    c.part_ml = off;
+    off += !c.direct || (mass && c.few) ? up256(size_t(c.units) * H * rows * 2 * sizeof(float)) : 0;
     c.part_o = off;
-    off += c.splits > 1 ? up256(size_t(S) * H * c.splits * rows * D * sizeof(float)) : 0;
+    off += !c.direct ? up256(size_t(c.units) * H * rows * D * sizeof(float)) : 0;
     c.scores = off;
-    off += mass && c.few ? up256(size_t(S) * blocks * H * rows * KV_BLOCK * sizeof(float)) : 0;
+    c.score_blocks = int64_t(S) * blocks <= n_pages ? blocks : 0;
+    if (mass && c.few)
+        off += up256(size_t(c.score_blocks ? int64_t(S) * blocks : n_pages) * H * rows * KV_BLOCK * sizeof(float));
     c.bytes = off;                              // (the log-sums of many rows follow: they go by n_rows)
     return c;
 }
@@ -838,37 +977,32 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
 {
     const int H = A.c.H, S = A.s.S;
     const int rows = A.s.max_rows * A.G;
-    if (c.few) {
-        const dim3 grid(c.splits, H * c.tiles, S);
-        with_shape(fmt, A.c.D, [&](auto f, auto d) {
-            if (c.tile_rows == 16)
-                launch_k(kv_few_rows_kernel<decltype(f)::value, decltype(d)::value, 1>, grid, 256, 0, st, A);
-            else
-                launch_k(kv_few_rows_kernel<decltype(f)::value, decltype(d)::value, 2>, grid, 256, 0, st, A);
-        });
-    } else {
-        const dim3 grid(c.tiles, H * c.splits, S);
-        with_shape(fmt, A.c.D, [&](auto f, auto d) {
-            launch_k(kv_many_rows_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, A);
-        });
-    }
+    const unsigned grid = unsigned(c.units) * unsigned(c.per);
+    with_shape(fmt, A.c.D, [&](auto f, auto d) {
+        constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
+        if (!c.few)
+            launch_k(kv_many_rows_kernel<FMT, D>, grid, 256, 0, st, A);
+        else if (c.tile_rows == 16)
+            launch_k(kv_few_rows_kernel<FMT, D, 1>, grid, 256, 0, st, A);
+        else
+            launch_k(kv_few_rows_kernel<FMT, D, 2>, grid, 256, 0, st, A);
+    });
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && c.splits > 1) {
-        launch_k(kv_join_kernel, dim3(rows, H, S), 256, 0, st, A);
+    const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
+    // a row's elements over several workgroups where there are few rows and many units of each
+    const int pieces = int64_t(rows) * H * S < 256 ? A.c.D / 64 : 1;
+    const int join = c.direct ? 0 : rows * pieces, groups = A.mass_rows && c.few ? (blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
+    if (e == hipSuccess && join + groups) {
+        launch_k(kv_finish_kernel, dim3(join + groups, H, S), 256, 0, st, A, join, pieces);
         e = hipGetLastError();
     }
-    if (e != hipSuccess || !A.mass_rows)
-        return e;
-    const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
-    if (blocks == 0)
-        return e;
-    if (c.few)
-        launch_k(kv_mass_scores_kernel, dim3((blocks + MASS_BLOCKS - 1) / MASS_BLOCKS, H, S), 256, size_t(rows) * 4, st, A);
-    else
+    if (e == hipSuccess && A.mass_rows && !c.few && blocks) {
         with_shape(fmt, A.c.D, [&](auto f, auto d) {
             launch_k(kv_mass_rows_kernel<decltype(f)::value, decltype(d)::value>, dim3(blocks, H, S), 256, 0, st, A);
         });
-    return hipGetLastError();
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace msi
