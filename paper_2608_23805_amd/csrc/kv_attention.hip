@@ -19,6 +19,7 @@
 // sum, the maxima, the scores and all accumulators are fp32.
 #include <algorithm>
 
+#include "gemm_ring.h"
 #include "kernels.h"
 #include "kv_device.h"
 
@@ -498,63 +499,70 @@ __global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
 
 // ---------------------------------------------------------------- many rows
 //
-// A workgroup of four wavefronts owns 128 packed rows, 32 a wavefront, and
-// walks the cache in steps of 64 tokens: K [64, D] and V^T [D, 64] go to LDS
-// as bf16 (converted once for all four wavefronts), v_mfma_f32_32x32x16_bf16
-// for both products.  V^T is stored in the order in which a lane holds the
-// scores: slot 8 (2 u + hf) + r of 16-token group u is token
-// 16 u + 4 hf + r (r < 4) or 16 u + 4 + 4 hf + r.
+// Bound by the matrix cores and the vector unit beside them.  A workgroup of
+// four wavefronts owns 128 packed rows, 32 a wavefront, and walks the cache a
+// block of 64 tokens at a time.  The blocks' codes are copied as they are into
+// a ring of four LDS buffers (half the LDS traffic of bf16 tiles, which would
+// bound 32-row wavefronts) and become bf16 on their way from LDS to
+// v_mfma_f32_32x32x16_bf16.  With D = 256 the 32 rows' outputs alone take 128
+// registers, so the queries lie in LDS as well, in the order of their fragments; that keeps
+// everything in the vector registers, where the rescaling needs the outputs (in
+// the accumulation registers every block would move all of them there and back).
+//
+// LDS: 16-byte chunk c of token row t (K rows, then V rows) sits at slot
+// c ^ many_swz(t) of its row: the 16-byte reads of eight consecutive K rows and the
+// transposing reads of the eight V rows of a lane group fall on distinct banks.
+// K: lane (i, hf) = (lane % 32, lane / 32) reads chunk 2 p + hf of token i: the
+// reduction order of MFMA 2 p + e is d = 16 (2 p + hf) + 8 e + 0..7, and the
+// queries are read in the same.  V: ds_read_b64_tr_b8 hands lane b + 8 x of a
+// 16-lane group byte b of the eight bytes that lanes x, x + 2, .. x + 14 point
+// at, so the lanes point at the eight tokens whose scores they hold and come
+// back with eight tokens of one element.
 template <int D>
 struct ManyRows {
-    static constexpr int TOK = KV_BLOCK;
-    static constexpr int KS = D * 2 + 16;                 // LDS row strides (bytes)
-    static constexpr int VS = TOK * 2 + 16;
-    static constexpr int KBYTES = TOK * KS, VBYTES = D * VS;
-    static constexpr int ROWS = 128;
+    static constexpr int ROWS = 128, NBUF = 3;
+    static constexpr int BLOCK = 2 * KV_BLOCK * D;        // bytes of a block's codes
+    static constexpr int COPIES = BLOCK / 4096;           // copy instructions of a wavefront and block
+    static constexpr int CPR = D / 16;                    // chunks of a row
+    static constexpr bool QLDS = D == 256;
+    static constexpr int QBYTES = QLDS ? ROWS * D * 2 : 0;
+    static constexpr size_t LDS = size_t(NBUF) * BLOCK + QBYTES;
+    static_assert(LDS <= 160 * 1024, "");
 };
 
-template <int FMT, int D>
-__device__ __forceinline__ void stage_k(uint8_t *lds, const uint8_t *block)
+template <int D>
+__device__ __forceinline__ int many_swz(int t)
 {
-    using M = ManyRows<D>;
-    // 16 codes per thread and pass
-    constexpr int CPR = D / 16, PASSES = KV_BLOCK * CPR / 256;
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-        const int idx = p * 256 + threadIdx.x, t = idx / CPR, c = idx % CPR;
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(block + t * D + c * 16);
-        bf16x8 *dst = reinterpret_cast<bf16x8 *>(lds + t * M::KS + c * 32);
-        dst[0] = codes_bf16<FMT>(w[0], w[1]);
-        dst[1] = codes_bf16<FMT>(w[2], w[3]);
-    }
+    return ((t & 3) | ((t >> 1) & 4) | ((t << 1) & 8)) & (D / 16 - 1);
 }
 
-template <int FMT, int D>
-__device__ __forceinline__ void stage_v(uint8_t *lds, const uint8_t *block, int valid)
-{
-    using M = ManyRows<D>;
-    // thread: four elements 4 e.. of the eight tokens of one slot group
-    constexpr int EQ = D / 4, PASSES = (EQ * 8 + 255) / 256;
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) {
-        const int idx = p * 256 + threadIdx.x, e = idx % EQ, sg = idx / EQ, u = sg >> 1, hf = sg & 1;
-        if (EQ * 8 % 256 && sg >= 8)
-            break;
-        uint32_t w[2][4];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const int t = 16 * u + 4 * hf + (x < 4 ? x : 4 + x);
-            const uint32_t c = *reinterpret_cast<const uint32_t *>(block + t * D + 4 * e);
-            w[x >> 2][x & 3] = t < valid ? c : 0u;
-        }
-        uint32_t lo[4], hi[4];
-        transpose4(w[0], lo);
-        transpose4(w[1], hi);
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<bf16x8 *>(lds + (4 * e + x) * M::VS + sg * 16) = codes_bf16<FMT>(lo[x], hi[x]);
+// Copies of one block into LDS: copy i of a wavefront covers 16-byte slots 64 (4 i + wave) .., whole groups of
+// 16 rows apart, so a lane's offset within the block is one number for all of them.  Rows past `valid` (none
+// of the block with valid = 0) become zeros: an offset past the buffer's end reads nothing.
+template <int D>
+struct CopyLane {
+    uint32_t offset;
+    int row;
+
+    __device__ __forceinline__ CopyLane()
+    {
+        const int at = int(threadIdx.x), c = at % ManyRows<D>::CPR;
+        row = at / ManyRows<D>::CPR;
+        offset = uint32_t(row * D + ((c ^ many_swz<D>(row)) << 4));
     }
-}
+
+    __device__ __forceinline__ void copy(uint8_t *lds, const uint8_t *block, int valid) const
+    {
+        using M = ManyRows<D>;
+        const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(block), 0, M::BLOCK, ring::RSRC_FLAGS);
+#pragma unroll
+        for (int i = 0; i < M::COPIES; ++i)
+            dma16_lds(r, lds + (i * 4 + wave) * 1024,
+                      row < valid - (i * 4096 / D & (KV_BLOCK - 1)) ? offset : 0x80000000u, i * 4096);
+    }
+};
 
 __device__ __forceinline__ float across32(float v, float (*op)(float, float))
 {
@@ -562,47 +570,102 @@ __device__ __forceinline__ float across32(float v, float (*op)(float, float))
     return op(__uint_as_float(s32[0]), __uint_as_float(s32[1]));
 }
 
-// Query fragments of 32 rows from r0 on: lane (col, hf) = (lane % 32, lane / 32), elements 16 c + 8 hf + 0..7.
+// Fragment c of the queries of 32 rows from r0 on (lane's row r0 + lane % 32); their sign takes a negative scale's.
 template <int D>
 __device__ __forceinline__ void load_q32(bf16x8 (&qf)[D / 16], const AttentionLaunch &A, const KvSeq &q, int h, int r0,
                                          int rows)
 {
     const int lane = threadIdx.x & 63;
     const int rc = min(r0 + (lane & 31), rows - 1), tr = rc / A.G, hd = rc - tr * A.G;
-    const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D + 8 * (lane >> 5);
+    const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D + 16 * (lane >> 5);
+    const uint32_t flip = A.scale_log2 < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-        qf[c] = *reinterpret_cast<const bf16x8 *>(src + 16 * c);
+    for (int c = 0; c < D / 16; ++c) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(src + 32 * (c / 2) + 8 * (c % 2));
+        qf[c] = as_bf16x8(v ^ u32x4{flip, flip, flip, flip});
+    }
 }
 
-// S^T of 64 tokens and 32 rows: sv[b][v] is token 32 b + 8 (v / 4) + 4 hf + v % 4 of row col.
-template <int D>
-__device__ __forceinline__ void scores32(f32x16 (&sv)[2], const uint8_t *lds, const bf16x8 (&qf)[D / 16])
+// S^T of 64 tokens and 32 rows: sv[b][v] is token 32 b + 8 (v / 4) + 4 hf + v % 4 of the lane's row.
+// query(c): fragment c.
+template <int FMT, int D, typename Query>
+__device__ __forceinline__ void scores32(f32x16 (&sv)[2], const uint8_t *__restrict__ lds, Query query)
 {
-    using M = ManyRows<D>;
     const int lane = threadIdx.x & 63;
-    const uint8_t *kp = lds + (lane & 31) * M::KS + 16 * (lane >> 5);
+    const int t = lane & 31, swz = many_swz<D>(t), hf = lane >> 5;   // (many_swz(t + 32) is the same)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
             sv[b][v] = 0.0f;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-            sv[b] = mfma32(*reinterpret_cast<const bf16x8 *>(kp + 32 * b * M::KS + 32 * c), qf[c], sv[b]);
+    for (int p = 0; p < D / 32; ++p) {
+        const bf16x8 q0 = query(2 * p), q1 = query(2 * p + 1);
+        u32x4 w[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            w[b] = *reinterpret_cast<const u32x4 *>(lds + (32 * b + t) * D + (((2 * p + hf) ^ swz) << 4));
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            sv[b] = mfma32(codes_bf16<FMT>(w[b][0], w[b][1]), q0, sv[b]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            sv[b] = mfma32(codes_bf16<FMT>(w[b][2], w[b][3]), q1, sv[b]);
     }
 }
 
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+// Eight tokens of one element for every lane, see above; `at`: the lane's own eight bytes.
+__device__ __forceinline__ i32x2 read_tr8(const uint8_t *at)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)at);
+#else
+    (void)at;
+    return i32x2{0, 0};
+#endif
+}
+
+// Copies of a later block into `later`, then the scores of the block at `tile`.  The
+// LDS parts are restricted parameters, here and below, or the compiler would have reads of one
+// buffer wait for every copy in flight into another.
+template <int FMT, int D, typename Query>
+__device__ __forceinline__ void copy_and_score(f32x16 (&sv)[2], const uint8_t *__restrict__ tile, Query query,
+                                               uint8_t *__restrict__ later, const CopyLane<D> &cl, const uint8_t *block,
+                                               int valid)
+{
+    cl.copy(later, block, valid);
+    scores32<FMT, D>(sv, tile, query);
+}
+
+// O^T += V^T P^T of the block at `tile`.
 template <int FMT, int D>
-__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(AttentionLaunch A)
+__device__ __forceinline__ void times_v(f32x16 (&acc)[D / 32], const bf16x8 (&pf)[4], const uint8_t *__restrict__ tile,
+                                        const uint32_t (&chunk)[D / 32])
+{
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            const i32x2 w = read_tr8(tile + 16 * u * D + chunk[c]);
+            acc[c] = mfma32(codes_bf16<FMT>(uint32_t(w[0]), uint32_t(w[1])), pf[u], acc[c]);
+        }
+}
+
+constexpr float NO_SCALE = 0x1p-126f;       // a scale of 0 counts as this (its logarithm is finite)
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 {
     using M = ManyRows<D>;
-    __shared__ __attribute__((aligned(16))) uint8_t kl[M::KBYTES];
-    __shared__ __attribute__((aligned(16))) uint8_t vl[M::VBYTES];
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
     const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
     if (unit.seq < 0)
         return;
-    const int i = unit.seq, sub = int(blockIdx.x) % A.per, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
+    // the last row tiles, which see the most tokens, start first
+    const int i = unit.seq, sub = A.per - 1 - int(blockIdx.x) % A.per, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
     const KvSeq q = kv_seq(A.s, i, false);
     if (!q.ok && sub == 0 && threadIdx.x == 0)
         kv_raise(A.status, KV_BAD_LENGTH);
@@ -627,64 +690,139 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
 
     bf16x8 qf[D / 16];
     load_q32<D>(qf, A, q, h, w0, rows);
+    bf16x8 *const ql = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK) + wave * (D / 16) * 64 + lane;
+    if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            ql[c * 64] = qf[c];
+    auto query = [&](int c) {
+        if constexpr (M::QLDS)
+            return ql[c * 64];
+        else
+            return qf[c];
+    };
     f32x16 acc[D / 32];
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
             acc[c][v] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f;                          // m: reference of the exponents, a whole number
+
+    // page (-1: bad), K factor and log2 of the V scale of the 64 blocks from `list_at` on, one a lane
+    int list_at = b0 - 64, pages = -1;
+    float kscale = 0.0f, vlog = 0.0f;
+    const float factor = fabsf(A.scale_log2);
+    auto make_list = [&](int b) {
+        list_at = b;
+        pages = -1;
+        kscale = 1e-37f, vlog = 0.0f;
+        if (b + lane < b1) {
+            pages = A.s.table[int64_t(i) * A.s.max_blocks + b + lane];
+            if (!kv_page_ok(pages, A.c.n_pages)) {
+                kv_raise(A.status, KV_BAD_PAGE);
+                pages = -1;
+            } else {
+                const float2 sc = *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(pages) * A.c.H + h) * 2);
+                kscale = fmaxf(sc.x * factor, 1e-37f);       // (not 0: times -infinity that would be NaN)
+                vlog = log2f(fmaxf(sc.y, NO_SCALE));         // whole for powers of two
+            }
+        }
+    };
+    int next_pages = -1, next_at = b0;                      // pages of the copies, which run ahead of the list
+    auto copy_list = [&](int b) {
+        next_at = b;
+        next_pages = -1;
+        if (b + lane < b1) {
+            next_pages = A.s.table[int64_t(i) * A.s.max_blocks + b + lane];
+            if (!kv_page_ok(next_pages, A.c.n_pages))
+                next_pages = -1;
+        }
+    };
+    copy_list(b0);
+    const CopyLane<D> cl;
+    auto block_at = [&](int b) {
+        if (b - next_at == 64)
+            copy_list(b);
+        return A.c.data + kv_offset(max(__builtin_amdgcn_readlane(next_pages, b - next_at), 0), h, A.c.H, D);
+    };
+    auto valid_at = [&](int b) {                            // (blocks past the end copy zeros: the waits count on them)
+        return __builtin_amdgcn_readlane(next_pages, b - next_at) >= 0 ? q.len - b * KV_BLOCK : 0;
+    };
+    auto issue = [&](int b) {
+        const uint8_t *block = block_at(b);
+        cl.copy(lds8 + (b - b0) % M::NBUF * M::BLOCK, block, valid_at(b));
+    };
+    auto arrive = [&](auto waitn) {
+        __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(decltype(waitn)::value));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's reads are done with
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    issue(b0);
+    issue(b0 + 1);
+    // this lane's bytes of V: token row 64 + 16 u + tv, elements 32 c + 16 (lane / 16 % 2) + 8 (lane % 2) ..
+    const int tl = (lane & 15) >> 1, tv = (tl < 4 ? tl : 4 + tl) + 4 * hf;
+    const int vswz = many_swz<D>(tv);                       // (the same for tv + 16 u)
+    const int vc = (lane >> 4) & 1;
+    uint32_t vchunk[D / 32];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+        vchunk[c] = uint32_t(((2 * c + vc) ^ vswz) << 4);
+    const uint32_t vrow = uint32_t((KV_BLOCK + tv) * D + 8 * (lane & 1));
 
     for (int b = b0; b < b1; ++b) {
-        const int page0 = __builtin_amdgcn_readfirstlane(A.s.table[int64_t(i) * A.s.max_blocks + b]);
-        const bool here = kv_page_ok(page0, A.c.n_pages);
-        const int page = here ? page0 : 0;
-        if (!here && tid == 0)
-            kv_raise(A.status, KV_BAD_PAGE);
-        const uint8_t *block = A.c.data + kv_offset(page, h, A.c.H, D);
-        __syncthreads();
-        stage_k<FMT, D>(kl, block);
-        stage_v<FMT, D>(vl, block + KV_BLOCK * D, here ? q.len - b * KV_BLOCK : 0);
-        __syncthreads();
+        // block b has landed (b + 1 is in flight); the buffer of block b - 1 is free
+        arrive(std::integral_constant<int, M::COPIES>{});
+        if (b - list_at == 64)
+            make_list(b);
         const int t0 = b * KV_BLOCK;
-        if (!here || t0 >= wave_most)
+        const uint8_t *block = block_at(b + 2);
+        const int valid = valid_at(b + 2);
+        const uint8_t *const tile = lds8 + (b - b0) % M::NBUF * M::BLOCK;
+        uint8_t *const later = lds8 + (b + 2 - b0) % M::NBUF * M::BLOCK;
+        if (t0 >= wave_most) {                              // (as is every later block)
+            cl.copy(later, block, valid);
             continue;
-        const float2 sc = *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(page) * A.c.H + h) * 2);
+        }
         f32x16 sv[2];
-        scores32<D>(sv, kl, qf);
-        const float ks = sc.x * A.scale_log2;
+        copy_and_score<FMT, D>(sv, tile, query, later, cl, block, valid);
+        const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kscale), b - list_at));
+        const float vl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog), b - list_at));
+        const bool here = __builtin_amdgcn_readlane(pages, b - list_at) >= 0;
+        if (!here || t0 + KV_BLOCK > least) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    sv[x][v] = here && t0 + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? sv[x][v] : -INFINITY;
+        }
         float top = -INFINITY;
-        const bool masked = t0 + KV_BLOCK > least || w0 + 32 > rows;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                float z = sv[x][v] * ks;
-                if (masked)
-                    z = t0 + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? z : -INFINITY;
-                sv[x][v] = z;
-                top = fmaxf(top, z);
-            }
-        top = across32(top, vmax);
-        const float m1 = fmaxf(m, top);
-        const float ref = m1 == -INFINITY ? 0.0f : m1;
-        if (__any(m1 != m)) {
-            const float a = __builtin_amdgcn_exp2f(m - ref);
+            for (int v = 0; v < 16; ++v)
+                top = fmaxf(top, sv[x][v]);
+        top = across32(top, vmax) * ks;
+        // the reference follows the maximum once it is 2^6 ahead: any reference gives the same quotients
+        if (__any(top > m + 6.0f)) {
+            const float m1 = ceilf(fmaxf(m, top));
+            const float a = m1 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m1);
             l *= a;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
                 acc[c] *= a;
             m = m1;
         }
+        const float shift = m == -INFINITY ? 0.0f : vl - m;  // whole (V scales are powers of two), so no rounding
         bf16x8 pf[4];
         float sum = 0.0f;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const float p = __builtin_amdgcn_exp2f(sv[x][v] - ref);
-                sum += p;
-                sv[x][v] = p * sc.y;
+                sv[x][v] = __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, shift));    // probability times V scale
+                sum += sv[x][v];
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -692,14 +830,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
                     bf16x8, u32x4{pack_bf16_hw(sv[x][8 * u], sv[x][8 * u + 1]), pack_bf16_hw(sv[x][8 * u + 2], sv[x][8 * u + 3]),
                                   pack_bf16_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
         }
-        l += sum;
-        const uint8_t *vp = vl + col * M::VS + 16 * hf;
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                acc[c] = mfma32(*reinterpret_cast<const bf16x8 *>(vp + 32 * c * M::VS + 32 * u), pf[u], acc[c]);
+        l = fmaf(sum, __builtin_amdgcn_exp2f(-vl), l);
+        times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
     }
+    __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));              // copies in flight write this workgroup's LDS
 
     // ---- lane (col, hf) holds elements 32 c + 8 (v / 4) + 4 hf + v % 4 of its row
     l = across32(l, vsum);
@@ -714,14 +848,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) kv_many_rows_kernel(Att
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
                 *reinterpret_cast<uint2 *>(dst + 32 * c + 2 * v) =
-                    make_uint2(pack_bf16x2(acc[c][v] * inv, acc[c][v + 1] * inv),
-                               pack_bf16x2(acc[c][v + 2] * inv, acc[c][v + 3] * inv));
+                    make_uint2(pack_bf16_hw(acc[c][v] * inv, acc[c][v + 1] * inv),
+                               pack_bf16_hw(acc[c][v + 2] * inv, acc[c][v + 3] * inv));
         if (A.lse && hf == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
     } else {
         const int64_t part = part_index(A, unit.first + unit.split, h, r);
         if (hf == 0) {
-            A.part_ml[2 * part] = m;
+            A.part_ml[2 * part] = l == 0.0f ? -INFINITY : m;
             A.part_ml[2 * part + 1] = l;
         }
 #pragma unroll
@@ -861,8 +995,7 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
 template <int FMT, int D>
 __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
 {
-    using M = ManyRows<D>;
-    __shared__ __attribute__((aligned(16))) uint8_t kl[M::KBYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t kl[KV_BLOCK * D];
     __shared__ float part[4][KV_BLOCK];
     const int i = blockIdx.z, h = blockIdx.y, b = blockIdx.x;
     const KvSeq q = kv_seq(A.s, i, false);
@@ -873,9 +1006,18 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int col = lane & 31, hf = lane >> 5;
-    stage_k<FMT, D>(kl, A.c.data + kv_offset(page, h, A.c.H, D));
+    {
+        const uint8_t *block = A.c.data + kv_offset(page, h, A.c.H, D);
+        constexpr int CPR = D / 16;
+#pragma unroll
+        for (int p = 0; p < KV_BLOCK * CPR / 256; ++p) {
+            const int at = p * 256 + int(threadIdx.x), t = at / CPR, c = at % CPR;
+            *reinterpret_cast<u32x4 *>(kl + t * D + ((c ^ many_swz<D>(t)) << 4)) =
+                *reinterpret_cast<const u32x4 *>(block + at * 16);
+        }
+    }
     __syncthreads();
-    const float ks = A.c.scales[(int64_t(page) * A.c.H + h) * 2] * A.scale_log2;
+    const float ks = A.c.scales[(int64_t(page) * A.c.H + h) * 2] * fabsf(A.scale_log2);
     const int rows = q.n * A.G;
     // rows below `from` do not count, or do not see the block
     const int from = max(max(q.n - A.mass_rows, 0), b * KV_BLOCK - (q.len - q.n)) * A.G;
@@ -889,7 +1031,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
         bf16x8 qf[D / 16];
         load_q32<D>(qf, A, q, h, r0, rows);
         f32x16 sv[2];
-        scores32<D>(sv, kl, qf);
+        scores32<FMT, D>(sv, kl, [&](int c) { return qf[c]; });
         const int r = r0 + col, rc = min(r, rows - 1), tr = rc / A.G;
         const int limit = r < rows ? row_limit(q, tr) : 0;
         const float z0 = A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + rc - tr * A.G];
@@ -978,16 +1120,21 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
     const int H = A.c.H, S = A.s.S;
     const int rows = A.s.max_rows * A.G;
     const unsigned grid = unsigned(c.units) * unsigned(c.per);
+    hipError_t e = hipSuccess;
     with_shape(fmt, A.c.D, [&](auto f, auto d) {
         constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
-        if (!c.few)
-            launch_k(kv_many_rows_kernel<FMT, D>, grid, 256, 0, st, A);
-        else if (c.tile_rows == 16)
+        if (!c.few) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D>),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, int(ManyRows<D>::LDS));
+            if (e == hipSuccess)
+                launch_k(kv_many_rows_kernel<FMT, D>, grid, 256, ManyRows<D>::LDS, st, A);
+        } else if (c.tile_rows == 16)
             launch_k(kv_few_rows_kernel<FMT, D, 1>, grid, 256, 0, st, A);
         else
             launch_k(kv_few_rows_kernel<FMT, D, 2>, grid, 256, 0, st, A);
     });
-    hipError_t e = hipGetLastError();
+    if (e == hipSuccess)
+        e = hipGetLastError();
     const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
     // a row's elements over several workgroups where there are few rows and many units of each
     const int pieces = int64_t(rows) * H * S < 256 ? A.c.D / 64 : 1;
