@@ -521,7 +521,7 @@ typedef struct {
  * v are [n_rows, n_heads, head_dim] bf16, strides in elements from row to row,
  * multiples of 8.  A block's scale is the least power of two s >= 2^-64 with
  * |x| <= 448 s (e4m3) or 127 s (int8) over its new finite elements, or the scale it had if it held
- * tokens and that is larger; codes are x / s rounded to nearest, ties to even; codes the block held move to a
+ * tokens and that is larger; codes are x times 1 / s, rounded to nearest, ties to even; codes the block held move to a
  * grown scale the same way.  The new tokens' mass becomes 0.  Bytes after the
  * last token stay as they were.  No page may be written for two sequences by
  * one call.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */

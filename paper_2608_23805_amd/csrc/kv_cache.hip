@@ -53,12 +53,6 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
     const int blk = start / KV_BLOCK + int(blockIdx.x);
     if (q.n == 0 || blk * KV_BLOCK >= q.len)
         return;
-    const int page = __builtin_amdgcn_readfirstlane(s.table[int64_t(i) * s.max_blocks + blk]);
-    if (!kv_page_ok(page, c.n_pages)) {
-        if (threadIdx.x == 0)
-            kv_raise(status, KV_BAD_PAGE);
-        return;
-    }
     const int lo = max(start - blk * KV_BLOCK, 0), hi = min(q.len - blk * KV_BLOCK, KV_BLOCK);   // new rows of the block
     const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
     const int64_t src0 = int64_t(q.row0) + (blk * KV_BLOCK - start);       // call's row of the block's row 0
@@ -72,6 +66,12 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
         } else {
             x[0][p] = x[1][p] = u32x4{0, 0, 0, 0};
         }
+    }
+    const int page = __builtin_amdgcn_readfirstlane(s.table[int64_t(i) * s.max_blocks + blk]);
+    if (!kv_page_ok(page, c.n_pages)) {
+        if (threadIdx.x == 0)
+            kv_raise(status, KV_BAD_PAGE);
+        return;
     }
     float *sc = c.scales + (int64_t(page) * c.H + h) * 2;
     const float was[2] = {lo ? sc[0] : 0.0f, lo ? sc[1] : 0.0f};   // (read before the barriers below, written after)
@@ -96,18 +96,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const float need = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT));
-        const float scale = fmaxf(need, was[j]);
+        const float scale = fmaxf(need, was[j]), inv = 1.0f / scale;
         uint8_t *dst = base + j * (KV_BLOCK * D);
         if (lo && scale != was[j]) {                      // the old rows move to the larger scale
             for (int r = r0; r < lo; r += R::ROWS) {
                 uint2 *o = reinterpret_cast<uint2 *>(dst + r * D + chunk * 8);
                 const uint2 w = *o;
                 const f32x4 a = kv_unpack4<FMT>(w.x), b = kv_unpack4<FMT>(w.y);
-                // (code * was is exact, or rounded once in fp32 where a caller's own scale is no power of two)
-                *o = make_uint2(kv_pack4<FMT>(a[0] * was[j] / scale, a[1] * was[j] / scale, a[2] * was[j] / scale,
-                                              a[3] * was[j] / scale),
-                                kv_pack4<FMT>(b[0] * was[j] / scale, b[1] * was[j] / scale, b[2] * was[j] / scale,
-                                              b[3] * was[j] / scale));
+                // (both products are exact unless a caller's own scale is no power of two)
+                const f32x4 x = a * was[j] * inv, y = b * was[j] * inv;
+                *o = make_uint2(kv_pack4<FMT>(x[0], x[1], x[2], x[3]), kv_pack4<FMT>(y[0], y[1], y[2], y[3]));
             }
         }
 #pragma unroll
@@ -118,7 +116,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
                 unpack_bf16x8(x[j][p], f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    f[e] = f[e] != f[e] ? 0.0f : f[e] / scale;      // NaN is stored as zero, infinities as the largest code
+                    f[e] = f[e] != f[e] ? 0.0f : f[e] * inv;      // NaN is stored as zero, infinities as the largest code
                 *reinterpret_cast<uint2 *>(dst + r * D + chunk * 8) =
                     make_uint2(kv_pack4<FMT>(f[0], f[1], f[2], f[3]), kv_pack4<FMT>(f[4], f[5], f[6], f[7]));
             }
@@ -187,22 +185,23 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint1
 //
 // Selection, one 1024-thread workgroup per (head, sequence): token t of the
 // chunk sits in round t / 1024 of thread t % 1024, so a wavefront's round is 64
-// consecutive tokens and reads one page's weights (256 bytes).  The weight of
-// the last kept token is found by three rounds of histograms over 11, 11 and
-// 10 bits of the order-preserving key; equal weights are kept from the lowest
+// consecutive tokens and reads one page's weights (256 bytes).  Every token has
+// a 32-bit key that orders as its weight does; protected tokens have the
+// largest key of all.  The key of the last kept token is found by three rounds
+// of histograms over 11, 11 and 10 bits; equal keys are kept from the lowest
 // index on, by a prefix count in index order.  Sequences of up to
 // 1024 * ROUNDS tokens keep their keys in registers through all passes; longer
 // ones read them again in chunks of that size.
 constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64, BINS = 2048;
 
-// Order-preserving key of a weight: larger weights have larger keys, -0 is
-// +0, NaN is below everything.
+// Keys: larger weights have larger ones, -0 is +0; NaN and the tokens of a bad
+// page are below every number, places past the last token below everything,
+// and protected tokens above (+infinity is 0xFF800000, -infinity 0x007FFFFF).
+constexpr uint32_t KEY_NONE = 0u, KEY_NAN = 1u, KEY_PROTECTED = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t mass_key(float m)
 {
-    if (m != m)
-        return 0u;
-    const uint32_t u = __float_as_uint(m == 0.0f ? 0.0f : m);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(m + 0.0f);          // (-0 + 0 is +0)
+    return m != m ? KEY_NAN : u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
 }
 
 template <int ROUNDS>
@@ -212,8 +211,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
 {
     constexpr int CHUNK = SELECT_THREADS * ROUNDS;
     __shared__ int hist[BINS];
-    __shared__ int counts[ROUNDS * SELECT_WAVES];
-    __shared__ int part[SELECT_WAVES];
+    __shared__ int counts[2][ROUNDS * SELECT_WAVES];
+    __shared__ int part[2][SELECT_WAVES];
     __shared__ int found[2];
     const int h = blockIdx.x, i = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -231,40 +230,45 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
             out[t] = t;
         return;
     }
-    const int first = sinks, last = len - recent;          // candidates [first, last); first <= last as sinks + recent <= budget < len
-    const int want = budget - sinks - recent;              // of them to keep
     const int32_t *table = s.table + int64_t(i) * s.max_blocks;
     const int chunks = (len + CHUNK - 1) / CHUNK;
+    static_assert(ROUNDS <= 64, "one page a lane");
     uint32_t key[ROUNDS];
     bool bad = false;
     auto load = [&](int base) {
-        int page[ROUNDS];
+        // the page of round l in lane l, then all the weights at once
+        const int tl = base + lane * SELECT_THREADS + wave * 64;
+        int page = -1;
+        if (lane < ROUNDS && tl < len) {
+            page = table[tl / KV_BLOCK];
+            if (!kv_page_ok(page, c.n_pages)) {
+                page = -1;
+                bad = true;
+            }
+        }
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            const int t = base + r * SELECT_THREADS + wave * 64;
-            page[r] = t < len ? table[t / KV_BLOCK] : -1;
+            const int64_t p = max(__builtin_amdgcn_readlane(page, r), 0);
+            key[r] = __float_as_uint(c.mass[(p * c.H + h) * KV_BLOCK + lane]);
         }
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
             const int t = base + r * SELECT_THREADS + tid;
-            const bool ok = kv_page_ok(page[r], c.n_pages);
-            bad |= t < len && !ok;
-            key[r] = 0;                                    // (a bad page's tokens go first)
-            if (t < len && ok)
-                key[r] = mass_key(c.mass[(int64_t(page[r]) * c.H + h) * KV_BLOCK + lane]);
+            const uint32_t k = __builtin_amdgcn_readlane(page, r) < 0 ? KEY_NAN : mass_key(__uint_as_float(key[r]));
+            key[r] = t >= len ? KEY_NONE : t < sinks || t >= len - recent ? KEY_PROTECTED : k;
         }
     };
-    auto candidate = [&](int t) { return t >= first && t < last; };
 
-    // ---- the key of the last kept candidate, and how many equal ones are kept
+    // ---- the key of the last kept token, and how many equal ones are kept (len > budget: it is above KEY_NONE)
     uint32_t prefix = 0, mask = 0;
-    int rest = want;
+    int rest = budget;
     if (chunks == 1)
         load(0);
-    if (want > 0) {
+    {
         constexpr int SHIFT[3] = {21, 10, 0}, WIDTH[3] = {11, 11, 10};
-#pragma unroll
+#pragma unroll 1
         for (int pass = 0; pass < 3; ++pass) {
+            const int shift = SHIFT[pass];
             const uint32_t digits = (1u << WIDTH[pass]) - 1;
             for (int b = tid; b < BINS; b += SELECT_THREADS)
                 hist[b] = 0;
@@ -273,22 +277,16 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
                 if (chunks > 1)
                     load(ch * CHUNK);
 #pragma unroll
-                for (int r = 0; r < ROUNDS; ++r) {
-                    const bool in = candidate(ch * CHUNK + r * SELECT_THREADS + tid) && (key[r] & mask) == prefix;
-                    const uint32_t d = (key[r] >> SHIFT[pass]) & digits;
-                    const uint64_t who = __ballot(in);
-                    if (who == 0)
-                        continue;
-                    // one addition where the whole wavefront agrees (all weights zero, or equal)
-                    const int leader = __ffsll((unsigned long long)who) - 1;
-                    const uint32_t d0 = __builtin_amdgcn_readlane(d, leader);
-                    if (__ballot(in && d != d0) == 0) {
-                        if (lane == leader)
-                            atomicAdd(&hist[d0], __popcll(who));
-                    } else if (in) {
-                        atomicAdd(&hist[d], 1);
+                for (int r = 0; r < ROUNDS; ++r)
+                    if (((key[r] ^ prefix) & mask) == 0) {
+                        const uint32_t d = (key[r] >> shift) & digits, d0 = __builtin_amdgcn_readfirstlane(d);
+                        const uint64_t same = __ballot(d == d0), all = __ballot(true);
+                        // one addition where every counted lane agrees (all weights zero, or equal)
+                        if (same != all)
+                            atomicAdd(&hist[d], 1);
+                        else if (lane == __ffsll((unsigned long long)all) - 1)
+                            atomicAdd(&hist[d], __popcll(all));
                     }
-                }
             }
             __syncthreads();
             // thread t owns bins b, b - 1 counted from the top: find the bin where the running count reaches `rest`
@@ -296,77 +294,80 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
             const int n1 = hist[b], n0 = hist[b - 1];
             const int incl = wave_scan_incl(n1 + n0);
             if (lane == 63)
-                part[wave] = incl;
+                part[0][wave] = incl;
             __syncthreads();
             int before = incl - (n1 + n0);
             for (int w = 0; w < wave; ++w)
-                before += part[w];
+                before += part[0][w];
             if (before < rest && before + n1 + n0 >= rest) {
                 const bool second = before + n1 < rest;
                 found[0] = second ? b - 1 : b;
                 found[1] = rest - before - (second ? n1 : 0);
             }
             __syncthreads();
-            prefix |= uint32_t(found[0]) << SHIFT[pass];
-            mask |= digits << SHIFT[pass];
+            prefix |= uint32_t(found[0]) << shift;
+            mask |= digits << shift;
             rest = found[1];                               // of the keys with this prefix, so many are kept
             __syncthreads();
         }
     }
 
-    // ---- kept tokens in ascending order: ranks by prefix counts over (round, wavefront)
-    int done_eq = 0, done = 0;                             // equal keys and kept tokens of earlier chunks
+    // ---- kept tokens in ascending order: counts of those kept for sure and of the equal ones by (round,
+    // wavefront), their prefixes in index order; of the equal ones before a token, at most `rest` are kept
     constexpr int CELLS = ROUNDS * SELECT_WAVES;
     static_assert(CELLS <= SELECT_THREADS, "one prefix per thread");
-    auto prefix_counts = [&]() {                           // counts[] -> exclusive prefixes; returns the total
-        __syncthreads();
-        const int v = tid < CELLS ? counts[tid] : 0;
-        const int incl = wave_scan_incl(v);
-        if (lane == 63)
-            part[wave] = incl;
-        __syncthreads();
-        int before = incl - v, total = 0;
-        for (int w = 0; w < SELECT_WAVES; ++w) {
-            before += w < wave ? part[w] : 0;
-            total += part[w];
-        }
-        if (tid < CELLS)
-            counts[tid] = before;
-        __syncthreads();
-        return total;
-    };
+    int done[2] = {0, 0};                                  // sure and equal tokens of earlier chunks
     for (int ch = 0; ch < chunks; ++ch) {
-        if (chunks > 1 || want <= 0)
+        if (chunks > 1)
             load(ch * CHUNK);
-        uint64_t eq[ROUNDS];
+        int mine[2] = {0, 0};                              // this wavefront's counts of round l in lane l
 #pragma unroll
         for (int r = 0; r < ROUNDS; ++r) {
-            eq[r] = __ballot(want > 0 && candidate(ch * CHUNK + r * SELECT_THREADS + tid) && key[r] == prefix);
-            if (lane == 0)
-                counts[r * SELECT_WAVES + wave] = __popcll(eq[r]);
+            const int ns = __popcll(__ballot(key[r] > prefix)), ne = __popcll(__ballot(key[r] == prefix));
+            mine[0] = lane == r ? ns : mine[0];
+            mine[1] = lane == r ? ne : mine[1];
         }
-        const int n_eq = prefix_counts();
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const int t = ch * CHUNK + r * SELECT_THREADS + tid;
-            const int rank = done_eq + counts[r * SELECT_WAVES + wave] + __popcll(eq[r] & lanemask_lt(lane));
-            const bool cand = candidate(t);
-            const bool in = t < len && (!cand || (want > 0 && (key[r] > prefix || (key[r] == prefix && rank < rest))));
-            eq[r] = __ballot(in);
+        if (lane < ROUNDS) {
+            counts[0][lane * SELECT_WAVES + wave] = mine[0];
+            counts[1][lane * SELECT_WAVES + wave] = mine[1];
         }
         __syncthreads();
+        int v[2], incl[2];
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r)
-            if (lane == 0)
-                counts[r * SELECT_WAVES + wave] = __popcll(eq[r]);
-        const int n_in = prefix_counts();
+        for (int j = 0; j < 2; ++j) {
+            v[j] = tid < CELLS ? counts[j][tid] : 0;
+            incl[j] = wave_scan_incl(v[j]);
+            if (lane == 63)
+                part[j][wave] = incl[j];
+        }
+        __syncthreads();
+        int total[2];
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r)
-            if (eq[r] >> lane & 1)
-                out[done + counts[r * SELECT_WAVES + wave] + __popcll(eq[r] & lanemask_lt(lane))] =
-                    ch * CHUNK + r * SELECT_THREADS + tid;
-        done_eq += n_eq;
-        done += n_in;
+        for (int j = 0; j < 2; ++j) {
+            int before = done[j] + incl[j] - v[j];
+            total[j] = 0;
+            for (int w = 0; w < SELECT_WAVES; ++w) {
+                before += w < wave ? part[j][w] : 0;
+                total[j] += part[j][w];
+            }
+            if (tid < CELLS)
+                counts[j][tid] = before;
+        }
+        __syncthreads();
+        if (lane < ROUNDS) {
+            mine[0] = counts[0][lane * SELECT_WAVES + wave];
+            mine[1] = counts[1][lane * SELECT_WAVES + wave];
+        }
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const uint64_t sure = __ballot(key[r] > prefix), eq = __ballot(key[r] == prefix);
+            const int ns = __builtin_amdgcn_readlane(mine[0], r) + __popcll(sure & lanemask_lt(lane));
+            const int ne = __builtin_amdgcn_readlane(mine[1], r) + __popcll(eq & lanemask_lt(lane));
+            if (key[r] > prefix || (key[r] == prefix && ne < rest))
+                out[ns + min(ne, rest)] = ch * CHUNK + r * SELECT_THREADS + tid;
+        }
+        done[0] += total[0];
+        done[1] += total[1];
         __syncthreads();
     }
     if (bad)
@@ -445,15 +446,14 @@ __global__ void __launch_bounds__(256) kv_compact_kernel(KvCache c, KvSeqs s, co
     uint8_t *base = c.data + kv_offset(to, h, c.H, D);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const float scale = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT));
+        const float scale = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT)), inv = 1.0f / scale;
 #pragma unroll
         for (int p = 0; p < R::N; ++p) {
             const int r = r0 + p * R::ROWS;
             if (r < n) {
-                const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * sc[j][p], d = kv_unpack4<FMT>(w[j][p].y) * sc[j][p];
+                const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * sc[j][p] * inv, d = kv_unpack4<FMT>(w[j][p].y) * sc[j][p] * inv;
                 *reinterpret_cast<uint2 *>(base + j * (KV_BLOCK * D) + r * D + chunk * 8) =
-                    make_uint2(kv_pack4<FMT>(a[0] / scale, a[1] / scale, a[2] / scale, a[3] / scale),
-                               kv_pack4<FMT>(d[0] / scale, d[1] / scale, d[2] / scale, d[3] / scale));
+                    make_uint2(kv_pack4<FMT>(a[0], a[1], a[2], a[3]), kv_pack4<FMT>(d[0], d[1], d[2], d[3]));
             }
         }
         if (threadIdx.x == 0)
