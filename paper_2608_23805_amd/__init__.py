@@ -198,12 +198,13 @@ def _load():
     L.msi_residual_init.argtypes = [_vp, _vp, _vp, _u32, _u32, _vp]
     L.msi_residual_add.argtypes = [_vp, _vp, _vp, _u32, _u32, _vp]
     L.msi_plan_timings.argtypes = [_vp, P(msi_timings), ctypes.c_int]
-    L.msi_linear.argtypes = [P(msi_linear_args), _vp]
+    # (argument structs of the attention block come as pointers or as packed bytes)
+    L.msi_linear.argtypes = [_vp, _vp]
     for n in ("msi_kv_append", "msi_kv_read"):
-        getattr(L, n).argtypes = [P(msi_kv_cache), P(msi_kv_seqs), _vp, _vp, _u64, _u64, _vp, _vp]
-    L.msi_kv_attention_workspace.argtypes = [P(msi_kv_cache), P(msi_kv_seqs), _u32, _u32, P(_u64)]
-    L.msi_kv_attention.argtypes = [P(msi_kv_cache), P(msi_kv_seqs), P(msi_kv_attention_args), _vp]
-    L.msi_kv_evict.argtypes = [P(msi_kv_cache), P(msi_kv_seqs), P(msi_kv_evict_args), _vp]
+        getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
+    L.msi_kv_attention_workspace.argtypes = [_vp, _vp, _u32, _u32, P(_u64)]
+    L.msi_kv_attention.argtypes = [_vp, _vp, _vp, _vp]
+    L.msi_kv_evict.argtypes = [_vp, _vp, _vp, _vp]
     L.msi_stream_threshold.argtypes = [_u32]
     L.msi_stream_threshold.restype = _u32
     for n in EXPORTS:
@@ -504,235 +505,18 @@ class Plan:
         _check(lib.msi_debug_source_release(self.h))
 
 
-# ---------------------------------------------------------------------------
-# attention block: projections and the paged 8-bit cache
-# ---------------------------------------------------------------------------
-
-def _refuse(msg: str):
-    raise MsiError(MSI_E_INVALID_ARG, msg)
+# The attention block's operators (projections, the paged 8-bit cache, its attention and eviction) live in
+# ``attention``, which imports torch; they are found here by name.
+_ATTENTION = ("linear", "KvCache", "KvSeqs", "kv_append", "kv_read", "kv_attention_workspace_size",
+              "kv_attention_workspace", "kv_attention", "kv_evict", "AttentionBlock")
 
 
-def _bf16_rows(name: str, t, device):
-    """(rows, row stride) of a bf16 tensor (or bf16 bits in int16) whose rows are contiguous in themselves."""
-    import torch
-    if t.dtype not in (torch.bfloat16, torch.int16) or t.device != device:
-        _refuse(f"{name} must be bf16 (or its bits in int16) on {device}, got {t.dtype} on {t.device}")
-    step = 1
-    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if n != 1 and s != step:
-            _refuse(f"{name}: the elements of a row must be contiguous")
-        step *= n
-    if t.shape[0] > 1 and t.stride(0) < step:
-        _refuse(f"{name}: rows overlap")
-    return t.shape[0], (t.stride(0) if t.shape[0] > 1 else (step + 7) // 8 * 8)
-
-
-def _dense(name: str, t, dtype, device, shape=None):
-    if t.dtype != dtype or t.device != device or not t.is_contiguous():
-        _refuse(f"{name} must be contiguous {dtype} on {device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _refuse(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-
-
-class _on:
-    """The tensors' device made current around a call where it is not."""
-
-    def __init__(self, device):
-        import torch
-        self.guard = None
-        if device.type == "cuda" and device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
-
-
-def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
-    """out = act(x w^T + bias) + residual (msi_linear).
-
-    x [M, K] and w [N, K] bf16 (x's rows may be strided), bias [N] float32,
-    residual and out [M, N] bf16 or float32 with strided rows; residual may be out."""
-    import torch
-    dev = x.device
-    if x.dim() != 2 or w.dim() != 2 or out.dim() != 2:
-        _refuse("x, w and out must be matrices")
-    M, xs = _bf16_rows("x", x, dev)
-    K, N = x.shape[1], w.shape[0]
-    if w.dtype not in (torch.bfloat16, torch.int16):
-        _refuse("w must be bf16 (or its bits in int16)")
-    _dense("w", w, w.dtype, dev, (N, K))
-    if act not in ACTIVATIONS:
-        _refuse(f"unknown activation {act!r}")
-    if bias is not None:
-        _dense("bias", bias, torch.float32, dev, (N,))
-
-    def matrix(name, t):
-        if tuple(t.shape) != (M, N) or t.device != dev or (N > 1 and t.stride(1) != 1):
-            _refuse(f"{name} must be [{M}, {N}] on {dev} with contiguous rows")
-        if t.dtype == torch.float32:
-            return MSI_F32, (t.stride(0) if M > 1 else N)
-        return MSI_BF16, (_bf16_rows(name, t, dev)[1] if M > 1 else N)
-    od, os_ = matrix("out", out)
-    rd, rs = matrix("residual", residual) if residual is not None else (0, 0)
-    a = msi_linear_args(x=_ptr(x), w=_ptr(w), bias=_ptr(bias), residual=_ptr(residual), out=_ptr(out), M=M, N=N, K=K,
-                        activation=ACTIVATIONS[act], residual_dtype=rd, out_dtype=od, x_stride=xs, residual_stride=rs,
-                        out_stride=os_)
-    with _on(dev):
-        _check(lib.msi_linear(ctypes.byref(a), _stream(stream)))
-
-
-class KvCache:
-    """One layer's pages of keys and values in 8 bits (msi_kv_cache).
-
-    data [n_pages, n_heads, 2, 64, head_dim] uint8, scales [n_pages, n_heads, 2]
-    float32, mass [n_pages, n_heads, 64] float32 or None; ``alloc`` makes them."""
-
-    def __init__(self, data, scales, mass=None, fmt: str = "e4m3"):
-        import torch
-        if fmt not in KV_FORMATS:
-            _refuse(f"unknown cache format {fmt!r}")
-        if data.dim() != 5 or data.shape[2] != 2 or data.shape[3] != MSI_KV_BLOCK:
-            _refuse("data must be [n_pages, n_heads, 2, 64, head_dim]")
-        P, H, _, _, D = data.shape
-        _dense("data", data, torch.uint8, data.device)
-        _dense("scales", scales, torch.float32, data.device, (P, H, 2))
-        if mass is not None:
-            _dense("mass", mass, torch.float32, data.device, (P, H, MSI_KV_BLOCK))
-        self.data, self.scales, self.mass, self.fmt = data, scales, mass, fmt
-        self.n_pages, self.n_heads, self.head_dim, self.device = P, H, D, data.device
-        self.c = msi_kv_cache(KV_FORMATS[fmt], P, H, D, _ptr(data), _ptr(scales), _ptr(mass))
-
-    @staticmethod
-    def alloc(n_pages: int, n_heads: int, head_dim: int, fmt: str = "e4m3", mass: bool = True, device="cuda") -> "KvCache":
-        import torch
-        data = torch.empty((n_pages, n_heads, 2, MSI_KV_BLOCK, head_dim), dtype=torch.uint8, device=device)
-        scales = torch.empty((n_pages, n_heads, 2), dtype=torch.float32, device=device)
-        m = torch.zeros((n_pages, n_heads, MSI_KV_BLOCK), dtype=torch.float32, device=device) if mass else None
-        return KvCache(data, scales, m, fmt)
-
-
-class KvSeqs:
-    """The sequences of a call (msi_kv_seqs): page table [n_seqs, max_blocks],
-    token counts [n_seqs] and row offsets [n_seqs + 1] in device int32 tensors,
-    whose contents may change between calls, and the host's bounds on them."""
-
-    def __init__(self, table, lens, cu_rows=None, *, n_rows: int = 0, max_rows: int = 0, max_len: Optional[int] = None):
-        import torch
-        dev = lens.device
-        if table.dim() != 2:
-            _refuse("table must be [n_seqs, max_blocks]")
-        S, nb = table.shape
-        _dense("table", table, torch.int32, dev)
-        _dense("lens", lens, torch.int32, dev, (S,))
-        if cu_rows is not None:
-            _dense("cu_rows", cu_rows, torch.int32, dev, (S + 1,))
-        self.table, self.lens, self.cu_rows = table, lens, cu_rows
-        self.n_rows, self.max_rows = int(n_rows), int(max_rows)
-        self.max_len = nb * MSI_KV_BLOCK if max_len is None else int(max_len)
-        self.n_seqs, self.max_blocks, self.device = S, nb, dev
-        if min(self.n_rows, self.max_rows, self.max_len) < 0 or max(self.n_rows, self.max_rows, self.max_len) >= 1 << 31:
-            _refuse("n_rows, max_rows and max_len must be 0 .. 2^31 - 1")
-        self.c = msi_kv_seqs(S, nb, self.n_rows, self.max_rows, self.max_len, 0, _ptr(table), _ptr(lens), _ptr(cu_rows))
-
-
-def _status_word(status, device):
-    import torch
-    if status is not None:
-        _dense("status", status, torch.int32, device)
-        if status.numel() < 1:
-            _refuse("status must hold a word")
-    return _ptr(status)
-
-
-def _kv_rows(cache: KvCache, seqs: KvSeqs, name: str, t, heads: int) -> int:
-    """Row stride of a [n_rows, heads, head_dim] tensor."""
-    if tuple(t.shape) != (seqs.n_rows, heads, cache.head_dim):
-        _refuse(f"{name} must be [{seqs.n_rows}, {heads}, {cache.head_dim}], got {tuple(t.shape)}")
-    return _bf16_rows(name, t, cache.device)[1]
-
-
-def _same_device(cache: KvCache, seqs: KvSeqs):
-    if seqs.device != cache.device:
-        _refuse("cache and sequences must be on one device")
-
-
-def kv_append(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
-    """Write the last rows of every sequence into its pages (msi_kv_append); k, v [n_rows, n_heads, head_dim] bf16."""
-    _same_device(cache, seqs)
-    ks, vs = _kv_rows(cache, seqs, "k", k, cache.n_heads), _kv_rows(cache, seqs, "v", v, cache.n_heads)
-    with _on(cache.device):
-        _check(lib.msi_kv_append(ctypes.byref(cache.c), ctypes.byref(seqs.c), _ptr(k), _ptr(v), ks, vs,
-                                 _status_word(status, cache.device), _stream(stream)))
-
-
-def kv_read(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
-    """The last rows of every sequence as bf16 into k, v [n_rows, n_heads, head_dim] (msi_kv_read)."""
-    _same_device(cache, seqs)
-    ks, vs = _kv_rows(cache, seqs, "k", k, cache.n_heads), _kv_rows(cache, seqs, "v", v, cache.n_heads)
-    with _on(cache.device):
-        _check(lib.msi_kv_read(ctypes.byref(cache.c), ctypes.byref(seqs.c), _ptr(k), _ptr(v), ks, vs,
-                               _status_word(status, cache.device), _stream(stream)))
-
-
-def kv_attention_workspace_size(cache: KvCache, seqs: KvSeqs, n_q_heads: int, mass_rows: int = 0) -> int:
-    n = _u64()
-    _check(lib.msi_kv_attention_workspace(ctypes.byref(cache.c), ctypes.byref(seqs.c), n_q_heads, mass_rows,
-                                          ctypes.byref(n)))
-    return n.value
-
-
-def kv_attention_workspace(cache: KvCache, seqs: KvSeqs, n_q_heads: int, mass_rows: int = 0):
-    """Workspace of kv_attention calls with these bounds (a uint8 tensor)."""
-    import torch
-    return torch.empty(kv_attention_workspace_size(cache, seqs, n_q_heads, mass_rows), dtype=torch.uint8,
-                       device=cache.device)
-
-
-def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: int = 0, mass_decay: float = 1.0,
-                 workspace=None, status=None, stream=None):
-    """Attention of q [n_rows, n_q_heads, head_dim] bf16 over the sequences' pages into out (msi_kv_attention)."""
-    import torch
-    _same_device(cache, seqs)
-    if q.dim() != 3:
-        _refuse("q must be [n_rows, n_q_heads, head_dim]")
-    Hq = q.shape[1]
-    if mass_rows < 0:
-        _refuse("mass_rows must not be negative")
-    qs, os_ = _kv_rows(cache, seqs, "q", q, Hq), _kv_rows(cache, seqs, "out", out, Hq)
-    if workspace is not None:
-        _dense("workspace", workspace, torch.uint8, cache.device)
-    a = msi_kv_attention_args(q=_ptr(q), out=_ptr(out), q_stride=qs, out_stride=os_, n_q_heads=Hq, scale=scale,
-                              mass_rows=min(mass_rows, 1 << 30), mass_decay=mass_decay, workspace=_ptr(workspace),
-                              workspace_bytes=0 if workspace is None else workspace.numel(),
-                              status=_status_word(status, cache.device))
-    with _on(cache.device):
-        _check(lib.msi_kv_attention(ctypes.byref(cache.c), ctypes.byref(seqs.c), ctypes.byref(a), _stream(stream)))
-
-
-def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget: int, sinks: int = 0, recent: int = 0,
-             status=None, stream=None):
-    """Cut every sequence back to ``budget`` tokens a head into the pages of dst_table [n_seqs, blocks]
-    (msi_kv_evict); new_lens [n_seqs] and keep [n_seqs, n_heads, budget] int32 receive what was kept."""
-    import torch
-    _same_device(cache, seqs)
-    dev = cache.device
-    if min(budget, sinks, recent) < 0 or max(budget, sinks, recent) >= 1 << 31:
-        _refuse("budget, sinks and recent must be 0 .. 2^31 - 1")
-    if dst_table.dim() != 2 or dst_table.shape[0] != seqs.n_seqs:
-        _refuse("dst_table must be [n_seqs, blocks]")
-    _dense("dst_table", dst_table, torch.int32, dev)
-    _dense("new_lens", new_lens, torch.int32, dev, (seqs.n_seqs,))
-    _dense("keep", keep, torch.int32, dev, (seqs.n_seqs, cache.n_heads, budget))
-    a = msi_kv_evict_args(budget=budget, sinks=sinks, recent=recent, dst_blocks=dst_table.shape[1],
-                          dst_table=_ptr(dst_table), new_lens=_ptr(new_lens), keep=_ptr(keep),
-                          status=_status_word(status, dev))
-    with _on(dev):
-        _check(lib.msi_kv_evict(ctypes.byref(cache.c), ctypes.byref(seqs.c), ctypes.byref(a), _stream(stream)))
+def __getattr__(name: str):
+    if name in _ATTENTION:
+        from . import attention
+        globals().update({n: getattr(attention, n) for n in _ATTENTION})
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def _window_ptr(w) -> int:

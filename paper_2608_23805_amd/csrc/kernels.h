@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <utility>
 
 #include "common.h"
@@ -61,6 +62,20 @@ inline hipError_t allow_large_lds(const void *f)
         return e;
     return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
                                int(160 * 1024 - a.sharedSizeBytes));
+}
+// Let kernel f use `bytes` of dynamic LDS on the current device; `done` is the
+// kernel's own: the devices (by bit) on which that has been said already.
+inline hipError_t allow_lds_once(const void *f, size_t bytes, std::atomic<uint64_t> &done)
+{
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    const uint64_t bit = uint64_t(1) << (device & 63);
+    if (e != hipSuccess || bytes <= 64 * 1024 || (done.load(std::memory_order_relaxed) & bit))
+        return e;
+    e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+    if (e == hipSuccess && device < 64)
+        done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 // Outputs of one routing (device arrays, see msi_routing).
 struct RouteOut {

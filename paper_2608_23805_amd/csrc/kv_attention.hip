@@ -1124,8 +1124,8 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
     with_shape(fmt, A.c.D, [&](auto f, auto d) {
         constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
         if (!c.few) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D>),
-                                    hipFuncAttributeMaxDynamicSharedMemorySize, int(ManyRows<D>::LDS));
+            static std::atomic<uint64_t> done{0};
+            e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D>), ManyRows<D>::LDS, done);
             if (e == hipSuccess)
                 launch_k(kv_many_rows_kernel<FMT, D>, grid, 256, ManyRows<D>::LDS, st, A);
         } else if (c.tile_rows == 16)

@@ -45,11 +45,12 @@ struct KvSeq {
 // ok = false otherwise.  cached: every row is one of the sequence's tokens.
 MSI_HD KvSeq kv_check_seq(int row0, int row1, int len, int n_rows, int max_rows, int max_len, bool cached)
 {
-    KvSeq s{row0, row1 - row0, len, true};
-    // (differences of values already known to lie in [0, n_rows] cannot overflow)
+    KvSeq s{row0, 0, len, true};
     s.ok = len >= 0 && len <= max_len && row0 >= 0 && row0 <= n_rows && row1 >= row0 && row1 <= n_rows;
-    if (s.ok)
-        s.ok = row1 - row0 <= max_rows && (!cached || row1 - row0 <= len);
+    if (s.ok) {
+        s.n = row1 - row0;                   // (of values in [0, n_rows]: no overflow)
+        s.ok = s.n <= max_rows && (!cached || s.n <= len);
+    }
     if (!s.ok)
         s.n = s.len = 0;
     return s;

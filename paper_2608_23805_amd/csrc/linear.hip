@@ -385,8 +385,8 @@ __global__ void __launch_bounds__(ring::THREADS, 2) linear_ring_kernel(LinearArg
 template <int ACT, class S>
 hipError_t launch_tile(const LinearArgs &A, hipStream_t st)
 {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(linear_tile_kernel<ACT, S>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, int(S::LDS));
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(linear_tile_kernel<ACT, S>), S::LDS, done);
     if (e != hipSuccess)
         return e;
     const int64_t tiles = int64_t((A.M + S::BM - 1) / S::BM) * ((A.N + S::TN - 1) / S::TN);
