@@ -17,7 +17,7 @@ from typing import Optional
 import torch
 
 from . import (ACTIVATIONS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
-               msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, residual_add, _check)
+               msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
 _F32, _I32 = torch.float32, torch.int32
@@ -300,4 +300,5 @@ class AttentionBlock:
                      workspace=self.workspace, status=status, stream=stream)
         linear(attn.view(n, -1), self.wo, out, stream=stream)
         if n:
-            residual_add(out, h, x, stream)
+            _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
+                  _stream(stream))

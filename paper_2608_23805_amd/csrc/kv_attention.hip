@@ -990,35 +990,27 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
     }
 }
 
-// For many rows the scores are computed again from K: one workgroup per
-// block, its wavefronts take every fourth group of 32 rows.
+// For many rows the scores are computed again from K.  A wavefront keeps a
+// block's K in registers (as bf16, with D = 256 as codes) and walks groups of
+// 32 rows; the next group's queries are on their way while the vector unit takes the
+// exponentials, which bound it.  With `share` = 4 the four wavefronts of a workgroup
+// have a block each and meet the same queries at about the same time (in L1);
+// with 1 they share one block and take every fourth group, for calls with few blocks.
 template <int FMT, int D>
-__global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
+__global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A, int share)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t kl[KV_BLOCK * D];
     __shared__ float part[4][KV_BLOCK];
-    const int i = blockIdx.z, h = blockIdx.y, b = blockIdx.x;
+    constexpr bool RAW = D == 256;
+    const int i = blockIdx.z, h = blockIdx.y;
     const KvSeq q = kv_seq(A.s, i, false);
-    if (b * KV_BLOCK >= q.len)
-        return;
-    const int page = __builtin_amdgcn_readfirstlane(A.s.table[int64_t(i) * A.s.max_blocks + b]);
-    if (!kv_page_ok(page, A.c.n_pages))
-        return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int b = int(blockIdx.x) * share + wave % share, group = wave / share, groups = 4 / share;
+    if (int(blockIdx.x) * share * KV_BLOCK >= q.len)
+        return;
     const int col = lane & 31, hf = lane >> 5;
-    {
-        const uint8_t *block = A.c.data + kv_offset(page, h, A.c.H, D);
-        constexpr int CPR = D / 16;
-#pragma unroll
-        for (int p = 0; p < KV_BLOCK * CPR / 256; ++p) {
-            const int at = p * 256 + int(threadIdx.x), t = at / CPR, c = at % CPR;
-            *reinterpret_cast<u32x4 *>(kl + t * D + ((c ^ many_swz<D>(t)) << 4)) =
-                *reinterpret_cast<const u32x4 *>(block + at * 16);
-        }
-    }
-    __syncthreads();
-    const float ks = A.c.scales[(int64_t(page) * A.c.H + h) * 2] * fabsf(A.scale_log2);
-    const int rows = q.n * A.G;
+    int page = b * KV_BLOCK < q.len ? A.s.table[int64_t(i) * A.s.max_blocks + b] : -1;
+    page = __builtin_amdgcn_readfirstlane(kv_page_ok(page, A.c.n_pages) ? page : -1);
+    const int rows = page < 0 ? 0 : q.n * A.G;
     // rows below `from` do not count, or do not see the block
     const int from = max(max(q.n - A.mass_rows, 0), b * KV_BLOCK - (q.len - q.n)) * A.G;
     f32x16 w[2];
@@ -1027,21 +1019,69 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
             w[x][v] = 0.0f;
-    for (int r0 = from + 32 * wave; r0 < rows; r0 += 128) {
-        bf16x8 qf[D / 16];
-        load_q32<D>(qf, A, q, h, r0, rows);
-        f32x16 sv[2];
-        scores32<FMT, D>(sv, kl, [&](int c) { return qf[c]; });
-        const int r = r0 + col, rc = min(r, rows - 1), tr = rc / A.G;
-        const int limit = r < rows ? row_limit(q, tr) : 0;
-        const float z0 = A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + rc - tr * A.G];
+    int r0 = from + 32 * group;
+    if (r0 < rows) {
+        u32x4 codes[RAW ? 2 : 1][RAW ? D / 32 : 1];
+        bf16x8 kf[RAW ? 1 : 2][RAW ? 1 : D / 16];
+        const uint8_t *block = A.c.data + kv_offset(page, h, A.c.H, D) + col * D + 16 * hf;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -z0));
-                w[x][v] += b * KV_BLOCK + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? p : 0.0f;
+            for (int p = 0; p < D / 32; ++p) {
+                const u32x4 c = *reinterpret_cast<const u32x4 *>(block + 32 * x * D + 32 * p);
+                if constexpr (RAW) {
+                    codes[x][p] = c;
+                } else {
+                    kf[x][2 * p] = codes_bf16<FMT>(c[0], c[1]);
+                    kf[x][2 * p + 1] = codes_bf16<FMT>(c[2], c[3]);
+                }
             }
+        const float ks = A.c.scales[(int64_t(page) * A.c.H + h) * 2] * fabsf(A.scale_log2);
+        auto log_sum_of = [&](int first) {
+            const int rc = min(first + col, rows - 1), tr = rc / A.G;
+            return A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + rc - tr * A.G];
+        };
+        bf16x8 qf[D / 16];
+        load_q32<D>(qf, A, q, h, r0, rows);
+        float z = log_sum_of(r0);
+        for (; r0 < rows; r0 += 32 * groups) {
+            f32x16 sv[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    sv[x][v] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    if constexpr (RAW)
+                        sv[x] = mfma32(codes_bf16<FMT>(codes[x][c / 2][2 * (c % 2)], codes[x][c / 2][2 * (c % 2) + 1]), qf[c],
+                                       sv[x]);
+                    else
+                        sv[x] = mfma32(kf[x][c], qf[c], sv[x]);
+                }
+            }
+            const float z0 = z;
+            const int next = min(r0 + 32 * groups, rows - 1);
+            load_q32<D>(qf, A, q, h, next, rows);
+            z = log_sum_of(next);
+            const int r = r0 + col, limit = r < rows ? row_limit(q, r / A.G) : 0;
+            // (a row past the last one, or one that does not see the whole block)
+            if (r0 + 32 > rows || row_limit(q, r0 / A.G) < (b + 1) * KV_BLOCK) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -z0));
+                        w[x][v] += b * KV_BLOCK + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? e : 0.0f;
+                    }
+            } else {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        w[x][v] += __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -z0));
+            }
+        }
     }
     // over the 32 columns: four steps within 16 lanes, then the other 16
 #pragma unroll
@@ -1059,10 +1099,11 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A)
                 part[wave][32 * x + 8 * (v >> 2) + 4 * hf + (v & 3)] = a;
         }
     __syncthreads();
-    if (threadIdx.x < KV_BLOCK && b * KV_BLOCK + int(threadIdx.x) < q.len) {
-        const int t = threadIdx.x;
-        const float sum = ((part[0][t] + part[1][t]) + part[2][t]) + part[3][t];
-        float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + t;
+    if (group == 0 && page >= 0 && b * KV_BLOCK + lane < q.len) {
+        float sum = part[wave][lane];
+        for (int g = 1; g < groups; ++g)
+            sum += part[wave + g * share][lane];
+        float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + lane;
         *dst = A.decay != 0.0f ? fmaf(A.decay, *dst, sum) : sum;
     }
 }
@@ -1144,8 +1185,10 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
         e = hipGetLastError();
     }
     if (e == hipSuccess && A.mass_rows && !c.few && blocks) {
+        const int share = int64_t(blocks) * H * S >= 4 * 256 ? 4 : 1;
         with_shape(fmt, A.c.D, [&](auto f, auto d) {
-            launch_k(kv_mass_rows_kernel<decltype(f)::value, decltype(d)::value>, dim3(blocks, H, S), 256, 0, st, A);
+            launch_k(kv_mass_rows_kernel<decltype(f)::value, decltype(d)::value>, dim3((blocks + share - 1) / share, H, S),
+                     256, 0, st, A, share);
         });
         e = hipGetLastError();
     }
