@@ -464,9 +464,11 @@ typedef struct {
     const void *x;               /* [M, K] bf16, x_stride >= K, a multiple of 8       */
     const void *w;               /* [N, K] bf16, row-major                             */
     const float *bias;           /* [N], or NULL                                       */
-    const void *residual;        /* [M, N] in residual_dtype, or NULL; may be `out`    */
-    void *out;                   /* [M, N] in out_dtype                                */
-    uint32_t M, N, K;            /* K a multiple of 8, 8 <= K <= 2^21; M or N may be 0 */
+    const void *residual;        /* [M, N] in residual_dtype, or NULL; may be `out`,
+                                    of its type and stride                             */
+    void *out;                   /* [M, N] in out_dtype; must not overlap x or w       */
+    uint32_t M, N, K;            /* K a multiple of 8, 8 <= K <= 2^21; M, N <= 2^29,
+                                    M * N <= 2^36, either may be 0                     */
     uint32_t activation;         /* msi_activation                                     */
     uint32_t residual_dtype, out_dtype;   /* msi_dtype                                 */
     uint64_t x_stride, residual_stride, out_stride;
@@ -479,8 +481,9 @@ msi_status msi_linear(const msi_linear_args *args, void *stream);
  * tokens of every head, handed to sequences by the caller's page tables.  Page
  * p, head h: 64 rows of K codes, then 64 rows of V codes, one byte an element;
  * value = scale * code, one fp32 scale for the block's K and one for its V.
- * Codes are OCP e4m3 (no NaN codes) or int8 in -127 .. 127.  `mass` holds each
- * token's accumulated attention weight, by head. */
+ * Codes are OCP e4m3 (no NaN codes) or int8 in -127 .. 127, scales positive
+ * and finite.  `mass` holds each token's accumulated attention weight, by head.
+ * Several sequences may hold a page that a call only reads. */
 #define MSI_KV_BLOCK 64u
 typedef enum { MSI_KV_E4M3 = 0, MSI_KV_INT8 = 1 } msi_kv_format;
 typedef struct {
@@ -507,8 +510,8 @@ typedef struct {
 #define MSI_KV_BAD_LENGTH 4u
 typedef struct {
     uint32_t n_seqs;             /* <= 65535                                           */
-    uint32_t max_blocks;         /* row length of table                                */
-    uint32_t n_rows;             /* rows of the call's row arrays                      */
+    uint32_t max_blocks;         /* row length of table, <= 2^23                       */
+    uint32_t n_rows;             /* rows of the call's row arrays, <= 2^29             */
     uint32_t max_rows;           /* bound of one sequence's rows                       */
     uint32_t max_len;            /* bound of lens, <= 64 * max_blocks                  */
     uint32_t reserved;
@@ -539,8 +542,9 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
  * allowed here).  With mass_rows > 0, mass[t] = mass_decay * mass[t] + the sum
  * of the probabilities that the sequence's last mass_rows rows and the head's
  * query heads give token t, for every token (with mass_decay 0 the old value
- * is not read).  Sums are taken in a fixed order: equal calls give equal
- * bits.  `out` must not overlap q. */
+ * is not read; a call with max_rows 0 does nothing).  Where it writes
+ * mass, no page may be in the call's tables twice.  Sums are taken in a fixed order: equal calls give equal
+ * bits.  `out` must not overlap q.  n_seqs * n_heads * ceil(max_rows * heads of a group / 128) is under 2^24. */
 typedef struct {
     const void *q;               /* [n_rows, n_q_heads, head_dim] bf16                 */
     void *out;                   /* the same shape, bf16                               */

@@ -16,7 +16,7 @@ from typing import Optional
 
 import torch
 
-from . import (ACTIVATIONS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
+from . import (ACTIVATIONS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
                msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
@@ -293,6 +293,9 @@ class AttentionBlock:
             _refuse(f"{n} rows, buffers for {self.qkv.shape[0]}")
         _dense("x", x, x.dtype, self.cache.device, (n, self.wqkv.shape[1]))
         _dense("h", h, _F32, self.cache.device, (n, self.wqkv.shape[1]))
+        need = kv_attention_workspace_size(self.cache, seqs, Hq, mass_rows)
+        if need > (0 if self.workspace is None else self.workspace.numel()):
+            raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step")
         qkv, attn, out = self.qkv[:n], self.attn[:n], self.out[:n]
         linear(x, self.wqkv, qkv.view(n, -1), bias=self.bias, stream=stream)
         kv_append(self.cache, seqs, qkv[:, Hq:Hq + H], qkv[:, Hq + H:], status=status, stream=stream)

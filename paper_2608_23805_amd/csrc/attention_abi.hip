@@ -17,7 +17,9 @@ msi_status launched(hipError_t e) { return e == hipSuccess ? MSI_OK : abi_error(
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 constexpr uint64_t MOST_STRIDE = 1u << 21;      // elements: tile offsets stay under 2^31 bytes
-constexpr uint32_t MOST = 1u << 30;
+constexpr uint32_t MOST = 1u << 29;              // rows, tokens, features: grids of 64 of them stay under 2^32 threads
+constexpr uint32_t MOST_PAGES = 1u << 30;
+constexpr uint64_t MOST_GROUPS = 1u << 24;       // workgroups of 256 along a grid's x
 
 // Cache and sequences as the kernels take them; nullptr if the call may go on, else what is wrong.
 const char *view_cache(const msi_kv_cache *c, KvCache &out)
@@ -30,7 +32,7 @@ const char *view_cache(const msi_kv_cache *c, KvCache &out)
         return "head_dim must be 64, 128 or 256";
     if (c->n_heads < 1 || c->n_heads > 256)
         return "n_heads must be 1 .. 256";
-    if (c->n_pages < 1 || c->n_pages > MOST)
+    if (c->n_pages < 1 || c->n_pages > MOST_PAGES)
         return "n_pages must be 1 .. 2^30";
     if (!c->data || !c->scales)
         return "null cache array";
@@ -47,12 +49,12 @@ const char *view_seqs(const msi_kv_seqs *s, bool rows, KvSeqs &out)
     if (s->n_seqs > 65535)
         return "n_seqs must be at most 65535";
     if (s->max_blocks > MOST / MSI_KV_BLOCK || s->max_len > uint64_t(s->max_blocks) * MSI_KV_BLOCK)
-        return "max_len must be at most 64 * max_blocks";
+        return "max_len must be at most 64 * max_blocks, max_blocks at most 2^23";
     if (s->n_seqs && (!s->lens || (s->max_len && !s->table)))
         return "null sequence array";
     if (rows) {
         if (s->n_rows > MOST || s->max_rows > s->n_rows)
-            return "max_rows must be at most n_rows, n_rows at most 2^30";
+            return "max_rows must be at most n_rows, n_rows at most 2^29";
         if (s->n_seqs && !s->cu_rows)
             return "null cu_rows";
     }
@@ -87,10 +89,13 @@ const char *check_heads(const KvCache &c, const KvSeqs &s, uint32_t n_q_heads)
 {
     if (n_q_heads == 0 || n_q_heads % uint32_t(c.H) || n_q_heads > 4096)
         return "n_q_heads must be a multiple of n_heads, at most 4096";
-    if (uint64_t(s.max_rows) * (n_q_heads / c.H) > MOST)
-        return "max_rows times the heads of a group must be at most 2^30";
+    const uint64_t rows = uint64_t(s.max_rows) * (n_q_heads / c.H);
+    if (rows > MOST)
+        return "max_rows times the heads of a group must be at most 2^29";
+    if ((rows + 127) / 128 * uint64_t(c.H) * uint64_t(s.S) >= MOST_GROUPS)
+        return "n_seqs * n_heads * (max_rows * heads of a group / 128) must be under 2^24";
     if (uint64_t(s.S) * ((s.max_len + KV_BLOCK - 1) / KV_BLOCK) > MOST)
-        return "n_seqs times the blocks of max_len must be at most 2^30";
+        return "n_seqs times the blocks of max_len must be at most 2^29";
     return nullptr;
 }
 
@@ -114,8 +119,8 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
         return bad("unknown dtype");
     if (a->K < 8 || a->K % 8 || a->K > MOST_STRIDE)
         return bad("K must be a multiple of 8, 8 .. 2^21");
-    if (a->M > MOST || a->N > MOST || uint64_t(a->M) * a->N > uint64_t(MOST) * 64)
-        return bad("M and N must be at most 2^30, M * N at most 2^36");
+    if (a->M > MOST || a->N > MOST || uint64_t(a->M) * a->N > uint64_t(MOST) * 128)
+        return bad("M and N must be at most 2^29, M * N at most 2^36");
     if (a->M == 0 || a->N == 0)
         return MSI_OK;
     if (!rows_ok(a->x, a->x_stride, a->K))
@@ -124,9 +129,13 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
         return bad("w must be a 16-byte aligned [N, K]");
     const size_t ob = a->out_dtype == MSI_F32 ? 4 : 2, rb = a->residual_dtype == MSI_F32 ? 4 : 2;
     if (!a->out || !aligned(a->out, ob) || a->out_stride < a->N || a->out_stride > MOST)
-        return bad("out needs rows of N, aligned to its type, a stride up to 2^30");
+        return bad("out needs rows of N, aligned to its type, a stride up to 2^29");
     if (a->residual && (!aligned(a->residual, rb) || a->residual_stride < a->N || a->residual_stride > MOST))
-        return bad("residual needs rows of N, aligned to its type, a stride up to 2^30");
+        return bad("residual needs rows of N, aligned to its type, a stride up to 2^29");
+    if (a->residual == a->out && (a->residual_dtype != a->out_dtype || a->residual_stride != a->out_stride))
+        return bad("a residual that is out needs its type and stride");
+    if (a->out == a->x || a->out == a->w)
+        return bad("out must not be x or w");
     if (!aligned(a->bias, 4))
         return bad("bias must be 4-byte aligned");
     LinearArgs l{};
@@ -217,8 +226,9 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
         return bad(e);
     if (const char *e = check_heads(c, s, a->n_q_heads))
         return bad(e);
-    if (!std::isfinite(a->scale))
-        return bad("scale must be finite");
+    const float scale_log2 = float(double(a->scale) * 1.4426950408889634);
+    if (!std::isfinite(scale_log2))
+        return bad("scale must be finite, under 2^127");
     if (a->mass_rows && !c.mass)
         return bad("mass_rows needs the cache's mass");
     if (a->mass_rows && !(a->mass_decay >= 0.0f && std::isfinite(a->mass_decay)))
@@ -246,7 +256,7 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     A.q_stride = int64_t(a->q_stride);
     A.out_stride = int64_t(a->out_stride);
     A.G = int(a->n_q_heads) / c.H;
-    A.scale_log2 = float(double(a->scale) * 1.4426950408889634);
+    A.scale_log2 = scale_log2;
     A.direct = cut.direct;
     A.per = cut.per;
     A.part_rows = s.max_rows * A.G;
@@ -280,7 +290,7 @@ msi_status msi_kv_evict(const msi_kv_cache *cache, const msi_kv_seqs *seqs, cons
     if (!c.mass)
         return bad("eviction needs the cache's mass");
     if (a->budget < 1 || a->budget > MOST || uint64_t(a->sinks) + a->recent > a->budget)
-        return bad("budget must be 1 .. 2^30 and at least sinks + recent");
+        return bad("budget must be 1 .. 2^29 and at least sinks + recent");
     if (s.S == 0)
         return MSI_OK;
     const uint32_t most = std::min<uint32_t>(a->budget, uint32_t(s.max_len));

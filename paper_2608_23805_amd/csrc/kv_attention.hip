@@ -228,7 +228,7 @@ struct FewRows {
 };
 
 template <int FMT, int D, int RT>
-__global__ void __launch_bounds__(256, 2) kv_few_rows_kernel(AttentionLaunch A)
+__global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel(AttentionLaunch A)
 {
     using F = FewRows<FMT, D, RT>;
     constexpr int TOK = F::TOK, GT = F::GT, W = F::W, VW = F::VW, OS = F::OS;

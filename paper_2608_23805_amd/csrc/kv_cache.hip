@@ -402,8 +402,10 @@ __global__ void __launch_bounds__(256) kv_compact_kernel(KvCache c, KvSeqs s, co
             const int t = keep[(int64_t(i) * c.H + h) * budget + b * KV_BLOCK + threadIdx.x];
             page = s.table[int64_t(i) * s.max_blocks + t / KV_BLOCK];
             slot = t % KV_BLOCK;
-            if (!kv_page_ok(page, c.n_pages))
+            if (!kv_page_ok(page, c.n_pages)) {
+                kv_raise(status, KV_BAD_PAGE);         // (selection skips the pages of a sequence within its budget)
                 page = -1;
+            }
         }
         row_page[threadIdx.x] = page;
         row_slot[threadIdx.x] = slot;

@@ -209,3 +209,50 @@ def test_graph_and_streams():
         torch.cuda.synchronize()
         for a, b in zip(got, (eager, s.data, s.scales, s.mass)):
             assert torch.equal(a, b), n
+
+
+def test_calls_at_once_on_two_streams():
+    """Few-rows and many-rows calls with workspaces of their own, in flight together on two streams; pages shared
+    between two sequences where the tokens' weights are not kept."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case two streams at once")
+    runs = []
+    for seed, rows in ((31, [1, 1]), (32, [64, 40])):
+        s = Setup(seed, [700, 300], rows, 2, 128, "e4m3")
+        table = s.table.copy()
+        table[1, :5] = table[0, :5]                        # a common beginning
+        seqs = s.make_seqs(table, s.lens, s.cu)
+        q = s.rows(8, 0.5)
+        out = torch.empty((s.cu[-1], 8, 128), dtype=torch.bfloat16, device="cuda")
+        runs.append((s, table, seqs, q, out, msi.kv_attention_workspace(s.cache, seqs, 8), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, table, seqs, q, out, ws, st in runs:
+            msi.kv_attention(s.cache, seqs, q[0], out, 0.1, workspace=ws, stream=st)
+    torch.cuda.synchronize()
+    for s, table, seqs, q, out, ws, st in runs:
+        want, tol, _ = attention(s.host, table, s.lens, s.cu, q[1], np.float64(np.float32(0.1)), 4)
+        assert np.all(np.abs(out.double().cpu().numpy() - want) <= tol)
+
+
+def test_block_needs_its_workspace():
+    """A block's step before ``reserve`` is refused where the attention needs workspace, and no output is touched."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case block without workspace")
+    s = Setup(33, [700], [1], 2, 64, "int8")
+    w = torch.zeros(((4 + 4) * 64, 64), dtype=torch.bfloat16, device="cuda")
+    b = msi.AttentionBlock(w, torch.zeros((64, 256), dtype=torch.bfloat16, device="cuda"), s.cache, 4, 2)
+    x, h = torch.ones((1, 64), device="cuda").bfloat16(), torch.ones((1, 64), device="cuda")
+    before = s.device_state()
+    with pytest.raises(msi.MsiError) as e:
+        b.step(x, h, s.seqs, mass_rows=1)
+    assert e.value.status == msi.MSI_E_NOMEM
+    after = s.device_state()
+    assert torch.all(h == 1) and torch.all(x == 1) and np.array_equal(before[2], after[2])
+    assert np.array_equal(before[0], after[0])             # (nor was the cache)
+    b.reserve(s.seqs, 1)
+    b.step(x, h, s.seqs, mass_rows=1)
+    torch.cuda.synchronize()
+    assert torch.all(h == 1)                               # zero weights add nothing

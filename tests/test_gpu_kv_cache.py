@@ -238,3 +238,50 @@ def test_evict_bad_pages():
     written = {int(p) for p in s.dst.reshape(-1) if p >= 0} - {int(s.dst[1, 0])}
     untouched = [p for p in range(data.shape[0]) if p not in written]
     assert np.array_equal(data[untouched], before[0][untouched])
+
+
+def test_evict_bad_page_of_a_short_sequence():
+    """A sequence within its budget is copied whole: a bad page of it is reported and its tokens become zeros."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case evict bad page, short sequence")
+    s = Setup(15, [100], [0], 2, 64, "int8", dst_lens=[100])
+    table = s.table.copy()
+    table[0, 1] = s.data.shape[0]
+    seqs = s.make_seqs(table, s.lens, s.cu)
+    keep = torch.zeros((1, 2, 128), dtype=torch.int32, device="cuda")
+    new = torch.zeros(1, dtype=torch.int32, device="cuda")
+    msi.kv_evict(s.cache, seqs, torch.from_numpy(s.dst).cuda(), new, keep, budget=128, status=s.status)
+    data, _, mass, st = s.device_state()
+    want = np.concatenate([np.arange(100), np.full(28, -1)])
+    assert st == 1 and new.tolist() == [100] and np.all(keep.cpu().numpy() == want)
+    assert not data[s.dst[0, 1], :, :, :36].any() and not mass[s.dst[0, 1], :, :36].any()
+    assert np.array_equal(mass[s.dst[0, 0]], s.host.mass[table[0, 0]])
+
+
+def test_evict_captured():
+    """An eviction captured once and replayed on changing weights and lengths, eager work in between."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case evict graph")
+    s = Setup(16, [500, 90], [0, 0], 2, 128, "e4m3", dst_lens=[100, 100])
+    keep = torch.zeros((2, 2, 100), dtype=torch.int32, device="cuda")
+    new = torch.zeros(2, dtype=torch.int32, device="cuda")
+    dst = torch.from_numpy(s.dst).cuda()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        msi.kv_evict(s.cache, s.seqs, dst, new, keep, budget=100, sinks=2, recent=8, status=s.status,
+                     stream=torch.cuda.current_stream())
+    for k in range(4):
+        s.lens = [500 - 37 * k, 90 - k]
+        s.seqs.lens.copy_(torch.tensor(s.lens))
+        m = np.roll(s.host.mass, 17, axis=-1)
+        s.host.mass[:] = m
+        s.mass.copy_(torch.from_numpy(m))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = evict(s.host, s.table, s.lens, s.dst, 100, 2, 8)
+        assert np.array_equal(keep.cpu().numpy(), want) and new.tolist() == [min(n, 100) for n in s.lens]
+        _same(s)

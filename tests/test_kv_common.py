@@ -113,6 +113,26 @@ def test_attention_refusals():
     assert call(s=_seqs(n_seqs=0)) == 0 and call(s=_seqs(n_rows=0, max_rows=0), q=0, out=0) == 0
 
 
+def test_launch_bounds():
+    """Bounds that would ask for more workgroups than a launch has are refused, the largest ones below are not."""
+    import paper_2608_23805_amd as msi
+    n = ctypes.c_uint64()
+
+    def size(heads, **over):
+        c = _cache(n_heads=heads.pop("n_heads", 2))
+        return msi.lib.msi_kv_attention_workspace(ctypes.byref(c), ctypes.byref(_seqs(**over)), heads["q"], 1, ctypes.byref(n))
+    most = 1 << 29
+    _refused(size(dict(q=4), n_rows=most + 1, max_rows=1), "max_rows")
+    _refused(size(dict(q=4), n_rows=most, max_rows=most), "heads of a group")
+    _refused(size(dict(q=2), n_rows=most, max_rows=most, n_seqs=2), "under 2^24")
+    _refused(size(dict(q=256, n_heads=256), n_rows=1 << 20, max_rows=1 << 20, n_seqs=8), "under 2^24")
+    _refused(size(dict(q=4), max_blocks=1 << 23, max_len=most, n_seqs=65), "blocks of max_len")
+    assert size(dict(q=2), n_rows=most, max_rows=most, n_seqs=1) == 0
+    assert size(dict(q=256, n_heads=256), n_rows=65535, max_rows=1, n_seqs=65535) == 0
+    a = msi.msi_kv_attention_args(q=P, out=2 * P, q_stride=256, out_stride=256, n_q_heads=4, scale=3e38)
+    _refused(msi.lib.msi_kv_attention(ctypes.byref(_cache()), ctypes.byref(_seqs()), ctypes.byref(a), None), "scale")
+
+
 def test_evict_refusals():
     import paper_2608_23805_amd as msi
 
@@ -134,17 +154,23 @@ def test_linear_refusals():
     import paper_2608_23805_amd as msi
 
     def call(**over):
-        kw = dict(x=P, w=P, bias=None, residual=None, out=P, M=4, N=6, K=16, activation=0, residual_dtype=0, out_dtype=1,
+        kw = dict(x=P, w=P, bias=None, residual=None, out=3 * P, M=4, N=6, K=16, activation=0, residual_dtype=0, out_dtype=1,
                   x_stride=16, residual_stride=6, out_stride=6)
         kw.update(over)
         return msi.lib.msi_linear(ctypes.byref(msi.msi_linear_args(**kw)), None)
     for over, fragment in ((dict(K=0), "K must"), (dict(K=12), "K must"), (dict(K=(1 << 21) + 8), "K must"), (dict(M=(1 << 30) + 1), "M and N"),
                            (dict(M=1 << 30, N=1 << 10), "M and N"), (dict(x=0), "x needs"), (dict(x=P + 2), "x needs"),
                            (dict(x_stride=8), "x needs"), (dict(x_stride=20), "x needs"), (dict(w=0), "w must"), (dict(w=P + 8), "w must"),
-                           (dict(out=0), "out needs"), (dict(out=P + 1), "out needs"), (dict(out_stride=5), "out needs"),
+                           (dict(out=0), "out needs"), (dict(out=3 * P + 1), "out needs"), (dict(out_stride=5), "out needs"),
                            (dict(residual=P, residual_stride=5), "residual needs"), (dict(residual=P + 2), "residual needs"),
                            (dict(residual=P, residual_dtype=2), "dtype"), (dict(out_dtype=2), "dtype"), (dict(activation=4), "activation"),
                            (dict(bias=P + 2), "bias")):
+        _refused(call(**over), fragment)
+    # out over another operand, or over a residual of another form
+    for over, fragment in ((dict(x=2 * P, out=2 * P), "out must not"), (dict(w=2 * P, out=2 * P), "out must not"),
+                           (dict(out=2 * P, residual=2 * P), "residual that is out"),
+                           (dict(out=2 * P, residual=2 * P, residual_dtype=1, residual_stride=8), "residual that is out"),
+                           (dict(M=(1 << 29) + 1), "M and N"), (dict(M=1 << 29, N=129, out_stride=129), "M and N")):
         _refused(call(**over), fragment)
     assert call(M=0) == 0 and call(N=0, x=0, w=0, out=0) == 0
     _refused(msi.lib.msi_linear(None, None), "null")
