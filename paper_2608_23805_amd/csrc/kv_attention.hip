@@ -993,9 +993,12 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
 // For many rows the scores are computed again from K.  A wavefront keeps a
 // block's K in registers (as bf16, with D = 256 as codes) and walks groups of
 // 32 rows; the next group's queries are on their way while the vector unit takes the
-// exponentials, which bound it.  With `share` = 4 the four wavefronts of a workgroup
-// have a block each and meet the same queries at about the same time (in L1);
-// with 1 they share one block and take every fourth group, for calls with few blocks.
+// exponentials, which bound it (with D = 256 they would not fit the registers
+// beside K: 438 us with them, 375 without, for all of 2048 rows of two sequences
+// of 4096 tokens, 2 heads of 256 with 8 query heads each; 4 heads of 128: 200 us).  With `share` = 4 the four
+// wavefronts of a workgroup have a block each and meet the same queries at about
+// the same time (in L1); with 1 they share one block and take every fourth
+// group, for calls with few blocks.
 template <int FMT, int D>
 __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A, int share)
 {
@@ -1046,6 +1049,8 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
         float z = log_sum_of(r0);
         for (; r0 < rows; r0 += 32 * groups) {
             f32x16 sv[2];
+            if constexpr (RAW)
+                load_q32<D>(qf, A, q, h, r0, rows);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -1062,7 +1067,8 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
             }
             const float z0 = z;
             const int next = min(r0 + 32 * groups, rows - 1);
-            load_q32<D>(qf, A, q, h, next, rows);
+            if constexpr (!RAW)
+                load_q32<D>(qf, A, q, h, next, rows);
             z = log_sum_of(next);
             const int r = r0 + col, limit = r < rows ? row_limit(q, r / A.G) : 0;
             // (a row past the last one, or one that does not see the whole block)
