@@ -133,6 +133,10 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
 // The mirror of append: row r of a sequence is its token len - n + r.  Values
 // leave as bf16: exact for scales that are powers of two, as append writes
 // them (a code has at most 8 significant bits), rounded to nearest otherwise.
+// The rows pass the caches by: a call's outputs are many times an L2 (the open
+// blocks of 64 sequences 10.4 -> 9.3 us, 16384 tokens of 2 heads of 256, 50 MB,
+// 15.1 -> 13.0 us).  (Codes are read again soon; past the caches append and the
+// copies of an eviction take 8% more.)
 template <int FMT, int D>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint16_t *__restrict__ k,
                                                       uint16_t *__restrict__ v, int64_t k_stride, int64_t v_stride,
@@ -175,8 +179,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint1
             if (r >= lo && r < hi) {
                 const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * scale[j], b = kv_unpack4<FMT>(w[j][p].y) * scale[j];
                 uint16_t *o = (j ? v + (dst0 + r) * v_stride : k + (dst0 + r) * k_stride) + h * D + chunk * 8;
-                *reinterpret_cast<u32x4 *>(o) = u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
-                                                      pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+                __builtin_nontemporal_store(u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                                  pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])}, reinterpret_cast<u32x4 *>(o));
             }
         }
 }
@@ -191,9 +195,11 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint1
 // of histograms over 11, 11 and 10 bits; equal keys are kept from the lowest
 // index on, by a prefix count in index order.  Sequences of up to
 // 1024 * ROUNDS tokens keep their keys in registers through all passes; longer
-// ones read them again in chunks of that size.  One CU a (head, sequence) bounds
-// it, in instructions: 16384 of 65536 tokens 41 us (weights 8, histograms 15,
-// indices 18), 2048 of 16384 for 16 sequences of 8 heads 16 us.  Four copies of
+// ones read them again in chunks of that size.  Where there are fewer (head,
+// sequence) pairs than CUs, several workgroups find the same key and each writes
+// a share of the indices.  A CU's instructions bound it: 16384 of 65536 tokens
+// take 36 us (weights 8, histograms 16, counts and indices 12; 43 us by one
+// workgroup), 2048 of 16384 for 16 sequences of 8 heads 16 us.  Four copies of
 // each bin halve the collisions of weights that are alike.  (Keys in LDS with
 // rolled loops: 70 and 20 us; indices gathered in LDS first: 3 us more.)
 constexpr int SELECT_THREADS = 1024, SELECT_WAVES = SELECT_THREADS / 64, BINS = 2048, COPIES = 4;
@@ -219,24 +225,24 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
                                                                    int32_t *__restrict__ new_lens, int budget, int sinks,
                                                                    int recent, uint32_t *status)
 {
-    constexpr int CHUNK = SELECT_THREADS * ROUNDS;
+    constexpr int CHUNK = SELECT_THREADS * ROUNDS, GROUP = 4;
     __shared__ __attribute__((aligned(16))) int hist[BINS * COPIES];
     __shared__ int counts[2][ROUNDS * SELECT_WAVES];
     __shared__ int part[2][SELECT_WAVES];
     __shared__ int found[2];
-    const int h = blockIdx.x, i = blockIdx.y;
+    const int h = blockIdx.x, i = blockIdx.y, share = blockIdx.z, shares = gridDim.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvSeq q = kv_seq(s, i, false);
     if (!q.ok && tid == 0)
         kv_raise(status, KV_BAD_LENGTH);
     const int len = q.len, kept = min(len, budget);
     int32_t *out = keep + (int64_t(i) * c.H + h) * budget;
-    if (h == 0 && tid == 0)
+    if (h == 0 && share == 0 && tid == 0)
         new_lens[i] = kept;
-    for (int t = kept + tid; t < budget; t += SELECT_THREADS)
+    for (int t = kept + share * SELECT_THREADS + tid; t < budget; t += shares * SELECT_THREADS)
         out[t] = -1;
     if (len <= budget) {
-        for (int t = tid; t < len; t += SELECT_THREADS)
+        for (int t = share * SELECT_THREADS + tid; t < len; t += shares * SELECT_THREADS)
             out[t] = t;
         return;
     }
@@ -379,13 +385,16 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
             mine[1] = counts[1][lane * SELECT_WAVES + wave];
         }
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const int ne = lanes_below(__ballot(key[r] == prefix), __builtin_amdgcn_readlane(mine[1], r));
-            const int ns = lanes_below(__ballot(key[r] > prefix), __builtin_amdgcn_readlane(mine[0], r));
-            if (key[r] + uint32_t(ne < rest) > prefix)      // (no key is 2^32 - 1)
-                *reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(out) + 4u * uint32_t(ns + min(ne, rest))) =
-                    ch * CHUNK + r * SELECT_THREADS + tid;
-        }
+        for (int g = 0; g < ROUNDS; g += GROUP)            // this workgroup's share of the rounds
+            if (g / GROUP % shares == share)
+#pragma unroll
+                for (int r = g; r < g + GROUP; ++r) {
+                    const int ne = lanes_below(__ballot(key[r] == prefix), __builtin_amdgcn_readlane(mine[1], r));
+                    const int ns = lanes_below(__ballot(key[r] > prefix), __builtin_amdgcn_readlane(mine[0], r));
+                    if (key[r] + uint32_t(ne < rest) > prefix)         // (no key is 2^32 - 1)
+                        *reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(out) + 4u * uint32_t(ns + min(ne, rest))) =
+                            ch * CHUNK + r * SELECT_THREADS + tid;
+                }
         done[0] += total[0];
         done[1] += total[1];
         __syncthreads();
@@ -530,7 +539,8 @@ hipError_t launch_kv_evict(const KvCache &c, int fmt, const KvSeqs &s, const int
                            int32_t *new_lens, int32_t *keep, int budget, int sinks, int recent, uint32_t *status,
                            hipStream_t st)
 {
-    const dim3 grid(c.H, s.S);
+    const int rounds = s.max_len <= 4 * SELECT_THREADS ? 4 : s.max_len <= 16 * SELECT_THREADS ? 16 : 64;
+    const dim3 grid(c.H, s.S, std::max(1, std::min(rounds / 4, 256 / (c.H * s.S))));
     if (s.max_len <= 4 * SELECT_THREADS)
         launch_k(kv_select_kernel<4>, grid, SELECT_THREADS, 0, st, c, s, keep, new_lens, budget, sinks, recent, status);
     else if (s.max_len <= 16 * SELECT_THREADS)
