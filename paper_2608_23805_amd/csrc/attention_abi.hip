@@ -158,8 +158,6 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
     l.M = int(a->M);
     l.N = int(a->N);
     l.K = int(a->K);
-    l.vec4 = a->N % 4 == 0 && a->out_stride % 4 == 0 && aligned(a->out, 4 * ob) && aligned(a->bias, 16) &&
-             (!a->residual || (a->residual_stride % 4 == 0 && aligned(a->residual, 4 * rb)));
     return launched(launch_linear(l, int(a->activation), static_cast<hipStream_t>(stream)));
 }
 

@@ -302,7 +302,6 @@ struct LinearArgs {
     uint16_t *out_bf16;
     int64_t x_stride, res_stride, out_stride;
     int M, N, K;
-    bool vec4;                   // four features of a row may be read and written together
 };
 hipError_t launch_linear(const LinearArgs &A, int act, hipStream_t st);
 

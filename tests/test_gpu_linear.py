@@ -74,6 +74,7 @@ def test_in_place(M, kind):
 def test_every_tile(M, K, N):
     _case(M, K, N, act="silu", residual="bf16", out="bf16")
     _case(M, K, N, act="none", residual="none", out="f32", pad=8)
+    _case(M, K, N, act="none", residual="f32", out="f32", inplace=True)
 
 
 def test_infinite_activation_arguments():
