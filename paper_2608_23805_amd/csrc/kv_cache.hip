@@ -35,21 +35,22 @@ __device__ __forceinline__ void unpack_bf16x8(const u32x4 &w, float (&x)[8])
 
 // ---------------------------------------------------------------- append
 //
-// One workgroup per (block, head, sequence) that receives rows.  Its new rows
-// of K and V stay in registers between the two passes (largest magnitude, then
+// One workgroup per (block, K or V, head, sequence) that receives rows.  Its new
+// rows stay in registers between the two passes (largest magnitude, then
 // codes); old rows of the block are touched only if its scale grows.  One token
-// of 64 sequences 5.7 us (launch and the chain of lengths, pages, scale);
-// prompts of 8 sequences, 14108 tokens of 8 heads of 128, 21 us, 87 MB at 4.1 TB/s.
+// of 64 sequences 5.1 us (launch and the chain of lengths, pages, scale);
+// prompts of 8 sequences, 14108 tokens of 8 heads of 128, 20 us, 87 MB at 4.4 TB/s
+// (K and V by one workgroup: 5.7 and 21 us).
 template <int FMT, int D>
 __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, const uint16_t *__restrict__ k,
                                                         const uint16_t *__restrict__ v, int64_t k_stride,
                                                         int64_t v_stride, uint32_t *status)
 {
     using R = RowChunks<D>;
-    __shared__ float part[8];
-    const int h = blockIdx.y, i = blockIdx.z;
+    __shared__ float part[4];
+    const int h = blockIdx.y >> 1, j = blockIdx.y & 1, i = blockIdx.z;
     const KvSeq q = kv_seq(s, i, true);
-    if (!q.ok && blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
         kv_raise(status, KV_BAD_LENGTH);
     const int start = q.len - q.n;                       // position of the first new row
     const int blk = start / KV_BLOCK + int(blockIdx.x);
@@ -58,16 +59,13 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
     const int lo = max(start - blk * KV_BLOCK, 0), hi = min(q.len - blk * KV_BLOCK, KV_BLOCK);   // new rows of the block
     const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
     const int64_t src0 = int64_t(q.row0) + (blk * KV_BLOCK - start);       // call's row of the block's row 0
-    u32x4 x[2][R::N];
+    const uint16_t *src = (j ? v + src0 * v_stride : k + src0 * k_stride) + h * D + chunk * 8;
+    const int64_t stride = j ? v_stride : k_stride;
+    u32x4 x[R::N];
 #pragma unroll
     for (int p = 0; p < R::N; ++p) {
         const int r = r0 + p * R::ROWS;
-        if (r >= lo && r < hi) {
-            x[0][p] = load_stream16(k + (src0 + r) * k_stride + h * D + chunk * 8);
-            x[1][p] = load_stream16(v + (src0 + r) * v_stride + h * D + chunk * 8);
-        } else {
-            x[0][p] = x[1][p] = u32x4{0, 0, 0, 0};
-        }
+        x[p] = r >= lo && r < hi ? load_stream16(src + r * stride) : u32x4{0, 0, 0, 0};
     }
     const int page = __builtin_amdgcn_readfirstlane(s.table[int64_t(i) * s.max_blocks + blk]);
     if (!kv_page_ok(page, c.n_pages)) {
@@ -75,58 +73,49 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
             kv_raise(status, KV_BAD_PAGE);
         return;
     }
-    float *sc = c.scales + (int64_t(page) * c.H + h) * 2;
-    const float was[2] = {lo ? sc[0] : 0.0f, lo ? sc[1] : 0.0f};   // (read before the barriers below, written after)
-    uint32_t flags = 0;
-    float top[2];
+    float *sc = c.scales + (int64_t(page) * c.H + h) * 2 + j;
+    const float was = lo ? *sc : 0.0f;                   // (read before the barrier below, written after)
+    uint32_t flags = 0, m = 0;                           // largest finite magnitude: bf16 bits order as integers
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        uint32_t m = 0;                                   // largest finite magnitude: bf16 bits order as integers
+    for (int p = 0; p < R::N; ++p)
 #pragma unroll
-        for (int p = 0; p < R::N; ++p)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t a = x[j][p][w] & 0x7FFFu, b = (x[j][p][w] >> 16) & 0x7FFFu;
-                if (a >= 0x7F80u || b >= 0x7F80u)
-                    flags = KV_NONFINITE;
-                m = max(m, max(a >= 0x7F80u ? 0u : a, b >= 0x7F80u ? 0u : b));
-            }
-        top[j] = block_max256(__uint_as_float(m << 16), part + 4 * j);
-    }
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t a = x[p][w] & 0x7FFFu, b = (x[p][w] >> 16) & 0x7FFFu;
+            if (a >= 0x7F80u || b >= 0x7F80u)
+                flags = KV_NONFINITE;
+            m = max(m, max(a >= 0x7F80u ? 0u : a, b >= 0x7F80u ? 0u : b));
+        }
     kv_raise(status, flags);
-    uint8_t *base = c.data + kv_offset(page, h, c.H, D);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const float need = __uint_as_float(kv_scale_bits(__float_as_uint(top[j]), FMT));
-        const float scale = fmaxf(need, was[j]), inv = 1.0f / scale;
-        uint8_t *dst = base + j * (KV_BLOCK * D);
-        if (lo && scale != was[j]) {                      // the old rows move to the larger scale
-            for (int r = r0; r < lo; r += R::ROWS) {
-                uint2 *o = reinterpret_cast<uint2 *>(dst + r * D + chunk * 8);
-                const uint2 w = *o;
-                const f32x4 a = kv_unpack4<FMT>(w.x), b = kv_unpack4<FMT>(w.y);
-                // (both products are exact unless a caller's own scale is no power of two)
-                const f32x4 x = a * was[j] * inv, y = b * was[j] * inv;
-                *o = make_uint2(kv_pack4<FMT>(x[0], x[1], x[2], x[3]), kv_pack4<FMT>(y[0], y[1], y[2], y[3]));
-            }
+    const float top = block_max256(__uint_as_float(m << 16), part);
+    const float need = __uint_as_float(kv_scale_bits(__float_as_uint(top), FMT));
+    const float scale = fmaxf(need, was), inv = 1.0f / scale;
+    uint8_t *dst = c.data + kv_offset(page, h, c.H, D) + j * (KV_BLOCK * D);
+    if (lo && scale != was) {                            // the old rows move to the larger scale
+        for (int r = r0; r < lo; r += R::ROWS) {
+            uint2 *o = reinterpret_cast<uint2 *>(dst + r * D + chunk * 8);
+            const uint2 w = *o;
+            const f32x4 a = kv_unpack4<FMT>(w.x), b = kv_unpack4<FMT>(w.y);
+            // (both products are exact unless a caller's own scale is no power of two)
+            const f32x4 y = a * was * inv, z = b * was * inv;
+            *o = make_uint2(kv_pack4<FMT>(y[0], y[1], y[2], y[3]), kv_pack4<FMT>(z[0], z[1], z[2], z[3]));
         }
-#pragma unroll
-        for (int p = 0; p < R::N; ++p) {
-            const int r = r0 + p * R::ROWS;
-            if (r >= lo && r < hi) {
-                float f[8];
-                unpack_bf16x8(x[j][p], f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    f[e] = f[e] != f[e] ? 0.0f : f[e] * inv;      // NaN is stored as zero, infinities as the largest code
-                *reinterpret_cast<uint2 *>(dst + r * D + chunk * 8) =
-                    make_uint2(kv_pack4<FMT>(f[0], f[1], f[2], f[3]), kv_pack4<FMT>(f[4], f[5], f[6], f[7]));
-            }
-        }
-        if (threadIdx.x == 0)
-            sc[j] = scale;
     }
-    if (c.mass && int(threadIdx.x) >= lo && int(threadIdx.x) < hi)
+#pragma unroll
+    for (int p = 0; p < R::N; ++p) {
+        const int r = r0 + p * R::ROWS;
+        if (r >= lo && r < hi) {
+            float f[8];
+            unpack_bf16x8(x[p], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                f[e] = f[e] != f[e] ? 0.0f : f[e] * inv;          // NaN is stored as zero, infinities as the largest code
+            *reinterpret_cast<uint2 *>(dst + r * D + chunk * 8) =
+                make_uint2(kv_pack4<FMT>(f[0], f[1], f[2], f[3]), kv_pack4<FMT>(f[4], f[5], f[6], f[7]));
+        }
+    }
+    if (threadIdx.x == 0)
+        *sc = scale;
+    if (j == 0 && c.mass && int(threadIdx.x) >= lo && int(threadIdx.x) < hi)
         c.mass[(int64_t(page) * c.H + h) * KV_BLOCK + threadIdx.x] = 0.0f;
 }
 
@@ -136,8 +125,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvCache c, KvSeqs s, con
 // leave as bf16: exact for scales that are powers of two, as append writes
 // them (a code has at most 8 significant bits), rounded to nearest otherwise.
 // The rows pass the caches by: a call's outputs are many times an L2 (the open
-// blocks of 64 sequences 10.4 -> 9.3 us, 16384 tokens of 2 heads of 256, 50 MB,
-// 15.1 -> 13.0 us).  (Codes are read again soon; past the caches append and the
+// blocks of 64 sequences 8.2 us, 10.4 without and with K and V by one workgroup;
+// 16384 tokens of 2 heads of 256, 50 MB, 10.2 and 15.1 us).  (Codes are read again soon; past the caches append and the
 // copies of an eviction take 8% more.)
 template <int FMT, int D>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint16_t *__restrict__ k,
@@ -145,9 +134,9 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint1
                                                       uint32_t *status)
 {
     using R = RowChunks<D>;
-    const int h = blockIdx.y, i = blockIdx.z;
+    const int h = blockIdx.y >> 1, j = blockIdx.y & 1, i = blockIdx.z;
     const KvSeq q = kv_seq(s, i, true);
-    if (!q.ok && blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+    if (!q.ok && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
         kv_raise(status, KV_BAD_LENGTH);
     const int start = q.len - q.n;
     const int blk = start / KV_BLOCK + int(blockIdx.x);
@@ -160,31 +149,28 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvCache c, KvSeqs s, uint1
     const int lo = max(start - blk * KV_BLOCK, 0), hi = min(q.len - blk * KV_BLOCK, KV_BLOCK);
     const int chunk = threadIdx.x % R::CPR, r0 = threadIdx.x / R::CPR;
     const int64_t dst0 = int64_t(q.row0) + (blk * KV_BLOCK - start);
-    const uint8_t *base = c.data + kv_offset(ok ? page : 0, h, c.H, D);
-    const float *sc = c.scales + (int64_t(ok ? page : 0) * c.H + h) * 2;
-    uint2 w[2][R::N];
+    uint16_t *dst = (j ? v + dst0 * v_stride : k + dst0 * k_stride) + h * D + chunk * 8;
+    const int64_t stride = j ? v_stride : k_stride;
+    const uint8_t *base = c.data + kv_offset(ok ? page : 0, h, c.H, D) + j * (KV_BLOCK * D) + chunk * 8;
+    const float scale = ok ? c.scales[(int64_t(page) * c.H + h) * 2 + j] : 0.0f;
+    uint2 w[R::N];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int p = 0; p < R::N; ++p) {
+        const int r = r0 + p * R::ROWS;
+        w[p] = make_uint2(0, 0);                           // a bad page reads as zeros
+        if (ok && r >= lo && r < hi)
+            w[p] = *reinterpret_cast<const uint2 *>(base + r * D);
+    }
 #pragma unroll
-        for (int p = 0; p < R::N; ++p) {
-            const int r = r0 + p * R::ROWS;
-            w[j][p] = make_uint2(0, 0);                    // a bad page reads as zeros
-            if (ok && r >= lo && r < hi)
-                w[j][p] = *reinterpret_cast<const uint2 *>(base + j * (KV_BLOCK * D) + r * D + chunk * 8);
+    for (int p = 0; p < R::N; ++p) {
+        const int r = r0 + p * R::ROWS;
+        if (r >= lo && r < hi) {
+            const f32x4 a = kv_unpack4<FMT>(w[p].x) * scale, b = kv_unpack4<FMT>(w[p].y) * scale;
+            __builtin_nontemporal_store(u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                              pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])},
+                                        reinterpret_cast<u32x4 *>(dst + r * stride));
         }
-    const float scale[2] = {ok ? sc[0] : 0.0f, ok ? sc[1] : 0.0f};
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int p = 0; p < R::N; ++p) {
-            const int r = r0 + p * R::ROWS;
-            if (r >= lo && r < hi) {
-                const f32x4 a = kv_unpack4<FMT>(w[j][p].x) * scale[j], b = kv_unpack4<FMT>(w[j][p].y) * scale[j];
-                uint16_t *o = (j ? v + (dst0 + r) * v_stride : k + (dst0 + r) * k_stride) + h * D + chunk * 8;
-                __builtin_nontemporal_store(u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
-                                                  pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])}, reinterpret_cast<u32x4 *>(o));
-            }
-        }
+    }
 }
 
 // ---------------------------------------------------------------- evict
@@ -519,7 +505,7 @@ hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const ui
                             int64_t k_stride, int64_t v_stride, uint32_t *status, hipStream_t st)
 {
     // n rows from any position touch at most (n + 126) / 64 blocks
-    const dim3 grid((s.max_rows + 126) / KV_BLOCK, c.H, s.S);
+    const dim3 grid((s.max_rows + 126) / KV_BLOCK, 2 * c.H, s.S);
     with_shape(fmt, c.D, [&](auto f, auto d) {
         launch_k(kv_append_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, c, s, k, v, k_stride,
                  v_stride, status);
@@ -530,7 +516,7 @@ hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const ui
 hipError_t launch_kv_read(const KvCache &c, int fmt, const KvSeqs &s, uint16_t *k, uint16_t *v, int64_t k_stride,
                           int64_t v_stride, uint32_t *status, hipStream_t st)
 {
-    const dim3 grid((s.max_rows + 126) / KV_BLOCK, c.H, s.S);
+    const dim3 grid((s.max_rows + 126) / KV_BLOCK, 2 * c.H, s.S);
     with_shape(fmt, c.D, [&](auto f, auto d) {
         launch_k(kv_read_kernel<decltype(f)::value, decltype(d)::value>, grid, 256, 0, st, c, s, k, v, k_stride,
                  v_stride, status);
