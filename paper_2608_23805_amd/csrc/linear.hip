@@ -51,8 +51,12 @@ __device__ __forceinline__ f32x4 residual4(const LinearArgs &A, int64_t m, int n
 }
 
 // Features n .. n + 3 of row m leave: act(v + bias) + residual; bias: their
-// four (zero past N).  `res`: their residual, where all four are inside.
-template <int ACT>
+// four (zero past N).  `res`: their residual, where all four are inside.  PAST:
+// stored past the caches, where the tiles make more than the L2s could hold for
+// whoever reads them next (4096 x 8192 bf16 of K 2048 with GELU 144.1 -> 136.6
+// us, fp32 of K 1024 143.3 -> 135.4; 64 rows of 8192 and the product that reads
+// them would go from 27.6 to 28.9).
+template <int ACT, bool PAST>
 __device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f32x4 v, const f32x4 &bias, const f32x4 &res)
 {
     v += bias;
@@ -61,11 +65,17 @@ __device__ __forceinline__ void store4(const LinearArgs &A, int64_t m, int n, f3
         v[i] = activate<ACT>(v[i]);
     if (n + 4 <= A.N) {
         v += res;
+        auto store = [](auto *p, auto w) {
+            if constexpr (PAST)
+                __builtin_nontemporal_store(w, p);
+            else
+                *p = w;
+        };
         if (A.out_f32)
-            *reinterpret_cast<f32x4_any *>(A.out_f32 + m * A.out_stride + n) = v;
+            store(reinterpret_cast<f32x4_any *>(A.out_f32 + m * A.out_stride + n), static_cast<f32x4_any>(v));
         else
-            *reinterpret_cast<bf16x4_any *>(A.out_bf16 + m * A.out_stride + n) =
-                bf16x4_any{pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])};
+            store(reinterpret_cast<bf16x4_any *>(A.out_bf16 + m * A.out_stride + n),
+                  bf16x4_any{pack_bf16x2_hw(v[0], v[1]), pack_bf16x2_hw(v[2], v[3])});
         return;
     }
 #pragma unroll
@@ -102,7 +112,7 @@ __device__ __forceinline__ f32x4 bias4(const LinearArgs &A, int n)
 template <int NB>
 constexpr int STORE_LDS = 2 * 16 * (16 * NB + 4);      // words of a wavefront
 
-template <int ACT, int NB, int MB>
+template <int ACT, bool PAST, int NB, int MB>
 __device__ __forceinline__ void store_block(const LinearArgs &A, float *mine, const f32x4 (&acc)[NB][MB], int m0, int rows,
                                             int n0)
 {
@@ -142,7 +152,7 @@ __device__ __forceinline__ void store_block(const LinearArgs &A, float *mine, co
         for (int r = r0; r < 16; r += RPI) {
             const int m = 16 * q + r, at = r * LD + 4 * (lane % LPR);
             if (m < rows && n < A.N)
-                store4<ACT>(A, int64_t(m0) + m, n, *reinterpret_cast<const f32x4 *>(mine + at), bias,
+                store4<ACT, PAST>(A, int64_t(m0) + m, n, *reinterpret_cast<const f32x4 *>(mine + at), bias,
                             residual ? *reinterpret_cast<const f32x4 *>(there + at) : f32x4{0.f, 0.f, 0.f, 0.f});
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -301,92 +311,98 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
                 for (int q = 0; q < MB; ++q)
                     acc[a][q] += sums[o * PER + ((wi * NB + a) * MB + q) * 64 + lane];
     }
-    store_block<ACT, NB, MB>(A, reinterpret_cast<float *>(lds8) + wi * STORE_LDS<NB>, acc, m0 + wm * MB * 16,
+    store_block<ACT, false, NB, MB>(A, reinterpret_cast<float *>(lds8) + wi * STORE_LDS<NB>, acc, m0 + wm * MB * 16,
                              vm - wm * MB * 16, n0 + wn * NB * 16);
 }
 
 // ---------------------------------------------------------------- 256 x 256 tiles
 //
 // Many tiles: bound by the matrix cores.  Eight wavefronts as 4 (rows) x 2
-// (features), each 64 rows x 128 features; K in stages of 32 elements through
-// a ring of four LDS buffers; the fragments of stage s + 1 are read between the
-// MFMAs of stage s.  Every step issues the same copies (those past the last
-// stage read nothing), so every wait is for the same count.  4096 rows, K 2048,
-// N 8192 with GELU: 136 us, 1010 TFLOP/s (the library's product alone 99 us).
+// (features), each 64 rows x 128 features; K in stages of 64 elements through
+// two LDS buffers, rows of 128 bytes with the tiles' slots.  A stage is two
+// halves of 32 elements: the fragments of the next half are read between the
+// MFMAs of this one, so by the middle of a stage all of its fragments are in
+// registers and, after the one barrier, its buffer takes the stage after next.
+// 4096 rows, K 2048, N 8192: 125 us, 1100 TFLOP/s (137 with GELU; the library's
+// product alone 99 us): 32 stages of 1.7 us a tile, 1290 TFLOP/s, and about 10 us
+// for its start and its rows' way out, which nothing overlaps.  (Stages of 32
+// elements in rows of 64 bytes, whose reads meet on banks: 133.6 us; four
+// wavefronts of 128 x 128: 187; without reads between the MFMAs: 132.)
 template <int ACT>
-__global__ void __launch_bounds__(ring::THREADS, 2) linear_ring_kernel(LinearArgs A)
+__global__ void __launch_bounds__(512, 2) linear_wide_kernel(LinearArgs A)
 {
-    using namespace ring;
-    constexpr int OUT = WAVES * STORE_LDS<8> * 4;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[NBUF * STAGE > OUT ? NBUF * STAGE : OUT];
-    const int2 at = tile_at(xcd_swizzle(int(blockIdx.x), int(gridDim.x)), (A.M + TM - 1) / TM, (A.N + TN - 1) / TN);
-    const int m0 = at.x * TM, n0 = at.y * TN;
+    constexpr int T = 256, ROWB = 128, STAGE = 2 * T * ROWB, OUT = 8 * STORE_LDS<8> * 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE > OUT ? 2 * STAGE : OUT];
+    const int2 at = tile_at(xcd_swizzle(int(blockIdx.x), int(gridDim.x)), (A.M + T - 1) / T, (A.N + T - 1) / T);
+    const int m0 = at.x * T, n0 = at.y * T;
     const int K = A.K;
-    const int vm = min(TM, A.M - m0), vn = min(TN, A.N - n0);
+    const int vm = min(T, A.M - m0), vn = min(T, A.N - n0);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    // copy i of this wavefront covers stage rows 16 (i WAVES + wave) + lane / 4; lane % 4 is the 16-byte slot it fills
-    const int rl = lane >> 2, ch = (lane & 3) ^ ring_swz(rl & 15);
-    uint32_t aoff[LA], boff[LB];
+    // copy i of this wavefront covers rows 8 (8 i + wave) + lane / 8; lane % 8 is the 16-byte slot it fills
+    const int ch = (lane & 7) ^ (lane >> 4 & 3) ^ ((wave & 1) << 2);
+    uint32_t aoff[4], boff[4];
 #pragma unroll
-    for (int i = 0; i < LA; ++i)
-        aoff[i] = uint32_t(min((i * WAVES + wave) * 16 + rl, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(ch << 4);
-#pragma unroll
-    for (int i = 0; i < LB; ++i)
-        boff[i] = uint32_t(min((i * WAVES + wave) * 16 + rl, vn - 1)) * uint32_t(K * 2) + uint32_t(ch << 4);
-    const int nstage = (K + SK - 1) / SK;
-    const bool past = SK * (nstage - 1) + 8 * ch >= K;      // this lane's chunk of the last stage lies past K
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * (8 * i + wave) + (lane >> 3);
+        aoff[i] = uint32_t(min(r, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(ch << 4);
+        boff[i] = uint32_t(min(r, vn - 1)) * uint32_t(K * 2) + uint32_t(ch << 4);
+    }
+    const int nstage = (K + 63) / 64;
+    const bool past = 64 * (nstage - 1) + 8 * ch >= K;      // this lane's chunk of the last stage lies past K
     const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t *>(A.x + int64_t(m0) * A.x_stride), 0, 0x7fffffff, RSRC_FLAGS);
+        const_cast<uint16_t *>(A.x + int64_t(m0) * A.x_stride), 0, 0x7fffffff, ring::RSRC_FLAGS);
     const __amdgpu_buffer_rsrc_t br = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(A.w + int64_t(n0) * K), 0,
-                                                                        0x7fffffff, RSRC_FLAGS);
+                                                                        0x7fffffff, ring::RSRC_FLAGS);
     auto issue = [&](int stage) {
-        uint8_t *buf = lds + (stage % NBUF) * STAGE;
+        if (stage >= nstage)
+            return;
+        uint8_t *buf = lds + (stage & 1) * STAGE;
         // offsets past the buffers' ends read nothing and leave zeros
-        const uint32_t none = stage >= nstage || (stage == nstage - 1 && past) ? 0x80000000u : 0u;
-        const uint32_t kb = uint32_t(stage * ROWB);
+        const uint32_t none = stage == nstage - 1 && past ? 0x80000000u : 0u, kb = uint32_t(stage * ROWB);
 #pragma unroll
-        for (int i = 0; i < LA; ++i)
-            dma16_lds(ar, buf + (i * WAVES + wave) * 1024, (aoff[i] + kb) | none, 0);
+        for (int i = 0; i < 4; ++i)
+            dma16_lds(br, buf + T * ROWB + (8 * i + wave) * 1024, (boff[i] + kb) | none, 0);
 #pragma unroll
-        for (int i = 0; i < LB; ++i)
-            dma16_lds(br, buf + TM * ROWB + (i * WAVES + wave) * 1024, (boff[i] + kb) | none, 0);
+        for (int i = 0; i < 4; ++i)
+            dma16_lds(ar, buf + (8 * i + wave) * 1024, (aoff[i] + kb) | none, 0);
     };
-    auto sync_stage = [&](auto waitn) {
-        __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(decltype(waitn)::value));
+    auto landed = [&]() {
+        __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wavefront's reads are done with
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    using W_STEADY = std::integral_constant<int, LPS * (NBUF - 3)>;   // stage s+1 landed, s+2 in flight
-    using W_FIRST = std::integral_constant<int, LPS * (NBUF - 2)>;    // stage 0 landed, 1 and 2 in flight
-    const int wm = wave >> 1, wn = wave & 1;
-    const uint32_t fofs = uint32_t((lane & 15) * ROWB + (((lane >> 4) ^ ring_swz(lane & 15)) << 4));
-    auto wrow = [&](int a) { return wn * 128 + a * 16; };
-
+    const int wm = wave >> 1, wn = wave & 1, r16 = lane & 15;
+    uint32_t fofs[2];                                       // of the halves
 #pragma unroll
-    for (int s = 0; s < NBUF - 1; ++s)
-        issue(s);
-    sync_stage(W_FIRST{});
-    f32x4 acc[8][4];   // [feature block][row block]
+    for (int kb = 0; kb < 2; ++kb)
+        fofs[kb] = uint32_t(r16 * ROWB + (((4 * kb + (lane >> 4)) ^ ((r16 >> 1) & 7)) << 4));
+    f32x4 acc[8][4];                                        // [feature block][row block]
 #pragma unroll
     for (int a = 0; a < 8; ++a)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
             acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     u32x4 fw[2][8], fx[4];
-    {
-        const uint8_t *b0 = lds + fofs;
+    auto read_w = [&](int stage, int kb, int a) {
+        return *reinterpret_cast<const u32x4 *>(lds + (stage & 1) * STAGE + T * ROWB + (wn * 128 + a * 16) * ROWB + fofs[kb]);
+    };
+    auto read_x = [&](int stage, int kb, int b) {
+        return *reinterpret_cast<const u32x4 *>(lds + (stage & 1) * STAGE + (wm * 64 + b * 16) * ROWB + fofs[kb]);
+    };
+    issue(0);
+    landed();
+    issue(1);
 #pragma unroll
-        for (int a = 0; a < 8; ++a)
-            fw[0][a] = *reinterpret_cast<const u32x4 *>(b0 + TM * ROWB + wrow(a) * ROWB);
+    for (int a = 0; a < 8; ++a)
+        fw[0][a] = read_w(0, 0, a);
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-            fx[b] = *reinterpret_cast<const u32x4 *>(b0 + (wm * 64 + b * 16) * ROWB);
-    }
-    // MFMAs of stage s from fw[H] / fx, reading stage s+1's fragments (after the last stage those are never used)
-    auto step = [&](int s, auto h) {
+    for (int b = 0; b < 4; ++b)
+        fx[b] = read_x(0, 0, b);
+    // MFMAs of the half whose fragments are in fw[H], fx; the fragments of half 1 - H (of `stage`) are read
+    auto half = [&](int stage, auto h) {
         constexpr int H = decltype(h)::value;
-        const uint8_t *nb = lds + ((s + 1) % NBUF) * STAGE + fofs;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
 #pragma unroll
@@ -394,8 +410,8 @@ __global__ void __launch_bounds__(ring::THREADS, 2) linear_ring_kernel(LinearArg
                 acc[a][b] = mfma16(as_bf16x8(fw[H][a]), as_bf16x8(fx[b]), acc[a][b]);
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                fw[H ^ 1][b * 2 + q] = *reinterpret_cast<const u32x4 *>(nb + TM * ROWB + wrow(b * 2 + q) * ROWB);
-            fx[b] = *reinterpret_cast<const u32x4 *>(nb + (wm * 64 + b * 16) * ROWB);
+                fw[H ^ 1][b * 2 + q] = read_w(stage, H ^ 1, b * 2 + q);
+            fx[b] = read_x(stage, H ^ 1, b);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -405,18 +421,14 @@ __global__ void __launch_bounds__(ring::THREADS, 2) linear_ring_kernel(LinearArg
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
     };
-    // (an odd last stage is followed by one of zeros)
-    for (int s = 0; s < nstage; s += 2) {
-        sync_stage(W_STEADY{});
-        issue(s + NBUF - 1);
-        step(s, std::integral_constant<int, 0>{});
-        sync_stage(W_STEADY{});
-        issue(s + NBUF);
-        step(s + 1, std::integral_constant<int, 1>{});
+    for (int s = 0; s < nstage; ++s) {
+        half(s, std::integral_constant<int, 0>{});
+        landed();                                           // stage s + 1
+        issue(s + 2);
+        half(s + 1, std::integral_constant<int, 1>{});      // (after the last stage its fragments are never used)
     }
-    __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));    // the last copies (zeros) have landed,
-    __syncthreads();                              // every fragment has been read: LDS changes its use
-    store_block<ACT, 8, 4>(A, reinterpret_cast<float *>(lds) + wave * STORE_LDS<8>, acc, m0 + wm * 64, vm - wm * 64,
+    __syncthreads();                                        // every fragment has been read: LDS changes its use
+    store_block<ACT, true, 8, 4>(A, reinterpret_cast<float *>(lds) + wave * STORE_LDS<8>, acc, m0 + wm * 64, vm - wm * 64,
                            n0 + wn * 128);
 }
 
@@ -458,7 +470,7 @@ hipError_t launch_act(const LinearArgs &A, hipStream_t st)
     const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
     if (37 * ((t256 + CUS - 1) / CUS) > 20 * ((t128 + 2 * CUS - 1) / (2 * CUS)))
         return launch_tile<ACT, LinearShape<128, 128, 4, 2, 1, 2, 2>>(A, st);
-    launch_k(linear_ring_kernel<ACT>, unsigned(t256), ring::THREADS, 0, st, A);
+    launch_k(linear_wide_kernel<ACT>, unsigned(t256), 512, 0, st, A);
     return hipGetLastError();
 }
 
