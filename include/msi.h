@@ -433,7 +433,7 @@ msi_status msi_plan_set_timing(msi_plan *plan, int enable);
 msi_status msi_plan_set_timing_period(msi_plan *plan, uint32_t period);
 msi_status msi_plan_timings(msi_plan *plan, msi_timings *out, int reset);
 
-/* Residual stream between stacked layers (attention omitted), row-major
+/* Residual stream between stacked layers (the attention block is below), row-major
  * [rows, cols]: msi_residual_init sets h = float(x0); msi_residual_add does
  * h += out.  Both then write the next layer's input x = bf16_rne(h / rms(h))
  * per row, rms(h) = sqrt(mean(h^2) + 1e-6) summed in fp32 in a fixed order
@@ -445,19 +445,19 @@ msi_status msi_residual_init(const uint16_t *x0_bf16, float *h, uint16_t *x_bf16
 msi_status msi_residual_add(const float *out, float *h, uint16_t *x_bf16, uint32_t rows, uint32_t cols,
                             void *stream);
 
-/* ---- Attention block of a stacked layer: projections, a bounded cache of
- * keys and values in 8 bits, the attention that reads it and the eviction that
- * keeps it bounded.  These calls need no plan.  They run asynchronously on
- * `stream`, on the current HIP device, which must be the one that holds the
- * arrays; they allocate nothing, keep nothing between calls and can be
- * captured into a graph.  Calls on different streams are independent as long
- * as they share no workspace and no pages that one of them writes. */
+/* ---- Attention block of a stacked layer: projections, a bounded cache of keys
+ * and values in 8 bits, the attention that reads it and the eviction that keeps
+ * it bounded.  These calls need no plan.  They run asynchronously on `stream`,
+ * on the current HIP device, which must be the one that holds the arrays; they
+ * allocate nothing, keep nothing between calls and can be captured into a
+ * graph.  Calls on different streams are independent as long as they share no
+ * workspace and no pages that one of them writes. */
 
 typedef enum { MSI_F32 = 0, MSI_BF16 = 1 } msi_dtype;
 typedef enum { MSI_ACT_NONE = 0, MSI_ACT_SILU = 1, MSI_ACT_GELU = 2, MSI_ACT_GELU_TANH = 3 } msi_activation;
 
-/* out[m, n] = act(sum_k x[m, k] w[n, k] + bias[n]) + residual[m, n].  GELU is
- * z Phi(z); GELU_TANH its form with tanh.  Sums, bias, activation and the
+/* out[m, n] = act(sum_k x[m, k] w[n, k] + bias[n]) + residual[m, n].  GELU is z
+ * Phi(z); GELU_TANH its form with tanh.  Sums, bias, activation and the
  * residual's addition in fp32, one rounding on the way out.  Strides are
  * elements from one row to the next; k is contiguous. */
 typedef struct {
@@ -477,13 +477,13 @@ typedef struct {
 /* Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 msi_status msi_linear(const msi_linear_args *args, void *stream);
 
-/* The cache of one layer: a pool of pages with stable addresses, each 64
- * tokens of every head, handed to sequences by the caller's page tables.  Page
- * p, head h: 64 rows of K codes, then 64 rows of V codes, one byte an element;
- * value = scale * code, one fp32 scale for the block's K and one for its V.
- * Codes are OCP e4m3 (no NaN codes) or int8 in -127 .. 127, scales positive
- * and finite.  `mass` holds each token's accumulated attention weight, by head.
- * Several sequences may hold a page that a call only reads. */
+/* The cache of one layer: a pool of pages with stable addresses, each 64 tokens
+ * of every head, handed to sequences by the caller's page tables.  Page p, head
+ * h: 64 rows of K codes, then 64 rows of V codes, one byte an element; value =
+ * scale * code, one fp32 scale for the block's K and one for its V. Codes are
+ * OCP e4m3 (no NaN codes) or int8 in -127 .. 127, scales positive and finite.
+ * `mass` holds each token's accumulated attention weight, by head. Several
+ * sequences may hold a page that a call only reads. */
 #define MSI_KV_BLOCK 64u
 typedef enum { MSI_KV_E4M3 = 0, MSI_KV_INT8 = 1 } msi_kv_format;
 typedef struct {
@@ -502,9 +502,9 @@ typedef struct {
  * arrays are on the device and read by the kernels; the host's bounds size the
  * launches.  A sequence whose numbers break a bound is left out, with its rows
  * of the output unwritten, and raises MSI_KV_BAD_LENGTH; a page index outside
- * the pool raises MSI_KV_BAD_PAGE, nothing is written there, and its tokens count as absent
- * (zeros when read).  Status words: a caller-owned device word (or NULL) into which the kernels OR what they
- * met; the caller clears it. */
+ * the pool raises MSI_KV_BAD_PAGE, nothing is written there, and its tokens
+ * count as absent (zeros when read).  Status words: a caller-owned device word
+ * (or NULL) into which the kernels OR what they met; the caller clears it. */
 #define MSI_KV_BAD_PAGE 1u
 #define MSI_KV_NONFINITE 2u      /* an appended element is infinite (stored as the largest code) or NaN (stored as 0) */
 #define MSI_KV_BAD_LENGTH 4u
@@ -520,14 +520,15 @@ typedef struct {
     const int32_t *cu_rows;      /* [n_seqs + 1] ascending from 0                      */
 } msi_kv_seqs;
 
-/* Write the last n tokens of every sequence (lens already counts them): k and
- * v are [n_rows, n_heads, head_dim] bf16, strides in elements from row to row,
+/* Write the last n tokens of every sequence (lens already counts them): k and v
+ * are [n_rows, n_heads, head_dim] bf16, strides in elements from row to row,
  * multiples of 8.  A block's scale is the least power of two s >= 2^-64 with
- * |x| <= 448 s (e4m3) or 127 s (int8) over its new finite elements, or the scale it had if it held
- * tokens and that is larger; codes are x times 1 / s, rounded to nearest, ties to even; codes the block held move to a
- * grown scale the same way.  The new tokens' mass becomes 0.  Bytes after the
- * last token stay as they were.  No page may be written for two sequences by
- * one call.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+ * |x| <= 448 s (e4m3) or 127 s (int8) over its new finite elements, or the
+ * scale it had if it held tokens and that is larger; codes are x times 1 / s,
+ * rounded to nearest, ties to even; codes the block held move to a grown scale
+ * the same way.  The new tokens' mass becomes 0.  Bytes after the last token
+ * stay as they were.  No page may be written for two sequences by one call.
+ * Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,
                          uint64_t k_stride, uint64_t v_stride, uint32_t *status, void *stream);
 
@@ -541,10 +542,11 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
  * out = softmax(scale q k^T) v, zero for a row that sees no token (n > len is
  * allowed here).  With mass_rows > 0, mass[t] = mass_decay * mass[t] + the sum
  * of the probabilities that the sequence's last mass_rows rows and the head's
- * query heads give token t, for every token (with mass_decay 0 the old value
- * is not read; a call with max_rows 0 does nothing).  Where it writes
- * mass, no page may be in the call's tables twice.  Sums are taken in a fixed order: equal calls give equal
- * bits.  `out` must not overlap q.  n_seqs * n_heads * ceil(max_rows * heads of a group / 128) is under 2^24. */
+ * query heads give token t, for every token (with mass_decay 0 the old value is
+ * not read; a call with max_rows 0 does nothing).  Where it writes mass, no
+ * page may be held twice by the call's sequences.  Sums are taken in a fixed
+ * order: equal calls give equal bits.  `out` must not overlap q.  n_seqs * n_heads *
+ * ceil(max_rows * heads of a group / 128) is under 2^24. */
 typedef struct {
     const void *q;               /* [n_rows, n_q_heads, head_dim] bf16                 */
     void *out;                   /* the same shape, bf16                               */
@@ -570,9 +572,10 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
  * (equal ones from the lowest index on; NaN below everything), in ascending
  * order.  Heads keep tokens of their own.  The kept tokens go to the pages of
  * dst_table [n_seqs, dst_blocks], which no sequence of the call may hold, with
- * their mass, coded again by blocks of 64 as an append to empty pages would; new_lens[i] =
- * min(lens[i], budget); keep [n_seqs, n_heads, budget] gets the kept indices, then -1.  A sequence
- * within its budget is copied whole.  cu_rows is not read.  Tokens of a page outside the pool are kept last, as
+ * their mass, coded again by blocks of 64 as an append to empty pages would;
+ * new_lens[i] = min(lens[i], budget); keep [n_seqs, n_heads, budget] gets the
+ * kept indices, then -1.  A sequence within its budget is copied whole.
+ * cu_rows is not read.  Tokens of a page outside the pool are kept last, as
  * zeros.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 typedef struct {
     uint32_t budget;             /* >= 1                                               */
@@ -605,9 +608,9 @@ msi_status msi_source_stats_get(const msi_plan *plan, msi_source_stats *stats);
  * `component` of (layer, expert) returns short (MSI_FAULT_SHORT), fails with
  * EIO (MSI_FAULT_EIO) or is held until msi_debug_source_release
  * (MSI_FAULT_HOLD; a held read completes by itself after 30 s).  The request
- * then fails closed: its window returns to Free, no copy is made and nothing
- * is published; a forward that needed it returns MSI_E_SHORT / MSI_E_IO with
- * out untouched. */
+ * then fails closed: its window returns to Free, no copy is made and nothing is
+ * published; a forward that needed it returns MSI_E_SHORT / MSI_E_IO with out
+ * untouched. */
 #define MSI_FAULT_SHORT 1u
 #define MSI_FAULT_EIO 2u
 #define MSI_FAULT_HOLD 3u

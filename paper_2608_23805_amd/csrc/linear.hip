@@ -450,8 +450,10 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t st)
 // with 128 x 128.  [us; 16 rows, K 2048, N 5120: 7.0 / 7.7 / 9.9 / 13.9 / 17.7; 256, 4096, 2048: 14.8 / 12.7 / 16.7
 // / 23.4 / 31.9; 509, 4096, 2048: 26.3 / 22.9 / 18.0 / 23.9 / 31.5; 1000, 1000, 3000: 27.7 / 30.9 / 20.0 / 20.9 / 14.1.]
 // Past that, 128 x 128 tiles two to a CU, about 1.0 us a pair and stage, or
-// 256 x 256 ones, about 1.85 us, whichever fills its rounds better [1024, 2048, 5120: 28.6
-// and 49.3; 4096, 4096, 2048: 63.5 and 88.4; 2048, 2048, 5120: 52.5 and 51.1; 4096, 2048, 8192: 133 and 121].
+// 256 x 256 ones, about 1.85 us with a tile's start and end, whichever fills its
+// rounds better [2500 rows, K 2048, N 2500: 34.6 and 50.5; 1500, 3000, 5000: 63.4
+// and 78.3; 2048, 4096, 2048: 41.7 and 41.9; 4096, 2048, 4096: 73.4 and 63.0;
+// 4096, 1024, 8192: 80 and 70].
 template <int ACT>
 hipError_t launch_act(const LinearArgs &A, hipStream_t st)
 {
