@@ -109,7 +109,10 @@ struct Unit {
 // through memory, until there are 2048 of them (131072 tokens of one sequence, 2 heads
 // of 256: 36 us with 16 blocks, 46 with 4; 48 sequences of up to 16384, 8 heads of 128:
 // 246, 233, 223 and 219 us with 256, 512, 1024 and 2048 workgroups).
-constexpr int LEAST_BLOCKS = 4, ENOUGH_BLOCKS = 16, FILL_WORKGROUPS = 256, MOST_WORKGROUPS = 2048;
+// Sequences of up to 8 blocks are not cut (4 to 16 sequences of 500 tokens: 9.3 and 10.1 us,
+// 11.6 and 13.5 cut; of 1000 tokens with heads of 256 17.0, 14.1 cut), of up to 4 where
+// the finish kernel has to run anyway for the weights (500 tokens: 12.9, 12.2 cut).
+constexpr int DIRECT_BLOCKS = 8, LEAST_BLOCKS = 4, ENOUGH_BLOCKS = 16, FILL_WORKGROUPS = 256, MOST_WORKGROUPS = 2048;
 
 __device__ __forceinline__ int unit_chunk(int64_t work)
 {
@@ -891,15 +894,20 @@ __device__ __forceinline__ void join_pair(float &m, float &l, float m1, float l1
 }
 
 constexpr int MASS_BLOCKS = 16;              // blocks of a workgroup
+constexpr int PIECE = 64;                    // elements of a workgroup that joins many units of one row
+constexpr int WIDE_ROWS = 512;               // (row, head, sequence) triples from which rows stand side by side
 
-// Workgroups [0, join) of a (head, sequence): D / pieces elements of one packed
-// row each, four a lane, the rest of the lanes over the units.  Then, where the
+// Workgroups [0, join) of a (head, sequence) join the units' results: with few
+// rows, 64 elements of one packed row each, four a lane, the rest of the lanes
+// over the units; with many (`wide`), whole rows side by side, four elements a
+// lane, which walks the units (one sequence of 1000 tokens, 8 heads of 128, 100 rows
+// with 8 heads each: 29.6 -> 21.7 us in all; 16 rows 18.1 -> 16.9).  Then, where the
 // few-rows kernel left scores for the weights, one workgroup per MASS_BLOCKS
 // blocks: lane = token, a wavefront's four blocks side by side.  Bound by
 // latency for usual batches, so loads depend on as few others as possible: 4.4
 // us for one sequence's 128 units, 23 us for the weights of 48 sequences of up
 // to 16384 tokens (80 MB of scores and weights).
-__global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int join, int pieces)
+__global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int join, bool wide)
 {
     __shared__ __attribute__((aligned(16))) float part[1024];
     __shared__ float ml[2][8][32];
@@ -912,8 +920,34 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     if (!q.ok && blockIdx.x == 0 && h == 0 && tid == 0)
         kv_raise(A.status, KV_BAD_LENGTH);           // (such a sequence has no units)
+    if (int(blockIdx.x) < join && wide) {
+        const int lanes = A.c.D / 4, r = int(blockIdx.x) * (256 / lanes) + tid / lanes, e = 4 * (tid % lanes);
+        if (r >= rows)
+            return;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int u = 0; u < n; ++u) {
+            const int64_t p = part_index(A, first + u, h, r);
+            const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * p);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(A.part_o + p * A.c.D + e);
+            const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(x.x - ref);
+            l = a * l + b * x.y;
+            o = a * o + b * v;
+            m = top;
+        }
+        const int tr = r / A.G, hd = r - tr * A.G;
+        o *= l == 0.0f ? 0.0f : 1.0f / l;
+        *reinterpret_cast<uint2 *>(A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * A.c.D + e) =
+            make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+        if (A.lse && e == 0)
+            A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = log_sum(m, l);
+        return;
+    }
     if (int(blockIdx.x) < join) {
-        const int width = A.c.D / pieces, r = int(blockIdx.x) / pieces, e0 = width * (int(blockIdx.x) % pieces);
+        constexpr int LANES = PIECE / 4, GROUPS = 256 / LANES;
+        const int pieces = A.c.D / PIECE, r = int(blockIdx.x) / pieces, e0 = PIECE * (int(blockIdx.x) % pieces);
         if (r >= rows)
             return;
         float m = -INFINITY, l = 0.0f;
@@ -923,20 +957,21 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
         }
         const float top = wave_max(m), ref = top == -INFINITY ? 0.0f : top;
         l = wave_sum(l * __builtin_amdgcn_exp2f(m - ref));
-        const int lanes = width / 4, groups = 256 / lanes, g = tid / lanes, e = 4 * (tid % lanes);
+        const int g = tid / LANES, e = 4 * (tid % LANES);
         f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int s = g; s < n; s += groups) {
+        for (int s = g; s < n; s += GROUPS) {
             const int64_t p = part_index(A, first + s, h, r);
             o += __builtin_amdgcn_exp2f(A.part_ml[2 * p] - ref) * *reinterpret_cast<const f32x4 *>(A.part_o + p * A.c.D + e0 + e);
         }
-        *reinterpret_cast<f32x4 *>(part + g * width + e) = o;
+        *reinterpret_cast<f32x4 *>(part + g * PIECE + e) = o;
         __syncthreads();
         const int tr = r / A.G, hd = r - tr * A.G;
-        if (tid < width) {
+        if (tid < PIECE) {
             float sum = 0.0f;
-            for (int k = 0; k < groups; ++k)
-                sum += part[k * width + tid];
+#pragma unroll
+            for (int k = 0; k < GROUPS; ++k)
+                sum += part[k * PIECE + tid];
             A.out[(int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * A.c.D + e0 + tid] =
                 f32_to_bf16(l == 0.0f ? 0.0f : sum / l);
         }
@@ -1157,7 +1192,7 @@ AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows
     c.few = rows <= 32;
     c.tile_rows = c.few ? (rows <= 16 ? 16 : 32) : 128;
     c.per = int((rows + c.tile_rows - 1) / c.tile_rows) * H;
-    c.direct = blocks <= LEAST_BLOCKS || int64_t(S) * c.per >= (c.few ? 8192 : 256);
+    c.direct = blocks <= (c.few && mass ? LEAST_BLOCKS : DIRECT_BLOCKS) || int64_t(S) * c.per >= (c.few ? 8192 : 256);
     // sum of ceil(blocks_i / chunk) <= total / chunk + S, and total * per <= chunk * MOST_WORKGROUPS
     c.units = c.direct ? S : int(std::min<int64_t>(int64_t(S) * ((blocks + LEAST_BLOCKS - 1) / LEAST_BLOCKS),
                                                    MOST_WORKGROUPS / c.per + S));
@@ -1195,11 +1230,12 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
     if (e == hipSuccess)
         e = hipGetLastError();
     const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
-    // a row's elements over several workgroups where there are few rows and many units of each
-    const int pieces = int64_t(rows) * H * S < 256 ? A.c.D / 64 : 1;
-    const int join = c.direct ? 0 : rows * pieces, groups = A.mass_rows && c.few ? (blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
+    const bool wide = int64_t(rows) * H * S >= WIDE_ROWS;
+    const int side = 1024 / A.c.D;                          // rows side by side
+    const int join = c.direct ? 0 : wide ? (rows + side - 1) / side : rows * (A.c.D / PIECE);
+    const int groups = A.mass_rows && c.few ? (blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
     if (e == hipSuccess && join + groups) {
-        launch_k(kv_finish_kernel, dim3(join + groups, H, S), 256, 0, st, A, join, pieces);
+        launch_k(kv_finish_kernel, dim3(join + groups, H, S), 256, 0, st, A, join, wide);
         e = hipGetLastError();
     }
     if (e == hipSuccess && A.mass_rows && !c.few && blocks) {

@@ -64,6 +64,21 @@ def test_many_rows(fmt, H, G, D, lens, rows):
     _check(s, s.seqs, s.table, s.lens, s.cu, G, mass_rows=1000, decay=0.0)
 
 
+@pytest.mark.parametrize("fmt,H,G,D,lens,rows", [
+    ("e4m3", 2, 8, 64, [700] * 39 + [0], [1] * 40),            # few rows each, many in all
+    ("int8", 2, 8, 128, [1200, 600, 3], [50, 20, 60]),         # some rows see nothing
+    ("e4m3", 1, 16, 256, [1500, 64], [40, 2]),
+    ("int8", 1, 3, 64, [512, 513, 577], [1, 90, 4]),           # at the side where sequences begin to be cut
+    ("e4m3", 1, 2, 128, [512, 500], [1, 1]),
+])
+def test_cut_sequences_with_many_rows(fmt, H, G, D, lens, rows):
+    """Units' results joined with rows side by side and one by one, and sequences at the length where cutting begins."""
+    log(f"case cut, many rows {fmt} H={H} G={G} D={D} lens={lens[:3]} rows={rows[:3]}")
+    s = Setup(sum(lens) + 2, lens, rows, H, D, fmt)
+    _check(s, s.seqs, s.table, s.lens, s.cu, G)
+    _check(s, s.seqs, s.table, s.lens, s.cu, G, mass_rows=40, decay=0.5)
+
+
 def test_rows_without_tokens():
     """More rows than tokens: the first ones see nothing and come out zero; a padded sequence of length 0 too."""
     log("case empty rows")
