@@ -258,12 +258,11 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     A.direct = cut.direct;
     A.per = cut.per;
     A.part_rows = s.max_rows * A.G;
-    if (cut.part_o > cut.part_ml)
-        A.part_ml = reinterpret_cast<float *>(ws + cut.part_ml);
-    if (!cut.direct)
+    if (!cut.direct) {
         A.plan = reinterpret_cast<int2 *>(ws);
-    if (!cut.direct)
+        A.part_ml = reinterpret_cast<float *>(ws + cut.part_ml);
         A.part_o = reinterpret_cast<float *>(ws + cut.part_o);
+    }
     if (a->mass_rows && cut.few)
         A.scores = reinterpret_cast<float *>(ws + cut.scores);
     A.score_blocks = cut.score_blocks;

@@ -79,6 +79,9 @@ __device__ __forceinline__ float across16(float v, Op op)      // over the lanes
 __device__ __forceinline__ float vmax(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float vsum(float a, float b) { return a + b; }
 
+// log2 of the sum of a row's powers; a row that sees nothing has none: +infinity makes its probabilities zero.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? INFINITY : m + log2f(l); }
+
 // Rows are numbered row * G + head of the group within a sequence and cache head.
 __device__ __forceinline__ int row_limit(const KvSeq &q, int token_row) { return q.len - q.n + token_row + 1; }
 
@@ -110,8 +113,7 @@ struct Unit {
 // of 256: 36 us with 16 blocks, 46 with 4; 48 sequences of up to 16384, 8 heads of 128:
 // 246, 233, 223 and 219 us with 256, 512, 1024 and 2048 workgroups).
 // Sequences of up to 8 blocks are not cut (4 to 16 sequences of 500 tokens: 9.3 and 10.1 us,
-// 11.6 and 13.5 cut; of 1000 tokens with heads of 256 17.0, 14.1 cut), of up to 4 where
-// the finish kernel has to run anyway for the weights (500 tokens: 12.9, 12.2 cut).
+// 11.6 and 13.5 cut; of 1000 tokens with heads of 256 17.0, 14.1 cut).
 constexpr int DIRECT_BLOCKS = 8, LEAST_BLOCKS = 4, ENOUGH_BLOCKS = 16, FILL_WORKGROUPS = 256, MOST_WORKGROUPS = 2048;
 
 __device__ __forceinline__ int unit_chunk(int64_t work)
@@ -243,6 +245,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     constexpr int TOK = F::TOK, GT = F::GT, W = F::W, VW = F::VW, OS = F::OS;
     __shared__ __attribute__((aligned(16))) float olds[4][16][OS];
     __shared__ float ml[4][RT][16][2];
+    __shared__ float lsum[16 * RT];
     constexpr bool QLDS = D == 256 && RT == 2;               // two tiles of long queries do not fit the registers
     __shared__ bf16x8 qlds[QLDS ? RT * (D / 32) * 64 : 1];
 
@@ -256,12 +259,33 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
         A.plan[i] = make_int2(unit.first, unit.n);
     const int rows = q.n * A.G, r0 = tile * 16 * RT;
-    if (r0 >= rows)
-        return;
     const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
     const int b0 = range.x, b1 = range.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, j = lane >> 4;
+    // the weights of a sequence that is not cut: its only workgroup has the rows' sums and reads its scores back (by
+    // the finish kernel: 4 sequences of 200 tokens 11.4 us for 8.5, 1024 of 2000 tokens 560 for 542)
+    auto weigh = [&]() {
+        for (int b = b0 + wave; b < b1; b += 4) {
+            const int page = A.s.table[int64_t(i) * A.s.max_blocks + b];
+            if (!kv_page_ok(page, A.c.n_pages) || b * KV_BLOCK + lane >= q.len)
+                continue;
+            const float *src = A.scores + score_index(A, i, b, page, h, 0) + lane;
+            float *dst = A.c.mass + (int64_t(page) * A.c.H + h) * KV_BLOCK + lane;
+            const float was = A.decay != 0.0f ? *dst : 0.0f;
+            float w = 0.0f;
+#pragma unroll 4
+            for (int r = max(q.n - A.mass_rows, 0) * A.G; r < rows; ++r)
+                w += __builtin_amdgcn_exp2f(src[r * KV_BLOCK] - lsum[r]);
+            *dst = A.decay != 0.0f ? fmaf(A.decay, was, w) : w;
+        }
+    };
+    const bool weighs = A.direct && A.scores;
+    if (r0 >= rows) {
+        if (weighs)
+            weigh();                                           // (no rows: the weights decay)
+        return;
+    }
 
     // pages of this wavefront's next 64 blocks, one a lane (-1: bad)
     auto page_list = [&](int k) {
@@ -479,10 +503,12 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
             a[w] = __builtin_amdgcn_exp2f(ml[w][x][row][0] - ref);
             sum += a[w] * ml[w][x][row][1];
         }
+        if ((tid & 15) == 0)
+            lsum[16 * x + row] = log_sum(mx, sum);
         if (r < rows) {
             const int tr = r / A.G, hd = r - tr * A.G;
             const int64_t part = part_index(A, unit.first + unit.split, h, r);
-            if ((tid & 15) == 0 && A.part_ml) {
+            if ((tid & 15) == 0 && !A.direct) {
                 A.part_ml[2 * part] = mx;
                 A.part_ml[2 * part + 1] = sum;
             }
@@ -503,6 +529,10 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
                 }
             }
         }
+    }
+    if (weighs) {
+        __syncthreads();                                       // (the scores that the four wavefronts stored, and lsum)
+        weigh();
     }
 }
 
@@ -882,9 +912,6 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 
 // ---------------------------------------------------------------- finish
 //
-// log2 of the sum of a row's powers; a row that sees nothing has none: +infinity makes its probabilities zero.
-__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? INFINITY : m + log2f(l); }
-
 // Two (maximum, sum) pairs of a row as one.
 __device__ __forceinline__ void join_pair(float &m, float &l, float m1, float l1)
 {
@@ -902,7 +929,7 @@ constexpr int WIDE_ROWS = 512;               // (row, head, sequence) triples fr
 // over the units; with many (`wide`), whole rows side by side, four elements a
 // lane, which walks the units (one sequence of 1000 tokens, 8 heads of 128, 100 rows
 // with 8 heads each: 29.6 -> 21.7 us in all; 16 rows 18.1 -> 16.9).  Then, where the
-// few-rows kernel left scores for the weights, one workgroup per MASS_BLOCKS
+// few-rows kernel left scores of cut sequences, one workgroup per MASS_BLOCKS
 // blocks: lane = token, a wavefront's four blocks side by side.  Bound by
 // latency for usual batches, so loads depend on as few others as possible: 4.4
 // us for one sequence's 128 units, 23 us for the weights of 48 sequences of up
@@ -913,10 +940,10 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
     __shared__ float ml[2][8][32];
     const int i = blockIdx.z, h = blockIdx.y;
     const KvSeq q = kv_seq(A.s, i, false);
-    const int2 units = A.plan ? A.plan[i] : make_int2(i, 1);
+    const int2 units = A.plan[i];
     const int rows = q.n * A.G, blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
     const int first = __builtin_amdgcn_readfirstlane(units.x);
-    const int n = A.plan && blocks == 0 ? 0 : __builtin_amdgcn_readfirstlane(units.y);     // (no unit wrote the plan)
+    const int n = blocks == 0 ? 0 : __builtin_amdgcn_readfirstlane(units.y);     // (no unit wrote the plan)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     if (!q.ok && blockIdx.x == 0 && h == 0 && tid == 0)
         kv_raise(A.status, KV_BAD_LENGTH);           // (such a sequence has no units)
@@ -1192,13 +1219,13 @@ AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows
     c.few = rows <= 32;
     c.tile_rows = c.few ? (rows <= 16 ? 16 : 32) : 128;
     c.per = int((rows + c.tile_rows - 1) / c.tile_rows) * H;
-    c.direct = blocks <= (c.few && mass ? LEAST_BLOCKS : DIRECT_BLOCKS) || int64_t(S) * c.per >= (c.few ? 8192 : 256);
+    c.direct = blocks <= DIRECT_BLOCKS || int64_t(S) * c.per >= (c.few ? 8192 : 256);
     // sum of ceil(blocks_i / chunk) <= total / chunk + S, and total * per <= chunk * MOST_WORKGROUPS
     c.units = c.direct ? S : int(std::min<int64_t>(int64_t(S) * ((blocks + LEAST_BLOCKS - 1) / LEAST_BLOCKS),
                                                    MOST_WORKGROUPS / c.per + S));
     size_t off = c.direct ? 0 : up256(size_t(S) * sizeof(int2));     // the plan comes first
     c.part_ml = off;
-    off += !c.direct || (mass && c.few) ? up256(size_t(c.units) * H * rows * 2 * sizeof(float)) : 0;
+    off += !c.direct ? up256(size_t(c.units) * H * rows * 2 * sizeof(float)) : 0;
     c.part_o = off;
     off += !c.direct ? up256(size_t(c.units) * H * rows * D * sizeof(float)) : 0;
     c.scores = off;
@@ -1233,7 +1260,7 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
     const bool wide = int64_t(rows) * H * S >= WIDE_ROWS;
     const int side = 1024 / A.c.D;                          // rows side by side
     const int join = c.direct ? 0 : wide ? (rows + side - 1) / side : rows * (A.c.D / PIECE);
-    const int groups = A.mass_rows && c.few ? (blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
+    const int groups = A.mass_rows && c.few && !c.direct ? (blocks + MASS_BLOCKS - 1) / MASS_BLOCKS : 0;
     if (e == hipSuccess && join + groups) {
         launch_k(kv_finish_kernel, dim3(join + groups, H, S), 256, 0, st, A, join, wide);
         e = hipGetLastError();
