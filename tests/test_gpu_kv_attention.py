@@ -79,6 +79,15 @@ def test_cut_sequences_with_many_rows(fmt, H, G, D, lens, rows):
     _check(s, s.seqs, s.table, s.lens, s.cu, G, mass_rows=40, decay=0.5)
 
 
+@pytest.mark.parametrize("decay", [0.0, 0.5])
+@pytest.mark.parametrize("lens,rows", [([200, 100, 0, 64], [1, 0, 0, 2]), ([900, 700], [1, 0]), ([300, 90], [40, 0])])
+def test_weights_of_sequences_without_rows(lens, rows, decay):
+    """A sequence of the call that brings no rows: its weights decay, nothing else happens to it."""
+    log(f"case weights without rows {lens} {rows} {decay}")
+    s = Setup(sum(lens) + 3, lens, rows, 2, 64, "int8")
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4, mass_rows=2, decay=decay)
+
+
 def test_rows_without_tokens():
     """More rows than tokens: the first ones see nothing and come out zero; a padded sequence of length 0 too."""
     log("case empty rows")
