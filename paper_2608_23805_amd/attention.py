@@ -32,13 +32,20 @@ def _refuse(msg: str):
     raise MsiError(MSI_E_INVALID_ARG, msg)
 
 
+# the current device without the public call's look whether HIP is initialised: a tensor on a device shows that it is
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _call(device, fn, *args):
     """The library call, with the tensors' device current."""
-    if device.type == "cuda" and device.index != torch.cuda.current_device():
+    index = device.index
+    if index is None:
+        _refuse(f"tensors must be on a HIP device, got {device}")
+    if index == _current_device():
+        st = fn(*args)
+    else:
         with torch.cuda.device(device):
             st = fn(*args)
-    else:
-        st = fn(*args)
     if st != MSI_OK:
         _check(st)
 

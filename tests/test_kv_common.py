@@ -221,5 +221,12 @@ def test_binding_refusals():
     refuses(msi.kv_evict, cache, s, i32(2, 2), i32(3), i32(2, 2, 100), budget=100)
     refuses(msi.kv_evict, cache, s, i32(2, 2), i32(2), i32(2, 2, 99), budget=100)
     refuses(msi.kv_evict, cache, s, i32(2, 2), i32(2), i32(2, 2, 100), budget=100, sinks=-1)
+    # host tensors that are right in everything else
+    for f, a, k in ((msi.linear, (x, w, out), {}), (msi.kv_append, (cache, s, z(4, 2, 64), z(4, 2, 64)), {}),
+                    (msi.kv_read, (cache, s, z(4, 2, 64), z(4, 2, 64)), {}),
+                    (msi.kv_attention, (cache, s, z(4, 4, 64), z(4, 4, 64), 1.0), {}),
+                    (msi.kv_evict, (cache, s, i32(2, 2), i32(2), i32(2, 2, 100)), dict(budget=100))):
+        with pytest.raises(msi.MsiError, match="HIP device"):
+            f(*a, **k)
     with pytest.raises(AttributeError):
         msi.no_such_name
