@@ -1048,7 +1048,7 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
         }
     }
     __syncthreads();
-#pragma unroll 2
+#pragma unroll 4
     for (int r = from; r < rows; ++r) {
         const float z = part[r];
 #pragma unroll
