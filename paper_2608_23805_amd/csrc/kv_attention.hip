@@ -549,8 +549,9 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // the accumulation registers every block would move all of them there and back:
 // 753 us for 640).  4096 rows on top of 4096 tokens, two sequences, 16 query heads
 // of 256: 890 us, 926 TFLOP/s; 32 of 128: 795 us, 1038 TFLOP/s (int8 codes, whose
-// conversion takes the vector unit twice as long: about 790).  A ragged batch loses up to a fifth to
-// its last workgroups.
+// conversion takes the vector unit twice as long: about 790).  The conversions
+// bound it: with heads of 256 and eight wavefronts of 16 rows, two a SIMD, every
+// wavefront converts the whole block, 928 us for 890.
 //
 // LDS: 16-byte chunk c of token row t (K rows, then V rows) sits at slot
 // c ^ many_swz(t) of its row: the 16-byte reads of eight consecutive K rows and the
@@ -932,7 +933,7 @@ constexpr int WIDE_ROWS = 512;               // (row, head, sequence) triples fr
 // few-rows kernel left scores of cut sequences, one workgroup per MASS_BLOCKS
 // blocks: lane = token, a wavefront's four blocks side by side.  Bound by
 // latency for usual batches, so loads depend on as few others as possible: 4.4
-// us for one sequence's 128 units, 23 us for the weights of 48 sequences of up
+// us for one sequence's 128 units, 20 us for the weights of 48 sequences of up
 // to 16384 tokens (80 MB of scores and weights).
 __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int join, bool wide)
 {
