@@ -48,12 +48,6 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t a, uint32_t b)
     return __builtin_bit_cast(bf16x8, r);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16_hw(float lo, float hi)
-{
-    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
-    return __builtin_bit_cast(uint32_t, bf16x2_t{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
-}
-
 // 4 x 4 bytes transposed: byte d of word t becomes byte t of word d.
 __device__ __forceinline__ void transpose4(const uint32_t (&in)[4], uint32_t (&out)[4])
 {
@@ -443,9 +437,9 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 #pragma unroll
             for (int u = 0; u < GT / 2; ++u)
                 pf[x][u] = __builtin_bit_cast(
-                    bf16x8, u32x4{pack_bf16_hw(sv[x][2 * u][0], sv[x][2 * u][1]), pack_bf16_hw(sv[x][2 * u][2], sv[x][2 * u][3]),
-                                  pack_bf16_hw(sv[x][2 * u + 1][0], sv[x][2 * u + 1][1]),
-                                  pack_bf16_hw(sv[x][2 * u + 1][2], sv[x][2 * u + 1][3])});
+                    bf16x8, u32x4{pack_bf16x2_hw(sv[x][2 * u][0], sv[x][2 * u][1]), pack_bf16x2_hw(sv[x][2 * u][2], sv[x][2 * u][3]),
+                                  pack_bf16x2_hw(sv[x][2 * u + 1][0], sv[x][2 * u + 1][1]),
+                                  pack_bf16x2_hw(sv[x][2 * u + 1][2], sv[x][2 * u + 1][3])});
         }
         // ---- O^T: lane (i, j) holds elements i D / 16 + c of the eight tokens
 #pragma unroll
@@ -871,8 +865,8 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 pf[2 * x + u] = __builtin_bit_cast(
-                    bf16x8, u32x4{pack_bf16_hw(sv[x][8 * u], sv[x][8 * u + 1]), pack_bf16_hw(sv[x][8 * u + 2], sv[x][8 * u + 3]),
-                                  pack_bf16_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
+                    bf16x8, u32x4{pack_bf16x2_hw(sv[x][8 * u], sv[x][8 * u + 1]), pack_bf16x2_hw(sv[x][8 * u + 2], sv[x][8 * u + 3]),
+                                  pack_bf16x2_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16x2_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
         }
         l = fmaf(sum, __builtin_amdgcn_exp2f(-vl), l);
         times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
@@ -892,8 +886,8 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
                 *reinterpret_cast<uint2 *>(dst + 32 * c + 2 * v) =
-                    make_uint2(pack_bf16_hw(acc[c][v] * inv, acc[c][v + 1] * inv),
-                               pack_bf16_hw(acc[c][v + 2] * inv, acc[c][v + 3] * inv));
+                    make_uint2(pack_bf16x2_hw(acc[c][v] * inv, acc[c][v + 1] * inv),
+                               pack_bf16x2_hw(acc[c][v + 2] * inv, acc[c][v + 3] * inv));
         if (A.lse && hf == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
     } else {
