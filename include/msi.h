@@ -508,13 +508,14 @@ typedef struct {
 #define MSI_KV_BAD_PAGE 1u
 #define MSI_KV_NONFINITE 2u      /* an appended element is infinite (stored as the largest code) or NaN (stored as 0) */
 #define MSI_KV_BAD_LENGTH 4u
+#define MSI_KV_ALL_ROWS 1u       /* msi_kv_attention writes every row of the call, see there */
 typedef struct {
     uint32_t n_seqs;             /* <= 65535                                           */
     uint32_t max_blocks;         /* row length of table, <= 2^23                       */
     uint32_t n_rows;             /* rows of the call's row arrays, <= 2^29             */
     uint32_t max_rows;           /* bound of one sequence's rows                       */
     uint32_t max_len;            /* bound of lens, <= 64 * max_blocks                  */
-    uint32_t reserved;
+    uint32_t flags;              /* 0, or MSI_KV_ALL_ROWS                              */
     const int32_t *table;        /* [n_seqs, max_blocks]                               */
     const int32_t *lens;         /* [n_seqs]                                           */
     const int32_t *cu_rows;      /* [n_seqs + 1] ascending from 0                      */
@@ -544,8 +545,11 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
  * of the probabilities that the sequence's last mass_rows rows and the head's
  * query heads give token t, for every token (with mass_decay 0 the old value is
  * not read; a call with max_rows 0 does nothing).  Where it writes mass, no
- * page may be held twice by the call's sequences.  Sums are taken in a fixed
- * order: equal calls give equal bits.  `out` must not overlap q.  n_seqs * n_heads *
+ * page may be held twice by the call's sequences.  With MSI_KV_ALL_ROWS a
+ * sequence with n > len is left out, as msi_kv_append and msi_kv_read leave it
+ * out, and the rows of `out` below n_rows that belong to no sequence, or to one
+ * that is left out, become zeros; without it they stay as they were.  Sums are
+ * taken in a fixed order: equal calls give equal bits.  `out` must not overlap q.  n_seqs * n_heads *
  * ceil(max_rows * heads of a group / 128) is under 2^24. */
 typedef struct {
     const void *q;               /* [n_rows, n_q_heads, head_dim] bf16                 */

@@ -113,6 +113,7 @@ MSI_F32, MSI_BF16 = 0, 1
 MSI_KV_BLOCK = 64
 KV_FORMATS = {"e4m3": 0, "int8": 1}
 KV_BAD_PAGE, KV_NONFINITE, KV_BAD_LENGTH = 1, 2, 4
+KV_ALL_ROWS = 1
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 
 
@@ -129,7 +130,8 @@ class msi_kv_cache(ctypes.Structure):
 
 class msi_kv_seqs(ctypes.Structure):
     _fields_ = [("n_seqs", _u32), ("max_blocks", _u32), ("n_rows", _u32), ("max_rows", _u32), ("max_len", _u32),
-                ("reserved", _u32), ("table", _vp), ("lens", _vp), ("cu_rows", _vp)]
+                ("flags", _u32), ("table", _vp), ("lens", _vp), ("cu_rows", _vp)]
+    reserved = property(lambda s: s.flags, lambda s, v: setattr(s, "flags", v))      # the word's name before it had flags
 
 
 class msi_kv_attention_args(ctypes.Structure):

@@ -16,7 +16,7 @@ from typing import Optional
 
 import torch
 
-from . import (ACTIVATIONS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
+from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
                msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
@@ -220,8 +220,10 @@ def kv_attention_workspace(cache: KvCache, seqs: KvSeqs, n_q_heads: int, mass_ro
 
 
 def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: int = 0, mass_decay: float = 1.0,
-                 workspace=None, status=None, stream=None):
-    """Attention of q [n_rows, n_q_heads, head_dim] bf16 over the sequences' pages into out (msi_kv_attention)."""
+                 workspace=None, status=None, stream=None, all_rows: bool = False):
+    """Attention of q [n_rows, n_q_heads, head_dim] bf16 over the sequences' pages into out (msi_kv_attention).
+
+    all_rows: every row of out is written, with zeros where no sequence answers for it (MSI_KV_ALL_ROWS)."""
     _same_device(cache, seqs)
     if q.dim() != 3:
         _refuse("q must be [n_rows, n_q_heads, head_dim]")
@@ -233,7 +235,12 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
     if workspace is not None:
         _dense("workspace", workspace, torch.uint8, dev)
         wp, wn = workspace.data_ptr(), workspace.numel()
-    _call(dev, lib.msi_kv_attention, cache._ref, seqs._ref,
+    ref = seqs._ref
+    if all_rows:
+        c = msi_kv_seqs.from_buffer_copy(seqs.c)
+        c.flags |= KV_ALL_ROWS
+        ref = ctypes.byref(c)
+    _call(dev, lib.msi_kv_attention, cache._ref, ref,
           _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30), mass_decay, wp,
                                wn, _status(status, dev)), _stream(stream))
 
@@ -264,7 +271,8 @@ class AttentionBlock:
 
     wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  Holds the
     buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace.  Steps allocate nothing and
-    can be captured; those of one block share its buffers, so they must not overlap."""
+    can be captured; those of one block share its buffers, so they must not overlap.  Rows below n_rows that no sequence
+    brings, and those of a sequence that breaks a bound or has more rows than tokens, get nothing added to h."""
 
     def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None):
         D, H = cache.head_dim, cache.n_heads
@@ -307,7 +315,7 @@ class AttentionBlock:
         linear(x, self.wqkv, qkv.view(n, -1), bias=self.bias, stream=stream)
         kv_append(self.cache, seqs, qkv[:, Hq:Hq + H], qkv[:, Hq + H:], status=status, stream=stream)
         kv_attention(self.cache, seqs, qkv[:, :Hq], attn, self.scale, mass_rows=mass_rows, mass_decay=mass_decay,
-                     workspace=self.workspace, status=status, stream=stream)
+                     workspace=self.workspace, status=status, stream=stream, all_rows=True)
         linear(attn.view(n, -1), self.wo, out, stream=stream)
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],

@@ -48,6 +48,8 @@ const char *view_seqs(const msi_kv_seqs *s, bool rows, KvSeqs &out)
         return "null sequences";
     if (s->n_seqs > 65535)
         return "n_seqs must be at most 65535";
+    if (s->flags & ~MSI_KV_ALL_ROWS)
+        return "unknown flags of the sequences";
     if (s->max_blocks > MOST / MSI_KV_BLOCK || s->max_len > uint64_t(s->max_blocks) * MSI_KV_BLOCK)
         return "max_len must be at most 64 * max_blocks, max_blocks at most 2^23";
     if (s->n_seqs && (!s->lens || (s->max_len && !s->table)))
@@ -61,7 +63,8 @@ const char *view_seqs(const msi_kv_seqs *s, bool rows, KvSeqs &out)
     if (!aligned(s->table, 4) || !aligned(s->lens, 4) || !aligned(s->cu_rows, 4))
         return "sequence arrays must be 4-byte aligned";
     out = KvSeqs{s->table, s->lens, rows ? s->cu_rows : nullptr, int(s->n_seqs), int(s->max_blocks),
-                 rows ? int(s->n_rows) : 0, rows ? int(s->max_rows) : 0, int(s->max_len)};
+                 rows ? int(s->n_rows) : 0, rows ? int(s->max_rows) : 0, int(s->max_len),
+                 (s->flags & MSI_KV_ALL_ROWS) != 0};
     return nullptr;
 }
 
@@ -231,13 +234,17 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
         return bad("mass_rows needs the cache's mass");
     if (a->mass_rows && !(a->mass_decay >= 0.0f && std::isfinite(a->mass_decay)))
         return bad("mass_decay must be finite and not negative");
-    if (s.S == 0 || s.max_rows == 0)
+    const bool go = s.S && s.max_rows, rest = s.all_rows && s.n_rows;
+    if (!go && !rest)
         return MSI_OK;
     const uint64_t least = uint64_t(a->n_q_heads) * c.D;
     if (!rows_ok(a->q, a->q_stride, least) || !rows_ok(a->out, a->out_stride, least))
         return bad("q and out need 16-byte aligned rows of n_q_heads * head_dim, strides a multiple of 8 up to 2^21");
     if (a->q == a->out)
         return bad("out must not be q");
+    if (!go)
+        return launched(launch_kv_rest(s, static_cast<uint16_t *>(a->out), int64_t(a->out_stride), int(least),
+                                       static_cast<hipStream_t>(stream)));
     const AttentionCut cut =
         attention_cut(s.S, c.H, int(a->n_q_heads) / c.H, c.D, c.n_pages, s.max_rows, s.max_len, a->mass_rows != 0);
     const size_t lse = lse_bytes(cut, s, a->n_q_heads, a->mass_rows), need = cut.bytes + lse;
@@ -271,6 +278,11 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     A.mass_rows = int(std::min(a->mass_rows, MOST));
     A.decay = a->mass_decay;
     A.status = a->status;
+    if (rest) {
+        const hipError_t e = launch_kv_rest(s, A.out, A.out_stride, int(least), static_cast<hipStream_t>(stream));
+        if (e != hipSuccess)
+            return launched(e);
+    }
     return launched(launch_kv_attention(A, int(cache->format), cut, static_cast<hipStream_t>(stream)));
 }
 

@@ -342,6 +342,8 @@ struct AttentionLaunch {
     float decay;
     uint32_t *status;
 };
+// zeros in the rows of `out` (`width` elements) that no sequence of the call answers for
+hipError_t launch_kv_rest(const KvSeqs &s, uint16_t *out, int64_t out_stride, int width, hipStream_t st);
 hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st);
 
 }  // namespace msi

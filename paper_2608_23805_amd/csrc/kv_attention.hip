@@ -92,7 +92,7 @@ __device__ __forceinline__ int blocks_of(const KvSeqs &s, int i)      // per lan
 {
     if (i >= s.S)
         return 0;
-    const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, false);
+    const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, s.all_rows);
     return q.n ? (q.len + KV_BLOCK - 1) / KV_BLOCK : 0;
 }
 
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     if (unit.seq < 0)
         return;
     const int i = unit.seq, sub = int(blockIdx.x) % A.per, h = sub % A.c.H, tile = sub / A.c.H;
-    const KvSeq q = kv_seq(A.s, i, false);
+    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
     if (!q.ok && sub == 0 && threadIdx.x == 0)
         kv_raise(A.status, KV_BAD_LENGTH);
     if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
         return;
     // the last row tiles, which see the most tokens, start first
     const int i = unit.seq, sub = A.per - 1 - int(blockIdx.x) % A.per, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
-    const KvSeq q = kv_seq(A.s, i, false);
+    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
     if (!q.ok && sub == 0 && threadIdx.x == 0)
         kv_raise(A.status, KV_BAD_LENGTH);
     if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
@@ -934,7 +934,7 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
     __shared__ __attribute__((aligned(16))) float part[1024];
     __shared__ float ml[2][8][32];
     const int i = blockIdx.z, h = blockIdx.y;
-    const KvSeq q = kv_seq(A.s, i, false);
+    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
     const int2 units = A.plan[i];
     const int rows = q.n * A.G, blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK;
     const int first = __builtin_amdgcn_readfirstlane(units.x);
@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
     __shared__ float part[4][KV_BLOCK];
     constexpr bool RAW = D == 256;
     const int i = blockIdx.z, h = blockIdx.y;
-    const KvSeq q = kv_seq(A.s, i, false);
+    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int b = int(blockIdx.x) * share + wave % share, group = wave / share, groups = 4 / share;
     if (int(blockIdx.x) * share * KV_BLOCK >= q.len)
@@ -1183,6 +1183,38 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
     }
 }
 
+// ---------------------------------------------------------------- other rows
+//
+// Rows that no sequence answers for: those between and behind the sequences'
+// rows and those of a sequence whose numbers break a bound.  A workgroup marks
+// which of its 64 rows some sequence brings (offsets that fall could overlap,
+// so every sequence is looked at) and clears the others; with all of them
+// brought, as usual, it reads the lengths and ends: a launch.
+constexpr int REST_ROWS = 64;
+
+__global__ void __launch_bounds__(256) kv_rest_kernel(KvSeqs s, uint16_t *__restrict__ out, int64_t stride, int chunks)
+{
+    __shared__ uint32_t brought[2];
+    const int r0 = int(blockIdx.x) * REST_ROWS, n = min(REST_ROWS, s.n_rows - r0);
+    if (threadIdx.x < 2)
+        brought[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < s.S; i += 256) {
+        const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, true);
+        const int lo = max(q.row0 - r0, 0), hi = min(q.row0 - r0 + q.n, n);
+        if (q.n > 0 && lo < hi) {
+            const uint64_t rows = (~uint64_t(0) >> (64 - (hi - lo))) << lo;
+            atomicOr(&brought[0], uint32_t(rows));
+            atomicOr(&brought[1], uint32_t(rows >> 32));
+        }
+    }
+    __syncthreads();
+    for (int r = 0; r < n; ++r)
+        if (!(brought[r >> 5] >> (r & 31) & 1))
+            for (int c = threadIdx.x; c < chunks; c += 256)
+                *reinterpret_cast<u32x4 *>(out + (int64_t(r0) + r) * stride + 8 * c) = u32x4{0, 0, 0, 0};
+}
+
 template <typename F>
 void with_shape(int fmt, int D, F f)
 {
@@ -1229,6 +1261,12 @@ AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows
         off += up256(size_t(c.score_blocks ? int64_t(S) * blocks : n_pages) * H * rows * KV_BLOCK * sizeof(float));
     c.bytes = off;                              // (the log-sums of many rows follow: they go by n_rows)
     return c;
+}
+
+hipError_t launch_kv_rest(const KvSeqs &s, uint16_t *out, int64_t out_stride, int width, hipStream_t st)
+{
+    launch_k(kv_rest_kernel, unsigned((s.n_rows + REST_ROWS - 1) / REST_ROWS), 256, 0, st, s, out, out_stride, width / 8);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st)

@@ -33,6 +33,7 @@ struct KvSeqs {
     const int32_t *lens;                    // [S]
     const int32_t *cu;                      // [S + 1]
     int S, max_blocks, n_rows, max_rows, max_len;
+    bool all_rows;                          // attention: a sequence has no more rows than tokens, other rows become zeros
 };
 
 // One sequence of a call: its rows [row0, row0 + n), its tokens [0, len).
