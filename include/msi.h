@@ -541,7 +541,8 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
 /* Attention of the rows over their sequences: row r of n sees the tokens up to
  * its own, t <= len - n + r; query head a reads head a / (n_q_heads / n_heads).
  * out = softmax(scale q k^T) v, zero for a row that sees no token (n > len is
- * allowed here).  With mass_rows > 0, mass[t] = mass_decay * mass[t] + the sum
+ * allowed here).  v may be anything the append takes, up to the largest bf16;
+ * the scores have to be numbers of fp32.  With mass_rows > 0, mass[t] = mass_decay * mass[t] + the sum
  * of the probabilities that the sequence's last mass_rows rows and the head's
  * query heads give token t, for every token (with mass_decay 0 the old value is
  * not read; a call with max_rows 0 does nothing).  Where it writes mass, no

@@ -79,6 +79,12 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? 
 // Rows are numbered row * G + head of the group within a sequence and cache head.
 __device__ __forceinline__ int row_limit(const KvSeq &q, int token_row) { return q.len - q.n + token_row + 1; }
 
+// The append takes every finite value, so V reaches the largest bf16 (scales up
+// to 2^122), and outputs are sums over up to 2^29 tokens of probabilities (up to
+// 2^7 with many rows) before they are divided: units' outputs are kept in units
+// of 2^40, which leaves those sums under 2^127.
+constexpr float V_LOG = 40.0f, V_DOWN = 0x1p-40f, V_UP = 0x1p40f;
+
 // ---------------------------------------------------------------- units
 //
 // The caches of a call are cut into units of about equally many blocks, sized
@@ -377,7 +383,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
         }
         F::load_k(cur.k, next, s1 % F::STEPS);                 // (the last step reads its own block again)
 
-        const float ks = (here ? sc.x : 0.0f) * A.scale_log2, vs = here ? sc.y : 0.0f;
+        const float ks = (here ? sc.x : 0.0f) * A.scale_log2, vs = here ? sc.y * V_DOWN : 0.0f;
         const bool tail = !here || t0 + TOK > q.len;
         if (tail) {                                            // bytes past the last token may be anything
 #pragma unroll
@@ -506,7 +512,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
                 A.part_ml[2 * part] = mx;
                 A.part_ml[2 * part + 1] = sum;
             }
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = sum == 0.0f ? 0.0f : V_UP / sum;
 #pragma unroll
             for (int k = 0; k < D / 64; ++k) {
                 const int e = (tid & 15) * 4 + 64 * k;
@@ -693,6 +699,31 @@ __device__ __forceinline__ void times_v(f32x16 (&acc)[D / 32], const bf16x8 (&pf
 }
 
 constexpr float NO_SCALE = 0x1p-126f;       // a scale of 0 counts as this (its logarithm is finite)
+// The exponent of a probability takes its block's V scale, and the rows' sums come from the same powers.  Up to V scales of
+// 2^60 that fits binary32 as it is.  From the first list of blocks with a larger one on, a wavefront goes over to units of
+// 2^40; blocks whose scale is under 2^-24 (vanishing V, zeros among them) then have their share of the rows' sums computed
+// by itself, since tokens below 2^-22 of the largest would be lost with scales of 2^-64.  Two sequences of 2041 and 3815
+// rows, heads of 256: 670 us, 667 without.
+constexpr float LARGE_V_LOG = 60.0f, LOW_V_LOG = -24.0f;
+
+// Running maximum and sum of a block's powers by themselves.
+__device__ __forceinline__ void add_low(const f32x16 (&sv)[2], float ks, float &m, float &l)
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            top = fmaxf(top, sv[x][v]);
+    const float m1 = fmaxf(m, across32(top, vmax) * ks), ref = m1 == -INFINITY ? 0.0f : m1;
+    l *= __builtin_amdgcn_exp2f(m - ref);
+    m = m1;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            l += __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -ref));
+}
 
 template <int FMT, int D>
 __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
@@ -746,10 +777,13 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
         for (int v = 0; v < 16; ++v)
             acc[c][v] = 0.0f;
     float m = -INFINITY, l = 0.0f;                          // m: reference of the exponents, a whole number
+    float m_low = -INFINITY, l_low = 0.0f;                  // maximum and sum of the low blocks
 
-    // page (-1: bad), K factor and log2 of the V scale of the 64 blocks from `list_at` on, one a lane
+    // page (-1: bad), K factor and log2 of the V scale in the present units of the 64 blocks from `list_at` on, one a lane;
+    // `lows`: those of low blocks
     int list_at = b0 - 64, pages = -1;
-    float kscale = 0.0f, vlog = 0.0f;
+    float kscale = 0.0f, vlog = 0.0f, v_units = 0.0f;
+    uint64_t lows = 0;
     const float factor = fabsf(A.scale_log2);
     auto make_list = [&](int b) {
         list_at = b;
@@ -766,6 +800,14 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
                 vlog = log2f(fmaxf(sc.y, NO_SCALE));         // whole for powers of two
             }
         }
+        if (v_units == 0.0f && __any(vlog > LARGE_V_LOG)) {
+            v_units = V_LOG;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                acc[c] *= V_DOWN;
+        }
+        lows = __ballot(v_units != 0.0f && vlog < LOW_V_LOG);
+        vlog -= v_units;
     };
     int next_pages = -1, next_at = b0;                      // pages of the copies, which run ahead of the list
     auto copy_list = [&](int b) {
@@ -828,12 +870,15 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kscale), b - list_at));
         const float vl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog), b - list_at));
         const bool here = __builtin_amdgcn_readlane(pages, b - list_at) >= 0;
-        if (!here || t0 + KV_BLOCK > least) {
+        const bool low = lows >> (b - list_at) & 1;
+        if (low || !here || t0 + KV_BLOCK > least) {
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
                     sv[x][v] = here && t0 + 32 * x + 8 * (v >> 2) + 4 * hf + (v & 3) < limit ? sv[x][v] : -INFINITY;
+            if (low)                                        // (in a branch of its own, further down: 689 to 722 us for 667)
+                add_low(sv, ks, m_low, l_low);
         }
         float top = -INFINITY;
 #pragma unroll
@@ -868,17 +913,19 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
                     bf16x8, u32x4{pack_bf16x2_hw(sv[x][8 * u], sv[x][8 * u + 1]), pack_bf16x2_hw(sv[x][8 * u + 2], sv[x][8 * u + 3]),
                                   pack_bf16x2_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16x2_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
         }
-        l = fmaf(sum, __builtin_amdgcn_exp2f(-vl), l);
+        l = fmaf(sum, low ? 0.0f : __builtin_amdgcn_exp2f(-vl), l);
         times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
     }
     __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));              // copies in flight write this workgroup's LDS
 
     // ---- lane (col, hf) holds elements 32 c + 8 (v / 4) + 4 hf + v % 4 of its row
     l = across32(l, vsum);
+    if (m_low != -INFINITY)                                 // (m followed these scores too: it is at most 2^6 behind)
+        l += across32(l_low, vsum) * __builtin_amdgcn_exp2f(m_low - m);
     if (r >= rows)
         return;
     const int tr = r / A.G, hd = r - tr * A.G;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : (v_units != 0.0f ? V_UP : 1.0f) / l, down = v_units != 0.0f ? 1.0f : V_DOWN;
     if (A.direct) {
         uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + 4 * hf;
 #pragma unroll
@@ -901,7 +948,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
                 *reinterpret_cast<f32x4 *>(A.part_o + part * D + 32 * c + 2 * v + 4 * hf) =
-                    f32x4{acc[c][v], acc[c][v + 1], acc[c][v + 2], acc[c][v + 3]};
+                    f32x4{acc[c][v] * down, acc[c][v + 1] * down, acc[c][v + 2] * down, acc[c][v + 3] * down};
     }
 }
 
@@ -960,7 +1007,7 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
             m = top;
         }
         const int tr = r / A.G, hd = r - tr * A.G;
-        o *= l == 0.0f ? 0.0f : 1.0f / l;
+        o *= l == 0.0f ? 0.0f : V_UP / l;
         *reinterpret_cast<uint2 *>(A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * A.c.D + e) =
             make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
         if (A.lse && e == 0)
@@ -995,7 +1042,7 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
             for (int k = 0; k < GROUPS; ++k)
                 sum += part[k * PIECE + tid];
             A.out[(int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * A.c.D + e0 + tid] =
-                f32_to_bf16(l == 0.0f ? 0.0f : sum / l);
+                f32_to_bf16(l == 0.0f ? 0.0f : sum / l * V_UP);
         }
         if (A.lse && tid == 0 && e0 == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = log_sum(top, l);

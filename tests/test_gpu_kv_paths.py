@@ -1,0 +1,65 @@
+"""Attention over the paged cache: batches and lengths that reach what the other tests' sizes do not (more than 64
+sequences, lists of pages that are read again, weights by four blocks at once), values at the ends of the range, and
+what a call leaves alone.  Bounds as in the oracle."""
+import numpy as np
+import pytest
+
+from _gpu_helpers import log
+from _kv_helpers import Setup
+from _kv_oracle import Cache
+from test_gpu_kv_attention import _check
+
+pytestmark = pytest.mark.gpu
+
+
+def _lens(g, n, most):
+    """Empty, one-token, short and cut sequences in turn."""
+    return [int(v) for v in np.where(np.arange(n) % 5 == 0, 0, np.where(np.arange(n) % 7 == 1, 1, g.integers(1, most, n)))]
+
+
+@pytest.mark.parametrize("fmt,scale", [("e4m3", 2.0 ** 119), ("int8", 2.0 ** 121)])
+@pytest.mark.parametrize("lens,rows", [([70, 200], [1, 3]), ([900], [1]), ([70, 300], [40, 33]), ([900], [40])])
+def test_values_at_the_ends_of_the_range(fmt, scale, lens, rows):
+    """V up to the largest bf16 (every finite value is accepted by the append) in blocks beside ones whose V is as
+    small as scales go: results are finite and right, one unit or several, few rows and many."""
+    import torch
+    log(f"case V at the range's ends {fmt} {lens} {rows}")
+    s = Setup(86 + sum(rows), lens, rows, 1, 64, fmt)
+    P = s.host.data.shape[0]
+    if fmt == "e4m3":
+        s.host.data[:, :, 1] = s.g.integers(0x70, 0x7F, s.host.data[:, :, 1].shape).astype(np.uint8)      # 128 .. 448
+    else:
+        s.host.data[:, :, 1] = s.g.integers(64, 128, s.host.data[:, :, 1].shape).astype(np.uint8)
+    s.host.scales[..., 1] = scale
+    small = [int(s.table[i, b]) for i in range(len(lens)) for b in range(1, -(-lens[i] // 64), 3)]
+    s.host.scales[small, :, 1] = 2.0 ** -64
+    assert P > len(small)
+    s.data.copy_(torch.from_numpy(s.host.data))
+    s.scales.copy_(torch.from_numpy(s.host.scales))
+    out = _check(s, s.seqs, s.table, s.lens, s.cu, 4)
+    assert torch.isfinite(out).all()
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4, mass_rows=50, decay=0.5)
+    # and with the small ones alone
+    s.host.scales[..., 1] = 2.0 ** -64
+    s.scales.copy_(torch.from_numpy(s.host.scales))
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_large_values_behind_others(rows):
+    """Blocks of ordinary and of vanishing V, then, past the first 64 blocks, some whose largest elements are at the
+    range's end while most of their elements are zero: the other elements' results are those of the ordinary blocks."""
+    import torch
+    log(f"case large V behind others rows={rows}")
+    s = Setup(89 + rows, [8530] + [3] * 51, [rows] + [1] * 51, 1, 64, "int8")
+    at = [int(p) for p in s.table[0, :134]]
+    for b in (70, 100, 131):
+        s.host.data[at[b], :, 1, :, 8:] = 0
+        s.host.scales[at[b], :, 1] = 2.0 ** 121
+    for b in (0, 5, 63, 64, 99, 101, 130, 133):
+        s.host.data[at[b], :, 1] = 0
+        s.host.scales[at[b], :, 1] = 2.0 ** -64
+    s.data.copy_(torch.from_numpy(s.host.data))
+    s.scales.copy_(torch.from_numpy(s.host.scales))
+    _check(s, s.seqs, s.table, s.lens, s.cu, 16)
+    _check(s, s.seqs, s.table, s.lens, s.cu, 16, mass_rows=5, decay=0.5)
