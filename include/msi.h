@@ -457,9 +457,9 @@ typedef enum { MSI_F32 = 0, MSI_BF16 = 1 } msi_dtype;
 typedef enum { MSI_ACT_NONE = 0, MSI_ACT_SILU = 1, MSI_ACT_GELU = 2, MSI_ACT_GELU_TANH = 3 } msi_activation;
 
 /* out[m, n] = act(sum_k x[m, k] w[n, k] + bias[n]) + residual[m, n].  GELU is z
- * Phi(z); GELU_TANH its form with tanh.  Sums, bias, activation and the
- * residual's addition in fp32, one rounding on the way out.  Strides are
- * elements from one row to the next; k is contiguous. */
+ * Phi(z), within (z^2 + 4) 2^-22 of itself; GELU_TANH its form with tanh.
+ * Sums, bias, activation and the residual's addition in fp32, one rounding on
+ * the way out.  Strides are elements from one row to the next; k is contiguous. */
 typedef struct {
     const void *x;               /* [M, K] bf16, x_stride >= K, a multiple of 8       */
     const void *w;               /* [N, K] bf16, row-major                             */

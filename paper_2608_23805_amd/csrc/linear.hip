@@ -10,10 +10,13 @@ namespace msi {
 namespace {
 
 // SiLU and the tanh form share z / (1 + e^-u) (u = z, or twice the tanh's
-// argument), with expf and a true division.  GELU takes Phi(-|z|) from erfc by
-// formula 7.1.26 of Abramowitz and Stegun, a polynomial in 1 / (1 + p x) times
-// e^-x^2 with an error under 1.5e-7 of erf, x = |z| / sqrt(2): a quarter of the
-// instructions of erff, and no cancellation for negative z.
+// argument), with expf and a true division.  GELU is max(z, 0) - |z| Phi(-|z|),
+// Phi(-x) = e^(-x^2 / 2) t P(t) with t = 1 / (1 + 0.35 x): P, of degree 8, is a
+// minimax fit of our own to the relative error (4.3e-8 over 0 <= x <= 14 with
+// its coefficients in fp32), so the negative tail is as good as the rest.  What
+// rounding adds stays under (z^2 + 4) 2^-22 of the value (z^2 2^-24 of it is
+// what a z rounded to fp32 leaves); over normal arguments 3.6e-8 of the root mean
+// square, 0.5 z (1 + erff) 3.8e-8.
 template <int ACT>
 __device__ __forceinline__ float activate(float z)
 {
@@ -22,14 +25,16 @@ __device__ __forceinline__ float activate(float z)
     } else if constexpr (ACT == LINEAR_GELU_TANH) {
         return z / (1.0f + expf(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
     } else if constexpr (ACT == LINEAR_GELU) {
-        const float x = fabsf(z) * 0.70710678118654752f;
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
-        float p = fmaf(1.061405429f, t, -1.453152027f);
-        p = fmaf(p, t, 1.421413741f);
-        p = fmaf(p, t, -0.284496736f);
-        p = fmaf(p, t, 0.254829592f);
-        const float q = 0.5f * p * t * __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);
-        return fmaxf(z, 0.0f) - fminf(fabsf(z), 3.0e38f) * q;
+        constexpr float P[9] = {0.13962140679359436f, 0.13986186683177948f, 0.11983285844326019f, 0.10550802946090698f,
+                                -0.02310989610850811f, 0.15917424857616425f, -0.2557143270969391f, 0.1439717411994934f,
+                                -0.029145939275622368f};
+        const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.35f, x, 1.0f));
+        float p = P[8];
+#pragma unroll
+        for (int i = 7; i >= 0; --i)
+            p = fmaf(p, t, P[i]);
+        const float q = p * t * __builtin_amdgcn_exp2f(-0.72134752044448170f * (z * z));
+        return fmaf(-fminf(x, 3.0e38f), q, fmaxf(z, 0.0f));
     } else {
         return z;
     }
