@@ -579,7 +579,8 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
  * dst_table [n_seqs, dst_blocks], which no sequence of the call may hold, with
  * their mass, coded again by blocks of 64 as an append to empty pages would;
  * new_lens[i] = min(lens[i], budget); keep [n_seqs, n_heads, budget] gets the
- * kept indices, then -1.  A sequence within its budget is copied whole.
+ * kept indices, then -1.  A sequence within its budget is copied whole; one that
+ * breaks a bound is left out, its entries of new_lens and keep as they were.
  * cu_rows is not read.  Tokens of a page outside the pool are kept last, as
  * zeros.  Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 typedef struct {

@@ -221,8 +221,11 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv_select_kernel(KvCache c, Kv
     const int h = blockIdx.x, i = blockIdx.y, share = blockIdx.z, shares = gridDim.z;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvSeq q = kv_seq(s, i, false);
-    if (!q.ok && tid == 0)
-        kv_raise(status, KV_BAD_LENGTH);
+    if (!q.ok) {                                           // left out: its new length and indices stay as they were
+        if (tid == 0)
+            kv_raise(status, KV_BAD_LENGTH);
+        return;
+    }
     const int len = q.len, kept = min(len, budget);
     int32_t *out = keep + (int64_t(i) * c.H + h) * budget;
     if (h == 0 && share == 0 && tid == 0)

@@ -63,3 +63,25 @@ def test_large_values_behind_others(rows):
     s.scales.copy_(torch.from_numpy(s.host.scales))
     _check(s, s.seqs, s.table, s.lens, s.cu, 16)
     _check(s, s.seqs, s.table, s.lens, s.cu, 16, mass_rows=5, decay=0.5)
+
+
+def test_eviction_leaves_a_broken_sequence_out():
+    """A sequence whose length breaks its bound keeps its entries of new_lens and keep, and its pages; the others are cut."""
+    import torch
+    import paper_2608_23805_amd as msi
+    from _kv_oracle import evict
+    log("case eviction, broken length")
+    for wrong in (201, -1, 2 ** 31 - 1):
+        s = Setup(88, [200, 150, 90], [0, 0, 0], 2, 64, "e4m3", dst_lens=[100, 100, 90])
+        seqs = s.make_seqs(s.table, s.lens, s.cu, max_len=200)
+        seqs.lens[1] = wrong
+        keep = torch.full((3, 2, 100), 77, dtype=torch.int32, device="cuda")
+        new = torch.full((3,), 77, dtype=torch.int32, device="cuda")
+        msi.kv_evict(s.cache, seqs, torch.from_numpy(s.dst).cuda(), new, keep, budget=100, sinks=4, recent=10, status=s.status)
+        host = Cache(s.host.data, s.host.scales, s.host.mass, "e4m3")
+        want = evict(host, [s.table[0], s.table[2]], [200, 90], [s.dst[0], s.dst[2]], 100, 4, 10)
+        data, scales, mass, st = s.device_state()
+        assert st == 4 and new.tolist() == [100, 77, 90]
+        k = keep.cpu().numpy()
+        assert np.array_equal(k[0], want[0]) and np.array_equal(k[2], want[1]) and np.all(k[1] == 77)
+        assert np.array_equal(data, host.data) and np.array_equal(scales, host.scales) and np.array_equal(mass, host.mass)
