@@ -82,6 +82,18 @@ def _matrix(name: str, t, M: int, N: int, device, dtypes) -> int:
 
 
 _ANY = _BF16 + (_F32,)
+_F32_MOST = torch.finfo(_F32).max
+
+
+def _scale(scale: float):
+    """The factor of the scores: as a power of two's exponent it has to be a number of fp32."""
+    if not abs(scale) * 1.4426950408889634 <= _F32_MOST:
+        _refuse(f"scale must be finite, under 2^127, got {scale}")
+
+
+def _decay(mass_decay: float):
+    if not 0.0 <= mass_decay <= _F32_MOST:
+        _refuse(f"mass_decay must be finite in fp32 and not negative, got {mass_decay}")
 
 
 def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
@@ -229,6 +241,9 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
         _refuse("q must be [n_rows, n_q_heads, head_dim]")
     if mass_rows < 0:
         _refuse("mass_rows must not be negative")
+    _scale(scale)
+    if mass_rows:
+        _decay(mass_decay)
     Hq, dev = q.shape[1], cache.device
     qs, os_ = _rows(cache, seqs, "q", q, Hq), _rows(cache, seqs, "out", out, Hq)
     wp = wn = 0
@@ -241,8 +256,8 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
         c.flags |= KV_ALL_ROWS
         ref = ctypes.byref(c)
     _call(dev, lib.msi_kv_attention, cache._ref, ref,
-          _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30), mass_decay, wp,
-                               wn, _status(status, dev)), _stream(stream))
+          _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30),
+                               mass_decay if mass_rows else 0.0, wp, wn, _status(status, dev)), _stream(stream))
 
 
 def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget: int, sinks: int = 0, recent: int = 0,
@@ -275,12 +290,20 @@ class AttentionBlock:
     brings, and those of a sequence that breaks a bound or has more rows than tokens, get nothing added to h."""
 
     def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None):
-        D, H = cache.head_dim, cache.n_heads
-        if wqkv.shape[0] != (n_q_heads + 2 * H) * D or wo.shape != (wqkv.shape[1], n_q_heads * D):
-            _refuse("wqkv must be [(n_q_heads + 2 n_kv_heads) head_dim, d], wo [d, n_q_heads head_dim]")
+        D, H, dev = cache.head_dim, cache.n_heads, cache.device
+        if n_q_heads < 1 or n_q_heads % H:
+            _refuse("n_q_heads must be a multiple of the cache's n_heads")
+        if wqkv.dim() != 2 or wqkv.shape[1] < 8 or wqkv.shape[1] % 8:
+            _refuse("wqkv must be a matrix whose rows are a multiple of 8")
+        for name, t, shape in (("wqkv", wqkv, ((n_q_heads + 2 * H) * D, wqkv.shape[1])), ("wo", wo, (wqkv.shape[1], n_q_heads * D))):
+            _dense(name, t, t.dtype if t.dtype in _BF16 else torch.bfloat16, dev, shape)
+        if bias is not None:
+            _dense("bias", bias, _F32, dev, (wqkv.shape[0],))
+        if max_rows < 0:
+            _refuse("max_rows must not be negative")
         self.wqkv, self.wo, self.bias, self.cache, self.n_q_heads = wqkv, wo, bias, cache, n_q_heads
         self.scale = D ** -0.5 if scale is None else scale
-        dev = cache.device
+        _scale(self.scale)
         self.qkv = torch.empty((max_rows, n_q_heads + 2 * H, D), dtype=torch.bfloat16, device=dev)
         self.attn = torch.empty((max_rows, n_q_heads, D), dtype=torch.bfloat16, device=dev)
         self.out = torch.empty((max_rows, wo.shape[0]), dtype=_F32, device=dev)
@@ -302,12 +325,17 @@ class AttentionBlock:
             self._settle()
 
     def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None):
-        """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place."""
+        """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place.  What is refused is
+        refused before the cache, x or h change."""
         n, Hq, H = seqs.n_rows, self.n_q_heads, self.cache.n_heads
         if n > self.qkv.shape[0]:
             _refuse(f"{n} rows, buffers for {self.qkv.shape[0]}")
-        _dense("x", x, x.dtype, self.cache.device, (n, self.wqkv.shape[1]))
+        _same_device(self.cache, seqs)
+        _dense("x", x, x.dtype if x.dtype in _BF16 else torch.bfloat16, self.cache.device, (n, self.wqkv.shape[1]))
         _dense("h", h, _F32, self.cache.device, (n, self.wqkv.shape[1]))
+        _status(status, self.cache.device)
+        if mass_rows:
+            _decay(mass_decay)
         need = kv_attention_workspace_size(self.cache, seqs, Hq, mass_rows)
         if need > (0 if self.workspace is None else self.workspace.numel()):
             raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step")

@@ -206,6 +206,8 @@ msi_status msi_kv_attention_workspace(const msi_kv_cache *cache, const msi_kv_se
         return bad(e);
     if (const char *e = check_heads(c, s, n_q_heads))
         return bad(e);
+    if (mass_rows && !c.mass)
+        return bad("mass_rows needs the cache's mass");
     *bytes = 0;
     if (s.S && s.max_rows) {
         const AttentionCut cut = attention_cut(s.S, c.H, int(n_q_heads) / c.H, c.D, c.n_pages, s.max_rows, s.max_len, mass_rows != 0);

@@ -36,3 +36,50 @@ def test_sequence_flags():
     for flags in (2, 1 << 31):
         _refused(msi.lib.msi_kv_attention_workspace(ctypes.byref(_cache()), ctypes.byref(_seqs(flags=flags)), 4, 0, ctypes.byref(n)), "flags")
     assert msi.lib.msi_kv_attention_workspace(ctypes.byref(_cache()), ctypes.byref(_seqs(flags=1)), 4, 0, ctypes.byref(n)) == 0
+
+
+def test_workspace_of_weights_needs_them():
+    import paper_2608_23805_amd as msi
+    n = ctypes.c_uint64()
+    _refused(msi.lib.msi_kv_attention_workspace(ctypes.byref(_cache(mass=0)), ctypes.byref(_seqs()), 4, 1, ctypes.byref(n)), "mass")
+    assert msi.lib.msi_kv_attention_workspace(ctypes.byref(_cache(mass=0)), ctypes.byref(_seqs()), 4, 0, ctypes.byref(n)) == 0
+
+
+def test_block_construction_refusals():
+    """What a step would trip over after it has written the cache is refused when the block is made."""
+    import paper_2608_23805_amd as msi
+    import torch
+    for over in (dict(wqkv=_w(512, 128).float()), dict(wo=_w(128, 256).float()), dict(wqkv=_w(128, 512).t()),
+                 dict(wo=_w(256, 128).t()), dict(wqkv=_w(520, 128)), dict(wo=_w(256, 128)), dict(bias=torch.zeros(511)),
+                 dict(bias=_w(512)), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=3e38), dict(n_q_heads=3),
+                 dict(n_q_heads=0), dict(wqkv=_w(512, 100), wo=_w(100, 256)), dict(max_rows=-1), dict(wqkv=_w(512))):
+        with pytest.raises(msi.MsiError) as e:
+            _block(**over)
+        assert e.value.status == msi.MSI_E_INVALID_ARG, over
+
+
+def test_block_step_refusals():
+    """Refusals that need no device come before the first call that does."""
+    import paper_2608_23805_amd as msi
+    import torch
+    x, h, s = _w(4, 128), torch.zeros((4, 128)), _cpu_seqs()
+    for match, b, a, kw in (("mass", _block(mass=False), (x, h, s), dict(mass_rows=1)),
+                            ("mass_decay", _block(), (x, h, s), dict(mass_rows=1, mass_decay=-0.5)),
+                            ("mass_decay", _block(), (x, h, s), dict(mass_rows=1, mass_decay=float("nan"))),
+                            ("mass_decay", _block(), (x, h, s), dict(mass_rows=1, mass_decay=1e39)),
+                            ("mass_rows", _block(), (x, h, s), dict(mass_rows=-1)),
+                            ("x must", _block(), (x.float(), h, s), {}), ("h must", _block(), (x, h.double(), s), {}),
+                            ("h must", _block(), (x, h[:3], s), {}), ("status", _block(), (x, h, s), dict(status=x)),
+                            ("rows", _block(max_rows=3), (x, h, s), {})):
+        with pytest.raises(msi.MsiError, match=match):
+            b.step(*a, **kw)
+
+
+def test_scales_that_no_float_holds():
+    """A scale or decay past fp32's range is refused like one that is infinite."""
+    import paper_2608_23805_amd as msi
+    s = _cpu_seqs()
+    for kw in (dict(scale=1e39), dict(scale=1.0, mass_rows=1, mass_decay=1e39), dict(scale=-1e300)):
+        with pytest.raises(msi.MsiError) as e:
+            msi.kv_attention(_cpu_cache(), s, _w(4, 4, 64), _w(4, 4, 64), **kw)
+        assert e.value.status == msi.MSI_E_INVALID_ARG

@@ -164,3 +164,23 @@ def test_many_sequences_answer_for_their_rows():
     torch.cuda.synchronize()
     zero = (out == 0).all(-1).all(-1).cpu().numpy()
     assert np.array_equal(zero, np.arange(S) % 11 == 0)
+
+
+def test_refusals_come_before_any_effect():
+    """What a step refuses, it refuses before the cache, the rows or the weights change."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case block, refusals")
+    s = Setup(97, [100, 60], [1, 1], H, D, "e4m3")
+    bare = Setup(97, [100, 60], [1, 1], H, D, "e4m3", mass=False)
+    for t, kw in ((bare, dict(mass_rows=1)), (s, dict(mass_rows=1, mass_decay=-1.0)),
+                  (s, dict(mass_rows=1, mass_decay=float("inf"))), (s, dict(mass_rows=-1))):
+        b = _block(t, 4)
+        b.workspace = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        x, h = _rows(2, 5)
+        x0, h0, before = x.clone(), h.clone(), t.device_state()
+        with pytest.raises(msi.MsiError):
+            b.step(x, h, t.seqs, status=t.status, **kw)
+        after = t.device_state()
+        assert torch.equal(x, x0) and torch.equal(h, h0)
+        assert np.array_equal(before[0], after[0]) and np.array_equal(before[1], after[1]) and after[3] == 0
