@@ -340,11 +340,11 @@ class AttentionBlock:
         if need > (0 if self.workspace is None else self.workspace.numel()):
             raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step")
         qkv, attn, out = self.qkv[:n], self.attn[:n], self.out[:n]
-        linear(x, self.wqkv, qkv.view(n, -1), bias=self.bias, stream=stream)
+        linear(x, self.wqkv, qkv.view(n, self.wqkv.shape[0]), bias=self.bias, stream=stream)
         kv_append(self.cache, seqs, qkv[:, Hq:Hq + H], qkv[:, Hq + H:], status=status, stream=stream)
         kv_attention(self.cache, seqs, qkv[:, :Hq], attn, self.scale, mass_rows=mass_rows, mass_decay=mass_decay,
                      workspace=self.workspace, status=status, stream=stream, all_rows=True)
-        linear(attn.view(n, -1), self.wo, out, stream=stream)
+        linear(attn.view(n, self.wo.shape[1]), self.wo, out, stream=stream)
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
                   _stream(stream))

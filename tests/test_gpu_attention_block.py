@@ -166,6 +166,21 @@ def test_many_sequences_answer_for_their_rows():
     assert np.array_equal(zero, np.arange(S) % 11 == 0)
 
 
+def test_step_without_rows():
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case block, no rows")
+    s = Setup(96, [100, 0], [0, 0], H, D, "int8")
+    b = _block(s, 4)
+    seqs = _seqs(s, s.table, s.lens, s.cu, 0, 0, max_len=128)
+    b.reserve(seqs, 1)
+    x, h = _rows(0, 4)
+    before = s.device_state()
+    b.step(x, h, seqs, mass_rows=1, status=s.status)
+    after = s.device_state()
+    assert all(np.array_equal(a, c) for a, c in zip(before, after))
+
+
 def test_refusals_come_before_any_effect():
     """What a step refuses, it refuses before the cache, the rows or the weights change."""
     import torch
