@@ -75,6 +75,8 @@ def _matrix(name: str, t, M: int, N: int, device, dtypes) -> int:
     if t.shape != (M, N) or t.dtype not in dtypes or t.device != device:
         _refuse(f"{name} must be [{M}, {N}] {' or '.join(map(str, dtypes))} on {device}, "
                 f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if M == 0:
+        return (N + 7) // 8 * 8              # (a tensor without elements may have any strides)
     rs, cs = t.stride()
     if (cs != 1 and N > 1) or (rs < N and M > 1):
         _refuse(f"{name}: rows must be contiguous in themselves and must not overlap")
@@ -187,6 +189,8 @@ def _rows(cache: KvCache, seqs: KvSeqs, name: str, t, heads: int) -> int:
     if t.shape != (n, heads, D) or t.dtype not in _BF16 or t.device != cache.device:
         _refuse(f"{name} must be [{n}, {heads}, {D}] bf16 (or its bits in int16) on {cache.device}, "
                 f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if n == 0:
+        return heads * D
     rs, hs, ds = t.stride()
     if ds != 1 or (hs != D and heads > 1) or (rs < heads * D and n > 1):
         _refuse(f"{name}: rows must be contiguous in themselves and must not overlap")

@@ -83,3 +83,17 @@ def test_scales_that_no_float_holds():
         with pytest.raises(msi.MsiError) as e:
             msi.kv_attention(_cpu_cache(), s, _w(4, 4, 64), _w(4, 4, 64), **kw)
         assert e.value.status == msi.MSI_E_INVALID_ARG
+
+
+def test_tensors_without_elements():
+    """A tensor of no rows may have any strides: only its shape counts."""
+    import paper_2608_23805_amd as msi
+    import torch
+    empty = torch.empty_strided((0, 16), (1, 1), dtype=torch.bfloat16)
+    rows = torch.empty_strided((0, 2, 64), (1, 1, 1), dtype=torch.bfloat16)
+    s = _cpu_seqs(n_rows=0, max_rows=0)
+    for f, a in ((msi.linear, (empty, _w(8, 16), torch.empty_strided((0, 8), (1, 1), dtype=torch.bfloat16))),
+                 (msi.kv_append, (_cpu_cache(), s, rows, rows)), (msi.kv_read, (_cpu_cache(), s, rows, rows)),
+                 (msi.kv_attention, (_cpu_cache(), s, rows, rows, 1.0))):
+        with pytest.raises(msi.MsiError, match="HIP device"):          # (and no complaint about strides)
+            f(*a)
