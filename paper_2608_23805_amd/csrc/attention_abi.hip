@@ -73,10 +73,14 @@ bool rows_ok(const void *p, uint64_t stride, uint64_t least)
     return p && aligned(p, 16) && stride >= least && stride % 8 == 0 && stride <= MOST_STRIDE;
 }
 
+constexpr const char *STATUS_TEXT = "status must be a 4-byte aligned word";
+
 // what append and read have in common; go: there is work
 const char *view_rows(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v, uint64_t ks,
-                      uint64_t vs, KvCache &c, KvSeqs &s, bool &go)
+                      uint64_t vs, const uint32_t *status, KvCache &c, KvSeqs &s, bool &go)
 {
+    if (!aligned(status, 4))
+        return STATUS_TEXT;
     if (const char *e = view_cache(cache, c))
         return e;
     if (const char *e = view_seqs(seqs, true, s))
@@ -170,7 +174,7 @@ msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, con
     KvCache c;
     KvSeqs s;
     bool go = false;
-    if (const char *e = view_rows(cache, seqs, k, v, k_stride, v_stride, c, s, go))
+    if (const char *e = view_rows(cache, seqs, k, v, k_stride, v_stride, status, c, s, go))
         return bad(e);
     if (!go)
         return MSI_OK;
@@ -185,7 +189,7 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
     KvCache c;
     KvSeqs s;
     bool go = false;
-    if (const char *e = view_rows(cache, seqs, k, v, k_stride, v_stride, c, s, go))
+    if (const char *e = view_rows(cache, seqs, k, v, k_stride, v_stride, status, c, s, go))
         return bad(e);
     if (!go)
         return MSI_OK;
@@ -232,6 +236,8 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     const float scale_log2 = float(double(a->scale) * 1.4426950408889634);
     if (!std::isfinite(scale_log2))
         return bad("scale must be finite, under 2^127");
+    if (!aligned(a->status, 4))
+        return bad(STATUS_TEXT);
     if (a->mass_rows && !c.mass)
         return bad("mass_rows needs the cache's mass");
     if (a->mass_rows && !(a->mass_decay >= 0.0f && std::isfinite(a->mass_decay)))
@@ -298,6 +304,8 @@ msi_status msi_kv_evict(const msi_kv_cache *cache, const msi_kv_seqs *seqs, cons
         return bad(e);
     if (const char *e = view_seqs(seqs, false, s))
         return bad(e);
+    if (!aligned(a->status, 4))
+        return bad(STATUS_TEXT);
     if (!c.mass)
         return bad("eviction needs the cache's mass");
     if (a->budget < 1 || a->budget > MOST || uint64_t(a->sinks) + a->recent > a->budget)

@@ -30,6 +30,18 @@ def _block(mass=True, **over):
     return msi.AttentionBlock(**kw)
 
 
+def test_status_words_are_aligned():
+    """A status word between two words would be an atomic at an address that has none."""
+    import paper_2608_23805_amd as msi
+    c, s = ctypes.byref(_cache()), ctypes.byref(_seqs(max_rows=1, max_len=100))
+    for f in (msi.lib.msi_kv_append, msi.lib.msi_kv_read):
+        _refused(f(c, s, P, P, 128, 128, P + 2, None), "status")
+    a = msi.msi_kv_attention_args(q=P, out=2 * P, q_stride=256, out_stride=256, n_q_heads=4, scale=1.0, status=P + 1)
+    _refused(msi.lib.msi_kv_attention(c, s, ctypes.byref(a), None), "status")
+    e = msi.msi_kv_evict_args(budget=100, sinks=4, recent=10, dst_blocks=2, dst_table=2 * P, new_lens=3 * P, keep=4 * P, status=P + 3)
+    _refused(msi.lib.msi_kv_evict(c, s, ctypes.byref(e), None), "status")
+
+
 def test_sequence_flags():
     import paper_2608_23805_amd as msi
     n = ctypes.c_uint64()
