@@ -288,10 +288,10 @@ class AttentionBlock:
 
         q, k, v = x wqkv^T + bias;  append k, v;  a = attention(q);  h += a wo^T;  x = bf16(rmsnorm(h))
 
-    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  Holds the
-    buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace.  Steps allocate nothing and
-    can be captured; those of one block share its buffers, so they must not overlap.  Rows below n_rows that no sequence
-    brings, and those of a sequence that breaks a bound or has more rows than tokens, get nothing added to h."""
+    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
+    in.  Steps allocate nothing and can be captured; those of one block share its buffers, so they must not overlap.  Rows
+    below n_rows that no sequence brings, and those of a sequence that breaks a bound or has more rows than tokens, get
+    nothing added to h."""
 
     def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None):
         D, H, dev = cache.head_dim, cache.n_heads, cache.device
@@ -321,34 +321,61 @@ class AttentionBlock:
             torch.cuda.current_stream(self.cache.device).synchronize()
 
     def reserve(self, seqs: KvSeqs, mass_rows: int = 0):
-        """Workspace for steps with these bounds (of the largest ones asked for so far)."""
+        """Workspace for steps with these bounds (of the largest ones asked for so far).  Captured steps go on using the one
+        they were captured with, so earlier ones are kept; each is at least twice the one before."""
         need = kv_attention_workspace_size(self.cache, seqs, self.n_q_heads, mass_rows)
-        if self.workspace is None or self.workspace.numel() < need:
-            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.cache.device)
+        have = 0 if self.workspace is None else self.workspace.numel()
+        if self.workspace is None or have < need:
+            self.workspace = torch.empty(max(need, 2 * have), dtype=torch.uint8, device=self.cache.device)
             self._kept.append(self.workspace)
             self._settle()
 
-    def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None):
-        """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place.  What is refused is
-        refused before the cache, x or h change."""
-        n, Hq, H = seqs.n_rows, self.n_q_heads, self.cache.n_heads
-        if n > self.qkv.shape[0]:
-            _refuse(f"{n} rows, buffers for {self.qkv.shape[0]}")
+    def _check_x(self, x, seqs: KvSeqs):
+        if seqs.n_rows > self.qkv.shape[0]:
+            _refuse(f"{seqs.n_rows} rows, buffers for {self.qkv.shape[0]}")
         _same_device(self.cache, seqs)
-        _dense("x", x, x.dtype if x.dtype in _BF16 else torch.bfloat16, self.cache.device, (n, self.wqkv.shape[1]))
-        _dense("h", h, _F32, self.cache.device, (n, self.wqkv.shape[1]))
-        _status(status, self.cache.device)
+        _dense("x", x, x.dtype if x.dtype in _BF16 else torch.bfloat16, self.cache.device, (seqs.n_rows, self.wqkv.shape[1]))
+
+    def _check_rest(self, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, status, workspace):
+        """The workspace of a step whose other arguments are right."""
+        dev = self.cache.device
+        _dense("h", h, _F32, dev, (seqs.n_rows, self.wqkv.shape[1]))
+        _status(status, dev)
         if mass_rows:
             _decay(mass_decay)
-        need = kv_attention_workspace_size(self.cache, seqs, Hq, mass_rows)
-        if need > (0 if self.workspace is None else self.workspace.numel()):
-            raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step")
-        qkv, attn, out = self.qkv[:n], self.attn[:n], self.out[:n]
+        need = kv_attention_workspace_size(self.cache, seqs, self.n_q_heads, mass_rows)
+        if workspace is None:
+            workspace = self.workspace
+        else:
+            _dense("workspace", workspace, torch.uint8, dev)
+            if workspace.data_ptr() % 16:
+                _refuse("workspace must be 16-byte aligned")
+        if need > (0 if workspace is None else workspace.numel()):
+            raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step, or a workspace of "
+                                        f"{need} bytes is handed in")
+        return workspace
+
+    def _project(self, x, n: int, stream):
+        qkv = self.qkv[:n]
         linear(x, self.wqkv, qkv.view(n, self.wqkv.shape[0]), bias=self.bias, stream=stream)
+        return qkv
+
+    def _attend(self, x, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, workspace, status, stream):
+        n, Hq, H = seqs.n_rows, self.n_q_heads, self.cache.n_heads
+        qkv, attn, out = self.qkv[:n], self.attn[:n], self.out[:n]
         kv_append(self.cache, seqs, qkv[:, Hq:Hq + H], qkv[:, Hq + H:], status=status, stream=stream)
         kv_attention(self.cache, seqs, qkv[:, :Hq], attn, self.scale, mass_rows=mass_rows, mass_decay=mass_decay,
-                     workspace=self.workspace, status=status, stream=stream, all_rows=True)
+                     workspace=workspace, status=status, stream=stream, all_rows=True)
         linear(attn.view(n, self.wo.shape[1]), self.wo, out, stream=stream)
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
                   _stream(stream))
+
+    def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None):
+        """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place.  What is refused is
+        refused before the cache, x or h change.  ``workspace`` (uint8, kv_attention_workspace_size bytes) takes the place of
+        the block's own: blocks whose steps run one after another can share one."""
+        self._check_x(x, seqs)
+        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace)
+        self._project(x, seqs.n_rows, stream)
+        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream)

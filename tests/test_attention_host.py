@@ -97,6 +97,18 @@ def test_scales_that_no_float_holds():
         assert e.value.status == msi.MSI_E_INVALID_ARG
 
 
+def test_growing_bounds_do_not_pile_up_workspaces():
+    """Captured steps go on using the workspace they were captured with, so a block keeps each; growing bounds must not
+    make that a sum over every size."""
+    import paper_2608_23805_amd as msi
+    b = _block()
+    for blocks in range(9, 200):
+        s = _cpu_seqs(max_len=64 * blocks, n_rows=2, max_rows=1)
+        b.reserve(s, 1)
+        assert b.workspace.numel() >= msi.kv_attention_workspace_size(b.cache, s, 4, 1)
+    assert sum(w.numel() for w in b._kept) <= 4 * msi.kv_attention_workspace_size(b.cache, s, 4, 1)
+
+
 def test_tensors_without_elements():
     """A tensor of no rows may have any strides: only its shape counts."""
     import paper_2608_23805_amd as msi

@@ -199,3 +199,27 @@ def test_refusals_come_before_any_effect():
         after = t.device_state()
         assert torch.equal(x, x0) and torch.equal(h, h0)
         assert np.array_equal(before[0], after[0]) and np.array_equal(before[1], after[1]) and after[3] == 0
+
+
+def test_blocks_that_share_a_workspace():
+    """Blocks of one stream with one workspace handed in, and one that is too small."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case block, shared workspace")
+    pairs = [(Setup(99, [900, 600], [1, 1], H, D, "int8"), Setup(99, [900, 600], [1, 1], H, D, "int8")) for _ in "ab"]
+    ws = None
+    for k, (s, t) in enumerate(pairs):
+        x, h = _rows(2, 7 + k)
+        x2, h2 = x.clone(), h.clone()
+        b, c = _block(s, 2, k), _block(t, 2, k)
+        if ws is None:
+            ws = msi.kv_attention_workspace(s.cache, s.seqs, HQ, 1)
+        b.step(x, h, s.seqs, mass_rows=1, workspace=ws)
+        c.reserve(t.seqs, 1)
+        c.step(x2, h2, t.seqs, mass_rows=1)
+        torch.cuda.synchronize()
+        assert torch.equal(x, x2) and torch.equal(h, h2) and b.workspace is None
+        with pytest.raises(msi.MsiError) as e:
+            b.step(x, h, s.seqs, mass_rows=1, workspace=ws[:-256])
+        assert e.value.status == msi.MSI_E_NOMEM
+        assert torch.equal(x, x2) and torch.equal(h, h2)
