@@ -288,7 +288,9 @@ class AttentionBlock:
 
         q, k, v = x wqkv^T + bias;  append k, v;  a = attention(q);  h += a wo^T;  x = bf16(rmsnorm(h))
 
-    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
+    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  ``step`` runs
+    it whole; ``project`` and ``attend`` are its halves, for a model that rotates or normalises queries and keys between
+    them.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
     in.  Steps allocate nothing and can be captured; those of one block share its buffers, so they must not overlap.  Rows
     below n_rows that no sequence brings, and those of a sequence that breaks a bound or has more rows than tokens, get
     nothing added to h."""
@@ -370,6 +372,18 @@ class AttentionBlock:
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
                   _stream(stream))
+
+    def project(self, x, seqs: KvSeqs, stream=None):
+        """First half: queries, keys and values of the rows x, [n_rows, n_q_heads + 2 n_kv_heads, head_dim] bf16 in the block's
+        buffer, where the caller may change them (on ``stream``) before ``attend``."""
+        self._check_x(x, seqs)
+        return self._project(x, seqs.n_rows, stream)
+
+    def attend(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None):
+        """Second half, with what ``project`` left: appends, attends, and updates h and x as a step does."""
+        self._check_x(x, seqs)
+        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace)
+        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream)
 
     def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None):
         """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place.  What is refused is

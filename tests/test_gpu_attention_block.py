@@ -201,6 +201,50 @@ def test_refusals_come_before_any_effect():
         assert np.array_equal(before[0], after[0]) and np.array_equal(before[1], after[1]) and after[3] == 0
 
 
+def test_work_between_the_halves():
+    """project, the caller's own change of queries and keys, attend: the same as the operators called one by one."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case block, halves")
+    s, t, u = (Setup(98, [100, 60], [2, 1], H, D, "e4m3") for _ in "abc")
+    x, h = _rows(3, 6)
+    x1, h1, x2, h2, x3, h3 = (v.clone() for v in (x, h, x, h, x, h))
+    # without a change: a step
+    b = _block(s, 4)
+    b.reserve(s.seqs, 1)
+    b.step(x, h, s.seqs, mass_rows=1)
+    c = _block(t, 4)
+    c.reserve(t.seqs, 1)
+    qkv = c.project(x1, t.seqs)
+    assert qkv.shape == (3, HQ + 2 * H, D)
+    c.attend(x1, h1, t.seqs, mass_rows=1)
+    torch.cuda.synchronize()
+    assert torch.equal(x, x1) and torch.equal(h, h1)
+    assert all(np.array_equal(a, e) for a, e in zip(s.device_state(), t.device_state()))
+    # with one: halves of every head's elements exchanged
+    t2 = Setup(98, [100, 60], [2, 1], H, D, "e4m3")
+    c = _block(t2, 4)
+    c.reserve(t2.seqs, 1)
+    qk = c.project(x2, t2.seqs)[:, :HQ + H]
+    qk.copy_(torch.cat((-qk[..., D // 2:], qk[..., :D // 2]), -1))
+    c.attend(x2, h2, t2.seqs, mass_rows=1)
+    wqkv, wo = _weights(1)
+    qkv = torch.empty((3, HQ + 2 * H, D), dtype=torch.bfloat16, device="cuda")
+    msi.linear(x3, wqkv, qkv.view(3, -1))
+    qk = qkv[:, :HQ + H]
+    qk.copy_(torch.cat((-qk[..., D // 2:], qk[..., :D // 2]), -1))
+    msi.kv_append(u.cache, u.seqs, qkv[:, HQ:HQ + H], qkv[:, HQ + H:])
+    a = torch.empty((3, HQ, D), dtype=torch.bfloat16, device="cuda")
+    msi.kv_attention(u.cache, u.seqs, qkv[:, :HQ], a, D ** -0.5, mass_rows=1,
+                     workspace=msi.kv_attention_workspace(u.cache, u.seqs, HQ, 1))
+    o = torch.empty((3, WIDTH), device="cuda")
+    msi.linear(a.view(3, -1), wo, o)
+    msi.residual_add(o, h3, x3)
+    torch.cuda.synchronize()
+    assert torch.equal(x2, x3) and torch.equal(h2, h3) and not torch.equal(h2, h)
+    assert all(np.array_equal(p, e) for p, e in zip(t2.device_state(), u.device_state()))
+
+
 def test_blocks_that_share_a_workspace():
     """Blocks of one stream with one workspace handed in, and one that is too small."""
     import torch
