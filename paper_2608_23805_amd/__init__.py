@@ -9,6 +9,7 @@ fallback).
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence, Tuple
@@ -170,9 +171,19 @@ class MsiError(RuntimeError):
         self.status = status
 
 
+def _load_hip():
+    """torch brings a HIP runtime of its own and a process can use one only: libmsi.so takes the one that is loaded
+    already, so torch's is loaded first, also where torch itself is imported later."""
+    torch = importlib.util.find_spec("torch")
+    path = os.path.join(os.path.dirname(torch.origin), "lib", "libamdhip64.so") if torch and torch.origin else ""
+    if os.path.exists(path):
+        ctypes.CDLL(path)
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() first")
+    _load_hip()
     L = ctypes.CDLL(LIB_PATH)
     P = ctypes.POINTER
     L.msi_last_error.restype = ctypes.c_char_p
