@@ -627,6 +627,10 @@ msi_status msi_debug_source_release(msi_plan *plan);
 /* Test hook: overwrite one slot's device generation word (synchronously). */
 msi_status msi_debug_set_device_gen(msi_plan *plan, uint32_t layer, uint32_t slot, uint32_t gen);
 
+/* For tests: the tiles that msi_linear cuts M rows and N features into (rows and
+ * features of a workgroup, workgroups that share a CU).  Errors: MSI_E_INVALID_ARG. */
+msi_status msi_debug_linear_tile(uint32_t M, uint32_t N, uint32_t *rows, uint32_t *features, uint32_t *per_cu);
+
 /* Expert-path selector of a forward, for tests: tokens-per-expert at or below
  * which the weight-streaming path runs (the rest take the tiled MFMA path).
  * Returns the current value; 0 keeps it.  The choice is a function of the

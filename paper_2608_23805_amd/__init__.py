@@ -161,8 +161,8 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_moe_forward_noalloc",
            "msi_slot_hold", "msi_slot_unhold", "msi_slot_query", "msi_plan_stats",
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
-           "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear", "msi_kv_append",
-           "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention", "msi_kv_evict"]
+           "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear",
+           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention", "msi_kv_evict"]
 
 
 class MsiError(RuntimeError):
@@ -213,6 +213,7 @@ def _load():
     L.msi_plan_timings.argtypes = [_vp, P(msi_timings), ctypes.c_int]
     # (argument structs of the attention block come as pointers or as packed bytes)
     L.msi_linear.argtypes = [_vp, _vp]
+    L.msi_debug_linear_tile.argtypes = [_u32, _u32, P(_u32), P(_u32), P(_u32)]
     for n in ("msi_kv_append", "msi_kv_read"):
         getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
     L.msi_kv_attention_workspace.argtypes = [_vp, _vp, _u32, _u32, P(_u64)]

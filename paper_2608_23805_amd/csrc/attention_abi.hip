@@ -18,6 +18,7 @@ bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % 
 
 constexpr uint64_t MOST_STRIDE = 1u << 21;      // elements: tile offsets stay under 2^31 bytes
 constexpr uint32_t MOST = 1u << 29;              // rows, tokens, features: grids of 64 of them stay under 2^32 threads
+constexpr uint64_t MOST_OUTPUTS = uint64_t(1) << 36;
 constexpr uint32_t MOST_PAGES = 1u << 30;
 constexpr uint64_t MOST_GROUPS = 1u << 24;       // workgroups of 256 along a grid's x
 
@@ -126,7 +127,7 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
         return bad("unknown dtype");
     if (a->K < 8 || a->K % 8 || a->K > MOST_STRIDE)
         return bad("K must be a multiple of 8, 8 .. 2^21");
-    if (a->M > MOST || a->N > MOST || uint64_t(a->M) * a->N > uint64_t(MOST) * 128)
+    if (a->M > MOST || a->N > MOST || uint64_t(a->M) * a->N > MOST_OUTPUTS)
         return bad("M and N must be at most 2^29, M * N at most 2^36");
     if (a->M == 0 || a->N == 0)
         return MSI_OK;
@@ -166,6 +167,19 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
     l.N = int(a->N);
     l.K = int(a->K);
     return launched(launch_linear(l, int(a->activation), static_cast<hipStream_t>(stream)));
+}
+
+msi_status msi_debug_linear_tile(uint32_t M, uint32_t N, uint32_t *rows, uint32_t *features, uint32_t *per_cu)
+{
+    if (!rows || !features || !per_cu)
+        return bad("null output");
+    if (M < 1 || N < 1 || M > MOST || N > MOST || uint64_t(M) * N > MOST_OUTPUTS)
+        return bad("M and N must be 1 .. 2^29, M * N at most 2^36");
+    const LinearTile t = linear_tile(M, N);
+    *rows = uint32_t(t.rows);
+    *features = uint32_t(t.features);
+    *per_cu = uint32_t(t.per_cu);
+    return MSI_OK;
 }
 
 msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,

@@ -304,6 +304,10 @@ struct LinearArgs {
     int M, N, K;
 };
 hipError_t launch_linear(const LinearArgs &A, int act, hipStream_t st);
+struct LinearTile {
+    int rows, features, per_cu;  // of a workgroup; workgroups that share a CU
+};
+LinearTile linear_tile(int64_t M, int64_t N);   // the tiles that M rows and N features are cut into
 
 // ---- paged 8-bit cache of keys and values (kv_cache.hip); strides in elements, fmt KV_E4M3 or KV_INT8
 hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,

@@ -449,6 +449,26 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t st)
     return hipGetLastError();
 }
 
+template <int ACT>
+hipError_t launch_act(const LinearArgs &A, hipStream_t st)
+{
+    const LinearTile t = linear_tile(A.M, A.N);
+    if (t.rows == 32)
+        return t.features == 32 ? launch_tile<ACT, LinearShape<32, 32, 2, 2, 2, 4, 2>>(A, st)
+                                : launch_tile<ACT, LinearShape<32, 64, 1, 2, 4, 3, 1>>(A, st);
+    if (t.rows == 64)
+        return t.features == 64 ? launch_tile<ACT, LinearShape<64, 64, 2, 2, 2, 4, 1>>(A, st)
+                                : launch_tile<ACT, LinearShape<64, 128, 2, 2, 2, 3, 1>>(A, st);
+    if (t.rows == 128)
+        return t.per_cu == 1 ? launch_tile<ACT, LinearShape<128, 128, 4, 4, 1, 3, 1>>(A, st)
+                             : launch_tile<ACT, LinearShape<128, 128, 4, 2, 1, 2, 2>>(A, st);
+    const int64_t tiles = int64_t((A.M + 255) / 256) * ((A.N + 255) / 256);
+    launch_k(linear_wide_kernel<ACT>, unsigned(tiles), 512, 0, st, A);
+    return hipGetLastError();
+}
+
+}  // namespace
+
 // The smallest tiles that give one to every CU at most, since one wave of
 // workgroups lasts as long as a tile does: a stage of 64 K elements takes a CU
 // 0.10 us with tiles of 32 x 32, 0.11 with 32 x 64, 0.19 with 64 x 64, 0.24 with 64 x 128, 0.42
@@ -459,29 +479,19 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t st)
 // rounds better [2500 rows, K 2048, N 2500: 34.6 and 50.5; 1500, 3000, 5000: 63.4
 // and 78.3; 2048, 4096, 2048: 41.7 and 41.9; 4096, 2048, 4096: 73.4 and 63.0;
 // 4096, 1024, 8192: 80 and 70].
-template <int ACT>
-hipError_t launch_act(const LinearArgs &A, hipStream_t st)
+LinearTile linear_tile(int64_t M, int64_t N)
 {
     constexpr int64_t CUS = 256;
-    auto tiles = [&](int64_t m, int64_t n) { return (A.M + m - 1) / m * ((A.N + n - 1) / n); };
-    if (tiles(32, 32) <= CUS)
-        return launch_tile<ACT, LinearShape<32, 32, 2, 2, 2, 4, 2>>(A, st);
-    if (tiles(32, 64) <= CUS)
-        return launch_tile<ACT, LinearShape<32, 64, 1, 2, 4, 3, 1>>(A, st);
-    if (tiles(64, 64) <= CUS)
-        return launch_tile<ACT, LinearShape<64, 64, 2, 2, 2, 4, 1>>(A, st);
-    if (tiles(64, 128) <= CUS)
-        return launch_tile<ACT, LinearShape<64, 128, 2, 2, 2, 3, 1>>(A, st);
-    if (tiles(128, 128) <= CUS)
-        return launch_tile<ACT, LinearShape<128, 128, 4, 4, 1, 3, 1>>(A, st);
+    auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
+    for (const LinearTile t : {LinearTile{32, 32, 2}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1}, LinearTile{64, 128, 1},
+                               LinearTile{128, 128, 1}})
+        if (tiles(t.rows, t.features) <= CUS)
+            return t;
     const int64_t t128 = tiles(128, 128), t256 = tiles(256, 256);
     if (37 * ((t256 + CUS - 1) / CUS) > 20 * ((t128 + 2 * CUS - 1) / (2 * CUS)))
-        return launch_tile<ACT, LinearShape<128, 128, 4, 2, 1, 2, 2>>(A, st);
-    launch_k(linear_wide_kernel<ACT>, unsigned(t256), 512, 0, st, A);
-    return hipGetLastError();
+        return LinearTile{128, 128, 2};
+    return LinearTile{256, 256, 1};
 }
-
-}  // namespace
 
 hipError_t launch_linear(const LinearArgs &A, int act, hipStream_t st)
 {

@@ -30,6 +30,29 @@ def _block(mass=True, **over):
     return msi.AttentionBlock(**kw)
 
 
+@pytest.mark.parametrize("M,N,tile", [
+    (1, 1, (32, 32, 2)), (16, 5120, (32, 32, 2)), (32, 8192, (32, 32, 2)), (32, 8193, (32, 64, 1)), (64, 8192, (32, 64, 1)),
+    (64, 8193, (64, 64, 1)), (512, 2048, (64, 64, 1)), (512, 2049, (64, 128, 1)), (512, 4096, (64, 128, 1)),
+    (512, 4097, (128, 128, 1)), (2048, 2048, (128, 128, 1)), (2048, 2049, (128, 128, 2)), (2500, 2500, (128, 128, 2)),
+    (4096, 4096, (256, 256, 1)), (4096, 8192, (256, 256, 1)), (1 << 29, 1, (128, 128, 2)), (1 << 29, 128, (128, 128, 2)),
+    (1 << 20, 1 << 16, (256, 256, 1)),
+])
+def test_linear_tile(M, N, tile):
+    import paper_2608_23805_amd as msi
+    v = [ctypes.c_uint32() for _ in range(3)]
+    assert msi.lib.msi_debug_linear_tile(M, N, *map(ctypes.byref, v)) == msi.MSI_OK
+    assert tuple(x.value for x in v) == tile
+
+
+def test_linear_tile_refusals():
+    import paper_2608_23805_amd as msi
+    v = [ctypes.byref(ctypes.c_uint32()) for _ in range(3)]
+    for a in ((0, 1), (1, 0), ((1 << 29) + 1, 1), (1 << 29, 129)):
+        _refused(msi.lib.msi_debug_linear_tile(*a, *v), "M and N")
+    for k in range(3):
+        _refused(msi.lib.msi_debug_linear_tile(1, 1, *[None if i == k else p for i, p in enumerate(v)]), "null")
+
+
 def test_status_words_are_aligned():
     """A status word between two words would be an atomic at an address that has none."""
     import paper_2608_23805_amd as msi

@@ -15,9 +15,29 @@ pytestmark = pytest.mark.gpu
 
 def _tile(M, N):
     import paper_2608_23805_amd as msi
-    r, f = ctypes.c_uint32(), ctypes.c_uint32()
-    msi._check(msi.lib.msi_debug_linear_tile(M, N, ctypes.byref(r), ctypes.byref(f)))
-    return r.value, f.value
+    v = [ctypes.c_uint32() for _ in range(3)]
+    msi._check(msi.lib.msi_debug_linear_tile(M, N, *map(ctypes.byref, v)))
+    return tuple(x.value for x in v)
+
+
+@pytest.mark.parametrize("M,N,tile", [
+    (33, 4095, (32, 32, 2)), (70, 5003, (32, 64, 1)), (300, 3000, (64, 64, 1)), (509, 4050, (64, 128, 1)),
+    (449, 4033, (64, 128, 1)), (1000, 3001, (128, 128, 1)), (1030, 4097, (128, 128, 2)), (2500, 2500, (128, 128, 2)),
+    (4000, 4050, (256, 256, 1)), (3841, 4033, (256, 256, 1)),
+])
+@pytest.mark.parametrize("K", [8, 64, 72, 136, 200])
+def test_form(M, N, tile, K):
+    """One stage, odd and even numbers of stages, tails of K inside every form's stages; rows and features that end
+    inside a tile, one of them by one row and one feature."""
+    assert _tile(M, N) == tile
+    _case(M, K, N, act="gelu", residual="bf16", out="bf16")
+    _case(M, K, N, residual="f32", out="f32", inplace=True)
+
+
+def test_forms_of_long_sums():
+    """The two-buffer loops over many stages, with and without a tail."""
+    for M, N, K in ((4000, 4050, 1096), (4000, 4050, 1024), (509, 4050, 1096), (1030, 4097, 1032)):
+        _case(M, K, N, act="silu", residual="f32", out="f32", pad=8)
 
 
 def _gelu(z):
