@@ -17,6 +17,85 @@ def _lens(g, n, most):
     return [int(v) for v in np.where(np.arange(n) % 5 == 0, 0, np.where(np.arange(n) % 7 == 1, 1, g.integers(1, most, n)))]
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("S", [64, 65, 130])
+@pytest.mark.parametrize("rows", [1, 12])
+def test_units_of_many_sequences(fmt, S, rows):
+    """Units found past the first 64 and 128 sequences; the last sequence is the longest one."""
+    log(f"case many sequences {fmt} S={S} rows={rows}")
+    g = np.random.default_rng([81, S])
+    lens = _lens(g, S, 600)
+    lens[0], lens[-1] = 1100, 1500
+    n = [min(rows, max(x, 1)) for x in lens]                   # (a row without tokens comes out zero)
+    s = Setup(S + rows, lens, n, 1, 64, fmt)
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4)
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4, mass_rows=2, decay=0.5)
+
+
+@pytest.mark.parametrize("bad", [False, True])
+def test_page_lists_of_many_rows(bad):
+    """A sequence of 134 blocks that is not cut: the lists of 64 pages are made three times, a bad page in each."""
+    log(f"case page lists, many rows, bad={bad}")
+    lens, rows = [8530] + [3] * 51, [40] + [1] * 51
+    s = Setup(82, lens, rows, 1, 64, "int8")
+    table = s.table.copy()
+    if bad:
+        for b in (10, 63, 64, 66, 100, 127, 128, 129, 133):
+            table[0, b] = 10 ** 6 + b
+    seqs = s.make_seqs(table, s.lens, s.cu)
+    _check(s, seqs, table, s.lens, s.cu, 16, status=int(bad))
+    _check(s, seqs, table, s.lens, s.cu, 16, mass_rows=17, decay=1.0, status=int(bad))
+
+
+@pytest.mark.parametrize("bad", [False, True])
+def test_page_lists_of_few_rows(bad):
+    """A sequence of 258 blocks among so many that none is cut: a wavefront's list of 64 pages is made twice."""
+    log(f"case page lists, few rows, bad={bad}")
+    lens, rows = [16500] + [1] * 1023, [1] * 1024
+    s = Setup(83, lens, rows, 8, 64, "e4m3")
+    table = s.table.copy()
+    if bad:
+        for b in (3, 255, 256, 257):
+            table[0, b] = -2
+    seqs = s.make_seqs(table, s.lens, s.cu)
+    _check(s, seqs, table, s.lens, s.cu, 1, status=int(bad))
+    _check(s, seqs, table, s.lens, s.cu, 1, mass_rows=1, decay=0.25, status=int(bad))
+
+
+@pytest.mark.parametrize("D", [64, 256])
+def test_weights_by_four_blocks(D):
+    """So many blocks that the four wavefronts of a workgroup take one each; sequences that end inside such a group."""
+    log(f"case weights, four blocks D={D}")
+    s = Setup(84, [8300, 700, 65, 0, 300], [40, 33, 1, 0, 5], 2, D, "e4m3" if D == 64 else "int8")
+    for mass_rows, decay in ((33, 1.0), (1, 0.0), (1000, 0.5)):
+        _check(s, s.seqs, s.table, s.lens, s.cu, 2, mass_rows=mass_rows, decay=decay)
+
+
+@pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("lens,rows", [([70, 5, 0], [1, 1, 1]), ([70, 5, 0], [40, 3, 0]), ([900, 130], [1, 1]), ([900, 130], [40, 1])])
+def test_weights_of_other_tokens_stay(lens, rows, decay):
+    """Weights past a sequence's last token and in pages that no sequence of the call holds keep their bits."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log(f"case weights that stay {lens} {rows} {decay}")
+    s = Setup(85 + sum(rows), lens, rows, 2, 64, "int8", spare=3)
+    live = np.zeros(s.host.mass.shape, dtype=bool)
+    for i, n in enumerate(lens):
+        for t in range(n):
+            live[s.table[i, t // 64], :, t % 64] = True
+    s.host.mass[~live & (np.arange(64) % 3 == 0)] = np.nan     # bits that arithmetic would not keep
+    s.mass.copy_(torch.from_numpy(s.host.mass))
+    q, _ = s.rows(4, 0.5)
+    out = torch.empty((s.cu[-1], 4, 64), dtype=torch.bfloat16, device="cuda")
+    ws = msi.kv_attention_workspace(s.cache, s.seqs, 4, 2)
+    msi.kv_attention(s.cache, s.seqs, q, out, 0.125, mass_rows=2, mass_decay=decay, workspace=ws)
+    torch.cuda.synchronize()
+    got = s.mass.cpu().numpy()
+    assert np.array_equal(got.view(np.uint32)[~live], s.host.mass.view(np.uint32)[~live])
+    if decay != 1.0:
+        assert np.all(got[live] != s.host.mass[live])          # (the others moved)
+
+
 @pytest.mark.parametrize("fmt,scale", [("e4m3", 2.0 ** 119), ("int8", 2.0 ** 121)])
 @pytest.mark.parametrize("lens,rows", [([70, 200], [1, 3]), ([900], [1]), ([70, 300], [40, 33]), ([900], [40])])
 def test_values_at_the_ends_of_the_range(fmt, scale, lens, rows):
@@ -63,6 +142,15 @@ def test_large_values_behind_others(rows):
     s.scales.copy_(torch.from_numpy(s.host.scales))
     _check(s, s.seqs, s.table, s.lens, s.cu, 16)
     _check(s, s.seqs, s.table, s.lens, s.cu, 16, mass_rows=5, decay=0.5)
+
+
+def test_a_chunk_beside_single_tokens():
+    """One prompt chunk and single tokens on long and short caches in one call, every kind of cut."""
+    log("case chunk beside single tokens")
+    lens = [700] + [int(v) for v in np.random.default_rng(87).integers(1, 900, 20)]
+    s = Setup(87, lens, [150] + [1] * 20, 2, 128, "e4m3")
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4)
+    _check(s, s.seqs, s.table, s.lens, s.cu, 4, mass_rows=1, decay=1.0)
 
 
 def test_eviction_leaves_a_broken_sequence_out():
