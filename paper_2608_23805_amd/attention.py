@@ -50,8 +50,13 @@ def _call(device, fn, *args):
         _check(st)
 
 
-def _stream(s) -> Optional[int]:
-    return None if s is None else getattr(s, "cuda_stream", s)
+def _stream(s, device) -> Optional[int]:
+    """The handle of a stream (torch's, or a handle already); torch's tell their device, which must be the tensors'."""
+    if s is None:
+        return None
+    if getattr(s, "device_index", device.index) != device.index:
+        _refuse(f"the stream is on device {s.device_index}, the tensors are on {device}")
+    return getattr(s, "cuda_stream", s)
 
 
 def _dense(name: str, t, dtype, device, shape=None):
@@ -124,7 +129,7 @@ def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
     _call(dev, lib.msi_linear,
           _pack_linear.pack(x.data_ptr(), w.data_ptr(), 0 if bias is None else bias.data_ptr(), rp, out.data_ptr(),
                             M, N, K, code, rt, MSI_F32 if out.dtype == _F32 else MSI_BF16, xs, rs, os_),
-          _stream(stream))
+          _stream(stream, dev))
 
 
 class KvCache:
@@ -208,7 +213,7 @@ def kv_append(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
     H, dev = cache.n_heads, cache.device
     ks, vs = _rows(cache, seqs, "k", k, H), _rows(cache, seqs, "v", v, H)
     _call(dev, lib.msi_kv_append, cache._ref, seqs._ref, k.data_ptr(), v.data_ptr(), ks, vs, _status(status, dev),
-          _stream(stream))
+          _stream(stream, dev))
 
 
 def kv_read(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
@@ -217,7 +222,7 @@ def kv_read(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
     H, dev = cache.n_heads, cache.device
     ks, vs = _rows(cache, seqs, "k", k, H), _rows(cache, seqs, "v", v, H)
     _call(dev, lib.msi_kv_read, cache._ref, seqs._ref, k.data_ptr(), v.data_ptr(), ks, vs, _status(status, dev),
-          _stream(stream))
+          _stream(stream, dev))
 
 
 def kv_attention_workspace_size(cache: KvCache, seqs: KvSeqs, n_q_heads: int, mass_rows: int = 0) -> int:
@@ -261,7 +266,7 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
         ref = ctypes.byref(c)
     _call(dev, lib.msi_kv_attention, cache._ref, ref,
           _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30),
-                               mass_decay if mass_rows else 0.0, wp, wn, _status(status, dev)), _stream(stream))
+                               mass_decay if mass_rows else 0.0, wp, wn, _status(status, dev)), _stream(stream, dev))
 
 
 def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget: int, sinks: int = 0, recent: int = 0,
@@ -279,7 +284,7 @@ def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget:
     _dense("keep", keep, _I32, dev, (S, cache.n_heads, budget))
     _call(dev, lib.msi_kv_evict, cache._ref, seqs._ref,
           _pack_evict.pack(budget, sinks, recent, dst_table.shape[1], dst_table.data_ptr(), new_lens.data_ptr(),
-                           keep.data_ptr(), _status(status, dev)), _stream(stream))
+                           keep.data_ptr(), _status(status, dev)), _stream(stream, dev))
 
 
 class AttentionBlock:
@@ -371,7 +376,7 @@ class AttentionBlock:
         linear(attn.view(n, self.wo.shape[1]), self.wo, out, stream=stream)
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
-                  _stream(stream))
+                  _stream(stream, h.device))
 
     def project(self, x, seqs: KvSeqs, stream=None):
         """First half: queries, keys and values of the rows x, [n_rows, n_q_heads + 2 n_kv_heads, head_dim] bf16 in the block's

@@ -144,3 +144,18 @@ def test_tensors_without_elements():
                  (msi.kv_attention, (_cpu_cache(), s, rows, rows, 1.0))):
         with pytest.raises(msi.MsiError, match="HIP device"):          # (and no complaint about strides)
             f(*a)
+
+
+def test_streams_of_another_device():
+    """A kernel goes to its stream's device, which cannot read the tensors of another: refused."""
+    import types
+    import paper_2608_23805_amd as msi
+    import torch
+    s, i32 = _cpu_seqs(), lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    other = types.SimpleNamespace(cuda_stream=0, device_index=1)
+    kv, q = _w(4, 2, 64), _w(4, 4, 64)
+    for f, a, k in ((msi.linear, (_w(4, 16), _w(8, 16), _w(4, 8)), {}), (msi.kv_append, (_cpu_cache(), s, kv, kv), {}),
+                    (msi.kv_read, (_cpu_cache(), s, kv, kv), {}), (msi.kv_attention, (_cpu_cache(), s, q, q, 1.0), {}),
+                    (msi.kv_evict, (_cpu_cache(), s, i32(2, 2), i32(2), i32(2, 2, 100)), dict(budget=100))):
+        with pytest.raises(msi.MsiError, match="stream"):
+            f(*a, stream=other, **k)
