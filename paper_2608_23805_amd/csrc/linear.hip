@@ -281,11 +281,13 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
             issue(j, j);
     int cur = 0, nxt = AHEAD;
     for (int s = 0; s < nstage; ++s) {
-        // stage s has landed; the buffer of stage s + AHEAD was last read at s - 1
+        // stage s has landed; the buffer of stage s + AHEAD was last read at s - 1, by reads that are waited for as well
+        // (LGKM_DONE: no LDS operation of this wavefront in flight)
+        constexpr int LGKM_DONE = ~(0xF << 8);
         if (s + AHEAD <= nstage)
-            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(LPS * (AHEAD - 1)));
+            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(LPS * (AHEAD - 1)) & LGKM_DONE);
         else
-            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));
+            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0) & LGKM_DONE);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (s + AHEAD < nstage)
