@@ -528,7 +528,8 @@ typedef struct {
  * scale it had if it held tokens and that is larger; codes are x times 1 / s,
  * rounded to nearest, ties to even; codes the block held move to a grown scale
  * the same way.  The new tokens' mass becomes 0.  Bytes after the last token
- * stay as they were.  No page may be written for two sequences by one call.
+ * stay as they were.  No page may be written twice by one call, for two sequences
+ * or for two blocks of one.
  * Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,
                          uint64_t k_stride, uint64_t v_stride, uint32_t *status, void *stream);
@@ -576,8 +577,8 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
  * and last `recent` tokens, and of the others those with the largest mass
  * (equal ones from the lowest index on; NaN below everything), in ascending
  * order.  Heads keep tokens of their own.  The kept tokens go to the pages of
- * dst_table [n_seqs, dst_blocks], which no sequence of the call may hold, with
- * their mass, coded again by blocks of 64 as an append to empty pages would;
+ * dst_table [n_seqs, dst_blocks], different ones that no sequence of the call
+ * holds, with their mass, coded again by blocks of 64 as an append to empty pages would;
  * new_lens[i] = min(lens[i], budget); keep [n_seqs, n_heads, budget] gets the
  * kept indices, then -1.  A sequence within its budget is copied whole; one that
  * breaks a bound is left out, its entries of new_lens and keep as they were.

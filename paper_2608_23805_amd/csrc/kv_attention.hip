@@ -14,9 +14,13 @@
 // lane column, and the token order of an MFMA's reduction is the one in which
 // the scores already lie, so P never moves between lanes.  Codes become bf16
 // exactly; the block's K scale multiplies the fp32 scores and its V scale the
-// probabilities.  Probabilities are rounded to bf16 for the second product
-// (at most 2^-9 relative each, the same as the output's own rounding); their
-// sum, the maxima, the scores and all accumulators are fp32.
+// probabilities.  Probabilities are rounded to bf16 for the second product,
+// the only operand type of its matrix instruction that holds V's codes and that
+// range: at most 2^-8 relative each, as the output's own rounding, and about as
+// much again in sum where few tokens carry a row (root mean square against 64
+// bits: prompt chunks 2.4e-3, single tokens 1.7e-3, of which the output's own
+// rounding is 1.7e-3); their sum, the maxima, the scores and all accumulators
+// are fp32.
 #include <algorithm>
 
 #include "gemm_ring.h"
@@ -1108,10 +1112,13 @@ __global__ void __launch_bounds__(256) kv_finish_kernel(AttentionLaunch A, int j
 
 // For many rows the scores are computed again from K.  A wavefront keeps a
 // block's K in registers (as bf16, with D = 256 as codes) and walks groups of
-// 32 rows; the next group's queries are on their way while the vector unit takes the
-// exponentials, which bound it (with D = 256 they would not fit the registers
-// beside K: 438 us with them, 375 without, for all of 2048 rows of two sequences
-// of 4096 tokens, 2 heads of 256 with 8 query heads each; 4 heads of 128: 200 us).  With `share` = 4 the four
+// 32 rows; the next group's queries are on their way during this one's products
+// and exponentials (with D = 256 they would not fit the registers beside K: 438
+// us with them, 375 without).  All of 2048 rows of two sequences of 4096 tokens, 8 query heads a head: 2
+// heads of 256 384 us, 4 heads of 128 229.  Bound by latency with heads of 256, where
+// a wavefront waits for its queries for 66 % of its time (one a SIMD; the vector
+// unit issues 20 % of it, the matrix cores work 10 %); with 128 it waits 33 %, and
+// another 36 % for its turn beside the second wavefront of its SIMD.  With `share` = 4 the four
 // wavefronts of a workgroup have a block each and meet the same queries at about
 // the same time (in L1); with 1 they share one block and take every fourth
 // group, for calls with few blocks.

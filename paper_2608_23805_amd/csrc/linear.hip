@@ -1,7 +1,7 @@
 // linear.hip -- projection y = act(x W^T + b) + r, gfx950: x [M, K] and
 // W [N, K] bf16 with the reduction axis contiguous, b fp32, r and y bf16 or
 // fp32.  Sums, bias, activation and the residual's addition are fp32; y is
-// rounded once (to nearest, at most 2^-9 relative, when it is bf16).
+// rounded once (to nearest, at most 2^-8 relative, when it is bf16).
 #include "gemm_ring.h"
 #include "kernels.h"
 
@@ -330,9 +330,9 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) linear_tile
 // halves of 32 elements: the fragments of the next half are read between the
 // MFMAs of this one, so by the middle of a stage all of its fragments are in
 // registers and, after the one barrier, its buffer takes the stage after next.
-// 4096 rows, K 2048, N 8192: 125 us, 1100 TFLOP/s (137 with GELU; the library's
-// product alone 99 us): 32 stages of 1.7 us a tile, 1290 TFLOP/s, and about 10 us
-// for its start and its rows' way out, which nothing overlaps.  (Stages of 32
+// 4096 rows, K 2048, N 8192, call after call: 111 us, 1240 TFLOP/s (with GELU 124, SiLU 130, GELU by tanh
+// 133; the library's product alone 95).  About 10 us a tile are its start and its
+// rows' way out, which nothing overlaps.  (At lower clocks, 125 us: stages of 32
 // elements in rows of 64 bytes, whose reads meet on banks: 133.6 us; four
 // wavefronts of 128 x 128: 187; without reads between the MFMAs: 132.)
 template <int ACT>
