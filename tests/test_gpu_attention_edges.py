@@ -99,6 +99,8 @@ def test_pool_past_four_gib():
     results = []
     for pool, first in ((n, 0), (P, P - n)):
         c = msi.KvCache.alloc(pool, H, D, "e4m3")
+        c.data.zero_()                                     # (bytes past the last token stay as they were)
+        c.scales.zero_()
         table = i32(first + np.arange(7, dtype=np.int32)[None, ::-1])
         dst = i32(first + 7 + np.arange(7, dtype=np.int32)[None])
         r = []
