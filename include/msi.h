@@ -552,7 +552,8 @@ msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void 
  * out, and the rows of `out` below n_rows that belong to no sequence, or to one
  * that is left out, become zeros; without it they stay as they were.  Sums are
  * taken in a fixed order: equal calls give equal bits.  `out` must not overlap q.  n_seqs * n_heads *
- * ceil(max_rows * heads of a group / 128) is under 2^24. */
+ * ceil(max_rows * heads of a group / 128) is under 2^24 (less 128 with
+ * MSI_KV_ALL_ROWS). */
 typedef struct {
     const void *q;               /* [n_rows, n_q_heads, head_dim] bf16                 */
     void *out;                   /* the same shape, bf16                               */

@@ -100,8 +100,8 @@ const char *check_heads(const KvCache &c, const KvSeqs &s, uint32_t n_q_heads)
     const uint64_t rows = uint64_t(s.max_rows) * (n_q_heads / c.H);
     if (rows > MOST)
         return "max_rows times the heads of a group must be at most 2^29";
-    if ((rows + 127) / 128 * uint64_t(c.H) * uint64_t(s.S) >= MOST_GROUPS)
-        return "n_seqs * n_heads * (max_rows * heads of a group / 128) must be under 2^24";
+    if ((rows + 127) / 128 * uint64_t(c.H) * uint64_t(s.S) >= MOST_GROUPS - (s.all_rows ? 128 : 0))
+        return "n_seqs * n_heads * (max_rows * heads of a group / 128) must be under 2^24 (less 128 with MSI_KV_ALL_ROWS)";
     if (uint64_t(s.S) * ((s.max_len + KV_BLOCK - 1) / KV_BLOCK) > MOST)
         return "n_seqs times the blocks of max_len must be at most 2^29";
     return nullptr;
@@ -300,11 +300,6 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
     A.mass_rows = int(std::min(a->mass_rows, MOST));
     A.decay = a->mass_decay;
     A.status = a->status;
-    if (rest) {
-        const hipError_t e = launch_kv_rest(s, A.out, A.out_stride, int(least), static_cast<hipStream_t>(stream));
-        if (e != hipSuccess)
-            return launched(e);
-    }
     return launched(launch_kv_attention(A, int(cache->format), cut, static_cast<hipStream_t>(stream)));
 }
 

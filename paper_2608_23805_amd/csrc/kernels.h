@@ -337,6 +337,7 @@ struct AttentionLaunch {
     int G;                       // query heads of a cache head
     float scale_log2;            // scale * log2(e): scores are powers of two
     int direct, per, part_rows;  // see AttentionCut; part_rows = max_rows * G
+    int main;                    // workgroups of the units; those behind them clear rows (launch_kv_attention sets it)
     int2 *plan;                  // [S] first unit and number of units of a sequence that has tokens; null if direct
     float *part_ml, *part_o;     // [units, H, part_rows, 2 | D] maxima and sums, unnormalised outputs
     float *scores;               // [S * score_blocks | n_pages, H, part_rows, 64], or null
@@ -346,7 +347,7 @@ struct AttentionLaunch {
     float decay;
     uint32_t *status;
 };
-// zeros in the rows of `out` (`width` elements) that no sequence of the call answers for
+// zeros in the rows of `out` (`width` elements) that no sequence of the call answers for, where a call has nothing else
 hipError_t launch_kv_rest(const KvSeqs &s, uint16_t *out, int64_t out_stride, int width, hipStream_t st);
 hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st);
 

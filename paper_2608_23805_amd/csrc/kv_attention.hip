@@ -174,6 +174,61 @@ __device__ __forceinline__ int64_t score_index(const AttentionLaunch &A, int i, 
     return ((at * A.c.H + h) * A.part_rows + row) * KV_BLOCK;
 }
 
+// ---------------------------------------------------------------- other rows
+//
+// Rows that no sequence answers for: those between and behind the sequences'
+// rows and those of a sequence whose numbers break a bound.  Workgroups behind
+// the grid's units take 64 rows at a time, mark which of them some sequence
+// brings (offsets that fall could overlap, so every sequence is looked at) and
+// clear the others.  They run beside the units (a block's step of 16 single tokens 38.5 us with and without them, 42
+// with a launch of their own).  Calls without them take kernels without their code, which costs those 0.5 to 2 %.
+constexpr int REST_ROWS = 64, MOST_REST = 128;
+
+__host__ __device__ __forceinline__ int rest_groups(const KvSeqs &s)
+{
+    return s.all_rows ? min((s.n_rows + REST_ROWS - 1) / REST_ROWS, MOST_REST) : 0;
+}
+
+// Rows 64 group .., 64 (group + groups) .. and so on; `words`: 8 words of LDS.
+__device__ __forceinline__ void clear_rest(const KvSeqs &s, uint16_t *__restrict__ out, int64_t stride, int width, int group,
+                                           int groups, uint32_t *words)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    for (int64_t first = int64_t(group) * REST_ROWS; first < s.n_rows; first += int64_t(groups) * REST_ROWS) {
+        const int r0 = int(first), n = min(REST_ROWS, s.n_rows - r0);
+        uint64_t rows = 0;
+        for (int i = threadIdx.x; i < s.S; i += 256) {
+            const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, true);
+            const int lo = max(q.row0 - r0, 0), hi = min(q.row0 - r0 + q.n, n);
+            if (q.n > 0 && lo < hi)
+                rows |= (~uint64_t(0) >> (64 - (hi - lo))) << lo;
+        }
+        auto either = [](float a, float b) { return __uint_as_float(__float_as_uint(a) | __float_as_uint(b)); };
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float w = wave_reduce(__uint_as_float(uint32_t(rows >> 32 * k)), either);
+            if ((threadIdx.x & 63) == 0)
+                words[2 * wave + k] = __float_as_uint(w);
+        }
+        __syncthreads();
+        uint32_t brought[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            brought[k] = __builtin_amdgcn_readfirstlane(words[k] | words[2 + k] | words[4 + k] | words[6 + k]);
+        for (int r = 0; r < n; ++r)
+            if (!(brought[r >> 5] >> (r & 31) & 1))
+                for (int c = threadIdx.x; c < width / 8; c += 256)
+                    *reinterpret_cast<u32x4 *>(out + (first + r) * stride + 8 * c) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+}
+
+__global__ void __launch_bounds__(256) kv_rest_kernel(KvSeqs s, uint16_t *out, int64_t stride, int width)
+{
+    __shared__ uint32_t words[8];
+    clear_rest(s, out, stride, width, int(blockIdx.x), int(gridDim.x), words);
+}
+
 // ---------------------------------------------------------------- few rows
 //
 // Up to 16 RT packed rows (single tokens, drafted tokens): bound by reading the
@@ -242,7 +297,7 @@ struct FewRows {
     }
 };
 
-template <int FMT, int D, int RT>
+template <int FMT, int D, int RT, bool ALL>
 __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel(AttentionLaunch A)
 {
     using F = FewRows<FMT, D, RT>;
@@ -253,6 +308,12 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     constexpr bool QLDS = D == 256 && RT == 2;               // two tiles of long queries do not fit the registers
     __shared__ bf16x8 qlds[QLDS ? RT * (D / 32) * 64 : 1];
 
+    if constexpr (ALL)
+        if (int(blockIdx.x) >= A.main) {
+            clear_rest(A.s, A.out, A.out_stride, A.c.H * A.G * D, int(blockIdx.x) - A.main, int(gridDim.x) - A.main,
+                       reinterpret_cast<uint32_t *>(lsum));
+            return;
+        }
     const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
     if (unit.seq < 0)
         return;
@@ -729,11 +790,17 @@ __device__ __forceinline__ void add_low(const f32x16 (&sv)[2], float ks, float &
             l += __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -ref));
 }
 
-template <int FMT, int D>
+template <int FMT, int D, bool ALL>
 __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
 {
     using M = ManyRows<D>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
+    if constexpr (ALL)
+        if (int(blockIdx.x) >= A.main) {
+            clear_rest(A.s, A.out, A.out_stride, A.c.H * A.G * D, int(blockIdx.x) - A.main, int(gridDim.x) - A.main,
+                       reinterpret_cast<uint32_t *>(lds8));
+            return;
+        }
     const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
     if (unit.seq < 0)
         return;
@@ -1237,38 +1304,6 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
     }
 }
 
-// ---------------------------------------------------------------- other rows
-//
-// Rows that no sequence answers for: those between and behind the sequences'
-// rows and those of a sequence whose numbers break a bound.  A workgroup marks
-// which of its 64 rows some sequence brings (offsets that fall could overlap,
-// so every sequence is looked at) and clears the others; with all of them
-// brought, as usual, it reads the lengths and ends: a launch.
-constexpr int REST_ROWS = 64;
-
-__global__ void __launch_bounds__(256) kv_rest_kernel(KvSeqs s, uint16_t *__restrict__ out, int64_t stride, int chunks)
-{
-    __shared__ uint32_t brought[2];
-    const int r0 = int(blockIdx.x) * REST_ROWS, n = min(REST_ROWS, s.n_rows - r0);
-    if (threadIdx.x < 2)
-        brought[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < s.S; i += 256) {
-        const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, true);
-        const int lo = max(q.row0 - r0, 0), hi = min(q.row0 - r0 + q.n, n);
-        if (q.n > 0 && lo < hi) {
-            const uint64_t rows = (~uint64_t(0) >> (64 - (hi - lo))) << lo;
-            atomicOr(&brought[0], uint32_t(rows));
-            atomicOr(&brought[1], uint32_t(rows >> 32));
-        }
-    }
-    __syncthreads();
-    for (int r = 0; r < n; ++r)
-        if (!(brought[r >> 5] >> (r & 31) & 1))
-            for (int c = threadIdx.x; c < chunks; c += 256)
-                *reinterpret_cast<u32x4 *>(out + (int64_t(r0) + r) * stride + 8 * c) = u32x4{0, 0, 0, 0};
-}
-
 template <typename F>
 void with_shape(int fmt, int D, F f)
 {
@@ -1319,7 +1354,7 @@ AttentionCut attention_cut(int S, int H, int G, int D, int n_pages, int max_rows
 
 hipError_t launch_kv_rest(const KvSeqs &s, uint16_t *out, int64_t out_stride, int width, hipStream_t st)
 {
-    launch_k(kv_rest_kernel, unsigned((s.n_rows + REST_ROWS - 1) / REST_ROWS), 256, 0, st, s, out, out_stride, width / 8);
+    launch_k(kv_rest_kernel, unsigned(rest_groups(s)), 256, 0, st, s, out, out_stride, width);
     return hipGetLastError();
 }
 
@@ -1327,19 +1362,27 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
 {
     const int H = A.c.H, S = A.s.S;
     const int rows = A.s.max_rows * A.G;
-    const unsigned grid = unsigned(c.units) * unsigned(c.per);
+    A.main = c.units * c.per;
+    const unsigned grid = unsigned(A.main + rest_groups(A.s));
     hipError_t e = hipSuccess;
-    with_shape(fmt, A.c.D, [&](auto f, auto d) {
+    auto launch = [&](auto f, auto d, auto all) {
         constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
+        constexpr bool ALL = decltype(all)::value;
         if (!c.few) {
             static std::atomic<uint64_t> done{0};
-            e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D>), ManyRows<D>::LDS, done);
+            e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, ALL>), ManyRows<D>::LDS, done);
             if (e == hipSuccess)
-                launch_k(kv_many_rows_kernel<FMT, D>, grid, 256, ManyRows<D>::LDS, st, A);
+                launch_k(kv_many_rows_kernel<FMT, D, ALL>, grid, 256, ManyRows<D>::LDS, st, A);
         } else if (c.tile_rows == 16)
-            launch_k(kv_few_rows_kernel<FMT, D, 1>, grid, 256, 0, st, A);
+            launch_k(kv_few_rows_kernel<FMT, D, 1, ALL>, grid, 256, 0, st, A);
         else
-            launch_k(kv_few_rows_kernel<FMT, D, 2>, grid, 256, 0, st, A);
+            launch_k(kv_few_rows_kernel<FMT, D, 2, ALL>, grid, 256, 0, st, A);
+    };
+    with_shape(fmt, A.c.D, [&](auto f, auto d) {
+        if (A.s.all_rows)
+            launch(f, d, std::true_type{});
+        else
+            launch(f, d, std::false_type{});
     });
     if (e == hipSuccess)
         e = hipGetLastError();

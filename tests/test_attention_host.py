@@ -159,3 +159,16 @@ def test_streams_of_another_device():
                     (msi.kv_evict, (_cpu_cache(), s, i32(2, 2), i32(2), i32(2, 2, 100)), dict(budget=100))):
         with pytest.raises(msi.MsiError, match="stream"):
             f(*a, stream=other, **k)
+
+
+def test_launch_bounds_of_all_rows():
+    """The workgroups that clear rows come on top of the units': both stay in one grid."""
+    import paper_2608_23805_amd as msi
+    n = ctypes.c_uint64()
+
+    def size(flags, S, rows):
+        s = _seqs(n_seqs=S, n_rows=1 << 29, max_rows=rows, max_blocks=1, max_len=64, flags=flags)
+        return msi.lib.msi_kv_attention_workspace(ctypes.byref(_cache(n_heads=1)), ctypes.byref(s), 1, 0, ctypes.byref(n))
+    assert size(0, 4095, 128 * 4097) == 0                      # 2^24 - 1 workgroups
+    _refused(size(1, 4095, 128 * 4097), "under 2^24")
+    assert size(1, 4094, 128 * 4097) == 0

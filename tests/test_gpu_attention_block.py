@@ -166,6 +166,28 @@ def test_many_sequences_answer_for_their_rows():
     assert np.array_equal(zero, np.arange(S) % 11 == 0)
 
 
+@pytest.mark.parametrize("most", [2, 100])
+def test_more_rows_than_are_cleared_in_a_turn(most):
+    """20001 rows of which three sequences bring a few, in both forms and where the call has nothing else to do."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log(f"case attention, all of 20001 rows, most={most}")
+    s = Setup(100, [100, 128, 64], [1, 1, 1], 1, D, "e4m3")
+    n, cu = 20001, [12000, 12001, 12003, 12004]
+    q, _ = bf16(s.g.standard_normal((n, 2, D)))
+    i32 = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32).cuda()  # noqa: E731
+    for offsets, rows in ((cu, most), ([0] * 4, most), ([0] * 4, 0)):
+        seqs = msi.KvSeqs(i32(s.table), i32(s.lens), i32(offsets), n_rows=n, max_rows=rows, max_len=128)
+        out = torch.full((n + 1, 2, D), 5.0, dtype=torch.bfloat16, device="cuda")
+        msi.kv_attention(s.cache, seqs, q, out[:n], 0.125, workspace=msi.kv_attention_workspace(s.cache, seqs, 2), all_rows=True)
+        torch.cuda.synchronize()
+        zero = (out == 0).all(-1).all(-1).cpu().numpy()
+        want = np.ones(n + 1, dtype=bool)
+        want[offsets[0]:offsets[-1]] = False
+        want[n] = False
+        assert np.array_equal(zero, want) and torch.all(out[n] == 5.0)
+
+
 def test_step_without_rows():
     import torch
     import paper_2608_23805_amd as msi
