@@ -308,6 +308,8 @@ class AttentionBlock:
             _refuse("wqkv must be a matrix whose rows are a multiple of 8")
         for name, t, shape in (("wqkv", wqkv, ((n_q_heads + 2 * H) * D, wqkv.shape[1])), ("wo", wo, (wqkv.shape[1], n_q_heads * D))):
             _dense(name, t, t.dtype if t.dtype in _BF16 else torch.bfloat16, dev, shape)
+            if t.data_ptr() % 16:
+                _refuse(f"{name} must be 16-byte aligned")
         if bias is not None:
             _dense("bias", bias, _F32, dev, (wqkv.shape[0],))
         if max_rows < 0:

@@ -87,7 +87,8 @@ def test_block_construction_refusals():
     for over in (dict(wqkv=_w(512, 128).float()), dict(wo=_w(128, 256).float()), dict(wqkv=_w(128, 512).t()),
                  dict(wo=_w(256, 128).t()), dict(wqkv=_w(520, 128)), dict(wo=_w(256, 128)), dict(bias=torch.zeros(511)),
                  dict(bias=_w(512)), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=3e38), dict(n_q_heads=3),
-                 dict(n_q_heads=0), dict(wqkv=_w(512, 100), wo=_w(100, 256)), dict(max_rows=-1), dict(wqkv=_w(512))):
+                 dict(n_q_heads=0), dict(wqkv=_w(512, 100), wo=_w(100, 256)), dict(max_rows=-1), dict(wqkv=_w(512)),
+                 dict(wo=_w(128 * 256 + 8)[1:1 + 128 * 256].view(128, 256)), dict(wqkv=_w(512 * 128 + 8)[4:4 + 512 * 128].view(512, 128))):
         with pytest.raises(msi.MsiError) as e:
             _block(**over)
         assert e.value.status == msi.MSI_E_INVALID_ARG, over
