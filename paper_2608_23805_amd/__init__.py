@@ -162,7 +162,8 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_slot_hold", "msi_slot_unhold", "msi_slot_query", "msi_plan_stats",
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
            "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear",
-           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention", "msi_kv_evict"]
+           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
+           "msi_kv_evict"]
 
 
 class MsiError(RuntimeError):

@@ -16,8 +16,8 @@ from typing import Optional
 
 import torch
 
-from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK, MSI_OK, MsiError, lib,
-               msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
+from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK,
+               MSI_OK, MsiError, lib, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
 _F32, _I32 = torch.float32, torch.int32
@@ -306,7 +306,8 @@ class AttentionBlock:
             _refuse("n_q_heads must be a multiple of the cache's n_heads")
         if wqkv.dim() != 2 or wqkv.shape[1] < 8 or wqkv.shape[1] % 8:
             _refuse("wqkv must be a matrix whose rows are a multiple of 8")
-        for name, t, shape in (("wqkv", wqkv, ((n_q_heads + 2 * H) * D, wqkv.shape[1])), ("wo", wo, (wqkv.shape[1], n_q_heads * D))):
+        for name, t, shape in (("wqkv", wqkv, ((n_q_heads + 2 * H) * D, wqkv.shape[1])),
+                               ("wo", wo, (wqkv.shape[1], n_q_heads * D))):
             _dense(name, t, t.dtype if t.dtype in _BF16 else torch.bfloat16, dev, shape)
             if t.data_ptr() % 16:
                 _refuse(f"{name} must be 16-byte aligned")
