@@ -477,6 +477,21 @@ typedef struct {
 /* Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
 msi_status msi_linear(const msi_linear_args *args, void *stream);
 
+/* The same with 4-bit weights: w[n, k] = scales[n, k / group] * q[n, k].
+ * linear.w holds the codes q, laid out as those of MSI_W_Q4B32: [N, K / 2] bytes,
+ * element 2j in the low nibble of byte j, 4-bit two's complement; 16-byte
+ * aligned.  Every weight counts as it is: the products of a group are summed and
+ * scaled in fp32. */
+typedef struct {
+    msi_linear_args linear;      /* K a multiple of group, at least group              */
+    const void *scales;          /* [N, K / group] fp16, row-major, 2-byte aligned     */
+    uint32_t group;              /* 32, 64 or 128                                      */
+    uint32_t reserved;           /* 0                                                  */
+} msi_linear_q4_args;
+
+/* Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+msi_status msi_linear_q4(const msi_linear_q4_args *args, void *stream);
+
 /* The cache of one layer: a pool of pages with stable addresses, each 64 tokens
  * of every head, handed to sequences by the caller's page tables.  Page p, head
  * h: 64 rows of K codes, then 64 rows of V codes, one byte an element; value =

@@ -124,6 +124,10 @@ class msi_linear_args(ctypes.Structure):
                 ("residual_stride", _u64), ("out_stride", _u64)]
 
 
+class msi_linear_q4_args(ctypes.Structure):
+    _fields_ = [("linear", msi_linear_args), ("scales", _vp), ("group", _u32), ("reserved", _u32)]
+
+
 class msi_kv_cache(ctypes.Structure):
     _fields_ = [("format", _u32), ("n_pages", _u32), ("n_heads", _u32), ("head_dim", _u32), ("data", _vp),
                 ("scales", _vp), ("mass", _vp)]
@@ -161,7 +165,7 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_moe_forward_noalloc",
            "msi_slot_hold", "msi_slot_unhold", "msi_slot_query", "msi_plan_stats",
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
-           "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear",
+           "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear", "msi_linear_q4",
            "msi_debug_linear_tile", "msi_kv_append", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
            "msi_kv_evict"]
 
@@ -214,6 +218,7 @@ def _load():
     L.msi_plan_timings.argtypes = [_vp, P(msi_timings), ctypes.c_int]
     # (argument structs of the attention block come as pointers or as packed bytes)
     L.msi_linear.argtypes = [_vp, _vp]
+    L.msi_linear_q4.argtypes = [_vp, _vp]
     L.msi_debug_linear_tile.argtypes = [_u32, _u32, P(_u32), P(_u32), P(_u32)]
     for n in ("msi_kv_append", "msi_kv_read"):
         getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
@@ -522,7 +527,7 @@ class Plan:
 
 # The attention block's operators (projections, the paged 8-bit cache, its attention and eviction) live in
 # ``attention``, which imports torch; they are found here by name.
-_ATTENTION = ("linear", "KvCache", "KvSeqs", "kv_append", "kv_read", "kv_attention_workspace_size",
+_ATTENTION = ("linear", "linear_q4", "KvCache", "KvSeqs", "kv_append", "kv_read", "kv_attention_workspace_size",
               "kv_attention_workspace", "kv_attention", "kv_evict", "AttentionBlock")
 
 

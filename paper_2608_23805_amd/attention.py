@@ -17,15 +17,19 @@ from typing import Optional
 import torch
 
 from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK,
-               MSI_OK, MsiError, lib, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args, _check)
+               MSI_OK, MsiError, lib, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args,
+               msi_linear_q4_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
+_F16 = (torch.float16, torch.int16)              # likewise fp16
 _F32, _I32 = torch.float32, torch.int32
 _pack_linear = struct.Struct("<5Q6I3Q")
+_pack_q4 = struct.Struct("<Q2I")
 _pack_attention = struct.Struct("<4QIfIf3Q")
 _pack_evict = struct.Struct("<4I4Q")
 for _s, _c in ((_pack_linear, msi_linear_args), (_pack_attention, msi_kv_attention_args), (_pack_evict, msi_kv_evict_args)):
     assert _s.size == ctypes.sizeof(_c)
+assert _pack_linear.size + _pack_q4.size == ctypes.sizeof(msi_linear_q4_args)
 
 
 def _refuse(msg: str):
@@ -103,19 +107,11 @@ def _decay(mass_decay: float):
         _refuse(f"mass_decay must be finite in fp32 and not negative, got {mass_decay}")
 
 
-def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
-    """out = act(x w^T + bias) + residual (msi_linear).
-
-    x [M, K] and w [N, K] bf16 (x's rows may be strided), bias [N] float32,
-    residual and out [M, N] bf16 or float32 with strided rows; residual may be out."""
+def _pack(x, w, N: int, out, bias, act: str, residual) -> bytes:
+    """The arguments of a projection (msi_linear_args) whose weights w [N, ...] have been checked."""
     dev = x.device
-    if x.dim() != 2 or w.dim() != 2:
-        _refuse("x and w must be matrices")
-    (M, K), N = x.shape, w.shape[0]
+    M, K = x.shape
     xs = _matrix("x", x, M, K, dev, _BF16)
-    if w.dtype not in _BF16:
-        _refuse(f"w must be bf16 (or its bits in int16), got {w.dtype}")
-    _dense("w", w, w.dtype, dev, (N, K))
     code = ACTIVATIONS.get(act)
     if code is None:
         _refuse(f"unknown activation {act!r}")
@@ -126,10 +122,43 @@ def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
     if residual is not None:
         rs = _matrix("residual", residual, M, N, dev, _ANY)
         rp, rt = residual.data_ptr(), MSI_F32 if residual.dtype == _F32 else MSI_BF16
-    _call(dev, lib.msi_linear,
-          _pack_linear.pack(x.data_ptr(), w.data_ptr(), 0 if bias is None else bias.data_ptr(), rp, out.data_ptr(),
-                            M, N, K, code, rt, MSI_F32 if out.dtype == _F32 else MSI_BF16, xs, rs, os_),
-          _stream(stream, dev))
+    return _pack_linear.pack(x.data_ptr(), w.data_ptr(), 0 if bias is None else bias.data_ptr(), rp, out.data_ptr(),
+                             M, N, K, code, rt, MSI_F32 if out.dtype == _F32 else MSI_BF16, xs, rs, os_)
+
+
+def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
+    """out = act(x w^T + bias) + residual (msi_linear).
+
+    x [M, K] and w [N, K] bf16 (x's rows may be strided), bias [N] float32,
+    residual and out [M, N] bf16 or float32 with strided rows; residual may be out."""
+    dev = x.device
+    if x.dim() != 2 or w.dim() != 2:
+        _refuse("x and w must be matrices")
+    if w.dtype not in _BF16:
+        _refuse(f"w must be bf16 (or its bits in int16), got {w.dtype}")
+    N = w.shape[0]
+    _dense("w", w, w.dtype, dev, (N, x.shape[1]))
+    _call(dev, lib.msi_linear, _pack(x, w, N, out, bias, act, residual), _stream(stream, dev))
+
+
+def linear_q4(x, w, scales, out, bias=None, act: str = "none", residual=None, stream=None):
+    """out = act(x W^T + bias) + residual with 4-bit weights W[n, k] = scales[n, k / group] * q[n, k] (msi_linear_q4).
+
+    w [N, K / 2] uint8: the codes q = -8 .. 7, element 2j in the low nibble of byte j; scales [N, K / group] float16 (or
+    its bits in int16), group 32, 64 or 128; the others as ``linear``'s."""
+    dev = x.device
+    if x.dim() != 2 or w.dim() != 2 or scales.dim() != 2:
+        _refuse("x, w and scales must be matrices")
+    K, N, groups = x.shape[1], w.shape[0], scales.shape[1]
+    group = K // groups if groups else 0
+    if group not in (32, 64, 128) or group * groups != K:
+        _refuse(f"scales must be [N, K / 32], [N, K / 64] or [N, K / 128], got {tuple(scales.shape)} for K = {K}")
+    _dense("w", w, torch.uint8, dev, (N, K // 2))
+    if scales.dtype not in _F16:
+        _refuse(f"scales must be float16 (or its bits in int16), got {scales.dtype}")
+    _dense("scales", scales, scales.dtype, dev, (N, groups))
+    _call(dev, lib.msi_linear_q4,
+          _pack(x, w, N, out, bias, act, residual) + _pack_q4.pack(scales.data_ptr(), group, 0), _stream(stream, dev))
 
 
 class KvCache:

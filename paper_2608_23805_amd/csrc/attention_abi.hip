@@ -107,46 +107,36 @@ const char *check_heads(const KvCache &c, const KvSeqs &s, uint32_t n_q_heads)
     return nullptr;
 }
 
-// bytes of the log-sums that follow the cut's workspace
-size_t lse_bytes(const AttentionCut &cut, const KvSeqs &s, uint32_t n_q_heads, uint32_t mass_rows)
-{
-    return mass_rows && !cut.few ? size_t(s.n_rows) * n_q_heads * sizeof(float) : 0;
-}
-
-}  // namespace
-
-extern "C" {
-
-msi_status msi_linear(const msi_linear_args *a, void *stream)
+// A projection's arguments as the kernels take them; go: there is work.
+const char *view_linear(const msi_linear_args *a, LinearArgs &l, bool &go)
 {
     if (!a)
-        return bad("null arguments");
+        return "null arguments";
     if (a->activation > MSI_ACT_GELU_TANH)
-        return bad("unknown activation");
+        return "unknown activation";
     if (a->out_dtype > MSI_BF16 || (a->residual && a->residual_dtype > MSI_BF16))
-        return bad("unknown dtype");
+        return "unknown dtype";
     if (a->K < 8 || a->K % 8 || a->K > MOST_STRIDE)
-        return bad("K must be a multiple of 8, 8 .. 2^21");
+        return "K must be a multiple of 8, 8 .. 2^21";
     if (a->M > MOST || a->N > MOST || uint64_t(a->M) * a->N > MOST_OUTPUTS)
-        return bad("M and N must be at most 2^29, M * N at most 2^36");
+        return "M and N must be at most 2^29, M * N at most 2^36";
     if (a->M == 0 || a->N == 0)
-        return MSI_OK;
+        return nullptr;
     if (!rows_ok(a->x, a->x_stride, a->K))
-        return bad("x needs 16-byte aligned rows of K, a stride that is a multiple of 8 up to 2^21");
+        return "x needs 16-byte aligned rows of K, a stride that is a multiple of 8 up to 2^21";
     if (!a->w || !aligned(a->w, 16))
-        return bad("w must be a 16-byte aligned [N, K]");
+        return "w must be a 16-byte aligned [N, K]";
     const size_t ob = a->out_dtype == MSI_F32 ? 4 : 2, rb = a->residual_dtype == MSI_F32 ? 4 : 2;
     if (!a->out || !aligned(a->out, ob) || a->out_stride < a->N || a->out_stride > MOST)
-        return bad("out needs rows of N, aligned to its type, a stride up to 2^29");
+        return "out needs rows of N, aligned to its type, a stride up to 2^29";
     if (a->residual && (!aligned(a->residual, rb) || a->residual_stride < a->N || a->residual_stride > MOST))
-        return bad("residual needs rows of N, aligned to its type, a stride up to 2^29");
+        return "residual needs rows of N, aligned to its type, a stride up to 2^29";
     if (a->residual == a->out && (a->residual_dtype != a->out_dtype || a->residual_stride != a->out_stride))
-        return bad("a residual that is out needs its type and stride");
+        return "a residual that is out needs its type and stride";
     if (a->out == a->x || a->out == a->w)
-        return bad("out must not be x or w");
+        return "out must not be x or w";
     if (!aligned(a->bias, 4))
-        return bad("bias must be 4-byte aligned");
-    LinearArgs l{};
+        return "bias must be 4-byte aligned";
     l.x = static_cast<const uint16_t *>(a->x);
     l.w = static_cast<const uint16_t *>(a->w);
     l.bias = a->bias;
@@ -166,7 +156,55 @@ msi_status msi_linear(const msi_linear_args *a, void *stream)
     l.M = int(a->M);
     l.N = int(a->N);
     l.K = int(a->K);
+    go = true;
+    return nullptr;
+}
+
+// bytes of the log-sums that follow the cut's workspace
+size_t lse_bytes(const AttentionCut &cut, const KvSeqs &s, uint32_t n_q_heads, uint32_t mass_rows)
+{
+    return mass_rows && !cut.few ? size_t(s.n_rows) * n_q_heads * sizeof(float) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+msi_status msi_linear(const msi_linear_args *a, void *stream)
+{
+    LinearArgs l{};
+    bool go = false;
+    if (const char *e = view_linear(a, l, go))
+        return bad(e);
+    if (!go)
+        return MSI_OK;
     return launched(launch_linear(l, int(a->activation), static_cast<hipStream_t>(stream)));
+}
+
+msi_status msi_linear_q4(const msi_linear_q4_args *a, void *stream)
+{
+    if (!a)
+        return bad("null arguments");
+    if (a->group != 32 && a->group != 64 && a->group != 128)
+        return bad("group must be 32, 64 or 128");
+    if (a->linear.K == 0 || a->linear.K % a->group)
+        return bad("K must be a multiple of group");
+    if (a->reserved)
+        return bad("reserved must be 0");
+    LinearQ4Args q{};
+    bool go = false;
+    if (const char *e = view_linear(&a->linear, q.l, go))
+        return bad(e);
+    if (!go)
+        return MSI_OK;
+    if (!a->scales || !aligned(a->scales, 2))
+        return bad("scales must be a 2-byte aligned [N, K / group]");
+    if (a->linear.out == a->scales)
+        return bad("out must not be scales");
+    q.codes = static_cast<const uint8_t *>(a->linear.w);
+    q.scales = static_cast<const uint16_t *>(a->scales);
+    q.group = int(a->group);
+    return launched(launch_linear_q4(q, int(a->linear.activation), static_cast<hipStream_t>(stream)));
 }
 
 msi_status msi_debug_linear_tile(uint32_t M, uint32_t N, uint32_t *rows, uint32_t *features, uint32_t *per_cu)

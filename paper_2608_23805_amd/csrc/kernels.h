@@ -309,6 +309,15 @@ struct LinearTile {
 };
 LinearTile linear_tile(int64_t M, int64_t N);   // the tiles that M rows and N features are cut into
 
+// ---- projection with 4-bit weights (linear_q4.hip)
+struct LinearQ4Args {
+    LinearArgs l;                // (w unused)
+    const uint8_t *codes;        // [N, K / 2]
+    const uint16_t *scales;      // [N, K / group] fp16
+    int group;                   // 32, 64 or 128, K a multiple
+};
+hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st);
+
 // ---- paged 8-bit cache of keys and values (kv_cache.hip); strides in elements, fmt KV_E4M3 or KV_INT8
 hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,
                             int64_t k_stride, int64_t v_stride, uint32_t *status, hipStream_t st);
