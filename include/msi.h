@@ -549,6 +549,39 @@ typedef struct {
 msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,
                          uint64_t k_stride, uint64_t v_stride, uint32_t *status, void *stream);
 
+/* msi_kv_append with queries and keys rotated by their positions on the way.  The
+ * pair i of the first rot_dim elements of a head -- (i, i + rot_dim / 2), or (2i,
+ * 2i + 1) with `interleaved` -- turns by the angle positions[axis[i], row] *
+ * frequency i: (a, b) -> (a cos - b sin, b cos + a sin) in fp32, rounded to bf16.
+ * q_out receives the queries (it may be q, with q's stride; otherwise it must not
+ * overlap an input), the cache what msi_kv_append makes of the rotated keys and
+ * of v; a pair with an infinity or NaN may become NaN.  Rows that belong to no
+ * sequence, or to one that is left out, stay as they were in q_out.  Positions
+ * are any 32-bit integers and need not be those of the tokens in the cache, whose
+ * order an eviction changes.  freq[i] is frequency i in turns (radians over 2
+ * pi), its fraction in units of 2^-64, so that the angle is right to 2^-33 turns
+ * however far the position. */
+typedef struct {
+    const void *q;               /* [n_rows, n_q_heads, head_dim] bf16, or NULL        */
+    void *q_out;                 /* the same shape                                     */
+    const void *k, *v;           /* as msi_kv_append's                                 */
+    uint64_t q_stride, q_out_stride, k_stride, v_stride;   /* elements, multiples of 8 */
+    uint32_t n_q_heads;          /* <= 4096; not read with q NULL                      */
+    uint32_t rot_dim;            /* a multiple of 16, 16 .. head_dim                   */
+    uint32_t n_axes;             /* positions of a row, 1 .. 4                         */
+    uint32_t interleaved;        /* 0 or 1                                             */
+    const uint64_t *freq;        /* device, [rot_dim / 2]                              */
+    const uint8_t *axis;         /* device, [rot_dim / 2], 8-byte aligned: the position that
+                                    turns a pair (n_axes and above: the last); NULL: the first */
+    const int32_t *positions;    /* device, [n_axes, n_rows]                           */
+    uint64_t position_stride;    /* elements from one axis to the next, >= n_rows, <= 2^32 */
+    uint32_t *status;
+} msi_kv_append_rotary_args;
+
+/* Errors: MSI_E_INVALID_ARG, MSI_E_DEVICE. */
+msi_status msi_kv_append_rotary(const msi_kv_cache *cache, const msi_kv_seqs *seqs,
+                                const msi_kv_append_rotary_args *args, void *stream);
+
 /* The last n tokens of every sequence as bf16: code * scale, exact for scales
  * that msi_kv_append or msi_kv_evict wrote.  Arguments as msi_kv_append's. */
 msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void *k, void *v, uint64_t k_stride,

@@ -139,6 +139,13 @@ class msi_kv_seqs(ctypes.Structure):
     reserved = property(lambda s: s.flags, lambda s, v: setattr(s, "flags", v))      # the word's name before it had flags
 
 
+class msi_kv_append_rotary_args(ctypes.Structure):
+    _fields_ = [("q", _vp), ("q_out", _vp), ("k", _vp), ("v", _vp), ("q_stride", _u64), ("q_out_stride", _u64),
+                ("k_stride", _u64), ("v_stride", _u64), ("n_q_heads", _u32), ("rot_dim", _u32), ("n_axes", _u32),
+                ("interleaved", _u32), ("freq", _vp), ("axis", _vp), ("positions", _vp), ("position_stride", _u64),
+                ("status", _vp)]
+
+
 class msi_kv_attention_args(ctypes.Structure):
     _fields_ = [("q", _vp), ("out", _vp), ("q_stride", _u64), ("out_stride", _u64), ("n_q_heads", _u32),
                 ("scale", ctypes.c_float), ("mass_rows", _u32), ("mass_decay", ctypes.c_float), ("workspace", _vp),
@@ -166,7 +173,7 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_slot_hold", "msi_slot_unhold", "msi_slot_query", "msi_plan_stats",
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
            "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear", "msi_linear_q4",
-           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
+           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_append_rotary", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
            "msi_kv_evict"]
 
 
@@ -224,6 +231,7 @@ def _load():
         getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
     L.msi_kv_attention_workspace.argtypes = [_vp, _vp, _u32, _u32, P(_u64)]
     L.msi_kv_attention.argtypes = [_vp, _vp, _vp, _vp]
+    L.msi_kv_append_rotary.argtypes = [_vp, _vp, _vp, _vp]
     L.msi_kv_evict.argtypes = [_vp, _vp, _vp, _vp]
     L.msi_stream_threshold.argtypes = [_u32]
     L.msi_stream_threshold.restype = _u32
@@ -527,7 +535,8 @@ class Plan:
 
 # The attention block's operators (projections, the paged 8-bit cache, its attention and eviction) live in
 # ``attention``, which imports torch; they are found here by name.
-_ATTENTION = ("linear", "linear_q4", "KvCache", "KvSeqs", "kv_append", "kv_read", "kv_attention_workspace_size",
+_ATTENTION = ("linear", "linear_q4", "KvCache", "KvSeqs", "kv_append", "KvRotary", "kv_append_rotary", "kv_read",
+              "kv_attention_workspace_size",
               "kv_attention_workspace", "kv_attention", "kv_evict", "AttentionBlock")
 
 

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libmsi.so")
 ARCH = "gfx950"
 
 SOURCES = ["plan_core.cpp", "source.cpp", "route.hip", "experts.hip", "tiles.hip", "experts_q4.hip", "experts_kq.hip", "combine.hip", "worklist.hip", "linear.hip", "linear_q4.hip",
-           "kv_cache.hip", "kv_attention.hip", "attention_abi.hip", "msi_abi.hip"]
+           "kv_cache.hip", "kv_rotary.hip", "kv_attention.hip", "attention_abi.hip", "msi_abi.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result",

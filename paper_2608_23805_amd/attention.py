@@ -11,14 +11,16 @@ tensors; a call whose tensors lie on several devices is refused."""
 from __future__ import annotations
 
 import ctypes
+import fractions
+import math
 import struct
 from typing import Optional
 
 import torch
 
 from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK,
-               MSI_OK, MsiError, lib, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args, msi_kv_seqs, msi_linear_args,
-               msi_linear_q4_args, _check)
+               MSI_OK, MsiError, lib, msi_kv_append_rotary_args, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args,
+               msi_kv_seqs, msi_linear_args, msi_linear_q4_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
 _F16 = (torch.float16, torch.int16)              # likewise fp16
@@ -26,8 +28,10 @@ _F32, _I32 = torch.float32, torch.int32
 _pack_linear = struct.Struct("<5Q6I3Q")
 _pack_q4 = struct.Struct("<Q2I")
 _pack_attention = struct.Struct("<4QIfIf3Q")
+_pack_rotary = struct.Struct("<8Q4I5Q")
 _pack_evict = struct.Struct("<4I4Q")
-for _s, _c in ((_pack_linear, msi_linear_args), (_pack_attention, msi_kv_attention_args), (_pack_evict, msi_kv_evict_args)):
+for _s, _c in ((_pack_linear, msi_linear_args), (_pack_attention, msi_kv_attention_args), (_pack_evict, msi_kv_evict_args),
+               (_pack_rotary, msi_kv_append_rotary_args)):
     assert _s.size == ctypes.sizeof(_c)
 assert _pack_linear.size + _pack_q4.size == ctypes.sizeof(msi_linear_q4_args)
 
@@ -242,6 +246,78 @@ def kv_append(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
     H, dev = cache.n_heads, cache.device
     ks, vs = _rows(cache, seqs, "k", k, H), _rows(cache, seqs, "v", v, H)
     _call(dev, lib.msi_kv_append, cache._ref, seqs._ref, k.data_ptr(), v.data_ptr(), ks, vs, _status(status, dev),
+          _stream(stream, dev))
+
+
+_TWO_PI = fractions.Fraction(6283185307179586476925286766559005768394338798750, 10 ** 48)     # to 48 places
+
+
+class KvRotary:
+    """How positions rotate queries and keys (the constant part of msi_kv_append_rotary's arguments).
+
+    inv_freq: the frequencies, radians for each position; pair i of a head's first 2 len(inv_freq) elements turns by
+    position * inv_freq[i], the pairs being (i, i + len(inv_freq)) or, ``interleaved``, (2 i, 2 i + 1).  ``axes`` gives
+    the pairs' axes for rows with several positions (time, height, width): a list as long as inv_freq, of 0 .. 3."""
+
+    def __init__(self, inv_freq, axes=None, interleaved: bool = False, device="cuda"):
+        f = [float(x) for x in inv_freq]
+        if len(f) % 8 or not 8 <= len(f) <= 128:
+            _refuse(f"inv_freq must hold a multiple of 8 frequencies, 8 .. 128, got {len(f)}")
+        if not all(math.isfinite(x) for x in f):
+            _refuse("inv_freq must be finite")
+        a = None if axes is None else [int(x) for x in axes]
+        if a is not None and (len(a) != len(f) or min(a) < 0 or max(a) > 3):
+            _refuse("axes must be as many as the frequencies, 0 .. 3")
+        # fractions of a turn in units of 2^-64, to the nearest
+        turns = [round(fractions.Fraction(x) / _TWO_PI * 2 ** 64) % 2 ** 64 for x in f]
+        self.rot_dim, self.interleaved = 2 * len(f), bool(interleaved)
+        self.n_axes = 1 if a is None else max(a) + 1
+        self.freq = torch.tensor([t - (t >> 63 << 64) for t in turns], dtype=torch.int64).to(device)
+        self.axis = None if self.n_axes == 1 else torch.tensor(a, dtype=torch.uint8).to(device)
+        self.device = self.freq.device
+        self._freq, self._axis = self.freq.data_ptr(), 0 if self.axis is None else self.axis.data_ptr()
+
+
+def _positions(rotary: KvRotary, positions, n: int, device) -> int:
+    """Stride from one axis of the positions to the next."""
+    if rotary.device != device:
+        _refuse(f"rotary must be on {device}, got {rotary.device}")
+    if positions is None:
+        _refuse("positions are needed")
+    shape = positions.shape
+    if positions.dtype != _I32 or positions.device != device or shape[-1:] != (n,) or positions.dim() > 2 or \
+            (shape[0] if positions.dim() == 2 else 1) != rotary.n_axes:
+        _refuse(f"positions must be int32 [{rotary.n_axes}, {n}] on {device}, got {tuple(shape)} {positions.dtype} on "
+                f"{positions.device}")
+    if n > 1 and positions.stride(-1) != 1:
+        _refuse("an axis of positions must be contiguous")
+    step = positions.stride(0) if positions.dim() == 2 and rotary.n_axes > 1 else n
+    if step < n:
+        _refuse("axes of positions must not overlap")
+    return step
+
+
+def kv_append_rotary(cache: KvCache, seqs: KvSeqs, rotary: KvRotary, positions, q, q_out, k, v, status=None, stream=None):
+    """kv_append with queries and keys rotated by their positions on the way (msi_kv_append_rotary).
+
+    positions int32 [rotary.n_axes, n_rows], or [n_rows] for one axis; q [n_rows, n_q_heads, head_dim] bf16 is rotated
+    into q_out (which may be q), or None; k, v [n_rows, n_heads, head_dim] bf16."""
+    _same_device(cache, seqs)
+    H, dev, n = cache.n_heads, cache.device, seqs.n_rows
+    step = _positions(rotary, positions, n, dev)
+    if rotary.rot_dim > cache.head_dim:
+        _refuse(f"{rotary.rot_dim} elements rotate, heads have {cache.head_dim}")
+    qp = op = qs = os_ = Hq = 0
+    if q is not None:
+        if q.dim() != 3:
+            _refuse("q must be [n_rows, n_q_heads, head_dim]")
+        Hq = q.shape[1]
+        qs, os_ = _rows(cache, seqs, "q", q, Hq), _rows(cache, seqs, "q_out", q_out, Hq)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    ks, vs = _rows(cache, seqs, "k", k, H), _rows(cache, seqs, "v", v, H)
+    _call(dev, lib.msi_kv_append_rotary, cache._ref, seqs._ref,
+          _pack_rotary.pack(qp, op, k.data_ptr(), v.data_ptr(), qs, os_, ks, vs, Hq, rotary.rot_dim, rotary.n_axes,
+                            rotary.interleaved, rotary._freq, rotary._axis, positions.data_ptr(), step, _status(status, dev)),
           _stream(stream, dev))
 
 

@@ -235,6 +235,58 @@ msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, con
                                      static_cast<hipStream_t>(stream)));
 }
 
+msi_status msi_kv_append_rotary(const msi_kv_cache *cache, const msi_kv_seqs *seqs,
+                                const msi_kv_append_rotary_args *a, void *stream)
+{
+    RotaryAppend A{};
+    bool go = false;
+    if (!a)
+        return bad("null arguments");
+    if (const char *e = view_rows(cache, seqs, a->k, a->v, a->k_stride, a->v_stride, a->status, A.c, A.s, go))
+        return bad(e);
+    if (a->rot_dim < 16 || a->rot_dim % 16 || a->rot_dim > uint32_t(A.c.D))
+        return bad("rot_dim must be a multiple of 16, 16 .. head_dim");
+    if (a->n_axes < 1 || a->n_axes > 4)
+        return bad("n_axes must be 1 .. 4");
+    if (a->interleaved > 1)
+        return bad("interleaved must be 0 or 1");
+    if (a->q && (a->n_q_heads < 1 || a->n_q_heads > 4096))
+        return bad("n_q_heads must be 1 .. 4096");
+    if (!go)
+        return MSI_OK;
+    if (!a->freq || !aligned(a->freq, 8) || !aligned(a->axis, 8))
+        return bad("freq and axis must be 8-byte aligned, freq not null");
+    if (!a->positions || !aligned(a->positions, 4) || a->position_stride > (uint64_t(1) << 32) ||
+        (a->n_axes > 1 && a->position_stride < uint64_t(A.s.n_rows)))
+        return bad("positions must be a 4-byte aligned [n_axes, n_rows], their stride at least n_rows, at most 2^32");
+    if (a->q) {
+        const uint64_t least = uint64_t(a->n_q_heads) * A.c.D;
+        if (!rows_ok(a->q, a->q_stride, least) || !rows_ok(a->q_out, a->q_out_stride, least))
+            return bad("q and q_out need 16-byte aligned rows of n_q_heads * head_dim, strides a multiple of 8 up to 2^21");
+        if (a->q == a->q_out && a->q_stride != a->q_out_stride)
+            return bad("a q_out that is q needs its stride");
+        if (a->q_out == a->k || a->q_out == a->v)
+            return bad("q_out must not be k or v");
+    }
+    A.q = static_cast<const uint16_t *>(a->q);
+    A.q_out = static_cast<uint16_t *>(a->q_out);
+    A.k = static_cast<const uint16_t *>(a->k);
+    A.v = static_cast<const uint16_t *>(a->v);
+    A.q_stride = int64_t(a->q_stride);
+    A.q_out_stride = int64_t(a->q_out_stride);
+    A.k_stride = int64_t(a->k_stride);
+    A.v_stride = int64_t(a->v_stride);
+    A.n_q_heads = int(a->n_q_heads);
+    A.rot = int(a->rot_dim);
+    A.n_axes = int(a->n_axes);
+    A.freq = a->freq;
+    A.axis = a->axis;
+    A.positions = a->positions;
+    A.position_stride = int64_t(a->position_stride);
+    A.status = a->status;
+    return launched(launch_kv_append_rotary(A, int(cache->format), a->interleaved != 0, static_cast<hipStream_t>(stream)));
+}
+
 msi_status msi_kv_read(const msi_kv_cache *cache, const msi_kv_seqs *seqs, void *k, void *v, uint64_t k_stride,
                        uint64_t v_stride, uint32_t *status, void *stream)
 {

@@ -321,6 +321,23 @@ hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st);
 // ---- paged 8-bit cache of keys and values (kv_cache.hip); strides in elements, fmt KV_E4M3 or KV_INT8
 hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,
                             int64_t k_stride, int64_t v_stride, uint32_t *status, hipStream_t st);
+// the same with queries and keys rotated on the way (kv_rotary.hip)
+struct RotaryAppend {
+    KvCache c;
+    KvSeqs s;
+    const uint16_t *q, *k, *v;   // q: null for none
+    uint16_t *q_out;             // may be q
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+    int n_q_heads;
+    int rot, n_axes;             // elements of a head that rotate (a multiple of 16), positions of a row
+    const uint64_t *freq;        // [rot / 2] turns per position in units of 2^-64
+    const uint8_t *axis;         // [rot / 2] or null
+    const int32_t *positions;    // [n_axes, n_rows]
+    int64_t position_stride;
+    int q_rows, q_heads;         // rows of a pass and heads of a workgroup of the queries (launch_kv_append_rotary sets them)
+    uint32_t *status;
+};
+hipError_t launch_kv_append_rotary(RotaryAppend A, int fmt, bool interleaved, hipStream_t st);
 hipError_t launch_kv_read(const KvCache &c, int fmt, const KvSeqs &s, uint16_t *k, uint16_t *v, int64_t k_stride,
                           int64_t v_stride, uint32_t *status, hipStream_t st);
 hipError_t launch_kv_evict(const KvCache &c, int fmt, const KvSeqs &s, const int32_t *dst_table, int dst_blocks,

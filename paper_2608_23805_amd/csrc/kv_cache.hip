@@ -24,15 +24,6 @@ struct RowChunks {
     static constexpr int N = KV_BLOCK / ROWS;     // passes over a block
 };
 
-__device__ __forceinline__ void unpack_bf16x8(const u32x4 &w, float (&x)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
-
 // ---------------------------------------------------------------- append
 //
 // One workgroup per (block, K or V, head, sequence) that receives rows.  Its new

@@ -20,6 +20,15 @@ __device__ __forceinline__ void kv_raise(uint32_t *status, uint32_t bits)
         atomicOr(status, bits);
 }
 
+__device__ __forceinline__ void unpack_bf16x8(const u32x4 &w, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+
 // Four codes of a word as floats.
 template <int FMT>
 __device__ __forceinline__ f32x4 kv_unpack4(uint32_t w)
