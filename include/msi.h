@@ -622,6 +622,35 @@ msi_status msi_kv_attention_workspace(const msi_kv_cache *cache, const msi_kv_se
 msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_attention_args *args,
                             void *stream);
 
+/* Groups of neighbouring sequences that hold the same first pages: group i is the
+ * sequences cu_seqs[i] .. cu_seqs[i + 1] - 1, whose tables start with the same
+ * blocks[i] pages.  The arrays are on the device, the host's bounds size the
+ * launches.  Sequences of no group share nothing. */
+typedef struct {
+    uint32_t n_groups;           /* <= 65535                                           */
+    uint32_t max_rows;           /* bound of a group's rows                            */
+    uint32_t max_blocks;         /* bound of blocks                                    */
+    uint32_t reserved;           /* 0                                                  */
+    const int32_t *cu_seqs;      /* [n_groups + 1] ascending                           */
+    const int32_t *blocks;       /* [n_groups]                                         */
+} msi_kv_groups;
+
+/* msi_kv_attention where sequences share their first pages, which are read once
+ * for all rows of a group, from the table of its first sequence.  The result is
+ * msi_kv_attention's up to the order of its sums; equal calls give equal bits.
+ * Shared pages serve rows behind them: a sequence of a group some of whose rows
+ * stand inside them (len - n < 64 blocks) is attended by itself, with all the pages
+ * of its own table.  So are, with MSI_KV_BAD_LENGTH, the sequences of a group
+ * whose numbers break a bound, and all of them where cu_seqs falls or leaves 0 .. n_seqs.
+ * (Where cu_rows falls, sequences may be left out.)  args->mass_rows must be 0.
+ * The workspace is never empty.  max_rows of a group times the heads that share a
+ * cache head is at most 2^29, max_rows of a sequence times n_q_heads under 2^24. */
+msi_status msi_kv_attention_shared_workspace(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_groups *groups,
+                                             uint32_t n_q_heads, uint64_t *bytes);
+/* Errors: MSI_E_INVALID_ARG, MSI_E_NOMEM (workspace), MSI_E_DEVICE. */
+msi_status msi_kv_attention_shared(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_groups *groups,
+                                   const msi_kv_attention_args *args, void *stream);
+
 /* Cut every sequence back to at most `budget` tokens a head: its first `sinks`
  * and last `recent` tokens, and of the others those with the largest mass
  * (equal ones from the lowest index on; NaN below everything), in ascending

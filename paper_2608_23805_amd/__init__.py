@@ -152,6 +152,11 @@ class msi_kv_attention_args(ctypes.Structure):
                 ("workspace_bytes", _u64), ("status", _vp)]
 
 
+class msi_kv_groups(ctypes.Structure):
+    _fields_ = [("n_groups", _u32), ("max_rows", _u32), ("max_blocks", _u32), ("reserved", _u32), ("cu_seqs", _vp),
+                ("blocks", _vp)]
+
+
 class msi_kv_evict_args(ctypes.Structure):
     _fields_ = [("budget", _u32), ("sinks", _u32), ("recent", _u32), ("dst_blocks", _u32), ("dst_table", _vp),
                 ("new_lens", _vp), ("keep", _vp), ("status", _vp)]
@@ -174,7 +179,7 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
            "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear", "msi_linear_q4",
            "msi_debug_linear_tile", "msi_kv_append", "msi_kv_append_rotary", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
-           "msi_kv_evict"]
+           "msi_kv_attention_shared_workspace", "msi_kv_attention_shared", "msi_kv_evict"]
 
 
 class MsiError(RuntimeError):
@@ -231,6 +236,8 @@ def _load():
         getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
     L.msi_kv_attention_workspace.argtypes = [_vp, _vp, _u32, _u32, P(_u64)]
     L.msi_kv_attention.argtypes = [_vp, _vp, _vp, _vp]
+    L.msi_kv_attention_shared_workspace.argtypes = [_vp, _vp, _vp, _u32, P(_u64)]
+    L.msi_kv_attention_shared.argtypes = [_vp, _vp, _vp, _vp, _vp]
     L.msi_kv_append_rotary.argtypes = [_vp, _vp, _vp, _vp]
     L.msi_kv_evict.argtypes = [_vp, _vp, _vp, _vp]
     L.msi_stream_threshold.argtypes = [_u32]
@@ -537,7 +544,8 @@ class Plan:
 # ``attention``, which imports torch; they are found here by name.
 _ATTENTION = ("linear", "linear_q4", "KvCache", "KvSeqs", "kv_append", "KvRotary", "kv_append_rotary", "kv_read",
               "kv_attention_workspace_size",
-              "kv_attention_workspace", "kv_attention", "kv_evict", "AttentionBlock")
+              "kv_attention_workspace", "kv_attention", "KvGroups", "kv_attention_shared_workspace_size",
+              "kv_attention_shared_workspace", "kv_attention_shared", "kv_evict", "AttentionBlock")
 
 
 def __getattr__(name: str):

@@ -20,7 +20,7 @@ import torch
 
 from . import (ACTIVATIONS, KV_ALL_ROWS, KV_FORMATS, MSI_BF16, MSI_E_INVALID_ARG, MSI_E_NOMEM, MSI_F32, MSI_KV_BLOCK,
                MSI_OK, MsiError, lib, msi_kv_append_rotary_args, msi_kv_attention_args, msi_kv_cache, msi_kv_evict_args,
-               msi_kv_seqs, msi_linear_args, msi_linear_q4_args, _check)
+               msi_kv_groups, msi_kv_seqs, msi_linear_args, msi_linear_q4_args, _check)
 
 _BF16 = (torch.bfloat16, torch.int16)            # bf16 tensors, or their bits
 _F16 = (torch.float16, torch.int16)              # likewise fp16
@@ -345,12 +345,9 @@ def kv_attention_workspace(cache: KvCache, seqs: KvSeqs, n_q_heads: int, mass_ro
                        device=cache.device)
 
 
-def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: int = 0, mass_decay: float = 1.0,
-                 workspace=None, status=None, stream=None, all_rows: bool = False):
-    """Attention of q [n_rows, n_q_heads, head_dim] bf16 over the sequences' pages into out (msi_kv_attention).
-
-    all_rows: every row of out is written, with zeros where no sequence answers for it (MSI_KV_ALL_ROWS)."""
-    _same_device(cache, seqs)
+def _attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: int, mass_decay: float, workspace, status,
+               all_rows: bool):
+    """The sequences and arguments of an attention call."""
     if q.dim() != 3:
         _refuse("q must be [n_rows, n_q_heads, head_dim]")
     if mass_rows < 0:
@@ -369,9 +366,64 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
         c = msi_kv_seqs.from_buffer_copy(seqs.c)
         c.flags |= KV_ALL_ROWS
         ref = ctypes.byref(c)
-    _call(dev, lib.msi_kv_attention, cache._ref, ref,
-          _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30),
-                               mass_decay if mass_rows else 0.0, wp, wn, _status(status, dev)), _stream(stream, dev))
+    return ref, _pack_attention.pack(q.data_ptr(), out.data_ptr(), qs, os_, Hq, scale, min(mass_rows, 1 << 30),
+                                     mass_decay if mass_rows else 0.0, wp, wn, _status(status, dev))
+
+
+def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: int = 0, mass_decay: float = 1.0,
+                 workspace=None, status=None, stream=None, all_rows: bool = False):
+    """Attention of q [n_rows, n_q_heads, head_dim] bf16 over the sequences' pages into out (msi_kv_attention).
+
+    all_rows: every row of out is written, with zeros where no sequence answers for it (MSI_KV_ALL_ROWS)."""
+    _same_device(cache, seqs)
+    ref, args = _attention(cache, seqs, q, out, scale, mass_rows, mass_decay, workspace, status, all_rows)
+    _call(cache.device, lib.msi_kv_attention, cache._ref, ref, args, _stream(stream, cache.device))
+
+
+class KvGroups:
+    """Groups of neighbouring sequences that hold the same first pages (msi_kv_groups): first sequence of every group
+    [n_groups + 1] and shared blocks [n_groups] in device int32 tensors, whose contents may change between calls, and the
+    host's bounds: ``max_rows`` rows of a group, ``max_blocks`` shared blocks."""
+
+    def __init__(self, cu_seqs, blocks, *, max_rows: int, max_blocks: int):
+        dev = blocks.device
+        if blocks.dim() != 1:
+            _refuse("blocks must be [n_groups]")
+        n = blocks.shape[0]
+        _dense("blocks", blocks, _I32, dev)
+        _dense("cu_seqs", cu_seqs, _I32, dev, (n + 1,))
+        self.cu_seqs, self.blocks, self.n_groups, self.device = cu_seqs, blocks, n, dev
+        self.max_rows, self.max_blocks = int(max_rows), int(max_blocks)
+        if min(self.max_rows, self.max_blocks) < 0 or max(self.max_rows, self.max_blocks) >= 1 << 31:
+            _refuse("max_rows and max_blocks must be 0 .. 2^31 - 1")
+        self.c = msi_kv_groups(n, self.max_rows, self.max_blocks, 0, cu_seqs.data_ptr(), blocks.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+
+def kv_attention_shared_workspace_size(cache: KvCache, seqs: KvSeqs, groups: KvGroups, n_q_heads: int) -> int:
+    """Bytes of workspace of kv_attention_shared calls with these bounds."""
+    n = ctypes.c_uint64()
+    if n_q_heads < 0:
+        _refuse("n_q_heads must not be negative")
+    _check(lib.msi_kv_attention_shared_workspace(cache._ref, seqs._ref, groups._ref, n_q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def kv_attention_shared_workspace(cache: KvCache, seqs: KvSeqs, groups: KvGroups, n_q_heads: int):
+    """Workspace of kv_attention_shared calls with these bounds (a uint8 tensor)."""
+    return torch.empty(kv_attention_shared_workspace_size(cache, seqs, groups, n_q_heads), dtype=torch.uint8,
+                       device=cache.device)
+
+
+def kv_attention_shared(cache: KvCache, seqs: KvSeqs, groups: KvGroups, q, out, scale: float, workspace=None, status=None,
+                        stream=None, all_rows: bool = False):
+    """kv_attention of sequences that share their first pages, each of which is read once for its group
+    (msi_kv_attention_shared).  The workspace is kv_attention_shared_workspace's."""
+    _same_device(cache, seqs)
+    if groups.device != cache.device:
+        _refuse("cache and groups must be on one device")
+    ref, args = _attention(cache, seqs, q, out, scale, 0, 0.0, workspace, status, all_rows)
+    _call(cache.device, lib.msi_kv_attention_shared, cache._ref, ref, groups._ref, args, _stream(stream, cache.device))
 
 
 def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget: int, sinks: int = 0, recent: int = 0,

@@ -107,6 +107,32 @@ const char *check_heads(const KvCache &c, const KvSeqs &s, uint32_t n_q_heads)
     return nullptr;
 }
 
+// Groups of a call and how it is cut; nullptr if the call may go on, else what is wrong.
+const char *view_groups(const msi_kv_groups *g, const KvCache &c, const KvSeqs &s, uint32_t n_q_heads, KvGroups &out, SharedCut &cut)
+{
+    if (!g)
+        return "null groups";
+    if (g->n_groups > 65535)
+        return "n_groups must be at most 65535";
+    if (g->reserved)
+        return "reserved must be 0";
+    if (g->n_groups && (!g->cu_seqs || !g->blocks))
+        return "null group array";
+    if (!aligned(g->cu_seqs, 4) || !aligned(g->blocks, 4))
+        return "group arrays must be 4-byte aligned";
+    const uint64_t G = n_q_heads / uint32_t(c.H);
+    const uint32_t max_rows = std::min(g->max_rows, uint32_t(s.n_rows)), max_blocks = std::min(g->max_blocks, uint32_t(s.max_blocks));
+    if (max_rows * G > MOST)
+        return "a group's max_rows times the heads of a cache head must be at most 2^29";
+    if (uint64_t(s.max_rows) * n_q_heads >= MOST_GROUPS)
+        return "max_rows times n_q_heads must be under 2^24";
+    out = KvGroups{g->cu_seqs, g->blocks, int(g->n_groups), int(max_rows), int(max_blocks)};
+    cut = shared_cut(s, out, c.H, int(G), c.D);
+    if ((uint64_t(cut.items_p) + uint64_t(cut.items_s)) * uint64_t(c.H) >= MOST_GROUPS)
+        return "the groups' and sequences' row tiles times n_heads must be under 2^24";
+    return nullptr;
+}
+
 // A projection's arguments as the kernels take them; go: there is work.
 const char *view_linear(const msi_linear_args *a, LinearArgs &l, bool &go)
 {
@@ -158,6 +184,52 @@ const char *view_linear(const msi_linear_args *a, LinearArgs &l, bool &go)
     l.K = int(a->K);
     go = true;
     return nullptr;
+}
+
+// What attention calls have in common: their views, and scale, status, q and out; go: there are rows to attend, rest:
+// there are rows to clear.
+const char *view_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_attention_args *a, AttentionLaunch &A,
+                           bool &go, bool &rest)
+{
+    if (!a)
+        return "null arguments";
+    if (const char *e = view_cache(cache, A.c))
+        return e;
+    if (const char *e = view_seqs(seqs, true, A.s))
+        return e;
+    if (const char *e = check_heads(A.c, A.s, a->n_q_heads))
+        return e;
+    A.scale_log2 = float(double(a->scale) * 1.4426950408889634);
+    if (!std::isfinite(A.scale_log2))
+        return "scale must be finite, under 2^127";
+    if (!aligned(a->status, 4))
+        return STATUS_TEXT;
+    if (a->mass_rows && !A.c.mass)
+        return "mass_rows needs the cache's mass";
+    if (a->mass_rows && !(a->mass_decay >= 0.0f && std::isfinite(a->mass_decay)))
+        return "mass_decay must be finite and not negative";
+    go = A.s.S && A.s.max_rows;
+    rest = A.s.all_rows && A.s.n_rows;
+    if (!go && !rest)
+        return nullptr;
+    const uint64_t least = uint64_t(a->n_q_heads) * A.c.D;
+    if (!rows_ok(a->q, a->q_stride, least) || !rows_ok(a->out, a->out_stride, least))
+        return "q and out need 16-byte aligned rows of n_q_heads * head_dim, strides a multiple of 8 up to 2^21";
+    if (a->q == a->out)
+        return "out must not be q";
+    A.q = static_cast<const uint16_t *>(a->q);
+    A.out = static_cast<uint16_t *>(a->out);
+    A.q_stride = int64_t(a->q_stride);
+    A.out_stride = int64_t(a->out_stride);
+    A.G = int(a->n_q_heads) / A.c.H;
+    A.part_rows = A.s.max_rows * A.G;
+    A.status = a->status;
+    return nullptr;
+}
+
+msi_status clear_all(const AttentionLaunch &A, hipStream_t st)
+{
+    return launched(launch_kv_rest(A.s, A.out, A.out_stride, A.c.H * A.G * A.c.D, st));
 }
 
 // bytes of the log-sums that follow the cut's workspace
@@ -327,56 +399,21 @@ msi_status msi_kv_attention_workspace(const msi_kv_cache *cache, const msi_kv_se
 msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_attention_args *a,
                             void *stream)
 {
-    KvCache c;
-    KvSeqs s;
-    if (!a)
-        return bad("null arguments");
-    if (const char *e = view_cache(cache, c))
+    AttentionLaunch A{};
+    bool go = false, rest = false;
+    if (const char *e = view_attention(cache, seqs, a, A, go, rest))
         return bad(e);
-    if (const char *e = view_seqs(seqs, true, s))
-        return bad(e);
-    if (const char *e = check_heads(c, s, a->n_q_heads))
-        return bad(e);
-    const float scale_log2 = float(double(a->scale) * 1.4426950408889634);
-    if (!std::isfinite(scale_log2))
-        return bad("scale must be finite, under 2^127");
-    if (!aligned(a->status, 4))
-        return bad(STATUS_TEXT);
-    if (a->mass_rows && !c.mass)
-        return bad("mass_rows needs the cache's mass");
-    if (a->mass_rows && !(a->mass_decay >= 0.0f && std::isfinite(a->mass_decay)))
-        return bad("mass_decay must be finite and not negative");
-    const bool go = s.S && s.max_rows, rest = s.all_rows && s.n_rows;
-    if (!go && !rest)
-        return MSI_OK;
-    const uint64_t least = uint64_t(a->n_q_heads) * c.D;
-    if (!rows_ok(a->q, a->q_stride, least) || !rows_ok(a->out, a->out_stride, least))
-        return bad("q and out need 16-byte aligned rows of n_q_heads * head_dim, strides a multiple of 8 up to 2^21");
-    if (a->q == a->out)
-        return bad("out must not be q");
     if (!go)
-        return launched(launch_kv_rest(s, static_cast<uint16_t *>(a->out), int64_t(a->out_stride), int(least),
-                                       static_cast<hipStream_t>(stream)));
-    const AttentionCut cut =
-        attention_cut(s.S, c.H, int(a->n_q_heads) / c.H, c.D, c.n_pages, s.max_rows, s.max_len, a->mass_rows != 0);
-    const size_t lse = lse_bytes(cut, s, a->n_q_heads, a->mass_rows), need = cut.bytes + lse;
+        return rest ? clear_all(A, static_cast<hipStream_t>(stream)) : MSI_OK;
+    const AttentionCut cut = attention_cut(A.s.S, A.c.H, A.G, A.c.D, A.c.n_pages, A.s.max_rows, A.s.max_len, a->mass_rows != 0);
+    const size_t lse = lse_bytes(cut, A.s, a->n_q_heads, a->mass_rows), need = cut.bytes + lse;
     if (need && (!a->workspace || a->workspace_bytes < need))
         return abi_error(MSI_E_NOMEM, "workspace smaller than msi_kv_attention_workspace says");
     if (!aligned(a->workspace, 16))
         return bad("workspace must be 16-byte aligned");
     uint8_t *ws = static_cast<uint8_t *>(a->workspace);
-    AttentionLaunch A{};
-    A.c = c;
-    A.s = s;
-    A.q = static_cast<const uint16_t *>(a->q);
-    A.out = static_cast<uint16_t *>(a->out);
-    A.q_stride = int64_t(a->q_stride);
-    A.out_stride = int64_t(a->out_stride);
-    A.G = int(a->n_q_heads) / c.H;
-    A.scale_log2 = scale_log2;
     A.direct = cut.direct;
     A.per = cut.per;
-    A.part_rows = s.max_rows * A.G;
     if (!cut.direct) {
         A.plan = reinterpret_cast<int2 *>(ws);
         A.part_ml = reinterpret_cast<float *>(ws + cut.part_ml);
@@ -389,8 +426,53 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
         A.lse = reinterpret_cast<float *>(ws + cut.bytes);
     A.mass_rows = int(std::min(a->mass_rows, MOST));
     A.decay = a->mass_decay;
-    A.status = a->status;
     return launched(launch_kv_attention(A, int(cache->format), cut, static_cast<hipStream_t>(stream)));
+}
+
+msi_status msi_kv_attention_shared_workspace(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_groups *groups,
+                                             uint32_t n_q_heads, uint64_t *bytes)
+{
+    KvCache c;
+    KvSeqs s;
+    KvGroups g;
+    SharedCut cut;
+    if (!bytes)
+        return bad("null bytes");
+    if (const char *e = view_cache(cache, c))
+        return bad(e);
+    if (const char *e = view_seqs(seqs, true, s))
+        return bad(e);
+    if (const char *e = check_heads(c, s, n_q_heads))
+        return bad(e);
+    if (const char *e = view_groups(groups, c, s, n_q_heads, g, cut))
+        return bad(e);
+    *bytes = cut.bytes;
+    return MSI_OK;
+}
+
+msi_status msi_kv_attention_shared(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_groups *groups,
+                                   const msi_kv_attention_args *a, void *stream)
+{
+    SharedLaunch A{};
+    bool go = false, rest = false;
+    if (const char *e = view_attention(cache, seqs, a, A, go, rest))
+        return bad(e);
+    if (const char *e = view_groups(groups, A.c, A.s, a->n_q_heads, A.g, A.cut))
+        return bad(e);
+    if (a->mass_rows)
+        return bad("mass_rows must be 0: a shared page has several sequences' weights");
+    if (!go)
+        return rest ? clear_all(A, static_cast<hipStream_t>(stream)) : MSI_OK;
+    if (!a->workspace || a->workspace_bytes < A.cut.bytes)
+        return abi_error(MSI_E_NOMEM, "workspace smaller than msi_kv_attention_shared_workspace says");
+    if (!aligned(a->workspace, 16))
+        return bad("workspace must be 16-byte aligned");
+    uint8_t *ws = static_cast<uint8_t *>(a->workspace);
+    A.owners = reinterpret_cast<KvOwner *>(ws);
+    A.first = reinterpret_cast<int32_t *>(ws + A.cut.first);
+    A.part_ml = reinterpret_cast<float *>(ws + A.cut.part_ml);
+    A.part_o = reinterpret_cast<float *>(ws + A.cut.part_o);
+    return launched(launch_kv_attention_shared(A, int(cache->format), static_cast<hipStream_t>(stream)));
 }
 
 msi_status msi_kv_evict(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const msi_kv_evict_args *a, void *stream)

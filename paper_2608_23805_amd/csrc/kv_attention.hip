@@ -22,6 +22,7 @@
 // rounding is 1.7e-3); their sum, the maxima, the scores and all accumulators
 // are fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_ring.h"
 #include "kernels.h"
@@ -189,16 +190,17 @@ __host__ __device__ __forceinline__ int rest_groups(const KvSeqs &s)
     return s.all_rows ? min((s.n_rows + REST_ROWS - 1) / REST_ROWS, MOST_REST) : 0;
 }
 
-// Rows 64 group .., 64 (group + groups) .. and so on; `words`: 8 words of LDS.
-__device__ __forceinline__ void clear_rest(const KvSeqs &s, uint16_t *__restrict__ out, int64_t stride, int width, int group,
-                                           int groups, uint32_t *words)
+// Rows 64 group .., 64 (group + groups) .. and so on; seq(i): sequence i; `words`: 8 words of LDS.
+template <typename Seq>
+__device__ __forceinline__ void clear_rest(const KvSeqs &s, Seq seq, uint16_t *__restrict__ out, int64_t stride, int width,
+                                           int group, int groups, uint32_t *words)
 {
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     for (int64_t first = int64_t(group) * REST_ROWS; first < s.n_rows; first += int64_t(groups) * REST_ROWS) {
         const int r0 = int(first), n = min(REST_ROWS, s.n_rows - r0);
         uint64_t rows = 0;
         for (int i = threadIdx.x; i < s.S; i += 256) {
-            const KvSeq q = kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, true);
+            const KvSeq q = seq(i);
             const int lo = max(q.row0 - r0, 0), hi = min(q.row0 - r0 + q.n, n);
             if (q.n > 0 && lo < hi)
                 rows |= (~uint64_t(0) >> (64 - (hi - lo))) << lo;
@@ -223,10 +225,73 @@ __device__ __forceinline__ void clear_rest(const KvSeqs &s, uint16_t *__restrict
     }
 }
 
+__device__ __forceinline__ void clear_rest(const KvSeqs &s, uint16_t *__restrict__ out, int64_t stride, int width, int group,
+                                           int groups, uint32_t *words)
+{
+    auto seq = [&](int i) {
+        return kv_check_seq(s.cu[i], s.cu[i + 1], s.lens[i], s.n_rows, s.max_rows, s.max_len, true);
+    };
+    clear_rest(s, seq, out, stride, width, group, groups, words);
+}
+
 __global__ void __launch_bounds__(256) kv_rest_kernel(KvSeqs s, uint16_t *out, int64_t stride, int width)
 {
     __shared__ uint32_t words[8];
     clear_rest(s, out, stride, width, int(blockIdx.x), int(gridDim.x), words);
+}
+
+// ---------------------------------------------------------------- forms
+//
+// What a kernel of units is compiled for: PLAIN; ALL, which clears other rows;
+// SHARED, whose units come from a list of owners (see below) and always leave
+// partial results.
+enum Form : int { PLAIN, ALL, SHARED };
+
+template <int FORM>
+using LaunchOf = std::conditional_t<FORM == SHARED, SharedLaunch, AttentionLaunch>;
+
+// One workgroup's share of a SHARED launch: a row tile and head of a unit.
+struct SharedItem {
+    KvSeq q;                                 // the owner's rows and tokens
+    int seq, h, tile, b0, b1;                // table, head, row tile, blocks
+    int64_t part;                            // partial result of its packed row 0
+    bool all, ok;
+};
+
+// The last of n ascending numbers that is at most `at` (the first is): 64 ways at a time.
+__device__ __forceinline__ int last_at_most(const int32_t *first, int n, int at)
+{
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    while (n > 1) {
+        const int run = (n + 63) >> 6, i = lane * run;
+        const int hit = __popcll(__ballot(i < n && first[base + min(i, n - 1)] <= at)) - 1;
+        base += hit * run;
+        n = min(run, n - hit * run);
+    }
+    return base;
+}
+
+__device__ __forceinline__ SharedItem find_item(const SharedLaunch &A)
+{
+    SharedItem it{};
+    const int n = A.g.n + A.s.S, H = A.c.H;
+    it.h = int(blockIdx.x) % H;
+    const int at = int(blockIdx.x) / H + (A.list == 1 ? A.first[A.g.n] : 0);
+    if (at >= A.first[A.list == 0 ? A.g.n : n])
+        return it;
+    const int o = __builtin_amdgcn_readfirstlane(last_at_most(A.first, n, at));
+    const KvOwner w = A.owners[o];
+    const int local = at - A.first[o], tiles = max(w.tiles, 1), unit = local / tiles;
+    it.ok = w.units > 0;
+    it.q = KvSeq{w.row0, w.n, w.len, true};
+    it.seq = w.seq;
+    it.tile = local % tiles;
+    it.b0 = w.b0 + int(int64_t(w.blocks) * unit / max(w.units, 1));
+    it.b1 = w.b0 + int(int64_t(w.blocks) * (unit + 1) / max(w.units, 1));
+    it.part = w.part + (int64_t(unit) * H + it.h) * (int64_t(w.n) * A.G);
+    it.all = w.all != 0;
+    return it;
 }
 
 // ---------------------------------------------------------------- few rows
@@ -297,8 +362,8 @@ struct FewRows {
     }
 };
 
-template <int FMT, int D, int RT, bool ALL>
-__global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel(AttentionLaunch A)
+template <int FMT, int D, int RT, int FORM>
+__global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel(LaunchOf<FORM> A)
 {
     using F = FewRows<FMT, D, RT>;
     constexpr int TOK = F::TOK, GT = F::GT, W = F::W, VW = F::VW, OS = F::OS;
@@ -308,24 +373,37 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     constexpr bool QLDS = D == 256 && RT == 2;               // two tiles of long queries do not fit the registers
     __shared__ bf16x8 qlds[QLDS ? RT * (D / 32) * 64 : 1];
 
-    if constexpr (ALL)
+    if constexpr (FORM == ALL)
         if (int(blockIdx.x) >= A.main) {
             clear_rest(A.s, A.out, A.out_stride, A.c.H * A.G * D, int(blockIdx.x) - A.main, int(gridDim.x) - A.main,
                        reinterpret_cast<uint32_t *>(lsum));
             return;
         }
-    const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
-    if (unit.seq < 0)
-        return;
-    const int i = unit.seq, sub = int(blockIdx.x) % A.per, h = sub % A.c.H, tile = sub / A.c.H;
-    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
-    if (!q.ok && sub == 0 && threadIdx.x == 0)
-        kv_raise(A.status, KV_BAD_LENGTH);
-    if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
-        A.plan[i] = make_int2(unit.first, unit.n);
+    int i, h, tile, b0, b1;
+    KvSeq q;
+    [[maybe_unused]] Unit unit{};
+    [[maybe_unused]] SharedItem item{};
+    if constexpr (FORM == SHARED) {
+        item = find_item(A);
+        if (!item.ok)
+            return;
+        i = item.seq, h = item.h, tile = item.tile, q = item.q, b0 = item.b0, b1 = item.b1;
+    } else {
+        unit = find_unit(A, int(blockIdx.x) / A.per);
+        if (unit.seq < 0)
+            return;
+        const int sub = int(blockIdx.x) % A.per;
+        i = unit.seq, h = sub % A.c.H, tile = sub / A.c.H;
+        q = kv_seq(A.s, i, A.s.all_rows);
+        if (!q.ok && sub == 0 && threadIdx.x == 0)
+            kv_raise(A.status, KV_BAD_LENGTH);
+        if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
+            A.plan[i] = make_int2(unit.first, unit.n);
+        const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+        b0 = range.x, b1 = range.y;
+    }
+    const bool sees_all = FORM == SHARED && item.all;          // (shared pages come before every row)
     const int rows = q.n * A.G, r0 = tile * 16 * RT;
-    const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
-    const int b0 = range.x, b1 = range.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, j = lane >> 4;
     // the weights of a sequence that is not cut: its only workgroup has the rows' sums and reads its scores back (by
@@ -345,7 +423,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
             *dst = A.decay != 0.0f ? fmaf(A.decay, was, w) : w;
         }
     };
-    const bool weighs = A.direct && A.scores;
+    const bool weighs = FORM != SHARED && A.direct && A.scores;
     if (r0 >= rows) {
         if (weighs)
             weigh();                                           // (no rows: the weights decay)
@@ -373,7 +451,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
     for (int x = 0; x < RT; ++x) {
         const int r = r0 + 16 * x + col, rc = min(r, rows - 1);
         const int tr = rc / A.G, hd = rc - tr * A.G;
-        limit[x] = r < rows ? row_limit(q, tr) : 0;
+        limit[x] = r >= rows ? 0 : sees_all ? q.len : row_limit(q, tr);
         const uint16_t *src = A.q + (int64_t(q.row0) + tr) * A.q_stride + (h * A.G + hd) * D;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -466,7 +544,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
         for (int x = 0; x < RT; ++x) {
             float top = -INFINITY;
             // every row sees the whole step unless the step reaches past the first row's limit
-            const bool masked = !here || t0 + TOK > q.len - q.n + 1 || r0 + 16 * (x + 1) > rows;
+            const bool masked = !here || t0 + TOK > (sees_all ? q.len : q.len - q.n + 1) || r0 + 16 * (x + 1) > rows;
 #pragma unroll
             for (int g = 0; g < GT; ++g)
 #pragma unroll
@@ -477,7 +555,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
                     sv[x][g][r] = z;
                     top = fmaxf(top, z);
                 }
-            if (A.scores && r0 + 16 * x + col < rows) {
+            if (FORM != SHARED && A.scores && r0 + 16 * x + col < rows) {
                 float *dst = A.scores + score_index(A, i, blk, page, h, r0 + 16 * x + col) + (s % F::STEPS) * TOK + 4 * j;
                 if (here || A.score_blocks)
 #pragma unroll
@@ -572,8 +650,9 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
             lsum[16 * x + row] = log_sum(mx, sum);
         if (r < rows) {
             const int tr = r / A.G, hd = r - tr * A.G;
-            const int64_t part = part_index(A, unit.first + unit.split, h, r);
-            if ((tid & 15) == 0 && !A.direct) {
+            const int64_t part = FORM == SHARED ? item.part + r : part_index(A, unit.first + unit.split, h, r);
+            const bool direct = FORM != SHARED && A.direct;
+            if ((tid & 15) == 0 && !direct) {
                 A.part_ml[2 * part] = mx;
                 A.part_ml[2 * part + 1] = sum;
             }
@@ -585,7 +664,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
                     o += a[w] * *reinterpret_cast<const f32x4 *>(&olds[w][row][e]);
-                if (A.direct) {
+                if (direct) {
                     uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + e;
                     *reinterpret_cast<uint2 *>(dst) =
                         make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
@@ -790,43 +869,58 @@ __device__ __forceinline__ void add_low(const f32x16 (&sv)[2], float ks, float &
             l += __builtin_amdgcn_exp2f(fmaf(sv[x][v], ks, -ref));
 }
 
-template <int FMT, int D, bool ALL>
-__global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
+template <int FMT, int D, int FORM>
+__global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
 {
     using M = ManyRows<D>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
-    if constexpr (ALL)
+    if constexpr (FORM == ALL)
         if (int(blockIdx.x) >= A.main) {
             clear_rest(A.s, A.out, A.out_stride, A.c.H * A.G * D, int(blockIdx.x) - A.main, int(gridDim.x) - A.main,
                        reinterpret_cast<uint32_t *>(lds8));
             return;
         }
-    const Unit unit = find_unit(A, int(blockIdx.x) / A.per);
-    if (unit.seq < 0)
-        return;
-    // the last row tiles, which see the most tokens, start first
-    const int i = unit.seq, sub = A.per - 1 - int(blockIdx.x) % A.per, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
-    const KvSeq q = kv_seq(A.s, i, A.s.all_rows);
-    if (!q.ok && sub == 0 && threadIdx.x == 0)
-        kv_raise(A.status, KV_BAD_LENGTH);
-    if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
-        A.plan[i] = make_int2(unit.first, unit.n);
+    int i, h, r0;
+    int2 range;
+    KvSeq q;
+    [[maybe_unused]] Unit unit{};
+    [[maybe_unused]] SharedItem item{};
+    if constexpr (FORM == SHARED) {
+        item = find_item(A);
+        if (!item.ok)
+            return;
+        i = item.seq, h = item.h, r0 = item.tile * M::ROWS, q = item.q, range = make_int2(item.b0, item.b1);
+    } else {
+        unit = find_unit(A, int(blockIdx.x) / A.per);
+        if (unit.seq < 0)
+            return;
+        // the last row tiles, which see the most tokens, start first
+        const int sub = A.per - 1 - int(blockIdx.x) % A.per;
+        i = unit.seq, h = sub % A.c.H, r0 = sub / A.c.H * M::ROWS;
+        q = kv_seq(A.s, i, A.s.all_rows);
+        if (!q.ok && sub == 0 && threadIdx.x == 0)
+            kv_raise(A.status, KV_BAD_LENGTH);
+        if (A.plan && unit.split == 0 && sub == 0 && threadIdx.x == 0)
+            A.plan[i] = make_int2(unit.first, unit.n);
+        range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+    }
+    const bool sees_all = FORM == SHARED && item.all;       // (shared pages come before every row)
     const int rows = q.n * A.G;
     if (r0 >= rows)
         return;
+    auto limit_of = [&](int row) { return sees_all ? q.len : row_limit(q, row); };
     // blocks up to the last row's limit
     const int last = min(r0 + M::ROWS, rows) - 1;
-    const int most = max(row_limit(q, last / A.G), 0);
-    const int2 range = unit_blocks(unit, (q.len + KV_BLOCK - 1) / KV_BLOCK);
+    const int most = max(limit_of(last / A.G), 0);
     const int b0 = range.x, b1 = min(range.y, (most + KV_BLOCK - 1) / KV_BLOCK);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, hf = lane >> 5;
     const int w0 = r0 + 32 * wave;                          // this wavefront's rows
     const bool idle = w0 >= rows;
     const int r = w0 + col;
-    const int limit = r < rows ? row_limit(q, r / A.G) : 0;
-    const int least = idle ? 0 : row_limit(q, w0 / A.G);    // the first row's limit: blocks below it need no mask
-    const int wave_most = idle ? 0 : row_limit(q, min(w0 + 31, rows - 1) / A.G);
+    const int limit = r < rows ? limit_of(r / A.G) : 0;
+    const int least = idle ? 0 : limit_of(w0 / A.G);        // the first row's limit: blocks below it need no mask
+    const int wave_most = idle ? 0 : limit_of(min(w0 + 31, rows - 1) / A.G);
 
     bf16x8 qf[D / 16];
     load_q32<D>(qf, A, q, h, w0, rows);
@@ -997,7 +1091,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
         return;
     const int tr = r / A.G, hd = r - tr * A.G;
     const float inv = l == 0.0f ? 0.0f : (v_units != 0.0f ? V_UP : 1.0f) / l, down = v_units != 0.0f ? 1.0f : V_DOWN;
-    if (A.direct) {
+    if (FORM != SHARED && A.direct) {
         uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + 4 * hf;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
@@ -1009,7 +1103,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(AttentionLaunch A)
         if (A.lse && hf == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
     } else {
-        const int64_t part = part_index(A, unit.first + unit.split, h, r);
+        const int64_t part = FORM == SHARED ? item.part + r : part_index(A, unit.first + unit.split, h, r);
         if (hf == 0) {
             A.part_ml[2 * part] = l == 0.0f ? -INFINITY : m;
             A.part_ml[2 * part + 1] = l;
@@ -1304,6 +1398,250 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
     }
 }
 
+// ---------------------------------------------------------------- shared pages
+//
+// Batches whose sequences hold the same first pages.  The rows of a group are
+// neighbours, so on its shared pages the group is one sequence whose rows see
+// every token: those pages are read once for all of them.  Every sequence's
+// rows meet its other pages as usual, and a row's result is joined from the
+// units of both.  One workgroup lays out the owners of units (groups, then
+// sequences), checks their numbers and cuts them.  Where a group's numbers break
+// a bound, or its pages reach past a sequence's first row, or offsets of groups
+// fall, the pages count as each sequence's own: what comes out is the same.
+constexpr int PLAN_THREADS = 1024;
+constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below, its partial results outweigh the codes
+
+__device__ __forceinline__ int64_t wave_scan64(int64_t v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t u = __shfl_up(v, d);
+        v += lane >= d ? u : 0;
+    }
+    return v;
+}
+
+// Inclusive sum over the workgroup's threads, and the total; `part`: a word a wavefront.
+__device__ __forceinline__ int64_t group_scan64(int64_t v, int64_t *part, int64_t &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t x = wave_scan64(v);
+    if (lane == 63)
+        part[wave] = x;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
+        before += w < wave ? part[w] : 0;
+        total += part[w];
+    }
+    __syncthreads();
+    return x + before;
+}
+
+__device__ __forceinline__ int shared_chunk(int64_t work, bool few, int most)
+{
+    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) / most));
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaunch A)
+{
+    __shared__ int64_t part[PLAN_THREADS / 64];
+    __shared__ int falling, dropped;
+    const int tid = threadIdx.x, H = A.c.H, G = A.G, N = A.g.n + A.s.S;
+    const SharedCut &cut = A.cut;
+    uint32_t status = 0;
+    if (tid == 0)
+        falling = dropped = 0;
+    __syncthreads();
+    // ---- the groups
+    int64_t work_p = 0;
+    for (int g = tid; g < A.g.n; g += PLAN_THREADS) {
+        const int a = A.g.cu[g], z = A.g.cu[g + 1], b = A.g.blocks[g];
+        KvOwner o{};
+        o.group = -1;
+        o.all = 1;
+        bool ok = a >= 0 && a <= z && z <= A.s.S;
+        if (!ok)
+            falling = 1;                                    // (offsets out of order: groups could overlap)
+        if (ok && a < z) {
+            const int row0 = A.s.cu[a], row1 = A.s.cu[z];
+            ok = b >= 0 && b <= A.g.max_blocks && row0 >= 0 && row1 >= row0 && row1 <= A.s.n_rows && row1 - row0 <= A.g.max_rows;
+            if (ok) {
+                o.row0 = row0, o.n = row1 - row0, o.seq = a;
+                o.len = b * KV_BLOCK, o.blocks = b;
+                o.tiles = int((int64_t(o.n) * G + cut.tile_p - 1) / cut.tile_p);
+                work_p += int64_t(b) * o.tiles * H;
+            }
+        }
+        if (!ok)
+            status |= KV_BAD_LENGTH;
+        A.owners[g] = o;
+    }
+    __syncthreads();                                        // (the sequences' threads read the groups)
+    const bool none = falling != 0;
+    if (none) {
+        work_p = 0;
+        for (int g = tid; g < A.g.n; g += PLAN_THREADS)
+            A.owners[g].n = A.owners[g].blocks = 0;
+    }
+    // ---- the sequences
+    int64_t work_s = 0;
+    for (int i = tid; i < A.s.S; i += PLAN_THREADS) {
+        const KvSeq q = kv_check_seq(A.s.cu[i], A.s.cu[i + 1], A.s.lens[i], A.s.n_rows, A.s.max_rows, A.s.max_len, A.s.all_rows);
+        if (!q.ok)
+            status |= KV_BAD_LENGTH;
+        KvOwner o{};
+        o.row0 = q.row0, o.n = q.n, o.len = q.len, o.seq = i;
+        o.group = -1;
+        int lo = 0, hi = A.g.n;                             // the group: the last that starts at or before i
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            (A.g.cu[mid] <= i ? lo : hi) = mid;
+        }
+        if (q.n && A.g.n && !none && A.g.cu[lo] <= i && i < A.g.cu[lo + 1]) {
+            const KvOwner w = A.owners[lo];
+            if (w.blocks && q.len - q.n >= w.len && q.row0 >= w.row0 && q.row0 + q.n <= w.row0 + w.n)
+                o.group = lo, o.b0 = w.blocks;
+        }
+        o.blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK - o.b0;
+        o.tiles = int((int64_t(q.n) * G + cut.tile_s - 1) / cut.tile_s);
+        if (q.n == 0)
+            o.blocks = 0;
+        work_s += int64_t(o.blocks) * o.tiles * H;
+        A.owners[A.g.n + i] = o;
+    }
+    kv_raise(A.status, status);
+    int64_t total_p, total_s;
+    group_scan64(work_p, part, total_p);
+    group_scan64(work_s, part, total_s);
+    if (cut.both)
+        total_p = total_s = total_p + total_s;
+    const int chunk_p = shared_chunk(total_p, cut.few_p, cut.most_p), chunk_s = shared_chunk(total_s, cut.few_s, cut.most_s);
+    // ---- units, items, places of the partial results
+    int64_t items = 0, parts = 0, items_p = 0;
+    for (int base = 0; base < N; base += PLAN_THREADS) {
+        const int e = base + tid;
+        const bool shared = e < A.g.n;
+        KvOwner o{};
+        if (e < N)
+            o = A.owners[e];                                // (written before the sums' barriers)
+        const int chunk = shared ? chunk_p : chunk_s;
+        o.units = o.n ? (o.blocks + chunk - 1) / chunk : 0;
+        const int64_t mine = int64_t(o.units) * o.tiles, rows = int64_t(o.units) * o.n * G * H;
+        int64_t all_items, all_rows;
+        const int64_t i1 = items + group_scan64(mine, part, all_items), p1 = parts + group_scan64(rows, part, all_rows);
+        int64_t group_items = 0;                            // of this step's groups
+        group_scan64(shared ? mine : 0, part, group_items);
+        items_p += group_items;
+        if (e < N) {
+            // (owners past the bounds: only offsets of rows or groups that fall can bring them there)
+            const int64_t most = shared ? cut.items_p : cut.both ? int64_t(cut.items_p) + cut.items_s : cut.items_s;
+            if (mine && (p1 > cut.parts || i1 - (shared || cut.both ? 0 : items_p) > most)) {
+                o.units = 0, o.n = 0;
+                status |= KV_BAD_LENGTH;
+                if (shared)
+                    dropped = 1;
+            }
+            o.part = p1 - rows;
+            A.owners[e] = o;
+            A.first[e] = int(min(i1 - mine, int64_t(0x7fffffff)));
+        }
+        items += all_items, parts += all_rows;
+    }
+    kv_raise(A.status, status);
+    if (tid == 0)
+        A.first[N] = int(min(items, int64_t(0x7fffffff)));
+    __syncthreads();
+    if (dropped)                                            // sequences without their group are left out, too
+        for (int i = tid; i < A.s.S; i += PLAN_THREADS) {
+            KvOwner *o = A.owners + A.g.n + i;
+            if (o->group >= 0 && A.owners[o->group].units == 0)
+                o->n = o->units = 0;
+        }
+}
+
+// Joins a row's partial results: `lanes` = D / 4 threads a (row, head), four
+// elements each; `ways` such sets share a row's units, four sets or more side by
+// side in a workgroup otherwise.  Units of the group first, then the sequence's
+// own, always in the same order.  Behind the sequences, the workgroups that
+// clear rows (MSI_KV_ALL_ROWS).
+__global__ void __launch_bounds__(256) kv_shared_finish_kernel(SharedLaunch A, int ways)
+{
+    __shared__ __attribute__((aligned(16))) float sums[1024];
+    __shared__ float ml[2][16];
+    __shared__ uint32_t words[8];
+    const int D = A.c.D, H = A.c.H, G = A.G, Hq = H * G;
+    if (int(blockIdx.z) == A.s.S) {
+        auto seq = [&](int i) {
+            const KvOwner o = A.owners[A.g.n + i];
+            return KvSeq{o.row0, o.n, o.len, true};
+        };
+        clear_rest(A.s, seq, A.out, A.out_stride, Hq * D, int(blockIdx.y * gridDim.x + blockIdx.x),
+                   int(gridDim.x * gridDim.y), words);
+        return;
+    }
+    const KvOwner o = A.owners[A.g.n + int(blockIdx.z)];
+    const int lanes = D / 4, sets = 256 / lanes, set = threadIdx.x / lanes, e = 4 * (threadIdx.x % lanes);
+    const int per = sets / ways;                            // (row, head) pairs of a workgroup
+    const int64_t at = int64_t(blockIdx.x) * per + set / ways;
+    const int way = set % ways;
+    if (int64_t(blockIdx.x) * per >= int64_t(o.n) * Hq)
+        return;
+    const bool in = at < int64_t(o.n) * Hq;
+    const int tr = in ? int(at / Hq) : 0, a = in ? int(at % Hq) : 0, h = a / G, hd = a - h * G;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    auto join = [&](const KvOwner &w, int row, int u0) {
+        const int64_t rows = int64_t(w.n) * G;
+        const int64_t p0 = w.part + h * rows + int64_t(row) * G + hd;
+#pragma unroll 4
+        for (int u = u0; u < w.units; u += ways) {
+            const int64_t p = p0 + u * (H * rows);
+            const float2 x = *reinterpret_cast<const float2 *>(A.part_ml + 2 * p);
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(A.part_o + p * D + e);
+            const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.0f : top;
+            const float f = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(x.x - ref);
+            l = f * l + b * x.y;
+            v = f * v + b * y;
+            m = top;
+        }
+    };
+    int shift = 0;
+    if (o.group >= 0) {
+        const KvOwner w = A.owners[o.group];
+        join(w, o.row0 - w.row0 + tr, way);
+        shift = w.units % ways;
+    }
+    join(o, tr, (way + ways - shift) % ways);               // (the sets go on in turn)
+    if (ways > 1) {                                         // the sets' results, in order
+        if (e == 0) {
+            ml[0][set] = m;
+            ml[1][set] = l;
+        }
+        *reinterpret_cast<f32x4 *>(sums + set * D + e) = v;
+        __syncthreads();
+        if (way)
+            return;
+        for (int k = 1; k < ways; ++k) {
+            const float m1 = ml[0][set + k], l1 = ml[1][set + k];
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(sums + (set + k) * D + e);
+            const float top = fmaxf(m, m1), ref = top == -INFINITY ? 0.0f : top;
+            const float f = __builtin_amdgcn_exp2f(m - ref), b = __builtin_amdgcn_exp2f(m1 - ref);
+            l = f * l + b * l1;
+            v = f * v + b * y;
+            m = top;
+        }
+    }
+    if (!in)
+        return;
+    v *= l == 0.0f ? 0.0f : V_UP / l;
+    *reinterpret_cast<uint2 *>(A.out + (int64_t(o.row0) + tr) * A.out_stride + a * D + e) =
+        make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+
 template <typename F>
 void with_shape(int fmt, int D, F f)
 {
@@ -1322,6 +1660,24 @@ void with_shape(int fmt, int D, F f)
 }
 
 size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+// The kernel of units for tiles of 16, 32 or 128 packed rows.
+template <int FMT, int D, int FORM>
+hipError_t launch_units(const LaunchOf<FORM> &A, int tile_rows, unsigned grid, hipStream_t st)
+{
+    if (tile_rows == 128) {
+        static std::atomic<uint64_t> done{0};
+        const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, FORM>), ManyRows<D>::LDS, done);
+        if (e != hipSuccess)
+            return e;
+        launch_k(kv_many_rows_kernel<FMT, D, FORM>, grid, 256, ManyRows<D>::LDS, st, A);
+    } else if (tile_rows == 16) {
+        launch_k(kv_few_rows_kernel<FMT, D, 1, FORM>, grid, 256, 0, st, A);
+    } else {
+        launch_k(kv_few_rows_kernel<FMT, D, 2, FORM>, grid, 256, 0, st, A);
+    }
+    return hipGetLastError();
+}
 
 }  // namespace
 
@@ -1365,27 +1721,13 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
     A.main = c.units * c.per;
     const unsigned grid = unsigned(A.main + rest_groups(A.s));
     hipError_t e = hipSuccess;
-    auto launch = [&](auto f, auto d, auto all) {
-        constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
-        constexpr bool ALL = decltype(all)::value;
-        if (!c.few) {
-            static std::atomic<uint64_t> done{0};
-            e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, ALL>), ManyRows<D>::LDS, done);
-            if (e == hipSuccess)
-                launch_k(kv_many_rows_kernel<FMT, D, ALL>, grid, 256, ManyRows<D>::LDS, st, A);
-        } else if (c.tile_rows == 16)
-            launch_k(kv_few_rows_kernel<FMT, D, 1, ALL>, grid, 256, 0, st, A);
-        else
-            launch_k(kv_few_rows_kernel<FMT, D, 2, ALL>, grid, 256, 0, st, A);
-    };
     with_shape(fmt, A.c.D, [&](auto f, auto d) {
+        constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
         if (A.s.all_rows)
-            launch(f, d, std::true_type{});
+            e = launch_units<FMT, D, ALL>(A, c.tile_rows, grid, st);
         else
-            launch(f, d, std::false_type{});
+            e = launch_units<FMT, D, PLAIN>(A, c.tile_rows, grid, st);
     });
-    if (e == hipSuccess)
-        e = hipGetLastError();
     const int blocks = (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK;
     const bool wide = int64_t(rows) * H * S >= WIDE_ROWS;
     const int side = 1024 / A.c.D;                          // rows side by side
@@ -1404,6 +1746,74 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
         e = hipGetLastError();
     }
     return e;
+}
+
+// How a call with shared pages is cut, by its host-side bounds alone.  Units are cut on the device so that at most `most`
+// workgroups (times heads and row tiles) come of them, besides one for every owner's row tile; that bounds the items and
+// the rows of partial results.
+SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
+{
+    SharedCut c{};
+    auto tile = [](int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 128; };
+    c.tile_p = tile(int64_t(g.max_rows) * G);
+    c.tile_s = tile(int64_t(s.max_rows) * G);
+    c.few_p = c.tile_p != 128;
+    c.few_s = c.tile_s != 128;
+    c.both = c.few_p && c.few_s;
+    if (c.both)
+        c.tile_p = c.tile_s = std::max(c.tile_p, c.tile_s);
+    const int fill = D == 256 ? 256 : 512;                  // 128-row workgroups that the card holds at once
+    c.most_p = c.few_p ? MOST_WORKGROUPS : fill;
+    c.most_s = c.few_s ? MOST_WORKGROUPS : fill;
+    const int64_t packed = int64_t(s.n_rows) * G;
+    auto bound = [&](int64_t owners, int64_t blocks, int tile_rows, int most, bool few, int64_t &parts) {
+        const int64_t tiles = packed / tile_rows + owners, units = (blocks + (few ? LEAST_BLOCKS : LEAST_MANY) - 1) / (few ? LEAST_BLOCKS : LEAST_MANY);
+        const int64_t items = std::min(most / H + tiles, units * tiles);
+        parts += std::min(units * packed, items * tile_rows) * H;
+        return int(std::min<int64_t>(items, 0x7fffffff));
+    };
+    const bool any = g.n && g.max_rows && g.max_blocks;
+    c.items_p = any ? bound(g.n, g.max_blocks, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
+    c.items_s = bound(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s, c.most_s, c.few_s, c.parts);
+    size_t off = up256(size_t(g.n + s.S) * sizeof(KvOwner));
+    c.first = off;
+    off += up256(size_t(g.n + s.S + 1) * sizeof(int32_t));
+    c.part_ml = off;
+    off += up256(size_t(c.parts) * 2 * sizeof(float));
+    c.part_o = off;
+    off += up256(size_t(c.parts) * D * sizeof(float));
+    c.bytes = off;
+    return c;
+}
+
+hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
+{
+    const SharedCut &c = A.cut;
+    const int H = A.c.H, Hq = H * A.G;
+    launch_k(kv_shared_plan_kernel, 1, PLAN_THREADS, 0, st, A);
+    hipError_t e = hipGetLastError();
+    auto units = [&](int list, int tile_rows, int64_t items) {
+        A.list = list;
+        if (e == hipSuccess && items)
+            with_shape(fmt, A.c.D, [&](auto f, auto d) {
+                e = launch_units<decltype(f)::value, decltype(d)::value, SHARED>(A, tile_rows, unsigned(items * H), st);
+            });
+    };
+    if (c.both) {
+        units(2, c.tile_p, int64_t(c.items_p) + c.items_s);
+    } else {
+        units(0, c.tile_p, c.items_p);
+        units(1, c.tile_s, c.items_s);
+    }
+    if (e != hipSuccess)
+        return e;
+    // few (row, head) pairs: each shared by all sets of a workgroup, since a row may have many units
+    const int sets = 1024 / A.c.D;
+    const int ways = int64_t(A.s.n_rows) * Hq <= 8192 ? sets : 1;
+    const int64_t pairs = int64_t(A.s.max_rows) * Hq, per = sets / ways;
+    launch_k(kv_shared_finish_kernel, dim3(unsigned((pairs + per - 1) / per), 1, unsigned(A.s.S + (A.s.all_rows ? 1 : 0))), 256, 0, st,
+             A, ways);
+    return hipGetLastError();
 }
 
 }  // namespace msi
