@@ -444,40 +444,75 @@ def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget:
                            keep.data_ptr(), _status(status, dev)), _stream(stream, dev))
 
 
+def _block_width(name: str, w) -> int:
+    """K of a block's matrix: bf16, or a pair of 4-bit codes and scales."""
+    m = w[0] if isinstance(w, tuple) else w
+    K = 0 if m.dim() != 2 else m.shape[1] * (2 if isinstance(w, tuple) else 1)
+    if K < 8 or K % 8:
+        _refuse(f"{name} must be a matrix whose rows are a multiple of 8")
+    return K
+
+
+def _block_weights(name: str, w, N: int, K: int, dev):
+    """What a projection would refuse of a block's matrix."""
+    m = w
+    if isinstance(w, tuple):
+        if len(w) != 2 or w[1].dim() != 2 or w[1].shape[1] < 1 or K % w[1].shape[1] or \
+                K // w[1].shape[1] not in (32, 64, 128):
+            _refuse(f"{name} must be a pair (codes, scales) with a scale for each 32, 64 or 128 of {K} weights")
+        m, scales = w
+        _dense(f"{name}'s codes", m, torch.uint8, dev, (N, K // 2))
+        _dense(f"{name}'s scales", scales, scales.dtype if scales.dtype in _F16 else torch.float16, dev, (N, scales.shape[1]))
+    else:
+        _dense(name, m, m.dtype if m.dtype in _BF16 else torch.bfloat16, dev, (N, K))
+    if m.data_ptr() % 16:
+        _refuse(f"{name} must be 16-byte aligned")
+
+
+def _block_linear(x, w, out, bias, stream):
+    if isinstance(w, tuple):
+        linear_q4(x, *w, out, bias=bias, stream=stream)
+    else:
+        linear(x, w, out, bias=bias, stream=stream)
+
+
 class AttentionBlock:
     """The attention block of one stacked layer on fixed buffers: with the layer's normalised input x (bf16) and the
     residual stream h (fp32),
 
-        q, k, v = x wqkv^T + bias;  append k, v;  a = attention(q);  h += a wo^T;  x = bf16(rmsnorm(h))
+        q, k, v = x wqkv^T + bias;  rotate q, k;  append k, v;  a = attention(q);  h += a wo^T;  x = bf16(rmsnorm(h))
 
-    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, bias float32 or None.  ``step`` runs
-    it whole; ``project`` and ``attend`` are its halves, for a model that rotates or normalises queries and keys between
-    them.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
+    wqkv [(n_q_heads + 2 n_kv_heads) head_dim, d] and wo [d, n_q_heads head_dim] bf16, or either a pair (codes, scales) of
+    4-bit weights as ``linear_q4`` takes them; bias float32 or None.  With ``rotary`` (KvRotary) queries and keys turn by the
+    ``positions`` of the step's rows on their way into the cache.  With ``groups`` (KvGroups) the step's sequences share their
+    first pages.  ``step`` runs it whole; ``project`` and ``attend`` are its halves, for a model that normalises (or rotates
+    in another way) queries and keys between them.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
     in.  Steps allocate nothing and can be captured; those of one block share its buffers, so they must not overlap.  Rows
     below n_rows that no sequence brings, and those of a sequence that breaks a bound or has more rows than tokens, get
     nothing added to h."""
 
-    def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None):
+    def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None,
+                 rotary: Optional[KvRotary] = None):
         D, H, dev = cache.head_dim, cache.n_heads, cache.device
         if n_q_heads < 1 or n_q_heads % H:
             _refuse("n_q_heads must be a multiple of the cache's n_heads")
-        if wqkv.dim() != 2 or wqkv.shape[1] < 8 or wqkv.shape[1] % 8:
-            _refuse("wqkv must be a matrix whose rows are a multiple of 8")
-        for name, t, shape in (("wqkv", wqkv, ((n_q_heads + 2 * H) * D, wqkv.shape[1])),
-                               ("wo", wo, (wqkv.shape[1], n_q_heads * D))):
-            _dense(name, t, t.dtype if t.dtype in _BF16 else torch.bfloat16, dev, shape)
-            if t.data_ptr() % 16:
-                _refuse(f"{name} must be 16-byte aligned")
+        self.rows_qkv, inner = (n_q_heads + 2 * H) * D, n_q_heads * D
+        self.d = _block_width("wqkv", wqkv)
+        for name, w, N, K in (("wqkv", wqkv, self.rows_qkv, self.d), ("wo", wo, self.d, inner)):
+            _block_weights(name, w, N, K, dev)
+        if rotary is not None and (rotary.device != dev or rotary.rot_dim > D):
+            _refuse(f"rotary must be on {dev} and rotate at most {D} elements")
         if bias is not None:
-            _dense("bias", bias, _F32, dev, (wqkv.shape[0],))
+            _dense("bias", bias, _F32, dev, (self.rows_qkv,))
         if max_rows < 0:
             _refuse("max_rows must not be negative")
         self.wqkv, self.wo, self.bias, self.cache, self.n_q_heads = wqkv, wo, bias, cache, n_q_heads
+        self.rotary = rotary
         self.scale = D ** -0.5 if scale is None else scale
         _scale(self.scale)
         self.qkv = torch.empty((max_rows, n_q_heads + 2 * H, D), dtype=torch.bfloat16, device=dev)
         self.attn = torch.empty((max_rows, n_q_heads, D), dtype=torch.bfloat16, device=dev)
-        self.out = torch.empty((max_rows, wo.shape[0]), dtype=_F32, device=dev)
+        self.out = torch.empty((max_rows, self.d), dtype=_F32, device=dev)
         self._kept = []                   # every workspace so far: captured steps go on using theirs
         self.workspace = None
         self._settle()
@@ -487,10 +522,18 @@ class AttentionBlock:
         if self.cache.device.type == "cuda":
             torch.cuda.current_stream(self.cache.device).synchronize()
 
-    def reserve(self, seqs: KvSeqs, mass_rows: int = 0):
+    def _need(self, seqs: KvSeqs, mass_rows: int, groups: Optional[KvGroups]) -> int:
+        """Bytes of workspace of a step."""
+        if groups is None:
+            return kv_attention_workspace_size(self.cache, seqs, self.n_q_heads, mass_rows)
+        if mass_rows:
+            _refuse("mass_rows must be 0 with groups: a shared page has several sequences' weights")
+        return kv_attention_shared_workspace_size(self.cache, seqs, groups, self.n_q_heads)
+
+    def reserve(self, seqs: KvSeqs, mass_rows: int = 0, groups: Optional[KvGroups] = None):
         """Workspace for steps with these bounds (of the largest ones asked for so far).  Captured steps go on using the one
         they were captured with, so earlier ones are kept; each is at least twice the one before."""
-        need = kv_attention_workspace_size(self.cache, seqs, self.n_q_heads, mass_rows)
+        need = self._need(seqs, mass_rows, groups)
         have = 0 if self.workspace is None else self.workspace.numel()
         if self.workspace is None or have < need:
             self.workspace = torch.empty(max(need, 2 * have), dtype=torch.uint8, device=self.cache.device)
@@ -501,16 +544,22 @@ class AttentionBlock:
         if seqs.n_rows > self.qkv.shape[0]:
             _refuse(f"{seqs.n_rows} rows, buffers for {self.qkv.shape[0]}")
         _same_device(self.cache, seqs)
-        _dense("x", x, x.dtype if x.dtype in _BF16 else torch.bfloat16, self.cache.device, (seqs.n_rows, self.wqkv.shape[1]))
+        _dense("x", x, x.dtype if x.dtype in _BF16 else torch.bfloat16, self.cache.device, (seqs.n_rows, self.d))
 
-    def _check_rest(self, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, status, workspace):
+    def _check_rest(self, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, status, workspace, positions, groups):
         """The workspace of a step whose other arguments are right."""
         dev = self.cache.device
-        _dense("h", h, _F32, dev, (seqs.n_rows, self.wqkv.shape[1]))
+        _dense("h", h, _F32, dev, (seqs.n_rows, self.d))
         _status(status, dev)
         if mass_rows:
             _decay(mass_decay)
-        need = kv_attention_workspace_size(self.cache, seqs, self.n_q_heads, mass_rows)
+        if self.rotary is not None:
+            _positions(self.rotary, positions, seqs.n_rows, dev)
+        elif positions is not None:
+            _refuse("positions need a block with rotary")
+        if groups is not None and groups.device != dev:
+            _refuse("cache and groups must be on one device")
+        need = self._need(seqs, mass_rows, groups)
         if workspace is None:
             workspace = self.workspace
         else:
@@ -518,22 +567,30 @@ class AttentionBlock:
             if workspace.data_ptr() % 16:
                 _refuse("workspace must be 16-byte aligned")
         if need > (0 if workspace is None else workspace.numel()):
-            raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows) comes before a step, or a workspace of "
+            raise MsiError(MSI_E_NOMEM, "reserve(seqs, mass_rows, groups) comes before a step, or a workspace of "
                                         f"{need} bytes is handed in")
         return workspace
 
     def _project(self, x, n: int, stream):
         qkv = self.qkv[:n]
-        linear(x, self.wqkv, qkv.view(n, self.wqkv.shape[0]), bias=self.bias, stream=stream)
+        _block_linear(x, self.wqkv, qkv.view(n, self.rows_qkv), self.bias, stream)
         return qkv
 
-    def _attend(self, x, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, workspace, status, stream):
+    def _attend(self, x, h, seqs: KvSeqs, mass_rows: int, mass_decay: float, workspace, status, stream, positions, groups):
         n, Hq, H = seqs.n_rows, self.n_q_heads, self.cache.n_heads
         qkv, attn, out = self.qkv[:n], self.attn[:n], self.out[:n]
-        kv_append(self.cache, seqs, qkv[:, Hq:Hq + H], qkv[:, Hq + H:], status=status, stream=stream)
-        kv_attention(self.cache, seqs, qkv[:, :Hq], attn, self.scale, mass_rows=mass_rows, mass_decay=mass_decay,
-                     workspace=workspace, status=status, stream=stream, all_rows=True)
-        linear(attn.view(n, self.wo.shape[1]), self.wo, out, stream=stream)
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:]
+        if self.rotary is None:
+            kv_append(self.cache, seqs, k, v, status=status, stream=stream)
+        else:
+            kv_append_rotary(self.cache, seqs, self.rotary, positions, q, q, k, v, status=status, stream=stream)
+        if groups is None:
+            kv_attention(self.cache, seqs, q, attn, self.scale, mass_rows=mass_rows, mass_decay=mass_decay,
+                         workspace=workspace, status=status, stream=stream, all_rows=True)
+        else:
+            kv_attention_shared(self.cache, seqs, groups, q, attn, self.scale, workspace=workspace, status=status,
+                                stream=stream, all_rows=True)
+        _block_linear(attn.view(n, Hq * self.cache.head_dim), self.wo, out, None, stream)
         if n:
             _call(h.device, lib.msi_residual_add, out.data_ptr(), h.data_ptr(), x.data_ptr(), n, h.shape[1],
                   _stream(stream, h.device))
@@ -544,17 +601,20 @@ class AttentionBlock:
         self._check_x(x, seqs)
         return self._project(x, seqs.n_rows, stream)
 
-    def attend(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None):
-        """Second half, with what ``project`` left: appends, attends, and updates h and x as a step does."""
+    def attend(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None,
+               positions=None, groups: Optional[KvGroups] = None):
+        """Second half, with what ``project`` left: rotates, appends, attends, and updates h and x as a step does."""
         self._check_x(x, seqs)
-        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace)
-        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream)
+        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace, positions, groups)
+        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream, positions, groups)
 
-    def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None):
+    def step(self, x, h, seqs: KvSeqs, mass_rows: int = 0, mass_decay: float = 1.0, status=None, stream=None, workspace=None,
+             positions=None, groups: Optional[KvGroups] = None):
         """x [n_rows, d] (bf16) and h [n_rows, d] (float32) of the call's rows, both updated in place.  What is refused is
-        refused before the cache, x or h change.  ``workspace`` (uint8, kv_attention_workspace_size bytes) takes the place of
-        the block's own: blocks whose steps run one after another can share one."""
+        refused before the cache, x or h change.  ``workspace`` (uint8, kv_attention_workspace_size bytes, with groups
+        kv_attention_shared_workspace_size) takes the place of the block's own: blocks whose steps run one after another can
+        share one.  ``positions``: as kv_append_rotary's, of a block with rotary."""
         self._check_x(x, seqs)
-        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace)
+        workspace = self._check_rest(h, seqs, mass_rows, mass_decay, status, workspace, positions, groups)
         self._project(x, seqs.n_rows, stream)
-        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream)
+        self._attend(x, h, seqs, mass_rows, mass_decay, workspace, status, stream, positions, groups)
