@@ -178,7 +178,7 @@ EXPORTS = ["msi_residual_init", "msi_residual_add", "msi_plan_set_timing", "msi_
            "msi_slot_hold", "msi_slot_unhold", "msi_slot_query", "msi_plan_stats",
            "msi_debug_set_device_gen", "msi_stream_threshold", "msi_source_stats_get",
            "msi_debug_source_fault", "msi_debug_source_release", "msi_prefetch", "msi_linear", "msi_linear_q4",
-           "msi_debug_linear_tile", "msi_kv_append", "msi_kv_append_rotary", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
+           "msi_debug_linear_tile", "msi_debug_linear_q4_tile", "msi_kv_append", "msi_kv_append_rotary", "msi_kv_read", "msi_kv_attention_workspace", "msi_kv_attention",
            "msi_kv_attention_shared_workspace", "msi_kv_attention_shared", "msi_kv_evict"]
 
 
@@ -232,6 +232,7 @@ def _load():
     L.msi_linear.argtypes = [_vp, _vp]
     L.msi_linear_q4.argtypes = [_vp, _vp]
     L.msi_debug_linear_tile.argtypes = [_u32, _u32, P(_u32), P(_u32), P(_u32)]
+    L.msi_debug_linear_q4_tile.argtypes = [_u32, _u32, _u32, P(_u32), P(_u32), P(_u32)]
     for n in ("msi_kv_append", "msi_kv_read"):
         getattr(L, n).argtypes = [_vp, _vp, _vp, _vp, _u64, _u64, _vp, _vp]
     L.msi_kv_attention_workspace.argtypes = [_vp, _vp, _u32, _u32, P(_u64)]

@@ -292,6 +292,19 @@ msi_status msi_debug_linear_tile(uint32_t M, uint32_t N, uint32_t *rows, uint32_
     return MSI_OK;
 }
 
+msi_status msi_debug_linear_q4_tile(uint32_t M, uint32_t N, uint32_t K, uint32_t *rows, uint32_t *features, uint32_t *per_cu)
+{
+    if (!rows || !features || !per_cu)
+        return bad("null output");
+    if (M < 1 || N < 1 || M > MOST || N > MOST || uint64_t(M) * N > MOST_OUTPUTS || K < 32 || K % 32 || K > MOST_STRIDE)
+        return bad("M and N must be 1 .. 2^29, M * N at most 2^36, K a multiple of 32, 32 .. 2^21");
+    const LinearTile t = linear_q4_tile(M, N, K);
+    *rows = uint32_t(t.rows);
+    *features = uint32_t(t.features);
+    *per_cu = uint32_t(t.per_cu);
+    return MSI_OK;
+}
+
 msi_status msi_kv_append(const msi_kv_cache *cache, const msi_kv_seqs *seqs, const void *k, const void *v,
                          uint64_t k_stride, uint64_t v_stride, uint32_t *status, void *stream)
 {

@@ -19,14 +19,17 @@ namespace {
 
 // ---------------------------------------------------------------- few rows
 //
-// Up to 64 rows: bound by the weights' bytes, small calls by the launch and one
-// chain of loads.  A workgroup owns 16 R features and 16 MT rows; its eight
-// wavefronts take chunks of 256 elements of K in turn and their sums meet in
-// LDS in wavefront order.  Rows of x are the MFMA's A operand, read straight
-// from memory (rows past M repeat the last one), weights the B operand, read
-// along their rows (a load covers 8 rows x 128 bytes) and rearranged in the
-// wavefront's own LDS part.  A lane's outputs are four rows of one feature, so
-// it applies that feature's scales.
+// Up to 16 rows: bound by the weights' bytes, small calls by the launch and one
+// chain of loads.  A workgroup owns 16 R features; its eight wavefronts take
+// chunks of 256 elements of K in turn and their sums meet in LDS in wavefront
+// order.  Rows of x are the MFMA's A operand, read straight from memory (rows
+// past M repeat the last one), weights the B operand, read along their rows (a
+// load covers 8 rows x 128 bytes) and rearranged in the wavefront's own LDS
+// part.  A lane's outputs are four rows of one feature, so it applies that
+// feature's scales.  Weights from HBM, one row: 2048 x 5120 5.1 us, 4096 x 8199
+// 8.3 us (2.1 TB/s), 8192 x 8192 11.6 us (3.2 TB/s).  (A lane's 16 bytes of x
+// come from another row than its neighbour's, which costs four times the L1's
+// cycles: 16 rows of 4096 x 8199 take 13.4 us, and more rows go through tiles.)
 constexpr int ROWS_WAVES = 8, CHUNK = 8;      // blocks of 32 elements in a chunk
 
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
@@ -85,15 +88,15 @@ __device__ __forceinline__ void store1(const LinearArgs &A, int act, int64_t m, 
         A.out_bf16[m * A.out_stride + n] = f32_to_bf16(z);
 }
 
-template <int MT, int R, int GB>
-__global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4_rows_kernel(LinearQ4Args Q, int act)
+template <int R, int GB>
+__global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kernel(LinearQ4Args Q, int act)
 {
     constexpr int RS = 16 * CHUNK + 16;                    // LDS bytes of a row of a chunk, padded against bank conflicts
     constexpr int NG = CHUNK / GB;                         // groups of a chunk
-    constexpr int STAGE = R * 16 * RS, SUMS = MT * R * 1024;
+    constexpr int STAGE = R * 16 * RS, SUMS = R * 1024;
     __shared__ __attribute__((aligned(16))) uint8_t lds[ROWS_WAVES * (STAGE > SUMS ? STAGE : SUMS)];
     const LinearArgs &A = Q.l;
-    const int n0 = int(blockIdx.x) * 16 * R, m0 = int(blockIdx.y) * 16 * MT;
+    const int n0 = int(blockIdx.x) * 16 * R;
     const int K = A.K, nblk = K / 32, nchunk = (nblk + CHUNK - 1) / CHUNK, ng = nblk / GB;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int r16 = lane & 15, g = lane >> 4;
@@ -102,7 +105,6 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
     // weights: load k of feature block m brings rows 8 k + lane / 8, the lane's 16 bytes are block lane % 8 of the chunk
     const uint8_t *wp[R][2];
     const uint16_t *sp[R];
-    const uint16_t *xp[MT];
 #pragma unroll
     for (int m = 0; m < R; ++m) {
 #pragma unroll
@@ -110,9 +112,7 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
             wp[m][k] = Q.codes + int64_t(min(n0 + 16 * m + 8 * k + (lane >> 3), A.N - 1)) * (K / 2) + 16 * (lane & 7);
         sp[m] = Q.scales + int64_t(min(n0 + 16 * m + r16, A.N - 1)) * ng;
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        xp[t] = A.x + int64_t(min(m0 + 16 * t + r16, A.M - 1)) * A.x_stride + 8 * g;
+    const uint16_t *const xp = A.x + int64_t(min(r16, A.M - 1)) * A.x_stride + 8 * g;
 
     u32x4 w[R][2];
     uint32_t sc[R][NG / 2];
@@ -131,29 +131,23 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
                 read_scales_tail<NG>(sc[m], sp[m] + NG * c, ng - NG * c);
         }
     };
-    f32x4 acc[MT][R];
+    f32x4 acc[R];
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int m = 0; m < R; ++m)
-            acc[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int m = 0; m < R; ++m)
+        acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (wave < nchunk)
         load_weights(wave);
     for (int c = wave; c < nchunk; c += ROWS_WAVES) {
-        u32x4 x[MT][CHUNK];
+        u32x4 x[CHUNK];
         const int left = nblk - CHUNK * c;                 // blocks from here on
         if (left >= CHUNK) {
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int u = 0; u < CHUNK; ++u)
-                    x[t][u] = *reinterpret_cast<const u32x4 *>(xp[t] + 32 * (CHUNK * c + u));
+            for (int u = 0; u < CHUNK; ++u)
+                x[u] = *reinterpret_cast<const u32x4 *>(xp + 32 * (CHUNK * c + u));
         } else {                                           // (nothing times whatever is there: the rest is zero)
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int u = 0; u < CHUNK; ++u)
-                    x[t][u] = u < left ? *reinterpret_cast<const u32x4 *>(xp[t] + 32 * (CHUNK * c + u)) : u32x4{0, 0, 0, 0};
+            for (int u = 0; u < CHUNK; ++u)
+                x[u] = u < left ? *reinterpret_cast<const u32x4 *>(xp + 32 * (CHUNK * c + u)) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int m = 0; m < R; ++m)
@@ -172,31 +166,25 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
             load_weights(c + ROWS_WAVES);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            f32x4 part[MT][R];
+            f32x4 part[R];
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int m = 0; m < R; ++m)
-                    part[t][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int m = 0; m < R; ++m)
+                part[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int b = 0; b < GB; ++b) {
                 const int u = j * GB + b;
 #pragma unroll
                 for (int m = 0; m < R; ++m) {
                     const bf16x8 wf = unpack_q4_16th(*reinterpret_cast<const uint32_t *>(mine + (16 * m + r16) * RS + 16 * u + 4 * g));
-#pragma unroll
-                    for (int t = 0; t < MT; ++t)
-                        part[t][m] = mfma16(as_bf16x8(x[t][u]), wf, part[t][m]);
+                    part[m] = mfma16(as_bf16x8(x[u]), wf, part[m]);
                 }
             }
 #pragma unroll
             for (int m = 0; m < R; ++m) {
                 const float s = half_to_float(uint16_t(now[m][j >> 1] >> (16 * (j & 1))));
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        acc[t][m][k] = fmaf(s, part[t][m][k], acc[t][m][k]);
+                for (int k = 0; k < 4; ++k)
+                    acc[m][k] = fmaf(s, part[m][k], acc[m][k]);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -204,17 +192,15 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
     __syncthreads();                                       // the rows' place becomes the sums'
     f32x4 *const sums = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int m = 0; m < R; ++m)
-            sums[(wave * MT * R + t * R + m) * 64 + lane] = acc[t][m];
+    for (int m = 0; m < R; ++m)
+        sums[(wave * R + m) * 64 + lane] = acc[m];
     __syncthreads();
-    for (int i = wave; i < MT * R; i += ROWS_WAVES) {
-        f32x4 z = sums[i * 64 + lane];
+    if (wave < R) {
+        f32x4 z = sums[wave * 64 + lane];
 #pragma unroll
         for (int o = 1; o < ROWS_WAVES; ++o)
-            z += sums[(o * MT * R + i) * 64 + lane];
-        const int n = n0 + 16 * (i % R) + r16, m = m0 + 16 * (i / R) + 4 * g;
+            z += sums[(o * R + wave) * 64 + lane];
+        const int n = n0 + 16 * wave + r16, m = 4 * g;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (m + k < A.M && n < A.N)
@@ -224,60 +210,67 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, MT == 1 && R == 1 ? 4 : 2) q4
 
 // ---------------------------------------------------------------- tiles
 //
-// BM rows x TN features a workgroup, K in stages of 64 elements copied straight
-// into one of two LDS buffers: rows of x as eight 16-byte chunks, chunk c of row
-// r in slot c ^ ((r / 2) % 8), codes as two, chunk c of feature r in slot
-// c ^ ((r / 8) % 2), which spreads a fragment read over the banks.  Weights are
-// the A operand, so a lane ends with four consecutive features of a row.  The
-// scales of 512 elements are brought to LDS at a time, by group, so that a lane
-// reads its four features' at once.
-template <int BM_, int TN_, int WR_, int WC_, int WPC_>
+// BM rows x TN features a workgroup; K in stages of 64 KG elements copied
+// straight into one of NBUF LDS buffers, NBUF - 1 in flight.  KG groups of WR x
+// WC wavefronts each multiply their own 64 elements of a stage, and their sums
+// meet in LDS in a fixed order.  Rows of x: 16-byte chunk c of a slice of stage
+// row r in slot c ^ ((r / 2) % 8); codes: chunk c (of 2 KG) of feature r in slot
+// c ^ (r KG / 8 % (2 KG)): both spread a fragment read over the banks.  Weights
+// are the A operand, so a lane ends with four consecutive features of a row.  The
+// scales of two to eight stages are brought to LDS at a time (a panel), by group,
+// so that a lane reads its four features' at once.
+//
+// Up to a few hundred rows a stage is one chain of LDS reads, conversion, MFMAs
+// and scaling with little beside it, 0.6 to 1 us; large calls are bound by the
+// vector unit, whose conversions and scaling take as long as the MFMAs: 2000 x
+// 8192 of K 2048 91 us, 738 TFLOP/s.
+template <int BM_, int TN_, int WR_, int WC_, int KG_, int NBUF_, int WPC_>
 struct Q4Shape {
-    static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, WPC = WPC_;
-    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
-    static constexpr int ROWB = 128, QROWB = 32, PANEL = 8;                  // stages of a panel of scales
+    static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, KG = KG_, NBUF = NBUF_, WPC = WPC_;
+    static constexpr int WAVES = WR * WC * KG, THREADS = 64 * WAVES;
+    static constexpr int ROWB = 128, QROWB = 32 * KG, CPR = 2 * KG, PANEL = KG > 2 ? 16 / KG : 8;   // bytes, code chunks of a row; stages of a panel
     static constexpr int MB = BM / WR / 16, NB = TN / WC / 16;
-    static constexpr int A_BYTES = BM * ROWB, STAGE = A_BYTES + TN * QROWB;
-    static constexpr int LA = BM / 8 / WAVES, LQ = TN / 32 / WAVES;
-    static constexpr int PIECES = THREADS / TN;                             // threads of a feature's scales
+    static constexpr int A_BYTES = KG * BM * ROWB, STAGE = A_BYTES + TN * QROWB;
+    static constexpr int LA = KG * BM / 8 / WAVES, QC = KG * TN / 32, LQ = (QC + WAVES - 1) / WAVES, LPS = LA + LQ;
     template <int GB>
-    static constexpr int SCALES = PANEL * 2 / GB * TN * 2;                  // bytes of a panel
-    static constexpr int OUT = WAVES * STORE_LDS<NB> * 4;
+    static constexpr int SCALES = PANEL * 2 * KG / GB * TN * 2;                    // bytes of a panel
+    static constexpr int OUT = WR * WC * STORE_LDS<NB> * 4, SUMS = OUT + (KG - 1) * BM * TN * 4;   // of the epilogue
     template <int GB>
-    static constexpr size_t LDS = size_t(2 * STAGE + 2 * SCALES<GB>) > OUT ? size_t(2 * STAGE + 2 * SCALES<GB>) : OUT;
-    static_assert(BM % (8 * WAVES) == 0 && TN % (32 * WAVES) == 0 && THREADS % TN == 0 && LDS<1> * WPC <= 160 * 1024, "");
+    static constexpr size_t LDS = NBUF * STAGE + 2 * SCALES<GB> > SUMS ? NBUF * STAGE + 2 * SCALES<GB> : SUMS;
+    static_assert(KG * BM % (8 * WAVES) == 0 && KG * TN % 32 == 0 && LDS<1> * WPC <= 160 * 1024, "");
+    static_assert(LA <= 16 && LQ <= 8 && LPS * (NBUF - 2) < 64, "");
 };
 
 template <int ACT, class S, int GB>
 __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_kernel(LinearQ4Args Q)
 {
-    constexpr int BM = S::BM, TN = S::TN, WAVES = S::WAVES, MB = S::MB, NB = S::NB, STAGE = S::STAGE, ROWB = S::ROWB,
-                  QROWB = S::QROWB, A_BYTES = S::A_BYTES;
-    constexpr int NGP = S::PANEL * 2 / GB, PER = NGP / S::PIECES;            // groups of a panel, scales of a thread
+    constexpr int BM = S::BM, TN = S::TN, KG = S::KG, NBUF = S::NBUF, WAVES = S::WAVES, MB = S::MB, NB = S::NB, STAGE = S::STAGE,
+                  ROWB = S::ROWB, QROWB = S::QROWB, CPR = S::CPR, A_BYTES = S::A_BYTES, LA = S::LA, LQ = S::LQ;
+    constexpr int NGP = S::PANEL * 2 * KG / GB, SPT = (TN * NGP + S::THREADS - 1) / S::THREADS;   // groups of a panel, scales of a thread
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
-    uint16_t *const panels = reinterpret_cast<uint16_t *>(lds8 + 2 * STAGE);
+    uint16_t *const panels = reinterpret_cast<uint16_t *>(lds8 + NBUF * STAGE);
     const LinearArgs &A = Q.l;
     const int2 at = tile_at(xcd_swizzle(int(blockIdx.x), int(gridDim.x)), (A.M + BM - 1) / BM, (A.N + TN - 1) / TN);
     const int m0 = at.x * BM, n0 = at.y * TN;
-    const int K = A.K, ng = K / (32 * GB), nstage = (K + 63) / 64;
+    const int K = A.K, ng = K / (32 * GB), nstage = (K + 64 * KG - 1) / (64 * KG), tail = K - 64 * KG * (nstage - 1);
     const int vm = min(BM, A.M - m0), vn = min(TN, A.N - n0);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / S::WC, wn = wave % S::WC, r16 = lane & 15, g = lane >> 4;
+    const int grp = wave / (S::WR * S::WC), wi = wave % (S::WR * S::WC), wm = wi / S::WC, wn = wi % S::WC;
+    const int r16 = lane & 15, g = lane >> 4;
     // offsets from the tile's first rows (under 2^31: strides are bounded); rows past the end repeat the last one
-    uint32_t aoff[S::LA], qoff[S::LQ];
+    uint32_t aoff[LA], qoff[LQ];
     int last = 0;                             // bit i: A copy i, bit 16 + i: code copy i of the last stage lies past K
-    const bool half = K % 64 != 0;
 #pragma unroll
-    for (int i = 0; i < S::LA; ++i) {
-        const int r = 8 * (WAVES * i + wave) + (lane >> 3), ch = (lane & 7) ^ ((r >> 1) & 7);
-        aoff[i] = uint32_t(min(r, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(ch << 4);
-        last |= int(ch >= 4) << i;
+    for (int i = 0; i < LA; ++i) {
+        const int c = WAVES * i + wave, r = 8 * (c % (BM / 8)) + (lane >> 3), slice = c / (BM / 8), ch = (lane & 7) ^ ((r >> 1) & 7);
+        aoff[i] = uint32_t(min(r, vm - 1)) * uint32_t(A.x_stride * 2) + uint32_t(slice * ROWB + (ch << 4));
+        last |= int(64 * slice + 8 * ch >= tail) << i;
     }
 #pragma unroll
-    for (int i = 0; i < S::LQ; ++i) {
-        const int c = 32 * (WAVES * i + wave) + (lane >> 1), ch = (lane & 1) ^ ((c >> 3) & 1);
-        qoff[i] = uint32_t(min(c, vn - 1)) * uint32_t(K / 2) + uint32_t(16 * ch);
-        last |= ch << (16 + i);
+    for (int i = 0; i < LQ; ++i) {
+        const int c = 64 * ((WAVES * i + wave) % S::QC) + lane, r = c / CPR, ch = (c % CPR) ^ (r * KG / 8 % CPR);
+        qoff[i] = uint32_t(min(r, vn - 1)) * uint32_t(K / 2) + uint32_t(16 * ch);
+        last |= int(32 * ch >= tail) << (16 + i);
     }
     const __amdgpu_buffer_rsrc_t ar = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(A.x + int64_t(m0) * A.x_stride), 0, 0x7fffffff, ring::RSRC_FLAGS);
@@ -285,32 +278,33 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
         const_cast<uint8_t *>(Q.codes + int64_t(n0) * (K / 2)), 0, 0x7fffffff, ring::RSRC_FLAGS);
     auto issue = [&](int stage, int buf) {
         uint8_t *st = lds8 + buf * STAGE;
-        const bool edge = half && stage == nstage - 1;     // an offset past the buffer's end leaves zeros
+        const bool edge = tail < 64 * KG && stage == nstage - 1;   // an offset past the buffer's end leaves zeros
 #pragma unroll
-        for (int i = 0; i < S::LQ; ++i)
-            dma16_lds(qr, st + A_BYTES + (WAVES * i + wave) * 1024,
+        for (int i = 0; i < LQ; ++i)
+            dma16_lds(qr, st + A_BYTES + (WAVES * i + wave) % S::QC * 1024,   // (with fewer copies than wavefronts: some twice)
+                     
                       edge && (last >> (16 + i) & 1) ? 0x80000000u : qoff[i] + uint32_t(stage * QROWB), 0);
 #pragma unroll
-        for (int i = 0; i < S::LA; ++i)
+        for (int i = 0; i < LA; ++i)
             dma16_lds(ar, st + (WAVES * i + wave) * 1024,
-                      edge && (last >> i & 1) ? 0x80000000u : aoff[i] + uint32_t(stage * ROWB), 0);
+                      edge && (last >> i & 1) ? 0x80000000u : aoff[i] + uint32_t(stage * (KG * ROWB)), 0);
     };
-    // scales: PER groups of one feature a thread, through registers
-    const int srow = tid / S::PIECES, sfirst = tid % S::PIECES * PER;
-    const uint16_t *sp = Q.scales + int64_t(n0 + min(srow, vn - 1)) * ng + sfirst;
-    uint32_t sw[PER / 2];
+    // scales: neighbouring threads take a feature's groups in turn, through registers
+    uint16_t sw[SPT];
     auto load_panel = [&](int p) {
-        const int have = ng - p * NGP - sfirst;
-        if (have >= PER)
-            read_scales<PER>(sw, sp + p * NGP);
-        else
-            read_scales_tail<PER>(sw, sp + p * NGP, have);
+#pragma unroll
+        for (int k = 0; k < SPT; ++k) {
+            const int e = tid + k * S::THREADS, r = e / NGP, j = p * NGP + e % NGP;
+            sw[k] = e < TN * NGP && j < ng ? Q.scales[int64_t(n0 + min(r, vn - 1)) * ng + j] : uint16_t(0);
+        }
     };
     auto keep_panel = [&](int p) {
-        uint16_t *to = panels + (p & 1) * (NGP * TN) + sfirst * TN + srow;
 #pragma unroll
-        for (int j = 0; j < PER; ++j)
-            to[j * TN] = uint16_t(sw[j >> 1] >> (16 * (j & 1)));
+        for (int k = 0; k < SPT; ++k) {
+            const int e = tid + k * S::THREADS;
+            if (e < TN * NGP)
+                panels[(p & 1) * (NGP * TN) + e % NGP * TN + e / NGP] = sw[k];
+        }
     };
 
     f32x4 acc[NB][MB];
@@ -319,10 +313,10 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
 #pragma unroll
         for (int b = 0; b < MB; ++b)
             acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto compute = [&](int stage) {
-        const uint8_t *st = lds8 + (stage & 1) * STAGE;
-        const uint16_t *scales = panels + (stage / S::PANEL & 1) * (NGP * TN);
-        const int j0 = (2 * stage / GB) % NGP;             // the stage's first group
+    auto compute = [&](int stage, int buf) {
+        const uint8_t *xa = lds8 + buf * STAGE + (grp * BM + wm * MB * 16) * ROWB, *qb = lds8 + buf * STAGE + A_BYTES;
+        const uint16_t *scales = panels + (stage / S::PANEL & 1) * (NGP * TN) + wn * NB * 16 + 4 * g;
+        const int j0 = 2 * (stage % S::PANEL * KG + grp) / GB;   // the slice's first group in the panel
         bf16x8 af[2][MB];
         uint32_t cw[2][NB];
 #pragma unroll
@@ -330,16 +324,14 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 const int c = (wn * NB + nb) * 16 + r16;
-                cw[kb][nb] = *reinterpret_cast<const uint32_t *>(st + A_BYTES + c * QROWB + 16 * (kb ^ ((c >> 3) & 1)) + 4 * g);
+                cw[kb][nb] = *reinterpret_cast<const uint32_t *>(qb + c * QROWB + (((2 * grp + kb) ^ (c * KG / 8 % CPR)) << 4) + 4 * g);
             }
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) {
-                const int r = (wm * MB + mb) * 16 + r16;
-                af[kb][mb] = as_bf16x8(*reinterpret_cast<const u32x4 *>(st + r * ROWB + (((4 * kb + g) ^ ((r >> 1) & 7)) << 4)));
-            }
+            for (int mb = 0; mb < MB; ++mb)
+                af[kb][mb] = as_bf16x8(*reinterpret_cast<const u32x4 *>(xa + (mb * 16 + r16) * ROWB + (((4 * kb + g) ^ ((r16 >> 1) & 7)) << 4)));
         }
         auto scaled = [&](int nb, int j, const f32x4 (&part)[MB]) {
-            const uint2 s = *reinterpret_cast<const uint2 *>(scales + j * TN + (wn * NB + nb) * 16 + 4 * g);
+            const uint2 s = *reinterpret_cast<const uint2 *>(scales + j * TN + nb * 16);
             const float f[4] = {half_to_float(uint16_t(s.x)), half_to_float(uint16_t(s.x >> 16)), half_to_float(uint16_t(s.y)),
                                 half_to_float(uint16_t(s.y >> 16))};
 #pragma unroll
@@ -371,44 +363,85 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
         }
     };
 
+    constexpr int AHEAD = NBUF - 1;
     load_panel(0);
-    issue(0, 0);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+        if (j < nstage)
+            issue(j, j);
     keep_panel(0);
-    for (int s = 0; s < nstage; ++s) {
-        __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));          // this stage landed ...
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (and this wavefront's LDS operations are done with)
-        __builtin_amdgcn_s_barrier();                       // ... for every wavefront; the other buffer was last read
-        asm volatile("" ::: "memory");                      //     one stage ago
-        if (s + 1 < nstage)
-            issue(s + 1, (s + 1) & 1);
-        // the next panel is read at this one's start and kept at its middle: its place was last read a panel ago
-        const int p = s / S::PANEL + 1;
-        if (s % S::PANEL == 0 && p * S::PANEL < nstage)
+    int cur = 0, nxt = AHEAD;
+    auto step = [&](int s) {
+        // stage s has landed; the buffer of stage s + AHEAD was last read at s - 1, by reads that are waited for as well
+        // (LGKM_DONE: no LDS operation of this wavefront in flight)
+        constexpr int LGKM_DONE = ~(0xF << 8);
+        if (s + AHEAD <= nstage)
+            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(S::LPS * (AHEAD - 1)) & LGKM_DONE);
+        else
+            __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0) & LGKM_DONE);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (s + AHEAD < nstage)
+            issue(s + AHEAD, nxt);
+        compute(s, cur);
+        cur = cur == NBUF - 1 ? 0 : cur + 1;
+        nxt = nxt == NBUF - 1 ? 0 : nxt + 1;
+    };
+    // the next panel is read at this one's start and kept at its middle: its place was last read a panel ago.  (Loops of
+    // their own: where a stage may or may not have read a panel, the compiler waits for every copy in every stage.)
+    for (int s = 0, p = 1; s < nstage; ++p) {
+        const int end = min(p * S::PANEL, nstage), middle = min(end, s + S::PANEL / 2);
+        const bool more = end < nstage;
+        if (more)
             load_panel(p);
-        compute(s);
-        if (s % S::PANEL == S::PANEL / 2 && p * S::PANEL < nstage)
+        for (; s < middle; ++s)
+            step(s);
+        if (more)
             keep_panel(p);
+        for (; s < end; ++s)
+            step(s);
     }
     __syncthreads();                                        // every fragment has been read: LDS changes its use
+    if constexpr (KG > 1) {
+        // groups 1 .. leave their sums, lane by lane; group 0 adds them in order
+        f32x4 *sums = reinterpret_cast<f32x4 *>(lds8 + S::OUT);
+        constexpr int PER = S::WR * S::WC * MB * NB * 64;
+        if (grp > 0) {
+#pragma unroll
+            for (int a = 0; a < NB; ++a)
+#pragma unroll
+                for (int q = 0; q < MB; ++q)
+                    sums[(grp - 1) * PER + ((wi * NB + a) * MB + q) * 64 + lane] = acc[a][q];
+        }
+        __syncthreads();
+        if (grp > 0)
+            return;
+        for (int o = 0; o < KG - 1; ++o)
+#pragma unroll
+            for (int a = 0; a < NB; ++a)
+#pragma unroll
+                for (int q = 0; q < MB; ++q)
+                    acc[a][q] += sums[o * PER + ((wi * NB + a) * MB + q) * 64 + lane];
+    }
 #pragma unroll
     for (int a = 0; a < NB; ++a)
 #pragma unroll
         for (int b = 0; b < MB; ++b)
             acc[a][b] *= 16.0f;                             // the codes were sixteenths
-    store_block<ACT, false, NB, MB>(A, reinterpret_cast<float *>(lds8) + wave * STORE_LDS<NB>, acc, m0 + wm * MB * 16,
+    store_block<ACT, false, NB, MB>(A, reinterpret_cast<float *>(lds8) + wi * STORE_LDS<NB>, acc, m0 + wm * MB * 16,
                                     vm - wm * MB * 16, n0 + wn * NB * 16);
 }
 
-template <int MT, int R>
+template <int R>
 hipError_t launch_rows(const LinearQ4Args &A, int act, hipStream_t st)
 {
-    const dim3 grid((A.l.N + 16 * R - 1) / (16 * R), (A.l.M + 16 * MT - 1) / (16 * MT));
+    const unsigned grid = unsigned((A.l.N + 16 * R - 1) / (16 * R));
     if (A.group == 32)
-        launch_k(q4_rows_kernel<MT, R, 1>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, 1>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     else if (A.group == 64)
-        launch_k(q4_rows_kernel<MT, R, 2>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, 2>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     else
-        launch_k(q4_rows_kernel<MT, R, 4>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, 4>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     return hipGetLastError();
 }
 
@@ -430,21 +463,59 @@ hipError_t launch_tile(const LinearQ4Args &A, hipStream_t st)
     return A.group == 64 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{});
 }
 
+template <int ACT>
+hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st)
+{
+    if (t.rows == 16)
+        return launch_tile<ACT, Q4Shape<16, 32, 1, 1, 8, 2, 2>>(A, st);
+    if (t.rows == 32)
+        return t.features == 32 ? launch_tile<ACT, Q4Shape<32, 32, 1, 1, 8, 2, 1>>(A, st)
+                                : launch_tile<ACT, Q4Shape<32, 64, 1, 4, 4, 3, 1>>(A, st);
+    if (t.rows == 64 && t.features == 64)
+        return launch_tile<ACT, Q4Shape<64, 64, 2, 2, 4, 3, 1>>(A, st);
+    if (t.rows == 128)
+        return launch_tile<ACT, Q4Shape<128, 128, 2, 4, 2, 2, 1>>(A, st);
+    return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<64, 128, 1, 8, 2, 3, 1>>(A, st)
+                         : launch_tile<ACT, Q4Shape<64, 128, 1, 4, 1, 3, 3>>(A, st);
+}
+
 }  // namespace
+
+// Up to 16 rows: no tiles (rows and features of a workgroup), 32 features where
+// they make 256 workgroups and the rows or K give them something to do [us, 16
+// and 32 features: 4 rows, K 4096, N 8199 10.1 and 10.4; K, N 8192 14.7 and 12.7;
+// 16 rows, 4096, 2048 7.7 and 8.7; 4096, 8199 15.9 and 13.4].  Above, the smallest
+// tiles that give one to every CU at most, since one wave of workgroups lasts as
+// long as a tile does, and that is the latency of its stages.  [16 x 32, 32 x 32,
+// 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.5 / 10.0 / 14.4 /
+// 20.0 / 27.1 / -; 61, 4096, 8199 29.3 / 32.4 / 23.2 / 23.2 / 32.1 / -; 128, 2048,
+// 5120 18.1 / 20.5 / 16.4 / 14.9 / 20.7 / -; 256, 2048, 8192 46 / 51 / 25.5 / 25.1 /
+// 17.9 / -; 509, 2048, 8192 - / - / - / 49 / 34 / 26.5; weights from HBM.]  Past that, tiles of
+// 64 x 128, three to a CU [2000, 2048, 8192 91 us, 128 x 128 two to a CU 90; 1000, 2048, 5120
+// 47 and 56].
+LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
+{
+    constexpr int64_t CUS = 256;
+    auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
+    if (M <= 16)
+        return LinearTile{0, tiles(16, 16) > CUS && (M > 8 || K > 4096) ? 32 : 16, 1};
+    for (const LinearTile t : {LinearTile{16, 32, 2}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
+                               LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
+        if (tiles(t.rows, t.features) <= CUS)
+            return t;
+    return LinearTile{64, 128, 3};
+}
 
 hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st)
 {
-    if (A.l.M <= 64) {
-        if (A.l.M <= 16)
-            return launch_rows<1, 1>(A, act, st);
-        return A.l.M <= 32 ? launch_rows<2, 2>(A, act, st) : launch_rows<4, 2>(A, act, st);
-    }
-    using Tile = Q4Shape<128, 128, 2, 2, 2>;
+    const LinearTile t = linear_q4_tile(A.l.M, A.l.N, A.l.K);
+    if (t.rows == 0)
+        return t.features == 16 ? launch_rows<1>(A, act, st) : launch_rows<2>(A, act, st);
     switch (act) {
-    case LINEAR_SILU: return launch_tile<LINEAR_SILU, Tile>(A, st);
-    case LINEAR_GELU: return launch_tile<LINEAR_GELU, Tile>(A, st);
-    case LINEAR_GELU_TANH: return launch_tile<LINEAR_GELU_TANH, Tile>(A, st);
-    default: return launch_tile<LINEAR_NONE, Tile>(A, st);
+    case LINEAR_SILU: return launch_act<LINEAR_SILU>(A, t, st);
+    case LINEAR_GELU: return launch_act<LINEAR_GELU>(A, t, st);
+    case LINEAR_GELU_TANH: return launch_act<LINEAR_GELU_TANH>(A, t, st);
+    default: return launch_act<LINEAR_NONE>(A, t, st);
     }
 }
 

@@ -89,15 +89,34 @@ def test_many_workgroups(M, K, N, group):
     _case(M, K, N, group, residual="f32", out="f32", inplace=True)
 
 
-@pytest.mark.parametrize("M", [2, 20, 50, 150])
-def test_infinities_stay_in_their_rows(M):
+FORMS = [((5, 4096, 300), (0, 16, 1)), ((12, 256, 4200), (0, 32, 1)), ((3, 8224, 4200), (0, 32, 1)), ((33, 544, 500), (16, 32, 2)),
+         ((100, 1056, 2000), (32, 32, 1)), ((70, 544, 4099), (32, 64, 1)), ((130, 800, 5001), (64, 64, 1)), ((200, 416, 8190), (64, 128, 1)),
+         ((600, 352, 5003), (128, 128, 1)), ((1100, 672, 4001), (64, 128, 3))]
+
+
+@pytest.mark.parametrize("size,form", FORMS)
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_every_form(size, form, group):
+    """Every kernel at odd edges of rows, features and K (which ends inside a stage, a chunk, a panel), every group."""
+    import ctypes
+    import paper_2608_23805_amd as msi
+    M, K, N = size
+    K = -(-K // group) * group
+    v = [ctypes.c_uint32() for _ in range(3)]
+    assert msi.lib.msi_debug_linear_q4_tile(M, N, K, *map(ctypes.byref, v)) == 0 and tuple(x.value for x in v) == form
+    _case(M, K, N, group, act="gelu", residual="bf16", out="bf16")
+    _case(M, K, N, group, residual="f32", out="f32", inplace=True)
+
+
+@pytest.mark.parametrize("M,N", [(2, 40), (12, 4200), (20, 40), (100, 2000), (70, 4099), (130, 5001), (200, 8190), (600, 5003), (1100, 4001)])
+def test_infinities_stay_in_their_rows(M, N):
     """An infinite element of x gives infinities of the weight's sign (NaN where the weight is zero), as the formula does,
     and only in its row; a NaN likewise.  Rows past the end and the tail of K bring nothing of theirs."""
     import torch
     import paper_2608_23805_amd as msi
-    log(f"case linear_q4 infinities M={M}")
+    log(f"case linear_q4 infinities M={M} N={N}")
     g = np.random.default_rng([81, 5, M])
-    K, N = 288, 40
+    K = 288
     x, xh = bf16(g.standard_normal((M, K)))
     w, s, wh = q4(g, N, K, 32)
     x[1, K - 1] = float("inf")

@@ -52,3 +52,12 @@ def test_binding_refusals():
         msi.linear_q4(x, w, s, y, act="relu")
     with pytest.raises(msi.MsiError, match="bias"):
         msi.linear_q4(x, w, s, y, bias=torch.zeros(7))
+
+
+def test_tile_refusals():
+    import paper_2608_23805_amd as msi
+    v = [ctypes.byref(ctypes.c_uint32()) for _ in range(3)]
+    for a in ((0, 1, 32), (1, 0, 32), ((1 << 29) + 1, 1, 32), (1 << 29, 129, 32), (1, 1, 0), (1, 1, 40), (1, 1, (1 << 21) + 32)):
+        _refused(msi.lib.msi_debug_linear_q4_tile(*a, *v), "M and N")
+    for k in range(3):
+        _refused(msi.lib.msi_debug_linear_q4_tile(1, 1, 32, *[None if i == k else p for i, p in enumerate(v)]), "null")
