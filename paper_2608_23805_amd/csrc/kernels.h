@@ -399,7 +399,8 @@ struct SharedCut {
     bool both;                   // one launch for both
     int tile_p, tile_s;          // packed rows of a workgroup
     int items_p, items_s;        // bounds of units times row tiles
-    int most_p, most_s;          // workgroups that units are cut for
+    int most_p, most_s;          // workgroups that units are cut for, at most
+    bool small;                  // every wavefront lays out the units by itself
     int64_t parts;               // bound of the partial results (rows)
     size_t first, part_ml, part_o, bytes;   // workspace offsets and size (the owners come first)
 };

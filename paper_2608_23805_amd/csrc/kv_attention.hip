@@ -250,6 +250,159 @@ enum Form : int { PLAIN, ALL, SHARED };
 template <int FORM>
 using LaunchOf = std::conditional_t<FORM == SHARED, SharedLaunch, AttentionLaunch>;
 
+// ---------------------------------------------------------------- shared pages
+//
+// Batches whose sequences hold the same first pages.  The rows of a group are
+// neighbours, so on its shared pages the group is one sequence whose rows see
+// every token: those pages are read once for all of them.  Every sequence's
+// rows meet its other pages as usual, and a row's result is joined from the
+// units of both.  The owners of units are the groups, then the sequences.  Where
+// a group's numbers break a bound, or its pages reach past a sequence's first
+// row, or offsets of groups fall, the pages count as each sequence's own: what
+// comes out is the same.
+//
+// With up to 64 groups and 64 sequences, one a lane, every wavefront of the first
+// launch lays the owners out by itself (its first workgroup leaves them for the
+// kernels behind it); larger batches take a launch of one workgroup (4 answers
+// from a prompt of 192 tokens: 19.5 us with it, 13 without).
+constexpr int PLAN_THREADS = 1024;
+constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below, its partial results outweigh the codes
+constexpr int SMALL_OWNERS = 64;
+constexpr int64_t SMALL_PARTS = 1 << 23;     // sums over the lanes stay in 32 bits
+
+// Group with the sequences [a, z) and `blocks` shared blocks, whose rows are [row0, row1); ok: its offsets are in order.
+__device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int z, int blocks, int row0, int row1, bool &ok)
+{
+    KvOwner o{};
+    o.group = -1;
+    o.all = 1;
+    if (!ok || a == z)
+        return o;
+    ok = blocks >= 0 && blocks <= A.g.max_blocks && row0 >= 0 && row1 >= row0 && row1 <= A.s.n_rows && row1 - row0 <= A.g.max_rows;
+    if (ok) {
+        o.row0 = row0, o.n = row1 - row0, o.seq = a;
+        o.len = blocks * KV_BLOCK, o.blocks = blocks;
+        o.tiles = int((int64_t(o.n) * A.G + A.cut.tile_p - 1) / A.cut.tile_p);
+    }
+    return o;
+}
+
+// Sequence i, which may belong to group g (-1: to none) with the rows [row0, row0 + n) and `blocks` shared blocks.
+__device__ __forceinline__ KvOwner seq_owner(const SharedLaunch &A, const KvSeq &q, int i, int g, int row0, int n, int blocks)
+{
+    KvOwner o{};
+    o.row0 = q.row0, o.n = q.n, o.len = q.len, o.seq = i;
+    o.group = -1;
+    if (q.n && g >= 0 && blocks && q.len - q.n >= blocks * KV_BLOCK && q.row0 >= row0 && q.row0 + q.n <= row0 + n)
+        o.group = g, o.b0 = blocks;
+    if (q.n) {
+        o.blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK - o.b0;
+        o.tiles = int((int64_t(q.n) * A.G + A.cut.tile_s - 1) / A.cut.tile_s);
+    }
+    return o;
+}
+
+__device__ __forceinline__ int shared_chunk(int64_t work, bool few, int most)
+{
+    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) / most));
+}
+
+// Blocks of a 128-row unit for up to 64 owners, one a lane (blocks, row tiles):
+// the card holds `fill` workgroups at once, and rounds of them last as long as
+// a unit and what a workgroup costs besides (about four blocks).  Lane l tries the
+// largest owner in l + 1 pieces.
+__device__ __forceinline__ int balanced_chunk(int blocks, int tiles, int H, int owners, int fill, int least)
+{
+    const int lane = threadIdx.x & 63;
+    const int most = int(wave_max(float(tiles ? blocks : 0)));
+    const int c = max((most + lane) / (lane + 1), least);
+    int64_t n = 0;
+    for (int o = 0; o < owners; ++o)
+        n += int64_t((__builtin_amdgcn_readlane(blocks, o) + c - 1) / c) * __builtin_amdgcn_readlane(tiles, o);
+    const float cost = float((n * H + fill - 1) / fill) * float(c + 4);
+    const float best = -wave_max(-cost);
+    return __builtin_amdgcn_readlane(c, __ffsll((unsigned long long)__ballot(cost == best)) - 1);
+}
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+        v += __shfl_xor(v, d);
+    return v;
+}
+
+// Owners of a small batch: group and sequence `lane`, and the first item of each.
+struct WavePlan {
+    KvOwner g, s;
+    int first_g, first_s, items_g, items;    // first items; items of all groups, of all owners
+};
+
+__device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &status)
+{
+    const int lane = threadIdx.x & 63, H = A.c.H, G = A.G;
+    const SharedCut &cut = A.cut;
+    WavePlan p;
+    int a = 0, z = 0, b = 0, c0 = 0, c1 = 0, len = 0;
+    if (lane < A.g.n)
+        a = A.g.cu[lane], z = A.g.cu[lane + 1], b = A.g.blocks[lane];
+    if (lane < A.s.S)
+        c0 = A.s.cu[lane], c1 = A.s.cu[lane + 1], len = A.s.lens[lane];
+    bool ok = a >= 0 && a <= z && z <= A.s.S;
+    status = 0;
+    const bool none = __ballot(!ok) != 0;                   // (offsets out of order: groups could overlap)
+    const int row0 = __shfl(c0, a & 63), row1 = __shfl(c1, (z - 1) & 63);
+    if (lane < A.g.n && !none) {
+        p.g = group_owner(A, a, z, b, row0, row1, ok);
+    } else {
+        p.g = KvOwner{};
+        p.g.group = -1, p.g.all = 1;
+    }
+    if (!ok || none)
+        status = KV_BAD_LENGTH;
+    KvSeq q{0, 0, 0, true};
+    if (lane < A.s.S)
+        q = kv_check_seq(c0, c1, len, A.s.n_rows, A.s.max_rows, A.s.max_len, A.s.all_rows);
+    if (!q.ok)
+        status = KV_BAD_LENGTH;
+    int mine = -1;
+    for (int g = 0; g < A.g.n && !none; ++g)
+        mine = lane >= __builtin_amdgcn_readlane(a, g) && lane < __builtin_amdgcn_readlane(z, g) ? g : mine;
+    const int from = max(mine, 0);
+    p.s = seq_owner(A, q, lane, mine, __shfl(p.g.row0, from), __shfl(p.g.n, from), __shfl(p.g.blocks, from));
+    const int64_t work_p = wave_sum64(int64_t(p.g.blocks) * p.g.tiles * H), work_s = wave_sum64(int64_t(p.s.blocks) * p.s.tiles * H);
+    const int64_t total_p = cut.both ? work_p + work_s : work_p, total_s = cut.both ? work_p + work_s : work_s;
+    int chunk_p = shared_chunk(total_p, cut.few_p, cut.most_p), chunk_s = shared_chunk(total_s, cut.few_s, cut.most_s);
+    const int fill = A.c.D == 256 ? 256 : 512;
+    if (!cut.few_p && cut.items_p)
+        chunk_p = balanced_chunk(p.g.blocks, p.g.tiles, H, A.g.n, fill, chunk_p);
+    if (!cut.few_s)
+        chunk_s = balanced_chunk(p.s.blocks, p.s.tiles, H, A.s.S, fill, chunk_s);
+    auto place = [&](KvOwner &o, int chunk, int64_t before, int most, int &first, int &items, int &rows) {
+        o.units = o.n ? (o.blocks + chunk - 1) / chunk : 0;
+        const int64_t n = int64_t(o.units) * o.tiles, r = int64_t(o.units) * o.n * G * H;
+        // (more than the bounds: only offsets of rows that fall bring that; held down, sums stay in 32 bits)
+        const int n1 = int(min(n, int64_t(most) + 1)), r1 = int(min(r, cut.parts + 1));
+        const int ni = wave_scan_incl(n1), ri = wave_scan_incl(r1);
+        items = __builtin_amdgcn_readlane(ni, 63), rows = __builtin_amdgcn_readlane(ri, 63);
+        first = ni - n1;
+        o.part = before + ri - r1;
+        if (n && (ni > most || before + ri > cut.parts)) {
+            o.n = o.units = 0;
+            status = KV_BAD_LENGTH;
+        }
+    };
+    int rows_g, rows_s, items_s;
+    place(p.g, chunk_p, 0, cut.items_p, p.first_g, p.items_g, rows_g);
+    place(p.s, chunk_s, rows_g, cut.both ? cut.items_p + cut.items_s - min(p.items_g, cut.items_p) : cut.items_s, p.first_s, items_s, rows_s);
+    p.first_s += p.items_g;
+    p.items = p.items_g + items_s;
+    const int whole = __shfl(p.g.units, max(p.s.group, 0));
+    if (p.s.group >= 0 && whole == 0)                       // (a sequence without its group is left out, too)
+        p.s.n = p.s.units = 0;
+    return p;
+}
+
 // One workgroup's share of a SHARED launch: a row tile and head of a unit.
 struct SharedItem {
     KvSeq q;                                 // the owner's rows and tokens
@@ -277,12 +430,46 @@ __device__ __forceinline__ SharedItem find_item(const SharedLaunch &A)
     SharedItem it{};
     const int n = A.g.n + A.s.S, H = A.c.H;
     it.h = int(blockIdx.x) % H;
-    const int at = int(blockIdx.x) / H + (A.list == 1 ? A.first[A.g.n] : 0);
-    if (at >= A.first[A.list == 0 ? A.g.n : n])
-        return it;
-    const int o = __builtin_amdgcn_readfirstlane(last_at_most(A.first, n, at));
-    const KvOwner w = A.owners[o];
-    const int local = at - A.first[o], tiles = max(w.tiles, 1), unit = local / tiles;
+    int at = int(blockIdx.x) / H, start;
+    KvOwner w;
+    if (A.cut.small && A.list != 1) {
+        uint32_t status;
+        const WavePlan p = plan_wave(A, status);
+        if (blockIdx.x == 0 && threadIdx.x < 64) {          // for the kernels behind this one
+            const int lane = threadIdx.x;
+            kv_raise(A.status, status);
+            if (lane < A.g.n) {
+                A.owners[lane] = p.g;
+                A.first[lane] = p.first_g;
+            }
+            if (lane < A.s.S) {
+                A.owners[A.g.n + lane] = p.s;
+                A.first[A.g.n + lane] = p.first_s;
+            }
+            if (lane == 0)
+                A.first[n] = p.items;
+        }
+        const bool shared = at < p.items_g;
+        if (at >= (A.list == 0 ? p.items_g : p.items))
+            return it;
+        // (owners without items have their neighbour's first one: the last lane that starts at or before `at`)
+        const int l = 63 - __clzll((unsigned long long)__ballot(shared ? p.first_g <= at && (threadIdx.x & 63) < A.g.n
+                                                                       : p.first_s <= at && (threadIdx.x & 63) < A.s.S));
+        auto field = [&](int g, int s) { return __builtin_amdgcn_readlane(shared ? g : s, l); };
+        w.row0 = field(p.g.row0, p.s.row0), w.n = field(p.g.n, p.s.n), w.len = field(p.g.len, p.s.len);
+        w.seq = field(p.g.seq, p.s.seq), w.b0 = field(p.g.b0, p.s.b0), w.blocks = field(p.g.blocks, p.s.blocks);
+        w.units = field(p.g.units, p.s.units), w.tiles = field(p.g.tiles, p.s.tiles), w.all = field(p.g.all, p.s.all);
+        w.part = field(int(p.g.part), int(p.s.part));       // (under SMALL_PARTS)
+        start = field(p.first_g, p.first_s);
+    } else {
+        at += A.list == 1 ? A.first[A.g.n] : 0;
+        if (at >= A.first[A.list == 0 ? A.g.n : n])
+            return it;
+        const int o = __builtin_amdgcn_readfirstlane(last_at_most(A.first, n, at));
+        w = A.owners[o];
+        start = A.first[o];
+    }
+    const int local = at - start, tiles = max(w.tiles, 1), unit = local / tiles;
     it.ok = w.units > 0;
     it.q = KvSeq{w.row0, w.n, w.len, true};
     it.seq = w.seq;
@@ -1398,41 +1585,23 @@ __global__ void __launch_bounds__(256, 2) kv_mass_rows_kernel(AttentionLaunch A,
     }
 }
 
-// ---------------------------------------------------------------- shared pages
-//
-// Batches whose sequences hold the same first pages.  The rows of a group are
-// neighbours, so on its shared pages the group is one sequence whose rows see
-// every token: those pages are read once for all of them.  Every sequence's
-// rows meet its other pages as usual, and a row's result is joined from the
-// units of both.  One workgroup lays out the owners of units (groups, then
-// sequences), checks their numbers and cuts them.  Where a group's numbers break
-// a bound, or its pages reach past a sequence's first row, or offsets of groups
-// fall, the pages count as each sequence's own: what comes out is the same.
-constexpr int PLAN_THREADS = 1024;
-constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below, its partial results outweigh the codes
-
-__device__ __forceinline__ int64_t wave_scan64(int64_t v)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t u = __shfl_up(v, d);
-        v += lane >= d ? u : 0;
-    }
-    return v;
-}
-
-// Inclusive sum over the workgroup's threads, and the total; `part`: a word a wavefront.
+// The owners of larger batches: one workgroup lays them out, checks their numbers and cuts them.
 __device__ __forceinline__ int64_t group_scan64(int64_t v, int64_t *part, int64_t &total)
 {
+    // inclusive sum over the workgroup's threads, and the total; `part`: a word a wavefront
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t x = wave_scan64(v);
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t u = __shfl_up(x, d);
+        x += lane >= d ? u : 0;
+    }
     if (lane == 63)
         part[wave] = x;
     __syncthreads();
     int64_t before = 0;
     total = 0;
-#pragma unroll
+#pragma unroll 1
     for (int w = 0; w < PLAN_THREADS / 64; ++w) {
         before += w < wave ? part[w] : 0;
         total += part[w];
@@ -1441,15 +1610,10 @@ __device__ __forceinline__ int64_t group_scan64(int64_t v, int64_t *part, int64_
     return x + before;
 }
 
-__device__ __forceinline__ int shared_chunk(int64_t work, bool few, int most)
-{
-    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) / most));
-}
-
 __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaunch A)
 {
     __shared__ int64_t part[PLAN_THREADS / 64];
-    __shared__ int falling, dropped;
+    __shared__ int falling, dropped, chunk;
     const int tid = threadIdx.x, H = A.c.H, G = A.G, N = A.g.n + A.s.S;
     const SharedCut &cut = A.cut;
     uint32_t status = 0;
@@ -1459,23 +1623,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
     // ---- the groups
     int64_t work_p = 0;
     for (int g = tid; g < A.g.n; g += PLAN_THREADS) {
-        const int a = A.g.cu[g], z = A.g.cu[g + 1], b = A.g.blocks[g];
-        KvOwner o{};
-        o.group = -1;
-        o.all = 1;
+        const int a = A.g.cu[g], z = A.g.cu[g + 1];
         bool ok = a >= 0 && a <= z && z <= A.s.S;
         if (!ok)
             falling = 1;                                    // (offsets out of order: groups could overlap)
-        if (ok && a < z) {
-            const int row0 = A.s.cu[a], row1 = A.s.cu[z];
-            ok = b >= 0 && b <= A.g.max_blocks && row0 >= 0 && row1 >= row0 && row1 <= A.s.n_rows && row1 - row0 <= A.g.max_rows;
-            if (ok) {
-                o.row0 = row0, o.n = row1 - row0, o.seq = a;
-                o.len = b * KV_BLOCK, o.blocks = b;
-                o.tiles = int((int64_t(o.n) * G + cut.tile_p - 1) / cut.tile_p);
-                work_p += int64_t(b) * o.tiles * H;
-            }
-        }
+        const int row0 = ok ? A.s.cu[a] : 0, row1 = ok ? A.s.cu[z] : 0;
+        const KvOwner o = group_owner(A, a, z, A.g.blocks[g], row0, row1, ok);
+        work_p += int64_t(o.blocks) * o.tiles * H;
         if (!ok)
             status |= KV_BAD_LENGTH;
         A.owners[g] = o;
@@ -1493,33 +1647,34 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
         const KvSeq q = kv_check_seq(A.s.cu[i], A.s.cu[i + 1], A.s.lens[i], A.s.n_rows, A.s.max_rows, A.s.max_len, A.s.all_rows);
         if (!q.ok)
             status |= KV_BAD_LENGTH;
-        KvOwner o{};
-        o.row0 = q.row0, o.n = q.n, o.len = q.len, o.seq = i;
-        o.group = -1;
-        int lo = 0, hi = A.g.n;                             // the group: the last that starts at or before i
+        int lo = 0, hi = none ? 0 : A.g.n;                  // the group: the last that starts at or before i
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             (A.g.cu[mid] <= i ? lo : hi) = mid;
         }
-        if (q.n && A.g.n && !none && A.g.cu[lo] <= i && i < A.g.cu[lo + 1]) {
-            const KvOwner w = A.owners[lo];
-            if (w.blocks && q.len - q.n >= w.len && q.row0 >= w.row0 && q.row0 + q.n <= w.row0 + w.n)
-                o.group = lo, o.b0 = w.blocks;
-        }
-        o.blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK - o.b0;
-        o.tiles = int((int64_t(q.n) * G + cut.tile_s - 1) / cut.tile_s);
-        if (q.n == 0)
-            o.blocks = 0;
+        const bool in = hi > 0 && A.g.cu[lo] <= i && i < A.g.cu[lo + 1];
+        const KvOwner *w = A.owners + (in ? lo : 0);
+        const KvOwner o = in ? seq_owner(A, q, i, lo, w->row0, w->n, w->blocks) : seq_owner(A, q, i, -1, 0, 0, 0);
         work_s += int64_t(o.blocks) * o.tiles * H;
         A.owners[A.g.n + i] = o;
     }
-    kv_raise(A.status, status);
     int64_t total_p, total_s;
     group_scan64(work_p, part, total_p);
     group_scan64(work_s, part, total_s);
     if (cut.both)
         total_p = total_s = total_p + total_s;
-    const int chunk_p = shared_chunk(total_p, cut.few_p, cut.most_p), chunk_s = shared_chunk(total_s, cut.few_s, cut.most_s);
+    int chunk_p = shared_chunk(total_p, cut.few_p, cut.most_p);
+    const int chunk_s = shared_chunk(total_s, cut.few_s, cut.most_s);
+    if (!cut.few_p && A.g.n <= 64) {                        // (written before the sums' barriers)
+        if (tid < 64) {
+            const KvOwner *w = A.owners + min(tid, max(A.g.n - 1, 0));
+            const int c = balanced_chunk(tid < A.g.n ? w->blocks : 0, tid < A.g.n ? w->tiles : 0, H, A.g.n, A.c.D == 256 ? 256 : 512, chunk_p);
+            if (tid == 0)
+                chunk = c;
+        }
+        __syncthreads();
+        chunk_p = chunk;
+    }
     // ---- units, items, places of the partial results
     int64_t items = 0, parts = 0, items_p = 0;
     for (int base = 0; base < N; base += PLAN_THREADS) {
@@ -1527,17 +1682,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
         const bool shared = e < A.g.n;
         KvOwner o{};
         if (e < N)
-            o = A.owners[e];                                // (written before the sums' barriers)
-        const int chunk = shared ? chunk_p : chunk_s;
-        o.units = o.n ? (o.blocks + chunk - 1) / chunk : 0;
+            o = A.owners[e];
+        const int c = shared ? chunk_p : chunk_s;
+        o.units = o.n ? (o.blocks + c - 1) / c : 0;
         const int64_t mine = int64_t(o.units) * o.tiles, rows = int64_t(o.units) * o.n * G * H;
-        int64_t all_items, all_rows;
+        int64_t all_items, all_rows, group_items;
         const int64_t i1 = items + group_scan64(mine, part, all_items), p1 = parts + group_scan64(rows, part, all_rows);
-        int64_t group_items = 0;                            // of this step's groups
-        group_scan64(shared ? mine : 0, part, group_items);
+        group_scan64(shared ? mine : 0, part, group_items); // of this step's groups
         items_p += group_items;
         if (e < N) {
-            // (owners past the bounds: only offsets of rows or groups that fall can bring them there)
+            // (owners past the bounds: only offsets of rows that fall can bring them there)
             const int64_t most = shared ? cut.items_p : cut.both ? int64_t(cut.items_p) + cut.items_s : cut.items_s;
             if (mine && (p1 > cut.parts || i1 - (shared || cut.both ? 0 : items_p) > most)) {
                 o.units = 0, o.n = 0;
@@ -1762,9 +1916,9 @@ SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
     c.both = c.few_p && c.few_s;
     if (c.both)
         c.tile_p = c.tile_s = std::max(c.tile_p, c.tile_s);
-    const int fill = D == 256 ? 256 : 512;                  // 128-row workgroups that the card holds at once
-    c.most_p = c.few_p ? MOST_WORKGROUPS : fill;
-    c.most_s = c.few_s ? MOST_WORKGROUPS : fill;
+    const int rounds = 4 * (D == 256 ? 256 : 512);          // four times the 128-row workgroups that the card holds at once
+    c.most_p = c.few_p ? MOST_WORKGROUPS : rounds;
+    c.most_s = c.few_s ? MOST_WORKGROUPS : rounds;
     const int64_t packed = int64_t(s.n_rows) * G;
     auto bound = [&](int64_t owners, int64_t blocks, int tile_rows, int most, bool few, int64_t &parts) {
         const int64_t tiles = packed / tile_rows + owners, units = (blocks + (few ? LEAST_BLOCKS : LEAST_MANY) - 1) / (few ? LEAST_BLOCKS : LEAST_MANY);
@@ -1775,6 +1929,7 @@ SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
     const bool any = g.n && g.max_rows && g.max_blocks;
     c.items_p = any ? bound(g.n, g.max_blocks, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
     c.items_s = bound(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s, c.most_s, c.few_s, c.parts);
+    c.small = g.n <= SMALL_OWNERS && s.S <= SMALL_OWNERS && c.parts < SMALL_PARTS && int64_t(c.items_p) + c.items_s < SMALL_PARTS;
     size_t off = up256(size_t(g.n + s.S) * sizeof(KvOwner));
     c.first = off;
     off += up256(size_t(g.n + s.S + 1) * sizeof(int32_t));
@@ -1790,8 +1945,11 @@ hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
 {
     const SharedCut &c = A.cut;
     const int H = A.c.H, Hq = H * A.G;
-    launch_k(kv_shared_plan_kernel, 1, PLAN_THREADS, 0, st, A);
-    hipError_t e = hipGetLastError();
+    hipError_t e = hipSuccess;
+    if (!c.small) {
+        launch_k(kv_shared_plan_kernel, 1, PLAN_THREADS, 0, st, A);
+        e = hipGetLastError();
+    }
     auto units = [&](int list, int tile_rows, int64_t items) {
         A.list = list;
         if (e == hipSuccess && items)
@@ -1802,7 +1960,7 @@ hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
     if (c.both) {
         units(2, c.tile_p, int64_t(c.items_p) + c.items_s);
     } else {
-        units(0, c.tile_p, c.items_p);
+        units(0, c.tile_p, std::max(c.items_p, c.small ? 1 : 0));    // (the first launch leaves the owners)
         units(1, c.tile_s, c.items_s);
     }
     if (e != hipSuccess)

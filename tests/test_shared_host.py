@@ -92,7 +92,7 @@ def test_workspace_covers_what_the_device_may_cut(H, G, D):
 
         def chunk(work, rows_of_tile):
             if rows_of_tile == 128:
-                most = 256 if D == 256 else 512
+                most = 4 * (256 if D == 256 else 512)      # (the smallest chunk that the balancing may take)
                 return max(8, -(-work // most))
             fill = -(-work // 256)
             return max(fill, 4) if fill <= 16 else max(16, -(-work // 2048))
