@@ -270,6 +270,14 @@ constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below,
 constexpr int SMALL_OWNERS = 64;
 constexpr int64_t SMALL_PARTS = 1 << 23;     // sums over the lanes stay in 32 bits
 
+__device__ __forceinline__ int log2_of(int power) { return __builtin_ctz(unsigned(power)); }
+
+// Row tiles of n rows (n G <= 2^29), tiles being powers of two.
+__device__ __forceinline__ int tiles_of(int n, int G, int tile_rows)
+{
+    return int((unsigned(n) * unsigned(G) + unsigned(tile_rows - 1)) >> log2_of(tile_rows));
+}
+
 // Group with the sequences [a, z) and `blocks` shared blocks, whose rows are [row0, row1); ok: its offsets are in order.
 __device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int z, int blocks, int row0, int row1, bool &ok)
 {
@@ -282,7 +290,7 @@ __device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int
     if (ok) {
         o.row0 = row0, o.n = row1 - row0, o.seq = a;
         o.len = blocks * KV_BLOCK, o.blocks = blocks;
-        o.tiles = int((int64_t(o.n) * A.G + A.cut.tile_p - 1) / A.cut.tile_p);
+        o.tiles = tiles_of(o.n, A.G, A.cut.tile_p);
     }
     return o;
 }
@@ -297,14 +305,14 @@ __device__ __forceinline__ KvOwner seq_owner(const SharedLaunch &A, const KvSeq 
         o.group = g, o.b0 = blocks;
     if (q.n) {
         o.blocks = (q.len + KV_BLOCK - 1) / KV_BLOCK - o.b0;
-        o.tiles = int((int64_t(q.n) * A.G + A.cut.tile_s - 1) / A.cut.tile_s);
+        o.tiles = tiles_of(q.n, A.G, A.cut.tile_s);
     }
     return o;
 }
 
 __device__ __forceinline__ int shared_chunk(int64_t work, bool few, int most)
 {
-    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) / most));
+    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) >> log2_of(most)));
 }
 
 // Blocks of a 128-row unit for up to 64 owners, one a lane (blocks, row tiles):
@@ -315,21 +323,13 @@ __device__ __forceinline__ int balanced_chunk(int blocks, int tiles, int H, int 
 {
     const int lane = threadIdx.x & 63;
     const int most = int(wave_max(float(tiles ? blocks : 0)));
-    const int c = max((most + lane) / (lane + 1), least);
+    const int c = max(int(unsigned(most + lane) / unsigned(lane + 1)), least);
     int64_t n = 0;
     for (int o = 0; o < owners; ++o)
-        n += int64_t((__builtin_amdgcn_readlane(blocks, o) + c - 1) / c) * __builtin_amdgcn_readlane(tiles, o);
-    const float cost = float((n * H + fill - 1) / fill) * float(c + 4);
+        n += int64_t(unsigned(__builtin_amdgcn_readlane(blocks, o) + c - 1) / unsigned(c)) * __builtin_amdgcn_readlane(tiles, o);
+    const float cost = float((n * H + fill - 1) >> log2_of(fill)) * float(c + 4);
     const float best = -wave_max(-cost);
     return __builtin_amdgcn_readlane(c, __ffsll((unsigned long long)__ballot(cost == best)) - 1);
-}
-
-__device__ __forceinline__ int64_t wave_sum64(int64_t v)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        v += __shfl_xor(v, d);
-    return v;
 }
 
 // Owners of a small batch: group and sequence `lane`, and the first item of each.
@@ -365,13 +365,19 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
         q = kv_check_seq(c0, c1, len, A.s.n_rows, A.s.max_rows, A.s.max_len, A.s.all_rows);
     if (!q.ok)
         status = KV_BAD_LENGTH;
-    int mine = -1;
-    for (int g = 0; g < A.g.n && !none; ++g)
-        mine = lane >= __builtin_amdgcn_readlane(a, g) && lane < __builtin_amdgcn_readlane(z, g) ? g : mine;
-    const int from = max(mine, 0);
-    p.s = seq_owner(A, q, lane, mine, __shfl(p.g.row0, from), __shfl(p.g.n, from), __shfl(p.g.blocks, from));
-    const int64_t work_p = wave_sum64(int64_t(p.g.blocks) * p.g.tiles * H), work_s = wave_sum64(int64_t(p.s.blocks) * p.s.tiles * H);
-    const int64_t total_p = cut.both ? work_p + work_s : work_p, total_s = cut.both ? work_p + work_s : work_s;
+    int mine = -1, g_row0 = 0, g_n = 0, g_blocks = 0;
+    for (int g = 0; g < A.g.n && !none; ++g) {
+        const bool in = lane >= __builtin_amdgcn_readlane(a, g) && lane < __builtin_amdgcn_readlane(z, g);
+        mine = in ? g : mine;
+        g_row0 = in ? __builtin_amdgcn_readlane(p.g.row0, g) : g_row0;
+        g_n = in ? __builtin_amdgcn_readlane(p.g.n, g) : g_n;
+        g_blocks = in ? __builtin_amdgcn_readlane(p.g.blocks, g) : g_blocks;
+    }
+    p.s = seq_owner(A, q, lane, mine, g_row0, g_n, g_blocks);
+    // (small batches' sums are under 2^30)
+    const int work_p = __builtin_amdgcn_readlane(wave_scan_incl(p.g.blocks * p.g.tiles * H), 63);
+    const int work_s = __builtin_amdgcn_readlane(wave_scan_incl(p.s.blocks * p.s.tiles * H), 63);
+    const int total_p = cut.both ? work_p + work_s : work_p, total_s = cut.both ? work_p + work_s : work_s;
     int chunk_p = shared_chunk(total_p, cut.few_p, cut.most_p), chunk_s = shared_chunk(total_s, cut.few_s, cut.most_s);
     const int fill = A.c.D == 256 ? 256 : 512;
     if (!cut.few_p && cut.items_p)
@@ -379,7 +385,7 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
     if (!cut.few_s)
         chunk_s = balanced_chunk(p.s.blocks, p.s.tiles, H, A.s.S, fill, chunk_s);
     auto place = [&](KvOwner &o, int chunk, int64_t before, int most, int &first, int &items, int &rows) {
-        o.units = o.n ? (o.blocks + chunk - 1) / chunk : 0;
+        o.units = o.n ? int(unsigned(o.blocks + chunk - 1) / unsigned(chunk)) : 0;
         const int64_t n = int64_t(o.units) * o.tiles, r = int64_t(o.units) * o.n * G * H;
         // (more than the bounds: only offsets of rows that fall bring that; held down, sums stay in 32 bits)
         const int n1 = int(min(n, int64_t(most) + 1)), r1 = int(min(r, cut.parts + 1));
@@ -397,9 +403,11 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
     place(p.s, chunk_s, rows_g, cut.both ? cut.items_p + cut.items_s - min(p.items_g, cut.items_p) : cut.items_s, p.first_s, items_s, rows_s);
     p.first_s += p.items_g;
     p.items = p.items_g + items_s;
-    const int whole = __shfl(p.g.units, max(p.s.group, 0));
-    if (p.s.group >= 0 && whole == 0)                       // (a sequence without its group is left out, too)
-        p.s.n = p.s.units = 0;
+    if (__ballot(p.g.blocks && p.g.tiles && p.g.units == 0)) {     // a group was left out: so are its sequences
+        const int whole = __shfl(p.g.units, max(p.s.group, 0));
+        if (p.s.group >= 0 && whole == 0)
+            p.s.n = p.s.units = 0;
+    }
     return p;
 }
 
@@ -469,13 +477,15 @@ __device__ __forceinline__ SharedItem find_item(const SharedLaunch &A)
         w = A.owners[o];
         start = A.first[o];
     }
-    const int local = at - start, tiles = max(w.tiles, 1), unit = local / tiles;
+    const unsigned local = at - start, tiles = max(w.tiles, 1), units = max(w.units, 1);
+    const int unit = int(local / tiles);
     it.ok = w.units > 0;
     it.q = KvSeq{w.row0, w.n, w.len, true};
     it.seq = w.seq;
-    it.tile = local % tiles;
-    it.b0 = w.b0 + int(int64_t(w.blocks) * unit / max(w.units, 1));
-    it.b1 = w.b0 + int(int64_t(w.blocks) * (unit + 1) / max(w.units, 1));
+    it.tile = int(local - unsigned(unit) * tiles);
+    const int each = int(unsigned(w.blocks) / units), more = w.blocks - each * int(units);   // the first units have one more
+    it.b0 = w.b0 + unit * each + min(unit, more);
+    it.b1 = it.b0 + each + (unit < more);
     it.part = w.part + (int64_t(unit) * H + it.h) * (int64_t(w.n) * A.G);
     it.all = w.all != 0;
     return it;
@@ -1110,12 +1120,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     const int wave_most = idle ? 0 : limit_of(min(w0 + 31, rows - 1) / A.G);
 
     bf16x8 qf[D / 16];
-    load_q32<D>(qf, A, q, h, w0, rows);
     bf16x8 *const ql = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK) + wave * (D / 16) * 64 + lane;
-    if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-            ql[c * 64] = qf[c];
     auto query = [&](int c) {
         if constexpr (M::QLDS)
             return ql[c * 64];
@@ -1133,25 +1138,26 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
 
     // page (-1: bad), K factor and log2 of the V scale in the present units of the 64 blocks from `list_at` on, one a lane;
     // `lows`: those of low blocks
+    int next_pages = -1, next_at = b0;                      // pages of the copies, which run ahead of the list
     int list_at = b0 - 64, pages = -1;
     float kscale = 0.0f, vlog = 0.0f, v_units = 0.0f;
     uint64_t lows = 0;
     const float factor = fabsf(A.scale_log2);
-    auto make_list = [&](int b) {
-        list_at = b;
-        pages = -1;
-        kscale = 1e-37f, vlog = 0.0f;
+    auto fetch_list = [&](int b) {                           // (the copies' list has come to the same blocks)
+        float2 sc{0.0f, 1.0f};
         if (b + lane < b1) {
-            pages = A.s.table[int64_t(i) * A.s.max_blocks + b + lane];
-            if (!kv_page_ok(pages, A.c.n_pages)) {
+            if (next_pages < 0)
                 kv_raise(A.status, KV_BAD_PAGE);
-                pages = -1;
-            } else {
-                const float2 sc = *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(pages) * A.c.H + h) * 2);
-                kscale = fmaxf(sc.x * factor, 1e-37f);       // (not 0: times -infinity that would be NaN)
-                vlog = log2f(fmaxf(sc.y, NO_SCALE));         // whole for powers of two
-            }
+            else
+                sc = *reinterpret_cast<const float2 *>(A.c.scales + (int64_t(next_pages) * A.c.H + h) * 2);
         }
+        return sc;
+    };
+    auto make_list = [&](int b, float2 sc) {
+        list_at = b;
+        pages = next_pages;
+        kscale = fmaxf(sc.x * factor, 1e-37f);               // (not 0: times -infinity that would be NaN)
+        vlog = log2f(fmaxf(sc.y, NO_SCALE));                 // whole for powers of two
         if (v_units == 0.0f && __any(vlog > LARGE_V_LOG)) {
             v_units = V_LOG;
 #pragma unroll
@@ -1161,7 +1167,6 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         lows = __ballot(v_units != 0.0f && vlog < LOW_V_LOG);
         vlog -= v_units;
     };
-    int next_pages = -1, next_at = b0;                      // pages of the copies, which run ahead of the list
     auto copy_list = [&](int b) {
         next_at = b;
         next_pages = -1;
@@ -1192,7 +1197,15 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         asm volatile("" ::: "memory");
     };
     issue(b0);
+    // the queries and scales come between the copies: waiting for them leaves the second block's in flight
+    load_q32<D>(qf, A, q, h, w0, rows);
+    const float2 first_scales = fetch_list(b0);
     issue(b0 + 1);
+    if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            ql[c * 64] = qf[c];
+    make_list(b0, first_scales);
     // this lane's bytes of V: token row 64 + 16 u + tv, elements 32 c + 16 (lane / 16 % 2) + 8 (lane % 2) ..
     const int tl = (lane & 15) >> 1, tv = (tl < 4 ? tl : 4 + tl) + 4 * hf;
     const int vswz = many_swz<D>(tv);                       // (the same for tv + 16 u)
@@ -1207,7 +1220,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         // block b has landed (b + 1 is in flight); the buffer of block b - 1 is free
         arrive(std::integral_constant<int, M::COPIES>{});
         if (b - list_at == 64)
-            make_list(b);
+            make_list(b, fetch_list(b));
         const int t0 = b * KV_BLOCK;
         const uint8_t *block = block_at(b + 2);
         const int valid = valid_at(b + 2);
@@ -1274,11 +1287,11 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     l = across32(l, vsum);
     if (m_low != -INFINITY)                                 // (m followed these scores too: it is at most 2^6 behind)
         l += across32(l_low, vsum) * __builtin_amdgcn_exp2f(m_low - m);
-    if (r >= rows)
-        return;
-    const int tr = r / A.G, hd = r - tr * A.G;
     const float inv = l == 0.0f ? 0.0f : (v_units != 0.0f ? V_UP : 1.0f) / l, down = v_units != 0.0f ? 1.0f : V_DOWN;
     if (FORM != SHARED && A.direct) {
+        if (r >= rows)
+            return;
+        const int tr = r / A.G, hd = r - tr * A.G;
         uint16_t *dst = A.out + (int64_t(q.row0) + tr) * A.out_stride + (h * A.G + hd) * D + 4 * hf;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
@@ -1290,17 +1303,32 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         if (A.lse && hf == 0)
             A.lse[(int64_t(q.row0) + tr) * (A.c.H * A.G) + h * A.G + hd] = l == 0.0f ? INFINITY : m + log2f(l);
     } else {
-        const int64_t part = FORM == SHARED ? item.part + r : part_index(A, unit.first + unit.split, h, r);
-        if (hf == 0) {
-            A.part_ml[2 * part] = l == 0.0f ? -INFINITY : m;
-            A.part_ml[2 * part + 1] = l;
+        const int64_t part = FORM == SHARED ? item.part : part_index(A, unit.first + unit.split, h, 0);
+        if (hf == 0 && r < rows) {
+            A.part_ml[2 * (part + r)] = l == 0.0f ? -INFINITY : m;
+            A.part_ml[2 * (part + r) + 1] = l;
         }
+        // 32 elements of the wavefront's 32 rows at a time through LDS of its own, so that a store covers whole lines of
+        // eight rows (lane by lane, 16 bytes of a row each, the way out of 128 rows of 256 takes 4.4 us)
+        __syncthreads();                                    // (the blocks' buffers are no longer read)
+        constexpr int LD = 36;
+        float *const mine = reinterpret_cast<float *>(lds8) + wave * 32 * LD;
+        const int r8 = lane >> 3, e8 = 4 * (lane & 7);
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c)
+        for (int c = 0; c < D / 32; ++c) {
 #pragma unroll
             for (int v = 0; v < 16; v += 4)
-                *reinterpret_cast<f32x4 *>(A.part_o + part * D + 32 * c + 2 * v + 4 * hf) =
+                *reinterpret_cast<f32x4 *>(mine + col * LD + 2 * v + 4 * hf) =
                     f32x4{acc[c][v] * down, acc[c][v + 1] * down, acc[c][v + 2] * down, acc[c][v + 3] * down};
+            // (a wavefront's LDS operations are in order; the fences keep the compiler from moving them)
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (w0 + 8 * k + r8 < rows)
+                    *reinterpret_cast<f32x4 *>(A.part_o + (part + w0 + 8 * k + r8) * D + 32 * c + e8) =
+                        *reinterpret_cast<const f32x4 *>(mine + (8 * k + r8) * LD + e8);
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
     }
 }
 
@@ -1929,7 +1957,9 @@ SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
     const bool any = g.n && g.max_rows && g.max_blocks;
     c.items_p = any ? bound(g.n, g.max_blocks, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
     c.items_s = bound(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s, c.most_s, c.few_s, c.parts);
-    c.small = g.n <= SMALL_OWNERS && s.S <= SMALL_OWNERS && c.parts < SMALL_PARTS && int64_t(c.items_p) + c.items_s < SMALL_PARTS;
+    auto work = [&](int64_t owners, int64_t blocks, int tile_rows) { return (packed / tile_rows + owners) * blocks * H; };
+    c.small = g.n <= SMALL_OWNERS && s.S <= SMALL_OWNERS && c.parts < SMALL_PARTS && int64_t(c.items_p) + c.items_s < SMALL_PARTS &&
+              work(g.n, g.max_blocks, c.tile_p) + work(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s) < int64_t(1) << 30;
     size_t off = up256(size_t(g.n + s.S) * sizeof(KvOwner));
     c.first = off;
     off += up256(size_t(g.n + s.S + 1) * sizeof(int32_t));
