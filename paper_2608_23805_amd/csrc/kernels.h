@@ -335,7 +335,7 @@ struct RotaryAppend {
     const uint8_t *axis;         // [rot / 2] or null
     const int32_t *positions;    // [n_axes, n_rows]
     int64_t position_stride;
-    int q_rows, q_heads;         // rows of a pass and heads of a workgroup of the queries (launch_kv_append_rotary sets them)
+    int q_rows, q_tiles, q_heads;   // of the queries: rows of a workgroup, those of 64 rows, heads (launch_kv_append_rotary sets them)
     uint32_t *status;
 };
 hipError_t launch_kv_append_rotary(RotaryAppend A, int fmt, bool interleaved, hipStream_t st);

@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "gemm_ring.h"
 #include "kernels.h"
 #include "kv_device.h"
 
@@ -81,17 +82,27 @@ __device__ __forceinline__ Frequencies load_frequencies(const RotaryAppend &A, i
     return q;
 }
 
-__device__ __forceinline__ Angles angles_of(const RotaryAppend &A, const Frequencies &q, int64_t row)
-{
-    Angles a;
+// The positions of a row.
+struct Position {
     int32_t p[4];
+};
+
+__device__ __forceinline__ Position load_position(const RotaryAppend &A, int64_t row)
+{
+    Position r;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-        p[x] = A.positions[min(x, A.n_axes - 1) * A.position_stride + row];
+        r.p[x] = x == 0 || x < A.n_axes ? A.positions[x * A.position_stride + row] : 0;
+    return r;
+}
+
+__device__ __forceinline__ Angles angles_of(const Frequencies &q, const Position &r)
+{
+    Angles a;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int x = q.axis[e];
-        const int32_t at = x == 0 ? p[0] : x == 1 ? p[1] : x == 2 ? p[2] : p[3];
+        const int32_t at = x == 0 ? r.p[0] : x == 1 ? r.p[1] : x == 2 ? r.p[2] : r.p[3];
         turn_sincos(turns(at, q.f[e]), a.s[e], a.c[e]);
     }
     return a;
@@ -115,58 +126,65 @@ __device__ __forceinline__ void rotate(u32x4 (&x)[2], const Angles &t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (INTERLEAVED) {
-            x[0][i] = pack_bf16x2(u[i], v[i]);
-            x[1][i] = pack_bf16x2(u[i + 4], v[i + 4]);
+            x[0][i] = pack_bf16x2_hw(u[i], v[i]);
+            x[1][i] = pack_bf16x2_hw(u[i + 4], v[i + 4]);
         } else {
-            x[0][i] = pack_bf16x2(u[2 * i], u[2 * i + 1]);
-            x[1][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            x[0][i] = pack_bf16x2_hw(u[2 * i], u[2 * i + 1]);
+            x[1][i] = pack_bf16x2_hw(v[2 * i], v[2 * i + 1]);
         }
     }
 }
 
-// The queries of up to 64 rows of a sequence and q_heads heads: threads over
-// (slot, row, head), a row's angles computed once for all of a thread's heads.
+// The queries of up to q_rows rows of a sequence and q_heads heads: threads over
+// (slot, row, head), a row's angles computed once for all of a thread's heads,
+// while the first heads are on their way.
 template <int D, bool INTERLEAVED>
-__device__ __forceinline__ void rotate_queries(const RotaryAppend &A, const KvSeq &q, int tile, int group)
+__device__ __forceinline__ void rotate_queries(const RotaryAppend &A, const KvSeq &q, int tile, int part)
 {
-    constexpr int SLOTS = D / 16;
-    const int n = min(q.n - tile * KV_BLOCK, KV_BLOCK);
-    const int s = threadIdx.x % SLOTS, t = threadIdx.x / SLOTS, sub = t / A.q_rows, subs = 256 / (SLOTS * A.q_rows);
-    const int h0 = group * A.q_heads + sub, h1 = min((group + 1) * A.q_heads, A.n_q_heads);
+    constexpr int SLOTS = D / 16, BATCH = 4;
+    const int subs = A.q_tiles, first = tile * KV_BLOCK + part % subs * A.q_rows, group = part / subs;
+    const int s = threadIdx.x % SLOTS, t = threadIdx.x / SLOTS, step = 256 / (SLOTS * A.q_rows);
+    const int r = first + t % A.q_rows, h0 = group * A.q_heads + t / A.q_rows, h1 = min((group + 1) * A.q_heads, A.n_q_heads);
     const bool turn = s < A.rot / 16;
-    if (!turn && A.q == A.q_out && A.q_stride == A.q_out_stride)
-        return;                                            // (in place: nothing to move)
+    if (r >= min(q.n, (tile + 1) * KV_BLOCK) || h0 >= h1 || (!turn && A.q == A.q_out))    // (in place: nothing to move)
+        return;
     const int2 ch = slot_chunks<INTERLEAVED>(s, A.rot);
-    Frequencies f;
-    if (turn)
-        f = load_frequencies(A, s);
-    for (int r = t % A.q_rows; r < n; r += A.q_rows) {
-        const int64_t row = int64_t(q.row0) + tile * KV_BLOCK + r;
-        const uint16_t *src = A.q + row * A.q_stride;
-        uint16_t *dst = A.q_out + row * A.q_out_stride;
-        Angles a;
-        if (turn)
-            a = angles_of(A, f, row);
-        constexpr int BATCH = 4;
-        for (int h = h0; h < h1; h += BATCH * subs) {
-            u32x4 x[BATCH][2];
+    const int64_t row = int64_t(q.row0) + r;
+    const uint16_t *src = A.q + row * A.q_stride;
+    uint16_t *dst = A.q_out + row * A.q_out_stride;
+    u32x4 x[BATCH][2];
+    auto load = [&](int h) {
 #pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                const int hb = min(h + b * subs, h1 - 1) * D;
-                x[b][0] = load_stream16(src + hb + 8 * ch.x);
-                x[b][1] = load_stream16(src + hb + 8 * ch.y);
-            }
-#pragma unroll
-            for (int b = 0; b < BATCH; ++b) {
-                if (h + b * subs >= h1)
-                    break;
-                if (turn)
-                    rotate<INTERLEAVED>(x[b], a);
-                uint16_t *to = dst + (h + b * subs) * D;
-                *reinterpret_cast<u32x4 *>(to + 8 * ch.x) = x[b][0];
-                *reinterpret_cast<u32x4 *>(to + 8 * ch.y) = x[b][1];
-            }
+        for (int b = 0; b < BATCH; ++b) {
+            const int hb = min(h + b * step, h1 - 1) * D;
+            x[b][0] = load_stream16(src + hb + 8 * ch.x);
+            x[b][1] = load_stream16(src + hb + 8 * ch.y);
         }
+    };
+    Angles a;
+    if (turn) {
+        const Position p = load_position(A, row);
+        const Frequencies f = load_frequencies(A, s);
+        load(h0);
+        a = angles_of(f, p);
+    } else {
+        load(h0);
+    }
+    for (int h = h0;;) {
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            if (h + b * step >= h1)
+                break;
+            if (turn)
+                rotate<INTERLEAVED>(x[b], a);
+            uint16_t *to = dst + (h + b * step) * D;
+            *reinterpret_cast<u32x4 *>(to + 8 * ch.x) = x[b][0];
+            *reinterpret_cast<u32x4 *>(to + 8 * ch.y) = x[b][1];
+        }
+        h += BATCH * step;
+        if (h >= h1)
+            return;
+        load(h);
     }
 }
 
@@ -204,6 +222,15 @@ __global__ void __launch_bounds__(256) kv_append_rotary_kernel(RotaryAppend A)
     const int64_t src0 = int64_t(q.row0) + (blk * KV_BLOCK - start);       // call's row of the block's row 0
     const int64_t stride = j ? A.v_stride : A.k_stride;
     const uint16_t *src = (j ? A.v : A.k) + src0 * stride + h * D;
+    // everything that does not depend on the page is on its way before it
+    Frequencies f;
+    Position pos[N];
+    if (turn) {
+        f = load_frequencies(A, s);
+#pragma unroll
+        for (int p = 0; p < N; ++p)
+            pos[p] = load_position(A, src0 + min(max(r0 + p * ROWS, lo), hi - 1));
+    }
     u32x4 x[N][2];
 #pragma unroll
     for (int p = 0; p < N; ++p) {
@@ -220,15 +247,13 @@ __global__ void __launch_bounds__(256) kv_append_rotary_kernel(RotaryAppend A)
     }
     float *sc = c.scales + (int64_t(page) * c.H + h) * 2 + j;
     const float was = lo ? *sc : 0.0f;                     // (read before the barrier below, written after)
-    if (turn) {
-        const Frequencies f = load_frequencies(A, s);
+    if (turn)
 #pragma unroll
         for (int p = 0; p < N; ++p) {
             const int r = r0 + p * ROWS;
             if (r >= lo && r < hi)
-                rotate<INTERLEAVED>(x[p], angles_of(A, f, src0 + r));
+                rotate<INTERLEAVED>(x[p], angles_of(f, pos[p]));
         }
-    }
     uint32_t flags = 0, m = 0;                             // largest finite magnitude: bf16 bits order as integers
 #pragma unroll
     for (int p = 0; p < N; ++p)
@@ -284,17 +309,18 @@ __global__ void __launch_bounds__(256) kv_append_rotary_kernel(RotaryAppend A)
 hipError_t launch_kv_append_rotary(RotaryAppend A, int fmt, bool interleaved, hipStream_t st)
 {
     const int slots = A.c.D / 16;
-    // rows of a pass: all that there may be, up to what leaves a thread a slot of one head
+    // rows of a workgroup: all that there may be, up to what leaves a thread a slot of one head
     A.q_rows = 1;
-    while (A.q_rows < A.s.max_rows && A.q_rows * slots < 256)
+    while (A.q_rows < A.s.max_rows && A.q_rows * slots < 256 && A.q_rows < KV_BLOCK)
         A.q_rows *= 2;
     const int tiles = (A.s.max_rows + KV_BLOCK - 1) / KV_BLOCK;
-    // heads of a workgroup: at least the side-by-side ones, then as many as still leave a thousand workgroups
+    A.q_tiles = std::min(KV_BLOCK, A.s.max_rows + A.q_rows - 1) / A.q_rows;
+    // heads of a workgroup: the side-by-side ones, then as many as still leave two thousand workgroups
     const int side = 256 / (slots * A.q_rows);
-    A.q_heads = std::max(side, int(std::min<int64_t>(A.n_q_heads, int64_t(A.n_q_heads) * tiles * A.s.S / 1024)));
-    const int groups = A.q ? (A.n_q_heads + A.q_heads - 1) / A.q_heads : 0;
+    A.q_heads = std::max(side, int(std::min<int64_t>(A.n_q_heads, int64_t(A.n_q_heads) * tiles * A.q_tiles * A.s.S / 2048)));
+    const int parts = A.q ? (A.n_q_heads + A.q_heads - 1) / A.q_heads * A.q_tiles : 0;
     const dim3 grid(std::min((A.s.max_rows + 2 * KV_BLOCK - 2) / KV_BLOCK, (A.s.max_len + KV_BLOCK - 1) / KV_BLOCK),
-                    2 * A.c.H + groups, A.s.S);
+                    2 * A.c.H + parts, A.s.S);
     auto by_d = [&](auto f, auto i) {
         constexpr int FMT = decltype(f)::value;
         constexpr bool I = decltype(i)::value;
