@@ -84,8 +84,8 @@ def test_workspace_covers_what_the_device_may_cut(H, G, D):
         need = ctypes.c_uint64()
         assert msi.lib.msi_kv_attention_shared_workspace(ctypes.byref(_cache(n_heads=H, head_dim=D)), ctypes.byref(seqs), ctypes.byref(g), H * G,
                                                          ctypes.byref(need)) == 0
-        tile = lambda n: 16 if n <= 16 else 32 if n <= 32 else 128  # noqa: E731
-        tp, ts = tile(max(n for n, _ in groups) * G), tile(max(rows) * G)
+        tile = lambda n, most: 16 if n <= 16 else 32 if n <= most else 128  # noqa: E731
+        tp, ts = tile(max(n for n, _ in groups) * G, 96 if D == 256 else 64), tile(max(rows) * G, 96)
         both = tp < 128 and ts < 128
         if both:
             tp = ts = max(tp, ts)
