@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
 // Up to a few hundred rows a stage is one chain of LDS reads, conversion, MFMAs
 // and scaling with little beside it, 0.6 to 1 us; large calls are bound by the
 // vector unit, whose conversions and scaling take as long as the MFMAs: 2000 x
-// 8192 of K 2048 91 us, 738 TFLOP/s.
+// 8192 of K 2048 85 us, 790 TFLOP/s.
 template <int BM_, int TN_, int WR_, int WC_, int KG_, int NBUF_, int WPC_>
 struct Q4Shape {
     static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, KG = KG_, NBUF = NBUF_, WPC = WPC_;
@@ -474,7 +474,8 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
     if (t.rows == 64 && t.features == 64)
         return launch_tile<ACT, Q4Shape<64, 64, 2, 2, 4, 3, 1>>(A, st);
     if (t.rows == 128)
-        return launch_tile<ACT, Q4Shape<128, 128, 2, 4, 2, 2, 1>>(A, st);
+        return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<128, 128, 2, 4, 2, 2, 1>>(A, st)
+                             : launch_tile<ACT, Q4Shape<128, 128, 1, 4, 1, 2, 2>>(A, st);
     return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<64, 128, 1, 8, 2, 3, 1>>(A, st)
                          : launch_tile<ACT, Q4Shape<64, 128, 1, 4, 1, 3, 3>>(A, st);
 }
@@ -490,9 +491,12 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 // 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.5 / 10.0 / 14.4 /
 // 20.0 / 27.1 / -; 61, 4096, 8199 29.3 / 32.4 / 23.2 / 23.2 / 32.1 / -; 128, 2048,
 // 5120 18.1 / 20.5 / 16.4 / 14.9 / 20.7 / -; 256, 2048, 8192 46 / 51 / 25.5 / 25.1 /
-// 17.9 / -; 509, 2048, 8192 - / - / - / 49 / 34 / 26.5; weights from HBM.]  Past that, tiles of
-// 64 x 128, three to a CU [2000, 2048, 8192 91 us, 128 x 128 two to a CU 90; 1000, 2048, 5120
-// 47 and 56].
+// 17.9 / -; 509, 2048, 8192 - / - / - / 49 / 34 / 26.5; weights from HBM.]  Past that,
+// tiles of 128 x 128, two to a CU (wavefronts of 128 x 32, which convert a weight
+// for eight row blocks), or of 64 x 128, three to a CU, whose rounds last about
+// three quarters as long, whichever fills its rounds better [1000, 2048, 8192 43.8
+// and 50.0; 2000, 2048, 8192 84.8 and 97.5; 2000, 2048, 5120 66.5 and 62.9; 4096, 4096, 4096
+// 160 and 179].
 LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
 {
     constexpr int64_t CUS = 256;
@@ -503,7 +507,8 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
         if (tiles(t.rows, t.features) <= CUS)
             return t;
-    return LinearTile{64, 128, 3};
+    const int64_t big = (tiles(128, 128) + 2 * CUS - 1) / (2 * CUS), small = (tiles(64, 128) + 3 * CUS - 1) / (3 * CUS);
+    return 4 * big <= 3 * small ? LinearTile{128, 128, 2} : LinearTile{64, 128, 3};
 }
 
 hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st)
