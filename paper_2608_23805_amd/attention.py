@@ -88,6 +88,11 @@ def _matrix(name: str, t, M: int, N: int, device, dtypes) -> int:
     if t.shape != (M, N) or t.dtype not in dtypes or t.device != device:
         _refuse(f"{name} must be [{M}, {N}] {' or '.join(map(str, dtypes))} on {device}, "
                 f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return _row_stride(name, t, M, N)
+
+
+def _row_stride(name: str, t, M: int, N: int) -> int:
+    """Row stride of a tensor of shape [M, N]."""
     if M == 0:
         return (N + 7) // 8 * 8              # (a tensor without elements may have any strides)
     rs, cs = t.stride()
@@ -111,11 +116,11 @@ def _decay(mass_decay: float):
         _refuse(f"mass_decay must be finite in fp32 and not negative, got {mass_decay}")
 
 
-def _pack(x, w, N: int, out, bias, act: str, residual) -> bytes:
-    """The arguments of a projection (msi_linear_args) whose weights w [N, ...] have been checked."""
-    dev = x.device
-    M, K = x.shape
-    xs = _matrix("x", x, M, K, dev, _BF16)
+def _pack(x, dev, M: int, K: int, w, N: int, out, bias, act: str, residual) -> bytes:
+    """The arguments of a projection (msi_linear_args) of x [M, K] whose weights w [N, ...] have been checked."""
+    if x.dtype not in _BF16:
+        _refuse(f"x must be {' or '.join(map(str, _BF16))}, got {x.dtype}")
+    xs = _row_stride("x", x, M, K)
     code = ACTIVATIONS.get(act)
     if code is None:
         _refuse(f"unknown activation {act!r}")
@@ -135,14 +140,14 @@ def linear(x, w, out, bias=None, act: str = "none", residual=None, stream=None):
 
     x [M, K] and w [N, K] bf16 (x's rows may be strided), bias [N] float32,
     residual and out [M, N] bf16 or float32 with strided rows; residual may be out."""
-    dev = x.device
-    if x.dim() != 2 or w.dim() != 2:
+    dev, xshape, wshape = x.device, x.shape, w.shape
+    if len(xshape) != 2 or len(wshape) != 2:
         _refuse("x and w must be matrices")
     if w.dtype not in _BF16:
         _refuse(f"w must be bf16 (or its bits in int16), got {w.dtype}")
-    N = w.shape[0]
-    _dense("w", w, w.dtype, dev, (N, x.shape[1]))
-    _call(dev, lib.msi_linear, _pack(x, w, N, out, bias, act, residual), _stream(stream, dev))
+    (M, K), N = xshape, wshape[0]
+    _dense("w", w, w.dtype, dev, (N, K))
+    _call(dev, lib.msi_linear, _pack(x, dev, M, K, w, N, out, bias, act, residual), _stream(stream, dev))
 
 
 def linear_q4(x, w, scales, out, bias=None, act: str = "none", residual=None, stream=None):
@@ -150,19 +155,18 @@ def linear_q4(x, w, scales, out, bias=None, act: str = "none", residual=None, st
 
     w [N, K / 2] uint8: the codes q = -8 .. 7, element 2j in the low nibble of byte j; scales [N, K / group] float16 (or
     its bits in int16), group 32, 64 or 128; the others as ``linear``'s."""
-    dev = x.device
-    if x.dim() != 2 or w.dim() != 2 or scales.dim() != 2:
+    dev, xshape, sshape = x.device, x.shape, scales.shape
+    if len(xshape) != 2 or len(sshape) != 2 or w.dim() != 2:
         _refuse("x, w and scales must be matrices")
-    K, N, groups = x.shape[1], w.shape[0], scales.shape[1]
+    (M, K), (N, groups) = xshape, sshape
     group = K // groups if groups else 0
     if group not in (32, 64, 128) or group * groups != K:
-        _refuse(f"scales must be [N, K / 32], [N, K / 64] or [N, K / 128], got {tuple(scales.shape)} for K = {K}")
+        _refuse(f"scales must be [N, K / 32], [N, K / 64] or [N, K / 128], got {tuple(sshape)} for K = {K}")
     _dense("w", w, torch.uint8, dev, (N, K // 2))
-    if scales.dtype not in _F16:
-        _refuse(f"scales must be float16 (or its bits in int16), got {scales.dtype}")
-    _dense("scales", scales, scales.dtype, dev, (N, groups))
+    if scales.dtype not in _F16 or scales.device != dev or not scales.is_contiguous():
+        _refuse(f"scales must be contiguous float16 (or its bits in int16) on {dev}, got {scales.dtype} on {scales.device}")
     _call(dev, lib.msi_linear_q4,
-          _pack(x, w, N, out, bias, act, residual) + _pack_q4.pack(scales.data_ptr(), group, 0), _stream(stream, dev))
+          _pack(x, dev, M, K, w, N, out, bias, act, residual) + _pack_q4.pack(scales.data_ptr(), group, 0), _stream(stream, dev))
 
 
 class KvCache:
@@ -280,21 +284,21 @@ class KvRotary:
 
 def _positions(rotary: KvRotary, positions, n: int, device) -> int:
     """Stride from one axis of the positions to the next."""
-    if rotary.device != device:
-        _refuse(f"rotary must be on {device}, got {rotary.device}")
     if positions is None:
         _refuse("positions are needed")
-    shape = positions.shape
-    if positions.dtype != _I32 or positions.device != device or shape[-1:] != (n,) or positions.dim() > 2 or \
-            (shape[0] if positions.dim() == 2 else 1) != rotary.n_axes:
-        _refuse(f"positions must be int32 [{rotary.n_axes}, {n}] on {device}, got {tuple(shape)} {positions.dtype} on "
-                f"{positions.device}")
-    if n > 1 and positions.stride(-1) != 1:
+    axes, shape = rotary.n_axes, positions.shape
+    if (shape != (axes, n) and (axes > 1 or shape != (n,))) or positions.dtype != _I32 or positions.device != device or \
+            rotary.device != device:
+        _refuse(f"positions must be int32 [{axes}, {n}] on {device}, as rotary, got {tuple(shape)} {positions.dtype} on "
+                f"{positions.device} and rotary on {rotary.device}")
+    strides = positions.stride()
+    if n > 1 and strides[-1] != 1:
         _refuse("an axis of positions must be contiguous")
-    step = positions.stride(0) if positions.dim() == 2 and rotary.n_axes > 1 else n
-    if step < n:
+    if axes == 1:
+        return n
+    if strides[0] < n:
         _refuse("axes of positions must not overlap")
-    return step
+    return strides[0]
 
 
 def kv_append_rotary(cache: KvCache, seqs: KvSeqs, rotary: KvRotary, positions, q, q_out, k, v, status=None, stream=None):
@@ -309,9 +313,10 @@ def kv_append_rotary(cache: KvCache, seqs: KvSeqs, rotary: KvRotary, positions, 
         _refuse(f"{rotary.rot_dim} elements rotate, heads have {cache.head_dim}")
     qp = op = qs = os_ = Hq = 0
     if q is not None:
-        if q.dim() != 3:
+        shape = q.shape
+        if len(shape) != 3:
             _refuse("q must be [n_rows, n_q_heads, head_dim]")
-        Hq = q.shape[1]
+        Hq = shape[1]
         qs, os_ = _rows(cache, seqs, "q", q, Hq), _rows(cache, seqs, "q_out", q_out, Hq)
         qp, op = q.data_ptr(), q_out.data_ptr()
     ks, vs = _rows(cache, seqs, "k", k, H), _rows(cache, seqs, "v", v, H)

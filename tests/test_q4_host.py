@@ -42,7 +42,7 @@ def test_binding_refusals():
     y = torch.zeros((4, 8))
     for a, match in (((x, w, s[:, :0], y), "scales must be"), ((x, w, torch.zeros((8, 3)).half(), y), "scales must be"),
                      ((x, w, torch.zeros((8, 64)).half(), y), "scales must be"), ((x, w.int(), s, y), "w must"),
-                     ((x, w[:, :31], s, y), "w must"), ((x, w, s.float(), y), "float16"), ((x, w, s[:7], y), "scales must"),
+                     ((x, w[:, :31], s, y), "w must"), ((x, w, s.float(), y), "float16"), ((x, w, s[:7], y), "w must"),
                      ((x, w, s.t().contiguous().t(), y), "scales must"), ((x[0], w, s, y), "matrices"), ((x, w, s[0], y), "matrices"),
                      ((x.float(), w, s, y), "x must"), ((x, w, s, y[:, :7]), "out must"), ((x, w, s, y.double()), "out must"),
                      ((x, w, s, y), "HIP device")):
