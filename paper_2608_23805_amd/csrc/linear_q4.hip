@@ -501,7 +501,7 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
 {
     constexpr int64_t CUS = 256;
     auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
-    if (M <= 16)
+    if (M <= 16 && N <= 1 << 22)              // (a grid holds under 2^32 threads)
         return LinearTile{0, tiles(16, 16) > CUS && (M > 8 || K > 4096) ? 32 : 16, 1};
     for (const LinearTile t : {LinearTile{16, 32, 2}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})

@@ -133,6 +133,24 @@ def test_infinities_stay_in_their_rows(M, N):
     assert rest.sum() == M - (2 if M > 3 else 1) and (M <= 3 or np.isnan(got[M - 1]).all())
 
 
+def test_more_features_than_a_grid_of_small_workgroups_holds():
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case linear_q4 many features")
+    N, K = (1 << 22) + 17, 32
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    w = torch.randint(0, 256, (N, K // 2), device="cuda", dtype=torch.uint8, generator=gen)
+    s = (torch.rand((N, 1), device="cuda", generator=gen) + 0.5).half()
+    x = torch.randn((3, K), device="cuda", generator=gen).bfloat16()
+    y = torch.empty((3, N), device="cuda")
+    msi.linear_q4(x, w, s, y)
+    b = w.to(torch.int32)
+    q = torch.stack([(b & 15 ^ 8) - 8, (b >> 4 ^ 8) - 8], -1).view(N, K).float()
+    want, size = (q @ x.float().t()).t() * s.float().t(), (q.abs() @ x.float().abs().t()).t() * s.float().t()
+    # both sums in fp32, of K products: K 2^-23 of their magnitude
+    assert torch.all((y - want).abs() <= K * 2.0 ** -23 * size)
+
+
 def test_scales_and_rows_of_the_largest_size():
     """Scales at fp16's ends with x of 2^110.  A group's sum, 224 * 2^110, is a number of fp32; times 65504 it is 2^133.8,
     past fp32's 2^128 (and still past it in the sixteenths that codes are), so the fp32 sum of the first feature is infinite
