@@ -1748,21 +1748,21 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
 // Joins a row's partial results: `lanes` = D / 4 threads a (row, head), four
 // elements each; `ways` such sets share a row's units, four sets or more side by
 // side in a workgroup otherwise.  Units of the group first, then the sequence's
-// own, always in the same order.  Behind the sequences, the workgroups that
-// clear rows (MSI_KV_ALL_ROWS).
-__global__ void __launch_bounds__(256) kv_shared_finish_kernel(SharedLaunch A, int ways)
+// own, always in the same order.  Behind the first `mine` workgroups of every
+// sequence, those that clear rows (MSI_KV_ALL_ROWS).
+__global__ void __launch_bounds__(256) kv_shared_finish_kernel(SharedLaunch A, int ways, int mine)
 {
     __shared__ __attribute__((aligned(16))) float sums[1024];
     __shared__ float ml[2][16];
     __shared__ uint32_t words[8];
     const int D = A.c.D, H = A.c.H, G = A.G, Hq = H * G;
-    if (int(blockIdx.z) == A.s.S) {
+    if (int(blockIdx.x) >= mine) {
         auto seq = [&](int i) {
             const KvOwner o = A.owners[A.g.n + i];
             return KvSeq{o.row0, o.n, o.len, true};
         };
-        clear_rest(A.s, seq, A.out, A.out_stride, Hq * D, int(blockIdx.y * gridDim.x + blockIdx.x),
-                   int(gridDim.x * gridDim.y), words);
+        const int each = int(gridDim.x) - mine;
+        clear_rest(A.s, seq, A.out, A.out_stride, Hq * D, int(blockIdx.z) * each + int(blockIdx.x) - mine, each * A.s.S, words);
         return;
     }
     const KvOwner o = A.owners[A.g.n + int(blockIdx.z)];
@@ -1990,10 +1990,11 @@ hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
                 e = launch_units<decltype(f)::value, decltype(d)::value, SHARED>(A, tile_rows, unsigned(items * H), st);
             });
     };
+    const int64_t least = c.small ? 1 : 0;                  // (the first launch leaves the owners)
     if (c.both) {
-        units(2, c.tile_p, int64_t(c.items_p) + c.items_s);
+        units(2, c.tile_p, std::max(least, int64_t(c.items_p) + c.items_s));
     } else {
-        units(0, c.tile_p, std::max(c.items_p, c.small ? 1 : 0));    // (the first launch leaves the owners)
+        units(0, c.tile_p, std::max(least, int64_t(c.items_p)));
         units(1, c.tile_s, c.items_s);
     }
     if (e != hipSuccess)
@@ -2002,8 +2003,8 @@ hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
     const int sets = 1024 / A.c.D;
     const int ways = int64_t(A.s.n_rows) * Hq <= 8192 ? sets : 1;
     const int64_t pairs = int64_t(A.s.max_rows) * Hq, per = sets / ways;
-    launch_k(kv_shared_finish_kernel, dim3(unsigned((pairs + per - 1) / per), 1, unsigned(A.s.S + (A.s.all_rows ? 1 : 0))), 256, 0, st,
-             A, ways);
+    const int mine = int((pairs + per - 1) / per), rest = A.s.all_rows ? (rest_groups(A.s) + A.s.S - 1) / A.s.S : 0;
+    launch_k(kv_shared_finish_kernel, dim3(unsigned(mine + rest), 1, unsigned(A.s.S)), 256, 0, st, A, ways, mine);
     return hipGetLastError();
 }
 

@@ -209,6 +209,22 @@ def test_rows_that_no_sequence_answers_for(rows):
     assert torch.all(out == 0.0)
 
 
+def test_nothing_cached():
+    """Sequences without tokens, and bounds that allow none: rows see nothing."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case shared nothing cached")
+    sh = Shared(826, [(3, 0)], [0, 0, 0], [2, 1, 0], 2, 64, "e4m3")
+    for rows, blocks in ((3, 0), (40, 2)):
+        seqs = msi.KvSeqs(sh.s.seqs.table[:, :0].contiguous(), sh.s.seqs.lens, sh.s.seqs.cu_rows, n_rows=3, max_rows=2, max_len=0)
+        groups = msi.KvGroups(sh.cu, sh.nb, max_rows=rows, max_blocks=blocks)
+        for G in (1, 16, 64):
+            _, out, st = _run(sh, 2 * G, seqs=seqs, groups=groups)
+            assert st == 0 and torch.all(out == 0.0)
+            _, out, st = _run(sh, 2 * G, groups=groups)
+            assert st == 0 and torch.all(out == 0.0)
+
+
 def test_bad_pages():
     """A bad shared page is absent for all of the group, a bad own page for its sequence."""
     log("case shared bad pages")
