@@ -11,7 +11,6 @@ tensors; a call whose tensors lie on several devices is refused."""
 from __future__ import annotations
 
 import ctypes
-import fractions
 import math
 import struct
 from typing import Optional
@@ -253,7 +252,14 @@ def kv_append(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
           _stream(stream, dev))
 
 
-_TWO_PI = fractions.Fraction(6283185307179586476925286766559005768394338798750, 10 ** 48)     # to 48 places
+_TWO_PI, _PLACES = 6283185307179586476925286766559005768394338798750, 10 ** 48
+
+
+def _turns(x: float) -> int:
+    """An angle's fraction of a turn in units of 2^-64, to the nearest."""
+    n, d = x.as_integer_ratio()
+    d *= _TWO_PI
+    return ((n * _PLACES << 65) + d) // (2 * d) % 2 ** 64
 
 
 class KvRotary:
@@ -272,8 +278,7 @@ class KvRotary:
         a = None if axes is None else [int(x) for x in axes]
         if a is not None and (len(a) != len(f) or min(a) < 0 or max(a) > 3):
             _refuse("axes must be as many as the frequencies, 0 .. 3")
-        # fractions of a turn in units of 2^-64, to the nearest
-        turns = [round(fractions.Fraction(x) / _TWO_PI * 2 ** 64) % 2 ** 64 for x in f]
+        turns = [_turns(x) for x in f]
         self.rot_dim, self.interleaved = 2 * len(f), bool(interleaved)
         self.n_axes = 1 if a is None else max(a) + 1
         self.freq = torch.tensor([t - (t >> 63 << 64) for t in turns], dtype=torch.int64).to(device)
