@@ -264,7 +264,8 @@ using LaunchOf = std::conditional_t<FORM == SHARED, SharedLaunch, AttentionLaunc
 // With up to 64 groups and 64 sequences, one a lane, every wavefront of the first
 // launch lays the owners out by itself (its first workgroup leaves them for the
 // kernels behind it); larger batches take a launch of one workgroup (4 answers
-// from a prompt of 192 tokens: 19.5 us with it, 13 without).
+// from a prompt of 192 tokens: 22.6 us with it, 12.8 without; 64 rows of 32768 shared
+// tokens: 105.7 and 94).
 constexpr int PLAN_THREADS = 1024;
 constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below, its partial results outweigh the codes
 constexpr int SMALL_OWNERS = 64;
@@ -1121,6 +1122,11 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
 
     bf16x8 qf[D / 16];
     bf16x8 *const ql = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK) + wave * (D / 16) * 64 + lane;
+    load_q32<D>(qf, A, q, h, w0, rows);
+    if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            ql[c * 64] = qf[c];
     auto query = [&](int c) {
         if constexpr (M::QLDS)
             return ql[c * 64];
@@ -1197,15 +1203,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         asm volatile("" ::: "memory");
     };
     issue(b0);
-    // the queries and scales come between the copies: waiting for them leaves the second block's in flight
-    load_q32<D>(qf, A, q, h, w0, rows);
-    const float2 first_scales = fetch_list(b0);
     issue(b0 + 1);
-    if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c)
-            ql[c * 64] = qf[c];
-    make_list(b0, first_scales);
     // this lane's bytes of V: token row 64 + 16 u + tv, elements 32 c + 16 (lane / 16 % 2) + 8 (lane % 2) ..
     const int tl = (lane & 15) >> 1, tv = (tl < 4 ? tl : 4 + tl) + 4 * hf;
     const int vswz = many_swz<D>(tv);                       // (the same for tv + 16 u)
