@@ -317,6 +317,8 @@ def kv_append_rotary(cache: KvCache, seqs: KvSeqs, rotary: KvRotary, positions, 
     if rotary.rot_dim > cache.head_dim:
         _refuse(f"{rotary.rot_dim} elements rotate, heads have {cache.head_dim}")
     qp = op = qs = os_ = Hq = 0
+    if (q is None) != (q_out is None):
+        _refuse("q and q_out go together")
     if q is not None:
         shape = q.shape
         if len(shape) != 3:

@@ -78,6 +78,23 @@ def test_binding_refusals():
                      ((c, s, r3, p[None].expand(3, 4), q, q, kv, kv), "overlap"), ((c, s, r, p, q[0], q, kv, kv), "q must"),
                      ((c, s, r, p, q, q[:, :3], kv, kv), "q_out must"), ((c, s, r, p, q, q, q, kv), "k must"),
                      ((c, s, msi.KvRotary([0.1] * 40, device="cpu"), p, q, q, kv, kv), "elements rotate"),
+                     ((c, s, r, p, q, None, kv, kv), "together"), ((c, s, r, p, None, q, kv, kv), "together"),
                      ((c, s, r, p, q, q, kv, kv), "HIP device"), ((c, s, r3, p3, None, None, kv, kv), "HIP device")):
         with pytest.raises(msi.MsiError, match=match):
             msi.kv_append_rotary(*a)
+
+
+def test_streams_of_another_device():
+    """A kernel goes to its stream's device, which cannot read the tensors of another: refused."""
+    import types
+    import paper_2608_23805_amd as msi
+    import torch
+    s, c, q, kv = _cpu_seqs(), _cpu_cache(), _w(4, 4, 64), _w(4, 2, 64)
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    other = types.SimpleNamespace(cuda_stream=0, device_index=1)
+    r, g = msi.KvRotary([0.1] * 32, device="cpu"), msi.KvGroups(i32(2), i32(1), max_rows=4, max_blocks=1)
+    w4 = torch.zeros((8, 16), dtype=torch.uint8), torch.zeros((8, 1)).half()
+    for f, a in ((msi.kv_append_rotary, (c, s, r, i32(4), q, q, kv, kv)), (msi.kv_attention_shared, (c, s, g, q, q, 1.0)),
+                 (msi.linear_q4, (_w(4, 32), *w4, _w(4, 8)))):
+        with pytest.raises(msi.MsiError, match="stream"):
+            f(*a, stream=other)
