@@ -467,16 +467,16 @@ template <int ACT>
 hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st)
 {
     if (t.rows == 16)
-        return launch_tile<ACT, Q4Shape<16, 32, 1, 1, 8, 2, 2>>(A, st);
+        return launch_tile<ACT, Q4Shape<16, 32, 1, 2, 8, 2, 1>>(A, st);
     if (t.rows == 32)
-        return t.features == 32 ? launch_tile<ACT, Q4Shape<32, 32, 1, 1, 8, 2, 1>>(A, st)
-                                : launch_tile<ACT, Q4Shape<32, 64, 1, 4, 4, 3, 1>>(A, st);
+        return t.features == 32 ? launch_tile<ACT, Q4Shape<32, 32, 1, 2, 8, 2, 1>>(A, st)
+                                : launch_tile<ACT, Q4Shape<32, 64, 1, 4, 4, 2, 1>>(A, st);
     if (t.rows == 64 && t.features == 64)
-        return launch_tile<ACT, Q4Shape<64, 64, 2, 2, 4, 3, 1>>(A, st);
+        return launch_tile<ACT, Q4Shape<64, 64, 1, 4, 4, 2, 1>>(A, st);
     if (t.rows == 128)
-        return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<128, 128, 2, 4, 2, 2, 1>>(A, st)
+        return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<128, 128, 1, 8, 2, 2, 1>>(A, st)
                              : launch_tile<ACT, Q4Shape<128, 128, 1, 4, 1, 2, 2>>(A, st);
-    return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<64, 128, 1, 8, 2, 3, 1>>(A, st)
+    return t.per_cu == 1 ? launch_tile<ACT, Q4Shape<64, 128, 1, 8, 2, 2, 1>>(A, st)
                          : launch_tile<ACT, Q4Shape<64, 128, 1, 4, 1, 3, 3>>(A, st);
 }
 
@@ -488,13 +488,15 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 // 16 rows, 4096, 2048 7.7 and 8.7; 4096, 8199 15.9 and 13.4].  Above, the smallest
 // tiles that give one to every CU at most, since one wave of workgroups lasts as
 // long as a tile does, and that is the latency of its stages.  [16 x 32, 32 x 32,
-// 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.5 / 10.0 / 14.4 /
-// 20.0 / 27.1 / -; 61, 4096, 8199 29.3 / 32.4 / 23.2 / 23.2 / 32.1 / -; 128, 2048,
-// 5120 18.1 / 20.5 / 16.4 / 14.9 / 20.7 / -; 256, 2048, 8192 46 / 51 / 25.5 / 25.1 /
-// 17.9 / -; 509, 2048, 8192 - / - / - / 49 / 34 / 26.5; weights from HBM.]  Past that,
-// tiles of 128 x 128, two to a CU (wavefronts of 128 x 32, which convert a weight
-// for eight row blocks), or of 64 x 128, three to a CU, whose rounds last about
-// three quarters as long, whichever fills its rounds better [1000, 2048, 8192 43.8
+// 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.8 / 10.3 / 14.3 /
+// 17.6 / 27.2 / 40.3; 61, 4096, 8199 30.0 / 31.2 / 23.7 / 21.6 / 32.1 / 42.9; 128,
+// 2048, 5120 19.2 / 19.9 / 16.3 / 13.6 / 21.3 / 32.9; 256, 2048, 8192 55 / 52 / 27.1 /
+// 25.2 / 18.7 / 26.3; 509, 2048, 8192 104 / 102 / 51 / 49 / 34.7 / 28.4; weights from
+// HBM.]  Their wavefronts, 16 a CU, have all of the tile's rows, so that a weight is
+// converted once (64 x 64, each converted twice and a third buffer: 24.5 for 21.6).
+// Past that, tiles of 128 x 128, two to a CU (wavefronts of 128 x 32, which convert
+// a weight for eight row blocks), or of 64 x 128, three to a CU, whose rounds last
+// about three quarters as long, whichever fills its rounds better [1000, 2048, 8192 43.8
 // and 50.0; 2000, 2048, 8192 84.8 and 97.5; 2000, 2048, 5120 66.5 and 62.9; 4096, 4096, 4096
 // 160 and 179].
 LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
@@ -503,7 +505,7 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
     auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
     if (M <= 16 && N <= 1 << 22)              // (a grid holds under 2^32 threads)
         return LinearTile{0, tiles(16, 16) > CUS && (M > 8 || K > 4096) ? 32 : 16, 1};
-    for (const LinearTile t : {LinearTile{16, 32, 2}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
+    for (const LinearTile t : {LinearTile{16, 32, 1}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
         if (tiles(t.rows, t.features) <= CUS)
             return t;
