@@ -1,7 +1,9 @@
 """Binding of the attention block's operators: projection with its epilogue
-(``linear``), the paged cache of keys and values in 8 bits (``KvCache``,
-``KvSeqs``, ``kv_append``, ``kv_read``), the attention that reads it
-(``kv_attention``) and its eviction (``kv_evict``); see ``include/msi.h``.
+(``linear``, with 4-bit weights ``linear_q4``), the paged cache of keys and
+values in 8 bits (``KvCache``, ``KvSeqs``, ``kv_append``, ``kv_read``, with
+rotation by positions ``KvRotary``, ``kv_append_rotary``), the attention that
+reads it (``kv_attention``, over pages that sequences share ``KvGroups``,
+``kv_attention_shared``) and its eviction (``kv_evict``); see ``include/msi.h``.
 ``AttentionBlock`` runs them in a row as the attention block of a stacked layer.
 
 A decode step makes several of these calls a layer, each a few microseconds
