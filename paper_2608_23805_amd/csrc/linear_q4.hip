@@ -471,6 +471,8 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
     if (t.rows == 32)
         return t.features == 32 ? launch_tile<ACT, Q4Shape<32, 32, 1, 2, 8, 2, 1>>(A, st)
                                 : launch_tile<ACT, Q4Shape<32, 64, 1, 4, 4, 2, 1>>(A, st);
+    if (t.rows == 64 && t.features == 32)
+        return launch_tile<ACT, Q4Shape<64, 32, 1, 2, 8, 2, 1>>(A, st);
     if (t.rows == 64 && t.features == 64)
         return launch_tile<ACT, Q4Shape<64, 64, 1, 4, 4, 2, 1>>(A, st);
     if (t.rows == 128)
@@ -494,6 +496,9 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 // 25.2 / 18.7 / 26.3; 509, 2048, 8192 104 / 102 / 51 / 49 / 34.7 / 28.4; weights from
 // HBM.]  Their wavefronts, 16 a CU, have all of the tile's rows, so that a weight is
 // converted once (64 x 64, each converted twice and a third buffer: 24.5 for 21.6).
+// Long K takes 64 x 32, stages of 512 elements, for 32 x 64 where as many tiles do
+// [61, 4096, 8192 17.2 and 19.2; 128, 4096, 4096 17.0 and 18.8; 61, 8192, 8192 28.3
+// and 32.1; 61, 2048, 8192 12.9 and 12.6; 128, 2048, 4096 11.7 and 11.0].
 // Past that, tiles of 128 x 128, two to a CU (wavefronts of 128 x 32, which convert
 // a weight for eight row blocks), or of 64 x 128, three to a CU, whose rounds last
 // about three quarters as long, whichever fills its rounds better [1000, 2048, 8192 43.8
@@ -508,7 +513,7 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
     for (const LinearTile t : {LinearTile{16, 32, 1}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
         if (tiles(t.rows, t.features) <= CUS)
-            return t;
+            return t.rows == 32 && t.features == 64 && K >= 4096 && tiles(64, 32) <= tiles(32, 64) ? LinearTile{64, 32, 1} : t;
     const int64_t big = (tiles(128, 128) + 2 * CUS - 1) / (2 * CUS), small = (tiles(64, 128) + 3 * CUS - 1) / (3 * CUS);
     return 4 * big <= 3 * small ? LinearTile{128, 128, 2} : LinearTile{64, 128, 3};
 }
