@@ -22,14 +22,14 @@ namespace {
 // Up to 16 rows: bound by the weights' bytes, small calls by the launch and one
 // chain of loads.  A workgroup owns 16 R features; its eight wavefronts take
 // chunks of 256 elements of K in turn and their sums meet in LDS in wavefront
-// order.  Rows of x are the MFMA's A operand, read straight from memory (rows
-// past M repeat the last one), weights the B operand, read along their rows (a
-// load covers 8 rows x 128 bytes) and rearranged in the wavefront's own LDS
-// part.  A lane's outputs are four rows of one feature, so it applies that
-// feature's scales.  Weights from HBM, one row: 2048 x 5120 5.1 us, 4096 x 8199
-// 8.3 us (2.1 TB/s), 8192 x 8192 11.6 us (3.2 TB/s).  (A lane's 16 bytes of x
-// come from another row than its neighbour's, which costs four times the L1's
-// cycles: 16 rows of 4096 x 8199 take 13.4 us, and more rows go through tiles.)
+// order.  Rows of x are the MFMA's A operand, weights the B operand: both are read
+// along their rows (a load covers 8 rows x 128 bytes of weights, 4 rows x 256 of x)
+// and rearranged in the wavefront's own LDS part; what lies there for rows past M
+// ends in results past M.  (Fragments of x straight from memory, every lane from
+// another row than its neighbour, cost four times the L1's cycles: 16 rows, K 4096,
+// N 2048 7.9 us for 5.9.)  A lane's outputs are four rows of one feature, so it
+// applies that feature's scales.  Weights from HBM, one row: 2048 x 5120 5.0 us,
+// 4096 x 8199 8.9 us (1.9 TB/s), 8192 x 8192 11.5 us (3.0 TB/s).
 constexpr int ROWS_WAVES = 8, CHUNK = 8;      // blocks of 32 elements in a chunk
 
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
@@ -93,14 +93,15 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
 {
     constexpr int RS = 16 * CHUNK + 16;                    // LDS bytes of a row of a chunk, padded against bank conflicts
     constexpr int NG = CHUNK / GB;                         // groups of a chunk
-    constexpr int STAGE = R * 16 * RS, SUMS = R * 1024;
+    constexpr int XS = 16 * CHUNK * 2 + 16;                // and of a row of half a chunk of x
+    constexpr int STAGE = R * 16 * RS + 16 * XS, SUMS = R * 1024;
     __shared__ __attribute__((aligned(16))) uint8_t lds[ROWS_WAVES * (STAGE > SUMS ? STAGE : SUMS)];
     const LinearArgs &A = Q.l;
     const int n0 = int(blockIdx.x) * 16 * R;
     const int K = A.K, nblk = K / 32, nchunk = (nblk + CHUNK - 1) / CHUNK, ng = nblk / GB;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    uint8_t *const mine = lds + wave * STAGE;
+    uint8_t *const mine = lds + wave * STAGE, *const xs = mine + R * 16 * RS;
 
     // weights: load k of feature block m brings rows 8 k + lane / 8, the lane's 16 bytes are block lane % 8 of the chunk
     const uint8_t *wp[R][2];
@@ -112,7 +113,11 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
             wp[m][k] = Q.codes + int64_t(min(n0 + 16 * m + 8 * k + (lane >> 3), A.N - 1)) * (K / 2) + 16 * (lane & 7);
         sp[m] = Q.scales + int64_t(min(n0 + 16 * m + r16, A.N - 1)) * ng;
     }
-    const uint16_t *const xp = A.x + int64_t(min(r16, A.M - 1)) * A.x_stride + 8 * g;
+    // x: load j of a half brings rows 4 j + lane / 16, the lane's 16 bytes lie in block lane % 16 / 4 of the half
+    const uint16_t *xp[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        xp[j] = A.x + int64_t(min(4 * j + g, A.M - 1)) * A.x_stride + 8 * r16;
 
     u32x4 w[R][2];
     uint32_t sc[R][NG / 2];
@@ -138,17 +143,16 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
     if (wave < nchunk)
         load_weights(wave);
     for (int c = wave; c < nchunk; c += ROWS_WAVES) {
-        u32x4 x[CHUNK];
+        u32x4 x[2][4];
         const int left = nblk - CHUNK * c;                 // blocks from here on
-        if (left >= CHUNK) {
 #pragma unroll
-            for (int u = 0; u < CHUNK; ++u)
-                x[u] = *reinterpret_cast<const u32x4 *>(xp + 32 * (CHUNK * c + u));
-        } else {                                           // (nothing times whatever is there: the rest is zero)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int u = 0; u < CHUNK; ++u)
-                x[u] = u < left ? *reinterpret_cast<const u32x4 *>(xp + 32 * (CHUNK * c + u)) : u32x4{0, 0, 0, 0};
-        }
+            for (int j = 0; j < 4; ++j)
+                if (4 * j < A.M)                           // (nothing times whatever is there: past K is zero)
+                    x[h][j] = left >= CHUNK || CHUNK / 2 * h + (r16 >> 2) < left
+                                  ? *reinterpret_cast<const u32x4 *>(xp[j] + (CHUNK * 32 * c + CHUNK * 16 * h))
+                                  : u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int m = 0; m < R; ++m)
 #pragma unroll
@@ -160,12 +164,18 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
 #pragma unroll
             for (int i = 0; i < NG / 2; ++i)
                 now[m][i] = sc[m][i];
-        // (a wavefront's LDS operations are in order; the fences keep the compiler from moving them)
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         if (c + ROWS_WAVES < nchunk)
             load_weights(c + ROWS_WAVES);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
+            if (j * GB % (CHUNK / 2) == 0) {               // (a wavefront's LDS operations are in order; the fences keep
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");   // the compiler from moving them)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * i < A.M)
+                        *reinterpret_cast<u32x4 *>(xs + (4 * i + g) * XS + 16 * r16) = x[j * GB / (CHUNK / 2)][i];
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            }
             f32x4 part[R];
 #pragma unroll
             for (int m = 0; m < R; ++m)
@@ -173,10 +183,11 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
 #pragma unroll
             for (int b = 0; b < GB; ++b) {
                 const int u = j * GB + b;
+                const bf16x8 xf = as_bf16x8(*reinterpret_cast<const u32x4 *>(xs + r16 * XS + u % (CHUNK / 2) * 64 + 16 * g));
 #pragma unroll
                 for (int m = 0; m < R; ++m) {
                     const bf16x8 wf = unpack_q4_16th(*reinterpret_cast<const uint32_t *>(mine + (16 * m + r16) * RS + 16 * u + 4 * g));
-                    part[m] = mfma16(as_bf16x8(x[u]), wf, part[m]);
+                    part[m] = mfma16(xf, wf, part[m]);
                 }
             }
 #pragma unroll
@@ -485,9 +496,10 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 }  // namespace
 
 // Up to 16 rows: no tiles (rows and features of a workgroup), 32 features where
-// they make 256 workgroups and the rows or K give them something to do [us, 16
-// and 32 features: 4 rows, K 4096, N 8199 10.1 and 10.4; K, N 8192 14.7 and 12.7;
-// 16 rows, 4096, 2048 7.7 and 8.7; 4096, 8199 15.9 and 13.4].  Above, the smallest
+// 16 make more than 256 workgroups and there are more than 8 rows, whose x is read
+// by half as many [us, 16 and 32 features: 1 row, K 8192, N 8192 11.5 and 12.4; 8
+// rows, 4096, 8199 10.0 and 10.5; 16 rows, 4096, 2048 5.8 and 7.5; 4096, 5120 9.0 and
+// 7.8; 8192, 8192 16.1 and 14.0].  Above, the smallest
 // tiles that give one to every CU at most, since one wave of workgroups lasts as
 // long as a tile does, and that is the latency of its stages.  [16 x 32, 32 x 32,
 // 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.8 / 10.3 / 14.3 /
@@ -509,7 +521,7 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
     constexpr int64_t CUS = 256;
     auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
     if (M <= 16 && N <= 1 << 22)              // (a grid holds under 2^32 threads)
-        return LinearTile{0, tiles(16, 16) > CUS && (M > 8 || K > 4096) ? 32 : 16, 1};
+        return LinearTile{0, tiles(16, 16) > CUS && M > 8 ? 32 : 16, 1};
     for (const LinearTile t : {LinearTile{16, 32, 1}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
         if (tiles(t.rows, t.features) <= CUS)
