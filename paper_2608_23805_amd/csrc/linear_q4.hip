@@ -19,13 +19,13 @@ namespace {
 
 // ---------------------------------------------------------------- few rows
 //
-// Up to 16 rows: bound by the weights' bytes, small calls by the launch and one
+// Up to 16 MB rows: bound by the weights' bytes, small calls by the launch and one
 // chain of loads.  A workgroup owns 16 R features; its eight wavefronts take
 // chunks of 256 elements of K in turn and their sums meet in LDS in wavefront
 // order.  Rows of x are the MFMA's A operand, weights the B operand: both are read
-// along their rows (a load covers 8 rows x 128 bytes of weights, 4 rows x 256 of x)
-// and rearranged in the wavefront's own LDS part; what lies there for rows past M
-// ends in results past M.  (Fragments of x straight from memory, every lane from
+// along their rows (a load covers 8 rows x 128 bytes of weights, 4 rows x 256 or 8 x
+// 128 of x) and rearranged in the wavefront's own LDS part; what lies there for rows
+// past M ends in results past M.  (Fragments of x straight from memory, every lane from
 // another row than its neighbour, cost four times the L1's cycles: 16 rows, K 4096,
 // N 2048 7.9 us for 5.9.)  A lane's outputs are four rows of one feature, so it
 // applies that feature's scales.  Weights from HBM, one row: 2048 x 5120 5.0 us,
@@ -88,13 +88,14 @@ __device__ __forceinline__ void store1(const LinearArgs &A, int act, int64_t m, 
         A.out_bf16[m * A.out_stride + n] = f32_to_bf16(z);
 }
 
-template <int R, int GB>
-__global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kernel(LinearQ4Args Q, int act)
+template <int R, int MB, int GB>
+__global__ void __launch_bounds__(64 * ROWS_WAVES, R * MB == 1 ? 4 : 2) q4_rows_kernel(LinearQ4Args Q, int act)
 {
     constexpr int RS = 16 * CHUNK + 16;                    // LDS bytes of a row of a chunk, padded against bank conflicts
     constexpr int NG = CHUNK / GB;                         // groups of a chunk
-    constexpr int XS = 16 * CHUNK * 2 + 16;                // and of a row of half a chunk of x
-    constexpr int STAGE = R * 16 * RS + 16 * XS, SUMS = R * 1024;
+    constexpr int XB = 4 / MB, XS = 64 * XB + 16;          // blocks of x in LDS at a time, bytes of such a row
+    constexpr int XL = 4 * XB, XR = 64 / XL;               // lanes of a row of a load of x, rows
+    constexpr int STAGE = R * 16 * RS + MB * 16 * XS, SUMS = R * MB * 1024;
     __shared__ __attribute__((aligned(16))) uint8_t lds[ROWS_WAVES * (STAGE > SUMS ? STAGE : SUMS)];
     const LinearArgs &A = Q.l;
     const int n0 = int(blockIdx.x) * 16 * R;
@@ -113,11 +114,10 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
             wp[m][k] = Q.codes + int64_t(min(n0 + 16 * m + 8 * k + (lane >> 3), A.N - 1)) * (K / 2) + 16 * (lane & 7);
         sp[m] = Q.scales + int64_t(min(n0 + 16 * m + r16, A.N - 1)) * ng;
     }
-    // x: load j of a half brings rows 4 j + lane / 16, the lane's 16 bytes lie in block lane % 16 / 4 of the half
     const uint16_t *xp[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        xp[j] = A.x + int64_t(min(4 * j + g, A.M - 1)) * A.x_stride + 8 * r16;
+        xp[j] = A.x + int64_t(min(XR * j + lane / XL, A.M - 1)) * A.x_stride + 8 * (lane % XL);
 
     u32x4 w[R][2];
     uint32_t sc[R][NG / 2];
@@ -136,22 +136,24 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
                 read_scales_tail<NG>(sc[m], sp[m] + NG * c, ng - NG * c);
         }
     };
-    f32x4 acc[R];
+    f32x4 acc[MB][R];
 #pragma unroll
-    for (int m = 0; m < R; ++m)
-        acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int m = 0; m < R; ++m)
+            acc[a][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (wave < nchunk)
         load_weights(wave);
     for (int c = wave; c < nchunk; c += ROWS_WAVES) {
-        u32x4 x[2][4];
+        u32x4 x[CHUNK / XB][4];
         const int left = nblk - CHUNK * c;                 // blocks from here on
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < CHUNK / XB; ++h)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (4 * j < A.M)                           // (nothing times whatever is there: past K is zero)
-                    x[h][j] = left >= CHUNK || CHUNK / 2 * h + (r16 >> 2) < left
-                                  ? *reinterpret_cast<const u32x4 *>(xp[j] + (CHUNK * 32 * c + CHUNK * 16 * h))
+                if (XR * j < A.M)                          // (nothing times whatever is there: past K is zero)
+                    x[h][j] = left >= CHUNK || XB * h + lane % XL / 4 < left
+                                  ? *reinterpret_cast<const u32x4 *>(xp[j] + 32 * (CHUNK * c + XB * h))
                                   : u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int m = 0; m < R; ++m)
@@ -168,34 +170,43 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
             load_weights(c + ROWS_WAVES);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            if (j * GB % (CHUNK / 2) == 0) {               // (a wavefront's LDS operations are in order; the fences keep
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");   // the compiler from moving them)
+            f32x4 part[MB][R];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (4 * i < A.M)
-                        *reinterpret_cast<u32x4 *>(xs + (4 * i + g) * XS + 16 * r16) = x[j * GB / (CHUNK / 2)][i];
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            }
-            f32x4 part[R];
+            for (int a = 0; a < MB; ++a)
 #pragma unroll
-            for (int m = 0; m < R; ++m)
-                part[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int m = 0; m < R; ++m)
+                    part[a][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int b = 0; b < GB; ++b) {
                 const int u = j * GB + b;
-                const bf16x8 xf = as_bf16x8(*reinterpret_cast<const u32x4 *>(xs + r16 * XS + u % (CHUNK / 2) * 64 + 16 * g));
+                if (u % XB == 0) {                         // (a wavefront's LDS operations are in order; the fences keep
+                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");   // the compiler from moving them)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (XR * i < A.M)
+                            *reinterpret_cast<u32x4 *>(xs + (XR * i + lane / XL) * XS + 16 * (lane % XL)) = x[u / XB][i];
+                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                }
+                bf16x8 xf[MB];
+#pragma unroll
+                for (int a = 0; a < MB; ++a)
+                    xf[a] = as_bf16x8(*reinterpret_cast<const u32x4 *>(xs + (16 * a + r16) * XS + u % XB * 64 + 16 * g));
 #pragma unroll
                 for (int m = 0; m < R; ++m) {
                     const bf16x8 wf = unpack_q4_16th(*reinterpret_cast<const uint32_t *>(mine + (16 * m + r16) * RS + 16 * u + 4 * g));
-                    part[m] = mfma16(xf, wf, part[m]);
+#pragma unroll
+                    for (int a = 0; a < MB; ++a)
+                        part[a][m] = mfma16(xf[a], wf, part[a][m]);
                 }
             }
 #pragma unroll
             for (int m = 0; m < R; ++m) {
                 const float s = half_to_float(uint16_t(now[m][j >> 1] >> (16 * (j & 1))));
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    acc[m][k] = fmaf(s, part[m][k], acc[m][k]);
+                for (int a = 0; a < MB; ++a)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        acc[a][m][k] = fmaf(s, part[a][m][k], acc[a][m][k]);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -203,15 +214,17 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R == 1 ? 4 : 2) q4_rows_kerne
     __syncthreads();                                       // the rows' place becomes the sums'
     f32x4 *const sums = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
-    for (int m = 0; m < R; ++m)
-        sums[(wave * R + m) * 64 + lane] = acc[m];
+    for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int m = 0; m < R; ++m)
+            sums[((wave * MB + a) * R + m) * 64 + lane] = acc[a][m];
     __syncthreads();
-    if (wave < R) {
+    if (wave < MB * R) {
         f32x4 z = sums[wave * 64 + lane];
 #pragma unroll
         for (int o = 1; o < ROWS_WAVES; ++o)
-            z += sums[(o * R + wave) * 64 + lane];
-        const int n = n0 + 16 * wave + r16, m = 4 * g;
+            z += sums[(o * MB * R + wave) * 64 + lane];
+        const int n = n0 + 16 * (wave % R) + r16, m = 16 * (wave / R) + 4 * g;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (m + k < A.M && n < A.N)
@@ -443,16 +456,16 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
                                     vm - wm * MB * 16, n0 + wn * NB * 16);
 }
 
-template <int R>
+template <int R, int MB>
 hipError_t launch_rows(const LinearQ4Args &A, int act, hipStream_t st)
 {
     const unsigned grid = unsigned((A.l.N + 16 * R - 1) / (16 * R));
     if (A.group == 32)
-        launch_k(q4_rows_kernel<R, 1>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, MB, 1>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     else if (A.group == 64)
-        launch_k(q4_rows_kernel<R, 2>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, MB, 2>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     else
-        launch_k(q4_rows_kernel<R, 4>, grid, 64 * ROWS_WAVES, 0, st, A, act);
+        launch_k(q4_rows_kernel<R, MB, 4>, grid, 64 * ROWS_WAVES, 0, st, A, act);
     return hipGetLastError();
 }
 
@@ -499,7 +512,9 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 // 16 make more than 256 workgroups and there are more than 8 rows, whose x is read
 // by half as many [us, 16 and 32 features: 1 row, K 8192, N 8192 11.5 and 12.4; 8
 // rows, 4096, 8199 10.0 and 10.5; 16 rows, 4096, 2048 5.8 and 7.5; 4096, 5120 9.0 and
-// 7.8; 8192, 8192 16.1 and 14.0].  Above, the smallest
+// 7.8; 8192, 8192 16.1 and 14.0].  Up to 32 rows likewise, while that makes no more than
+// 256 workgroups [20, 8192, 2048 11.3 for 16.9 in tiles; 24, 4096, 2048 7.3 for 8.5; 32,
+// 4096, 5120 9.9 for 11.7; 32, 2048, 16384 13.7 for 11.1].  Above, the smallest
 // tiles that give one to every CU at most, since one wave of workgroups lasts as
 // long as a tile does, and that is the latency of its stages.  [16 x 32, 32 x 32,
 // 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.8 / 10.3 / 14.3 /
@@ -522,6 +537,8 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
     auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
     if (M <= 16 && N <= 1 << 22)              // (a grid holds under 2^32 threads)
         return LinearTile{0, tiles(16, 16) > CUS && M > 8 ? 32 : 16, 1};
+    if (M <= 32 && tiles(32, 32) <= CUS)
+        return LinearTile{0, tiles(32, 16) > CUS ? 32 : 16, 1};
     for (const LinearTile t : {LinearTile{16, 32, 1}, LinearTile{32, 32, 1}, LinearTile{32, 64, 1}, LinearTile{64, 64, 1},
                                LinearTile{64, 128, 1}, LinearTile{128, 128, 1}})
         if (tiles(t.rows, t.features) <= CUS)
@@ -533,8 +550,11 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
 hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st)
 {
     const LinearTile t = linear_q4_tile(A.l.M, A.l.N, A.l.K);
-    if (t.rows == 0)
-        return t.features == 16 ? launch_rows<1>(A, act, st) : launch_rows<2>(A, act, st);
+    if (t.rows == 0) {
+        if (A.l.M <= 16)
+            return t.features == 16 ? launch_rows<1, 1>(A, act, st) : launch_rows<2, 1>(A, act, st);
+        return t.features == 16 ? launch_rows<1, 2>(A, act, st) : launch_rows<2, 2>(A, act, st);
+    }
     switch (act) {
     case LINEAR_SILU: return launch_act<LINEAR_SILU>(A, t, st);
     case LINEAR_GELU: return launch_act<LINEAR_GELU>(A, t, st);

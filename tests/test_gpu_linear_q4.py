@@ -89,8 +89,10 @@ def test_many_workgroups(M, K, N, group):
     _case(M, K, N, group, residual="f32", out="f32", inplace=True)
 
 
-FORMS = [((5, 4096, 300), (0, 16, 1)), ((12, 256, 4200), (0, 32, 1)), ((9, 8224, 4200), (0, 32, 1)), ((3, 8224, 4200), (0, 16, 1)), ((33, 544, 500), (16, 32, 1)),
-         ((100, 1056, 2000), (32, 32, 1)), ((70, 544, 4099), (32, 64, 1)), ((130, 800, 5001), (64, 64, 1)), ((200, 416, 8190), (64, 128, 1)),
+FORMS = [((5, 4096, 300), (0, 16, 1)), ((12, 256, 4200), (0, 32, 1)), ((17, 4128, 300), (0, 16, 1)), ((25, 288, 4001), (0, 16, 1)),
+         ((32, 1056, 8190), (0, 32, 1)), ((21, 2400, 5003), (0, 32, 1)), ((32, 1056, 8200), (32, 64, 1)),
+         ((9, 8224, 4200), (0, 32, 1)), ((3, 8224, 4200), (0, 16, 1)), ((33, 544, 500), (16, 32, 1)), ((100, 1056, 2000), (32, 32, 1)),
+         ((70, 544, 4099), (32, 64, 1)), ((130, 800, 5001), (64, 64, 1)), ((200, 416, 8190), (64, 128, 1)),
          ((61, 4128, 8190), (64, 32, 1)), ((40, 4608, 5001), (64, 32, 1)), ((65, 4128, 5001), (32, 64, 1)),
          ((600, 352, 5003), (128, 128, 1)), ((1100, 672, 4001), (64, 128, 3)), ((990, 416, 8190), (128, 128, 2))]
 

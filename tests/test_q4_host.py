@@ -58,7 +58,8 @@ def test_tiles_of_many_features():
     """A grid holds under 2^32 threads: past 2^22 features few rows go through tiles as well."""
     import paper_2608_23805_amd as msi
     v = [ctypes.c_uint32() for _ in range(3)]
-    for M, N, few in ((1, 1 << 22, True), (1, (1 << 22) + 1, False), (16, 1 << 29, False), (17, 1, False)):
+    for M, N, few in ((1, 1 << 22, True), (1, (1 << 22) + 1, False), (16, 1 << 29, False), (17, 1, True), (32, 8192, True),
+                      (32, 8193, False), (33, 1, False)):
         assert msi.lib.msi_debug_linear_q4_tile(M, N, 32, *map(ctypes.byref, v)) == msi.MSI_OK
         rows, features, _ = (x.value for x in v)
         assert (rows == 0) == few
