@@ -890,10 +890,17 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // everything in the vector registers, where the rescaling needs the outputs (in
 // the accumulation registers every block would move all of them there and back:
 // 753 us for 640).  4096 rows on top of 4096 tokens, two sequences, 16 query heads
-// of 256: 890 us, 926 TFLOP/s; 32 of 128: 795 us, 1038 TFLOP/s (int8 codes, whose
-// conversion takes the vector unit twice as long: about 790).  The conversions
+// of 256: 890 us, 926 TFLOP/s; 32 of 128: 795 us, 1038 TFLOP/s.  The conversions
 // bound it: with heads of 256 and eight wavefronts of 16 rows, two a SIMD, every
 // wavefront converts the whole block, 928 us for 890.
+//
+// int8 codes take the vector unit twice as long as e4m3 to convert.  With heads up
+// to 128 the four wavefronts convert a quarter of a block each and leave it in LDS
+// as the fragments in bf16 that all of them then read (2048 rows on 2048 tokens, two
+// sequences, 32 query heads of 128: 237 us for 263, of 64: 148 for 185; 64 rows of
+// 32768 shared tokens 88 for 95).  For e4m3 those reads take longer than the
+// conversions (8 questions of 256 rows on 16384 shared tokens 414 us for 391).
+// With heads of 256 LDS has no room for them.
 //
 // LDS: 16-byte chunk c of token row t (K rows, then V rows) sits at slot
 // c ^ many_swz(t) of its row: the 16-byte reads of eight consecutive K rows and the
@@ -912,8 +919,11 @@ struct ManyRows {
     static constexpr int CPR = D / 16;                    // chunks of a row
     static constexpr bool QLDS = D == 256;
     static constexpr int QBYTES = QLDS ? ROWS * D * 2 : 0;
-    static constexpr size_t LDS = size_t(NBUF) * BLOCK + QBYTES;
-    static_assert(LDS <= 160 * 1024, "");
+    template <int FMT>
+    static constexpr bool TURNS = FMT == KV_INT8 && D <= 128;    // the wavefronts convert a quarter of a block each
+    template <int FMT>
+    static constexpr size_t LDS = size_t(NBUF) * BLOCK + QBYTES + (TURNS<FMT> ? 2 * BLOCK : 0);
+    static_assert(LDS<KV_INT8> <= 160 * 1024 && LDS<KV_E4M3> <= 160 * 1024, "");
 };
 
 template <int D>
@@ -1024,6 +1034,55 @@ __device__ __forceinline__ void copy_and_score(f32x16 (&sv)[2], const uint8_t *_
 {
     cl.copy(later, block, valid);
     scores32<FMT, D>(sv, tile, query);
+}
+
+// Copies of a later block into `later`, and this wavefront's quarter of the block at `tile` as bf16 fragments: K's 4 p +
+// 2 e + b as scores32 reads them, then V's (D / 32) u + c as times_v does, 1024 bytes each, lane by lane.
+template <int FMT, int D>
+__device__ __forceinline__ void copy_and_convert(bf16x8 *__restrict__ frags, const uint8_t *__restrict__ tile,
+                                                 uint8_t *__restrict__ later, const CopyLane<D> &cl, const uint8_t *block, int valid,
+                                                 int wave, uint32_t vrow, uint32_t vswz)
+{
+    cl.copy(later, block, valid);
+    const int lane = threadIdx.x & 63;
+    const int t = lane & 31, swz = many_swz<D>(t), hf = lane >> 5, vc = (lane >> 4) & 1;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {                       // (row block b, chunk pair p: both halves e of its chunk)
+        const int at = wave * (D / 64) + i, p = at >> 1, b = at & 1;
+        const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + (32 * b + t) * D + (((2 * p + hf) ^ swz) << 4));
+        frags[(4 * p + b) * 64 + lane] = codes_bf16<FMT>(w[0], w[1]);
+        frags[(4 * p + 2 + b) * 64 + lane] = codes_bf16<FMT>(w[2], w[3]);
+    }
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {                       // V's token rows 16 wave ..
+        const i32x2 w = read_tr8(tile + vrow + 16 * wave * D + (((2 * c + vc) ^ vswz) << 4));
+        frags[(D / 8 + wave * (D / 32) + c) * 64 + lane] = codes_bf16<FMT>(uint32_t(w[0]), uint32_t(w[1]));
+    }
+}
+
+template <int D, typename Query>
+__device__ __forceinline__ void score_frags(f32x16 (&sv)[2], const bf16x8 *__restrict__ frags, Query query)
+{
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            sv[b][v] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            sv[b] = mfma32(frags[(2 * c + b) * 64], query(c), sv[b]);
+}
+
+template <int D>
+__device__ __forceinline__ void frags_times_v(f32x16 (&acc)[D / 32], const bf16x8 (&pf)[4], const bf16x8 *__restrict__ frags)
+{
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+            acc[c] = mfma32(frags[(D / 8 + u * (D / 32) + c) * 64], pf[u], acc[c]);
 }
 
 // O^T += V^T P^T of the block at `tile`.
@@ -1213,6 +1272,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     for (int c = 0; c < D / 32; ++c)
         vchunk[c] = uint32_t(((2 * c + vc) ^ vswz) << 4);
     const uint32_t vrow = uint32_t((KV_BLOCK + tv) * D + 8 * (lane & 1));
+    bf16x8 *const frags = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK + M::QBYTES);
 
     for (int b = b0; b < b1; ++b) {
         // block b has landed (b + 1 is in flight); the buffer of block b - 1 is free
@@ -1224,12 +1284,22 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         const int valid = valid_at(b + 2);
         const uint8_t *const tile = lds8 + (b - b0) % M::NBUF * M::BLOCK;
         uint8_t *const later = lds8 + (b + 2 - b0) % M::NBUF * M::BLOCK;
-        if (t0 >= wave_most) {                              // (as is every later block)
-            cl.copy(later, block, valid);
-            continue;
-        }
         f32x16 sv[2];
-        copy_and_score<FMT, D>(sv, tile, query, later, cl, block, valid);
+        if constexpr (M::template TURNS<FMT>) {
+            copy_and_convert<FMT, D>(frags, tile, later, cl, block, valid, wave, vrow, uint32_t(vswz));
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();                   // the block is there in bf16
+            asm volatile("" ::: "memory");
+            if (t0 >= wave_most)                            // (as is every later block)
+                continue;
+            score_frags<D>(sv, frags + lane, query);
+        } else {
+            if (t0 >= wave_most) {
+                cl.copy(later, block, valid);
+                continue;
+            }
+            copy_and_score<FMT, D>(sv, tile, query, later, cl, block, valid);
+        }
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kscale), b - list_at));
         const float vl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vlog), b - list_at));
         const bool here = __builtin_amdgcn_readlane(pages, b - list_at) >= 0;
@@ -1277,7 +1347,10 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
                                   pack_bf16x2_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16x2_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
         }
         l = fmaf(sum, low ? 0.0f : __builtin_amdgcn_exp2f(-vl), l);
-        times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
+        if constexpr (M::template TURNS<FMT>)
+            frags_times_v<D>(acc, pf, frags + lane);
+        else
+            times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
     }
     __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(0));              // copies in flight write this workgroup's LDS
 
@@ -1847,10 +1920,10 @@ hipError_t launch_units(const LaunchOf<FORM> &A, int tile_rows, unsigned grid, h
 {
     if (tile_rows == 128) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, FORM>), ManyRows<D>::LDS, done);
+        const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, FORM>), ManyRows<D>::template LDS<FMT>, done);
         if (e != hipSuccess)
             return e;
-        launch_k(kv_many_rows_kernel<FMT, D, FORM>, grid, 256, ManyRows<D>::LDS, st, A);
+        launch_k(kv_many_rows_kernel<FMT, D, FORM>, grid, 256, ManyRows<D>::template LDS<FMT>, st, A);
     } else if (tile_rows == 16) {
         launch_k(kv_few_rows_kernel<FMT, D, 1, FORM>, grid, 256, 0, st, A);
     } else {
