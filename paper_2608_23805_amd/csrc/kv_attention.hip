@@ -883,7 +883,7 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // Bound by the matrix cores and the vector unit beside them.  A workgroup of
 // four wavefronts owns 128 packed rows, 32 a wavefront, and walks the cache a
 // block of 64 tokens at a time.  The blocks' codes are copied as they are into
-// a ring of three LDS buffers (half the LDS traffic of bf16 tiles, which would
+// a ring of two or three LDS buffers (half the LDS traffic of bf16 tiles, which would
 // bound 32-row wavefronts) and become bf16 on their way from LDS to
 // v_mfma_f32_32x32x16_bf16.  With D = 256 the 32 rows' outputs alone take 128
 // registers, so the queries lie in LDS as well, in the order of their fragments; that keeps
@@ -894,13 +894,14 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // bound it: with heads of 256 and eight wavefronts of 16 rows, two a SIMD, every
 // wavefront converts the whole block, 928 us for 890.
 //
-// int8 codes take the vector unit twice as long as e4m3 to convert.  With heads up
-// to 128 the four wavefronts convert a quarter of a block each and leave it in LDS
-// as the fragments in bf16 that all of them then read (2048 rows on 2048 tokens, two
-// sequences, 32 query heads of 128: 237 us for 263, of 64: 148 for 185; 64 rows of
-// 32768 shared tokens 88 for 95).  For e4m3 those reads take longer than the
-// conversions (8 questions of 256 rows on 16384 shared tokens 414 us for 391).
-// With heads of 256 LDS has no room for them.
+// int8 codes take the vector unit twice as long as e4m3 to convert.  The four
+// wavefronts convert a quarter of a block each and leave it in LDS as the fragments
+// in bf16 that all of them then read; with heads of 256 LDS has room for those of V
+// (two sequences of 4096 tokens: the last 2048 rows, 32 query heads of 128 237 us for
+// 263, of 64 148 for 185; the last 1024 rows, 16 of 256 198 for 220.  64 rows of 32768
+// shared tokens 88 for 95).  For e4m3 those reads take longer than the conversions
+// (8 questions of 256 rows on 16384 shared tokens 414 us for 391, two sequences of
+// 2041 and 3815 rows with heads of 256 700 for 663).
 //
 // LDS: 16-byte chunk c of token row t (K rows, then V rows) sits at slot
 // c ^ many_swz(t) of its row: the 16-byte reads of eight consecutive K rows and the
@@ -913,17 +914,22 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // back with eight tokens of one element.
 template <int D>
 struct ManyRows {
-    static constexpr int ROWS = 128, NBUF = 3;
+    static constexpr int ROWS = 128;
     static constexpr int BLOCK = 2 * KV_BLOCK * D;        // bytes of a block's codes
     static constexpr int COPIES = BLOCK / 4096;           // copy instructions of a wavefront and block
     static constexpr int CPR = D / 16;                    // chunks of a row
     static constexpr bool QLDS = D == 256;
     static constexpr int QBYTES = QLDS ? ROWS * D * 2 : 0;
-    template <int FMT>
-    static constexpr bool TURNS = FMT == KV_INT8 && D <= 128;    // the wavefronts convert a quarter of a block each
-    template <int FMT>
-    static constexpr size_t LDS = size_t(NBUF) * BLOCK + QBYTES + (TURNS<FMT> ? 2 * BLOCK : 0);
-    static_assert(LDS<KV_INT8> <= 160 * 1024 && LDS<KV_E4M3> <= 160 * 1024, "");
+};
+
+// What a workgroup converts once (K, V: each wavefront a quarter of a block), and its LDS: codes, queries, fragments.
+template <int FMT, int D>
+struct ManyForm {
+    static constexpr bool K = FMT == KV_INT8 && D <= 128, V = FMT == KV_INT8;
+    static constexpr int NBUF = V && !K ? 2 : 3, AHEAD = NBUF - 1;
+    static constexpr int QUERIES = NBUF * ManyRows<D>::BLOCK, FRAGS = QUERIES + ManyRows<D>::QBYTES;
+    static constexpr size_t LDS = FRAGS + (int(K) + int(V)) * ManyRows<D>::BLOCK;
+    static_assert(LDS <= 160 * 1024, "");
 };
 
 template <int D>
@@ -1036,8 +1042,8 @@ __device__ __forceinline__ void copy_and_score(f32x16 (&sv)[2], const uint8_t *_
     scores32<FMT, D>(sv, tile, query);
 }
 
-// Copies of a later block into `later`, and this wavefront's quarter of the block at `tile` as bf16 fragments: K's 4 p +
-// 2 e + b as scores32 reads them, then V's (D / 32) u + c as times_v does, 1024 bytes each, lane by lane.
+// Copies of a later block into `later`, and this wavefront's quarter of the block at `tile` as bf16 fragments: K's (if they
+// are shared) 4 p + 2 e + b as scores32 reads them, then V's (D / 32) u + c as times_v does, 1024 bytes each, lane by lane.
 template <int FMT, int D>
 __device__ __forceinline__ void copy_and_convert(bf16x8 *__restrict__ frags, const uint8_t *__restrict__ tile,
                                                  uint8_t *__restrict__ later, const CopyLane<D> &cl, const uint8_t *block, int valid,
@@ -1046,8 +1052,9 @@ __device__ __forceinline__ void copy_and_convert(bf16x8 *__restrict__ frags, con
     cl.copy(later, block, valid);
     const int lane = threadIdx.x & 63;
     const int t = lane & 31, swz = many_swz<D>(t), hf = lane >> 5, vc = (lane >> 4) & 1;
+    constexpr bool K = ManyForm<FMT, D>::K;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {                       // (row block b, chunk pair p: both halves e of its chunk)
+    for (int i = 0; i < (K ? D / 64 : 0); ++i) {             // (row block b, chunk pair p: both halves e of its chunk)
         const int at = wave * (D / 64) + i, p = at >> 1, b = at & 1;
         const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + (32 * b + t) * D + (((2 * p + hf) ^ swz) << 4));
         frags[(4 * p + b) * 64 + lane] = codes_bf16<FMT>(w[0], w[1]);
@@ -1056,7 +1063,7 @@ __device__ __forceinline__ void copy_and_convert(bf16x8 *__restrict__ frags, con
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {                       // V's token rows 16 wave ..
         const i32x2 w = read_tr8(tile + vrow + 16 * wave * D + (((2 * c + vc) ^ vswz) << 4));
-        frags[(D / 8 + wave * (D / 32) + c) * 64 + lane] = codes_bf16<FMT>(uint32_t(w[0]), uint32_t(w[1]));
+        frags[((K ? D / 8 : 0) + wave * (D / 32) + c) * 64 + lane] = codes_bf16<FMT>(uint32_t(w[0]), uint32_t(w[1]));
     }
 }
 
@@ -1082,7 +1089,7 @@ __device__ __forceinline__ void frags_times_v(f32x16 (&acc)[D / 32], const bf16x
     for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
-            acc[c] = mfma32(frags[(D / 8 + u * (D / 32) + c) * 64], pf[u], acc[c]);
+            acc[c] = mfma32(frags[(u * (D / 32) + c) * 64], pf[u], acc[c]);
 }
 
 // O^T += V^T P^T of the block at `tile`.
@@ -1130,6 +1137,7 @@ template <int FMT, int D, int FORM>
 __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
 {
     using M = ManyRows<D>;
+    using F = ManyForm<FMT, D>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds8[];
     if constexpr (FORM == ALL)
         if (int(blockIdx.x) >= A.main) {
@@ -1180,7 +1188,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     const int wave_most = idle ? 0 : limit_of(min(w0 + 31, rows - 1) / A.G);
 
     bf16x8 qf[D / 16];
-    bf16x8 *const ql = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK) + wave * (D / 16) * 64 + lane;
+    bf16x8 *const ql = reinterpret_cast<bf16x8 *>(lds8 + F::QUERIES) + wave * (D / 16) * 64 + lane;
     load_q32<D>(qf, A, q, h, w0, rows);
     if constexpr (M::QLDS)                                  // (each lane reads what it wrote)
 #pragma unroll
@@ -1253,7 +1261,7 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     };
     auto issue = [&](int b) {
         const uint8_t *block = block_at(b);
-        cl.copy(lds8 + (b - b0) % M::NBUF * M::BLOCK, block, valid_at(b));
+        cl.copy(lds8 + (b - b0) % F::NBUF * M::BLOCK, block, valid_at(b));
     };
     auto arrive = [&](auto waitn) {
         __builtin_amdgcn_s_waitcnt(VMCNT_WAIT(decltype(waitn)::value));
@@ -1262,7 +1270,8 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
         asm volatile("" ::: "memory");
     };
     issue(b0);
-    issue(b0 + 1);
+    if constexpr (F::AHEAD > 1)
+        issue(b0 + 1);
     // this lane's bytes of V: token row 64 + 16 u + tv, elements 32 c + 16 (lane / 16 % 2) + 8 (lane % 2) ..
     const int tl = (lane & 15) >> 1, tv = (tl < 4 ? tl : 4 + tl) + 4 * hf;
     const int vswz = many_swz<D>(tv);                       // (the same for tv + 16 u)
@@ -1272,27 +1281,31 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
     for (int c = 0; c < D / 32; ++c)
         vchunk[c] = uint32_t(((2 * c + vc) ^ vswz) << 4);
     const uint32_t vrow = uint32_t((KV_BLOCK + tv) * D + 8 * (lane & 1));
-    bf16x8 *const frags = reinterpret_cast<bf16x8 *>(lds8 + M::NBUF * M::BLOCK + M::QBYTES);
+    bf16x8 *const frags = reinterpret_cast<bf16x8 *>(lds8 + F::FRAGS);
 
     for (int b = b0; b < b1; ++b) {
         // block b has landed (b + 1 is in flight); the buffer of block b - 1 is free
-        arrive(std::integral_constant<int, M::COPIES>{});
+        arrive(std::integral_constant<int, M::COPIES * (F::AHEAD - 1)>{});
         if (b - list_at == 64)
             make_list(b, fetch_list(b));
         const int t0 = b * KV_BLOCK;
-        const uint8_t *block = block_at(b + 2);
-        const int valid = valid_at(b + 2);
-        const uint8_t *const tile = lds8 + (b - b0) % M::NBUF * M::BLOCK;
-        uint8_t *const later = lds8 + (b + 2 - b0) % M::NBUF * M::BLOCK;
+        const uint8_t *block = block_at(b + F::AHEAD);
+        const int valid = valid_at(b + F::AHEAD);
+        const uint8_t *const tile = lds8 + (b - b0) % F::NBUF * M::BLOCK;
+        uint8_t *const later = lds8 + (b + F::AHEAD - b0) % F::NBUF * M::BLOCK;
         f32x16 sv[2];
-        if constexpr (M::template TURNS<FMT>) {
+        if constexpr (F::V) {
             copy_and_convert<FMT, D>(frags, tile, later, cl, block, valid, wave, vrow, uint32_t(vswz));
+            if constexpr (!F::K)
+                if (t0 < wave_most)
+                    scores32<FMT, D>(sv, tile, query);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();                   // the block is there in bf16
             asm volatile("" ::: "memory");
             if (t0 >= wave_most)                            // (as is every later block)
                 continue;
-            score_frags<D>(sv, frags + lane, query);
+            if constexpr (F::K)
+                score_frags<D>(sv, frags + lane, query);
         } else {
             if (t0 >= wave_most) {
                 cl.copy(later, block, valid);
@@ -1347,8 +1360,8 @@ __global__ void __launch_bounds__(256, 2) kv_many_rows_kernel(LaunchOf<FORM> A)
                                   pack_bf16x2_hw(sv[x][8 * u + 4], sv[x][8 * u + 5]), pack_bf16x2_hw(sv[x][8 * u + 6], sv[x][8 * u + 7])});
         }
         l = fmaf(sum, low ? 0.0f : __builtin_amdgcn_exp2f(-vl), l);
-        if constexpr (M::template TURNS<FMT>)
-            frags_times_v<D>(acc, pf, frags + lane);
+        if constexpr (F::V)
+            frags_times_v<D>(acc, pf, frags + (F::K ? D / 8 * 64 : 0) + lane);
         else
             times_v<FMT, D>(acc, pf, tile + vrow, vchunk);
     }
@@ -1920,10 +1933,10 @@ hipError_t launch_units(const LaunchOf<FORM> &A, int tile_rows, unsigned grid, h
 {
     if (tile_rows == 128) {
         static std::atomic<uint64_t> done{0};
-        const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, FORM>), ManyRows<D>::template LDS<FMT>, done);
+        const hipError_t e = allow_lds_once(reinterpret_cast<const void *>(kv_many_rows_kernel<FMT, D, FORM>), ManyForm<FMT, D>::LDS, done);
         if (e != hipSuccess)
             return e;
-        launch_k(kv_many_rows_kernel<FMT, D, FORM>, grid, 256, ManyRows<D>::template LDS<FMT>, st, A);
+        launch_k(kv_many_rows_kernel<FMT, D, FORM>, grid, 256, ManyForm<FMT, D>::LDS, st, A);
     } else if (tile_rows == 16) {
         launch_k(kv_few_rows_kernel<FMT, D, 1, FORM>, grid, 256, 0, st, A);
     } else {
