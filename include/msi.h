@@ -481,7 +481,8 @@ msi_status msi_linear(const msi_linear_args *args, void *stream);
  * linear.w holds the codes q, laid out as those of MSI_W_Q4B32: [N, K / 2] bytes,
  * element 2j in the low nibble of byte j, 4-bit two's complement; 16-byte
  * aligned.  Every weight counts as it is: the products of a group are summed and
- * scaled in fp32. */
+ * scaled in fp32 (so a scale that is not finite spoils its feature, whatever the
+ * group's codes are). */
 typedef struct {
     msi_linear_args linear;      /* K a multiple of group, at least group              */
     const void *scales;          /* [N, K / group] fp16, row-major, 2-byte aligned     */

@@ -460,6 +460,9 @@ def kv_evict(cache: KvCache, seqs: KvSeqs, dst_table, new_lens, keep, *, budget:
 
 def _block_width(name: str, w) -> int:
     """K of a block's matrix: bf16, or a pair of 4-bit codes and scales."""
+    if not isinstance(w, torch.Tensor) and not (isinstance(w, tuple) and len(w) == 2 and
+                                                all(isinstance(t, torch.Tensor) for t in w)):
+        _refuse(f"{name} must be a matrix or a pair (codes, scales)")
     m = w[0] if isinstance(w, tuple) else w
     K = 0 if m.dim() != 2 else m.shape[1] * (2 if isinstance(w, tuple) else 1)
     if K < 8 or K % 8:
@@ -471,7 +474,7 @@ def _block_weights(name: str, w, N: int, K: int, dev):
     """What a projection would refuse of a block's matrix."""
     m = w
     if isinstance(w, tuple):
-        if len(w) != 2 or w[1].dim() != 2 or w[1].shape[1] < 1 or K % w[1].shape[1] or \
+        if w[1].dim() != 2 or w[1].shape[1] < 1 or K % w[1].shape[1] or \
                 K // w[1].shape[1] not in (32, 64, 128):
             _refuse(f"{name} must be a pair (codes, scales) with a scale for each 32, 64 or 128 of {K} weights")
         m, scales = w
@@ -512,6 +515,7 @@ class AttentionBlock:
             _refuse("n_q_heads must be a multiple of the cache's n_heads")
         self.rows_qkv, inner = (n_q_heads + 2 * H) * D, n_q_heads * D
         self.d = _block_width("wqkv", wqkv)
+        _block_width("wo", wo)
         for name, w, N, K in (("wqkv", wqkv, self.rows_qkv, self.d), ("wo", wo, self.d, inner)):
             _block_weights(name, w, N, K, dev)
         if rotary is not None and (rotary.device != dev or rotary.rot_dim > D):

@@ -129,7 +129,8 @@ def test_block_with_rotation_groups_and_4_bit_weights():
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
     q4 = lambda n, k, g=32: (torch.zeros((n, k // 2), dtype=torch.uint8), torch.zeros((n, k // g)).half())  # noqa: E731
     r = msi.KvRotary([0.1] * 32, device="cpu")
-    for over in (dict(wqkv=q4(512, 128)[:1]), dict(wqkv=(q4(512, 128)[0], torch.zeros((512, 3)).half())), dict(wqkv=(q4(512, 128)[0].int(), q4(512, 128)[1])),
+    for over in (dict(wqkv=q4(512, 128)[:1]), dict(wqkv=list(q4(512, 128))), dict(wo=()), dict(wo=(q4(128, 256)[0], None)),
+                 dict(wqkv=(q4(512, 128)[0], torch.zeros((512, 3)).half())), dict(wqkv=(q4(512, 128)[0].int(), q4(512, 128)[1])),
                  dict(wo=(q4(128, 256)[0], q4(128, 256)[1].float())), dict(wo=q4(128, 128)), dict(wqkv=q4(520, 128)),
                  dict(wqkv=q4(512, 128, 16)), dict(rotary=msi.KvRotary([0.1] * 40, device="cpu"))):
         with pytest.raises(msi.MsiError) as e:
