@@ -306,7 +306,6 @@ __global__ void __launch_bounds__(S::THREADS, S::WPC * S::WAVES / 4) q4_tile_ker
 #pragma unroll
         for (int i = 0; i < LQ; ++i)
             dma16_lds(qr, st + A_BYTES + (WAVES * i + wave) % S::QC * 1024,   // (with fewer copies than wavefronts: some twice)
-                     
                       edge && (last >> (16 + i) & 1) ? 0x80000000u : qoff[i] + uint32_t(stage * QROWB), 0);
 #pragma unroll
         for (int i = 0; i < LA; ++i)
