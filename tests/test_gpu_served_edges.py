@@ -12,22 +12,24 @@ from _kv_helpers import bf16
 pytestmark = pytest.mark.gpu
 
 FIRST = """
+import sys
 import torch
 import paper_2608_23805_amd as msi
 x = torch.randn(64, 512, device="cuda").bfloat16()
 w = torch.randint(0, 256, (5003, 256), device="cuda", dtype=torch.uint8)
 sc = torch.rand(5003, 16, device="cuda").half()
 y = torch.zeros((64, 5003), device="cuda")
-c = msi.KvCache.alloc(24, 2, 256, "e4m3")
+D, fmt = int(sys.argv[1]), sys.argv[2]
+c = msi.KvCache.alloc(24, 2, D, fmt)
 i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
 s = msi.KvSeqs(i32([[3, 5, 0], [3, 5, 9]]), i32([150, 170]), i32([0, 22, 64]), n_rows=64, max_rows=42)
 g2 = msi.KvGroups(i32([0, 2]), i32([2]), max_rows=64, max_blocks=2)
-r = msi.KvRotary([0.1] * 64)
+r = msi.KvRotary([0.1] * (D // 4))
 pos = i32(list(range(64)))
-kv, q = torch.randn(64, 2, 256, device="cuda").bfloat16(), torch.randn(64, 16, 256, device="cuda").bfloat16()
+kv, q = torch.randn(64, 2, D, device="cuda").bfloat16(), torch.randn(64, 16, D, device="cuda").bfloat16()
 c.data.random_(0, 120)
 c.scales.fill_(0.25)
-out, turned = torch.zeros((64, 16, 256), device="cuda").bfloat16(), torch.zeros((64, 16, 256), device="cuda").bfloat16()
+out, turned = torch.zeros((64, 16, D), device="cuda").bfloat16(), torch.zeros((64, 16, D), device="cuda").bfloat16()
 ws = msi.kv_attention_shared_workspace(c, s, g2, 16)
 def run(st):
     msi.linear_q4(x, w, sc, y, stream=st)
@@ -52,10 +54,11 @@ assert all(t.float().abs().sum(-1).gt(0).all() for t in got[0])
 """
 
 
-def test_first_call_in_a_capture():
+@pytest.mark.parametrize("D,fmt", [(256, "e4m3"), (128, "int8"), (256, "int8")])
+def test_first_call_in_a_capture(D, fmt):
     """Kernels with more than 64 KiB of LDS whose first call in the process is recorded into a graph."""
-    log("case served first call captured")
-    r = subprocess.run([sys.executable, "-c", FIRST], capture_output=True, text=True, timeout=100)
+    log(f"case served first call captured {D} {fmt}")
+    r = subprocess.run([sys.executable, "-c", FIRST, str(D), fmt], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0, r.stderr
 
 
