@@ -1,5 +1,6 @@
 """4-bit projections, append with rotation and attention over shared pages at calls that sizes alone do not reach: arrays
-past 4 GiB, a first call inside a capture, two streams at once."""
+past 4 GiB, a first call inside a capture, two streams at once; lists of pages that are read again by every form of the
+kernel of many rows."""
 import subprocess
 import sys
 
@@ -7,7 +8,8 @@ import numpy as np
 import pytest
 
 from _gpu_helpers import log
-from _kv_helpers import bf16
+from _kv_helpers import Setup, bf16
+from test_gpu_kv_attention import _check
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +160,17 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for side, (out, y) in zip(sides, want):
         assert torch.equal(side[7], out) and torch.equal(side[8], y) and out.any() and y.any()
+
+
+@pytest.mark.parametrize("bad", [False, True])
+@pytest.mark.parametrize("D,fmt", [(128, "int8"), (256, "int8"), (128, "e4m3"), (256, "e4m3")])
+def test_page_lists_of_many_rows(D, fmt, bad):
+    """A sequence of 134 blocks that is not cut: the lists of 64 pages are made three times, a bad page in each."""
+    log(f"case page lists, many rows, {D} {fmt} bad={bad}")
+    lens, rows = [8530] + [3] * 51, [40] + [1] * 51
+    s = Setup(870 + D, lens, rows, 1, D, fmt)
+    table = s.table.copy()
+    if bad:
+        for b in (10, 63, 64, 65, 66, 100, 127, 128, 129, 133):
+            table[0, b] = 10 ** 6 + b
+    _check(s, s.make_seqs(table, s.lens, s.cu), table, s.lens, s.cu, 16, status=int(bad))
