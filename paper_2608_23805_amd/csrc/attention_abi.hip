@@ -126,7 +126,8 @@ const char *view_groups(const msi_kv_groups *g, const KvCache &c, const KvSeqs &
         return "a group's max_rows times the heads of a cache head must be at most 2^29";
     if (uint64_t(s.max_rows) * n_q_heads >= MOST_GROUPS)
         return "max_rows times n_q_heads must be under 2^24";
-    out = KvGroups{g->cu_seqs, g->blocks, int(g->n_groups), int(max_rows), int(max_blocks)};
+    out = KvGroups{g->cu_seqs, g->blocks, int(g->n_groups), int(max_rows), int(max_blocks),
+                   std::min(int(max_blocks), s.max_len / KV_BLOCK)};
     cut = shared_cut(s, out, c.H, int(G), c.D);
     if ((uint64_t(cut.items_p) + uint64_t(cut.items_s)) * uint64_t(c.H) >= MOST_GROUPS)
         return "the groups' and sequences' row tiles times n_heads must be under 2^24";

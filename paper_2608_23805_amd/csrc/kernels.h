@@ -383,6 +383,7 @@ struct KvGroups {
     const int32_t *cu;           // [n + 1] first sequence of every group
     const int32_t *blocks;       // [n] shared blocks
     int n, max_rows, max_blocks;
+    int usable;                  // blocks that rows can stand behind (max_len / 64): groups with more serve nobody
 };
 // What units are cut from: the shared pages of a group with the rows of its sequences, or the other pages of a sequence
 // with its rows.

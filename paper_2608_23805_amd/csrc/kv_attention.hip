@@ -288,7 +288,7 @@ __device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int
     if (!ok || a == z)
         return o;
     ok = blocks >= 0 && blocks <= A.g.max_blocks && row0 >= 0 && row1 >= row0 && row1 <= A.s.n_rows && row1 - row0 <= A.g.max_rows;
-    if (ok) {
+    if (ok && blocks <= A.g.usable) {                       // (more blocks than any sequence has: their table entries are nobody's)
         o.row0 = row0, o.n = row1 - row0, o.seq = a;
         o.len = blocks * KV_BLOCK, o.blocks = blocks;
         o.tiles = tiles_of(o.n, A.G, A.cut.tile_p);
@@ -2041,12 +2041,12 @@ SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
         parts += std::min(units * packed, items * tile_rows) * H;
         return int(std::min<int64_t>(items, 0x7fffffff));
     };
-    const bool any = g.n && g.max_rows && g.max_blocks;
-    c.items_p = any ? bound(g.n, g.max_blocks, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
+    const bool any = g.n && g.max_rows && g.usable;
+    c.items_p = any ? bound(g.n, g.usable, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
     c.items_s = bound(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s, c.most_s, c.few_s, c.parts);
     auto work = [&](int64_t owners, int64_t blocks, int tile_rows) { return (packed / tile_rows + owners) * blocks * H; };
     c.small = g.n <= SMALL_OWNERS && s.S <= SMALL_OWNERS && c.parts < SMALL_PARTS && int64_t(c.items_p) + c.items_s < SMALL_PARTS &&
-              work(g.n, g.max_blocks, c.tile_p) + work(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s) < int64_t(1) << 30;
+              work(g.n, g.usable, c.tile_p) + work(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s) < int64_t(1) << 30;
     size_t off = up256(size_t(g.n + s.S) * sizeof(KvOwner));
     c.first = off;
     off += up256(size_t(g.n + s.S + 1) * sizeof(int32_t));
