@@ -624,9 +624,10 @@ msi_status msi_kv_attention(const msi_kv_cache *cache, const msi_kv_seqs *seqs, 
                             void *stream);
 
 /* Groups of neighbouring sequences that hold the same first pages: group i is the
- * sequences cu_seqs[i] .. cu_seqs[i + 1] - 1, whose tables start with the same
- * blocks[i] pages.  The arrays are on the device, the host's bounds size the
- * launches.  Sequences of no group share nothing. */
+ * sequences cu_seqs[i] .. cu_seqs[i + 1] - 1; the tables of those whose rows stand
+ * behind blocks[i] pages (len - n >= 64 blocks) start with the same ones.  The
+ * arrays are on the device, the host's bounds size the launches.  Sequences of no
+ * group share nothing. */
 typedef struct {
     uint32_t n_groups;           /* <= 65535                                           */
     uint32_t max_rows;           /* bound of a group's rows                            */
@@ -637,8 +638,9 @@ typedef struct {
 } msi_kv_groups;
 
 /* msi_kv_attention where sequences share their first pages, which are read once
- * for all rows of a group, from the table of its first sequence.  The result is
- * msi_kv_attention's up to the order of its sums; equal calls give equal bits.
+ * for all rows of a group, from the table of the first sequence that stands behind
+ * them.  The result is msi_kv_attention's up to the order of its sums; equal calls
+ * give equal bits.
  * Shared pages serve rows behind them: a sequence of a group some of whose rows
  * stand inside them (len - n < 64 blocks) is attended by itself, with all the pages
  * of its own table.  So are, with MSI_KV_BAD_LENGTH, the sequences of a group

@@ -397,7 +397,8 @@ def kv_attention(cache: KvCache, seqs: KvSeqs, q, out, scale: float, mass_rows: 
 class KvGroups:
     """Groups of neighbouring sequences that hold the same first pages (msi_kv_groups): first sequence of every group
     [n_groups + 1] and shared blocks [n_groups] in device int32 tensors, whose contents may change between calls, and the
-    host's bounds: ``max_rows`` rows of a group, ``max_blocks`` shared blocks."""
+    host's bounds: ``max_rows`` rows of a group, ``max_blocks`` shared blocks.  A sequence whose rows do not all stand behind
+    the shared blocks is attended by itself, with a table of its own."""
 
     def __init__(self, cu_seqs, blocks, *, max_rows: int, max_blocks: int):
         dev = blocks.device

@@ -259,7 +259,8 @@ using LaunchOf = std::conditional_t<FORM == SHARED, SharedLaunch, AttentionLaunc
 // units of both.  The owners of units are the groups, then the sequences.  Where
 // a group's numbers break a bound, or its pages reach past a sequence's first
 // row, or offsets of groups fall, the pages count as each sequence's own: what
-// comes out is the same.
+// comes out is the same.  A group's pages are read through the table of the first
+// sequence that stands behind them; where none does, nobody reads them.
 //
 // With up to 64 groups and 64 sequences, one a lane, every wavefront of the first
 // launch lays the owners out by itself (its first workgroup leaves them for the
@@ -279,6 +280,8 @@ __device__ __forceinline__ int tiles_of(int n, int G, int tile_rows)
     return int((unsigned(n) * unsigned(G) + unsigned(tile_rows - 1)) >> log2_of(tile_rows));
 }
 
+constexpr int NO_SEQ = 0x7fffffff;
+
 // Group with the sequences [a, z) and `blocks` shared blocks, whose rows are [row0, row1); ok: its offsets are in order.
 __device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int z, int blocks, int row0, int row1, bool &ok)
 {
@@ -289,7 +292,7 @@ __device__ __forceinline__ KvOwner group_owner(const SharedLaunch &A, int a, int
         return o;
     ok = blocks >= 0 && blocks <= A.g.max_blocks && row0 >= 0 && row1 >= row0 && row1 <= A.s.n_rows && row1 - row0 <= A.g.max_rows;
     if (ok && blocks <= A.g.usable) {                       // (more blocks than any sequence has: their table entries are nobody's)
-        o.row0 = row0, o.n = row1 - row0, o.seq = a;
+        o.row0 = row0, o.n = row1 - row0, o.seq = NO_SEQ;       // (its sequences say who is the first)
         o.len = blocks * KV_BLOCK, o.blocks = blocks;
         o.tiles = tiles_of(o.n, A.G, A.cut.tile_p);
     }
@@ -375,6 +378,13 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
         g_blocks = in ? __builtin_amdgcn_readlane(p.g.blocks, g) : g_blocks;
     }
     p.s = seq_owner(A, q, lane, mine, g_row0, g_n, g_blocks);
+    for (int g = 0; g < A.g.n && !none; ++g) {
+        const uint64_t behind = __ballot(p.s.group == g);
+        if (lane == g && behind)
+            p.g.seq = __ffsll((unsigned long long)behind) - 1;
+    }
+    if (p.g.seq == NO_SEQ)
+        p.g.n = p.g.blocks = p.g.tiles = 0;
     // (small batches' sums are under 2^30)
     const int work_p = __builtin_amdgcn_readlane(wave_scan_incl(p.g.blocks * p.g.tiles * H), 63);
     const int work_s = __builtin_amdgcn_readlane(wave_scan_incl(p.s.blocks * p.s.tiles * H), 63);
@@ -1733,7 +1743,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
         falling = dropped = 0;
     __syncthreads();
     // ---- the groups
-    int64_t work_p = 0;
     for (int g = tid; g < A.g.n; g += PLAN_THREADS) {
         const int a = A.g.cu[g], z = A.g.cu[g + 1];
         bool ok = a >= 0 && a <= z && z <= A.s.S;
@@ -1741,18 +1750,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
             falling = 1;                                    // (offsets out of order: groups could overlap)
         const int row0 = ok ? A.s.cu[a] : 0, row1 = ok ? A.s.cu[z] : 0;
         const KvOwner o = group_owner(A, a, z, A.g.blocks[g], row0, row1, ok);
-        work_p += int64_t(o.blocks) * o.tiles * H;
         if (!ok)
             status |= KV_BAD_LENGTH;
         A.owners[g] = o;
     }
     __syncthreads();                                        // (the sequences' threads read the groups)
     const bool none = falling != 0;
-    if (none) {
-        work_p = 0;
-        for (int g = tid; g < A.g.n; g += PLAN_THREADS)
-            A.owners[g].n = A.owners[g].blocks = 0;
-    }
     // ---- the sequences
     int64_t work_s = 0;
     for (int i = tid; i < A.s.S; i += PLAN_THREADS) {
@@ -1769,6 +1772,20 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_shared_plan_kernel(SharedLaun
         const KvOwner o = in ? seq_owner(A, q, i, lo, w->row0, w->n, w->blocks) : seq_owner(A, q, i, -1, 0, 0, 0);
         work_s += int64_t(o.blocks) * o.tiles * H;
         A.owners[A.g.n + i] = o;
+        const int left = __shfl_up(o.group, 1);             // (of a run of lanes, the first alone)
+        if (o.group >= 0 && ((tid & 63) == 0 || left != o.group))
+            __hip_atomic_fetch_min(&A.owners[o.group].seq, i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    __syncthreads();
+    int64_t work_p = 0;
+    for (int g = tid; g < A.g.n; g += PLAN_THREADS) {
+        const int seq = __hip_atomic_load(&A.owners[g].seq, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        KvOwner o = A.owners[g];
+        o.seq = seq;
+        if (none || seq == NO_SEQ)
+            o.n = o.blocks = o.tiles = 0;
+        A.owners[g] = o;
+        work_p += int64_t(o.blocks) * o.tiles * H;
     }
     int64_t total_p, total_s;
     group_scan64(work_p, part, total_p);

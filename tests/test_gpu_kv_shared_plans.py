@@ -7,7 +7,8 @@ import numpy as np
 import pytest
 
 from _gpu_helpers import log
-from test_gpu_kv_shared import Shared, _check
+from _kv_oracle import attention
+from test_gpu_kv_shared import Shared, _check, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,50 @@ def test_no_tokens_and_no_table(n):
         assert msi.lib.msi_kv_attention_shared(c, sq, gr, ctypes.byref(a), None) == 0
         torch.cuda.synchronize()
         assert int(s.status) == 0 and torch.all(out == 0.0)
+
+
+@pytest.mark.parametrize("n", [5, 90])
+@pytest.mark.parametrize("first", ["empty", "without rows", "short", "short, other pages", "left out"])
+def test_table_of_a_sequence_that_is_attended_by_itself(n, first):
+    """The first sequences of a group do not stand behind its shared pages: their tables are their own affair, and the others
+    still share."""
+    log(f"case shared table n={n} first={first}")
+    rows = [1, 1] + [1] * (n - 2)
+    if first in ("empty", "without rows"):
+        rows[:2] = [0, 0]
+    sh = Shared(920 + n, [(n, 3), (2, 1)], [20 + i % 70 for i in range(n + 2)], rows + [1, 1], 2, 64, "e4m3")
+    s = sh.s
+    for i in (0, 1):
+        s.lens[i] = {"empty": 0, "without rows": s.lens[i], "left out": s.lens[i]}.get(first, 70 + i)
+        s.table[i, :3] = s.table[n - 1, 3] if first == "short, other pages" else -1
+        if first == "short":
+            s.table[i, :2] = s.table[n + i, 0], s.table[n - 1, 3]
+    if first == "left out":
+        s.lens[0] = s.lens[1] = 1 << 20
+    max_len = max(x for x in s.lens if x < 1 << 20)
+    s.seqs = s.make_seqs(s.table, s.lens, s.cu, max_len=max_len)
+    for G in (2, 64):
+        if first == "left out":
+            q, out, st = _run(sh, 2 * G)
+            want, tol, _ = attention(s.host, s.table[2:], s.lens[2:], [c - 2 for c in s.cu[2:]], q[1][2:], 0.125, G)
+            assert st == 4 and np.all(np.abs(out.double().cpu().numpy()[2:] - want) <= tol + 2.0 ** -86 * max_len)
+            assert (out[:2] == 5.0).all()
+        else:
+            _check(sh, 2 * G)
+
+
+@pytest.mark.parametrize("n", [5, 90])
+def test_group_that_no_sequence_stands_behind(n):
+    """All of a group's sequences are shorter than its shared pages: nobody reads those, and no status tells of them."""
+    log(f"case shared nobody behind n={n}")
+    sh = Shared(930 + n, [(n, 3), (2, 1)], [20] * (n + 2), [1] * (n + 2), 2, 64, "int8")
+    s = sh.s
+    s.lens[:n] = [64 + i % 60 for i in range(n)]
+    s.table[:n, 2:] = -1
+    s.lens[n] += 200
+    s.table[n, 1:5] = s.table[n + 1, 1]
+    s.table = np.ascontiguousarray(np.concatenate([s.table, s.table * 0 - 1], axis=1))
+    s.table[n, 4:6] = s.table[n + 1, 1]
+    s.seqs = s.make_seqs(s.table, s.lens, s.cu)
+    for G in (2, 64):
+        _check(sh, 2 * G)
