@@ -411,7 +411,8 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
     };
     int rows_g, rows_s, items_s;
     place(p.g, chunk_p, 0, cut.items_p, p.first_g, p.items_g, rows_g);
-    place(p.s, chunk_s, rows_g, cut.both ? cut.items_p + cut.items_s - min(p.items_g, cut.items_p) : cut.items_s, p.first_s, items_s, rows_s);
+    // (of one launch for both, the sequences have what the groups leave, left-out ones among them)
+    place(p.s, chunk_s, rows_g, cut.both ? max(cut.items_p + cut.items_s - p.items_g, 0) : cut.items_s, p.first_s, items_s, rows_s);
     p.first_s += p.items_g;
     p.items = p.items_g + items_s;
     if (__ballot(p.g.blocks && p.g.tiles && p.g.units == 0)) {     // a group was left out: so are its sequences

@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 
 from _gpu_helpers import log
+from _kv_helpers import bf16
 from _kv_oracle import attention
 from test_gpu_kv_shared import Shared, _check, _run
 
@@ -100,3 +101,33 @@ def test_group_that_no_sequence_stands_behind(n):
     s.seqs = s.make_seqs(s.table, s.lens, s.cu)
     for G in (2, 64):
         _check(sh, 2 * G)
+
+
+def test_sequences_past_the_items_of_overlapping_groups():
+    """Offsets of rows that fall, so that groups overlap and take more units than their rows allow: what is left for the
+    sequences behind them ends with the launch, and a sequence past that is left out as a whole.  (128 heads: 59 groups and
+    sequences of 65 packed rows, three tiles of 32 each, where 10 rows allow 79 for the groups and as many for the sequences.
+    The groups take 90, so the last 68 of 158 go to the sequences, 22 of them; rows 5 .. 9 belong to the 24th and later ones.)"""
+    import torch
+    import paper_2608_23805_amd as msi
+    log("case shared items of overlapping groups")
+    H, G, D, pairs = 128, 13, 256, (23, 7)
+    sh = Shared(940, [(1, 2)], [30], [5], H, D, "e4m3")
+    s = sh.s
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    cu = [0, 5] * pairs[0] + [5, 10] * pairs[1]
+    S = len(cu) - 1
+    table = torch.full((S, 80), -1, dtype=torch.int32, device="cuda")
+    table[:, :3] = i32(s.table[0, :3])
+    seqs = msi.KvSeqs(table, i32([s.lens[0]] * S), i32(cu), n_rows=10, max_rows=5, max_len=64 * 80)
+    groups = msi.KvGroups(i32(list(range(S + 1))), i32([2] * S), max_rows=5, max_blocks=80)
+    q = bf16(s.g.standard_normal((10, H * G, D)) * 1.5)
+    for all_rows in (False, True):
+        _, out, st = _run(sh, H * G, seqs=seqs, groups=groups, q=q, all_rows=all_rows)
+        assert st == 4
+        got = out.double().cpu().numpy()
+        for a, z in ((0, 5), (5, 10)):
+            want, tol, _ = attention(s.host, s.table, s.lens, [0, 5], q[1][a:z], 0.125, G)
+            right = np.all(np.abs(got[a:z] - want) <= tol + 2.0 ** -86 * s.lens[0])
+            assert right or np.all(got[a:z] == (0.0 if all_rows else 5.0))
+            assert right == (a == 0)
