@@ -15,8 +15,9 @@
 //
 // Angles are fixed-point turns: freq is the frequency's fraction of a turn in
 // units of 2^-64, so the low 64 bits of position * freq are the angle with its
-// whole turns already gone, off by at most 2^-33 turns at any 32-bit position
-// (in fp32 a position of 2^20 would leave 2^-5 radians).
+// whole turns already gone, off by at most 2^-34 turns at any 32-bit position
+// (in fp32 a position of 2^20 would leave 2^-5 radians), and cutting what is left
+// of a quarter turn to 32 bits costs another 2^-34.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,14 +29,15 @@ namespace msi {
 
 namespace {
 
-// Sine and cosine of an angle of `turn` 2^-32 turns (two's complement).  The
-// nearest quarter turn comes off exactly; what is left, |x| <= pi / 4, goes
-// through the Taylor polynomials up to x^9 and x^10 (their next terms are under
-// 2^-28), each rounded operation 2^-24 of its value.
-__device__ __forceinline__ void turn_sincos(uint32_t turn, float &s, float &c)
+// Sine and cosine of an angle of `turn` 2^-64 turns (two's complement).  The
+// nearest quarter turn comes off exactly; what is left, 62 bits, is cut to units of
+// 2^-34 turns, and |x| <= pi / 4 goes through the Taylor polynomials up to x^9 and
+// x^10 (their next terms are under 2^-28), each rounded operation 2^-24 of its value.
+__device__ __forceinline__ void turn_sincos(uint64_t turn, float &s, float &c)
 {
-    const uint32_t k = (turn + 0x20000000u) >> 30;                     // quarter turns
-    const float x = float(int32_t(turn - (k << 30))) * 0x1.921fb6p-30f;   // 2 pi 2^-32
+    const uint32_t hi = uint32_t(turn >> 32), k = (hi + 0x20000000u) >> 30;            // quarter turns
+    const uint32_t rest = (hi - (k << 30)) << 2 | uint32_t(turn) >> 30;
+    const float x = float(int32_t(rest)) * 0x1.921fb6p-32f;            // 2 pi 2^-34
     const float z = x * x;
     float ps = 2.7557319224e-6f, pc = -2.7557319224e-7f;               // 1 / 9!, -1 / 10!
     ps = fmaf(ps, z, -1.9841269841e-4f), pc = fmaf(pc, z, 2.4801587302e-5f);
@@ -48,11 +50,8 @@ __device__ __forceinline__ void turn_sincos(uint32_t turn, float &s, float &c)
     c = (k + 1) & 2 ? -b : b;
 }
 
-// Top 32 bits of the low 64 of position * freq.
-__device__ __forceinline__ uint32_t turns(int32_t position, uint64_t freq)
-{
-    return uint32_t((uint64_t(int64_t(position)) * freq) >> 32);
-}
+// position * freq without whole turns.
+__device__ __forceinline__ uint64_t turns(int32_t position, uint64_t freq) { return uint64_t(int64_t(position)) * freq; }
 
 // The 16 elements that a thread owns of a head's row: slot s is chunks s and
 // s + rot / 16 of 8 elements (pairs of halves), or chunks 2 s and 2 s + 1; slots
