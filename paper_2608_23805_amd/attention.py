@@ -254,14 +254,27 @@ def kv_append(cache: KvCache, seqs: KvSeqs, k, v, status=None, stream=None):
           _stream(stream, dev))
 
 
-_TWO_PI, _PLACES = 6283185307179586476925286766559005768394338798750, 10 ** 48
+def _arctan_of(n: int, one: int) -> int:
+    """arctan(1 / n) in units of 1 / one, by its power series."""
+    power = total = one // n
+    k = 1
+    while power:
+        power //= -n * n
+        k += 2
+        total += power // k
+    return total
+
+
+# 2 pi (Machin's formula): a double reaches 2^1024, whose fraction of a turn to 2^-65 takes 2 pi to 2^-1090 of itself
+_PI_BITS = 1200
+_TWO_PI = 8 * (4 * _arctan_of(5, 1 << _PI_BITS) - _arctan_of(239, 1 << _PI_BITS))
 
 
 def _turns(x: float) -> int:
     """An angle's fraction of a turn in units of 2^-64, to the nearest."""
     n, d = x.as_integer_ratio()
     d *= _TWO_PI
-    return ((n * _PLACES << 65) + d) // (2 * d) % 2 ** 64
+    return ((n << _PI_BITS + 65) + d) // (2 * d) % 2 ** 64
 
 
 class KvRotary:
