@@ -131,3 +131,99 @@ def test_sequences_past_the_items_of_overlapping_groups():
             right = np.all(np.abs(got[a:z] - want) <= tol + 2.0 ** -86 * s.lens[0])
             assert right or np.all(got[a:z] == (0.0 if all_rows else 5.0))
             assert right == (a == 0)
+
+
+@pytest.mark.parametrize("fmt,D", [("e4m3", 64), ("int8", 128), ("e4m3", 256), ("int8", 256)])
+@pytest.mark.parametrize("groups", [[(100, 20)], [(70, 9), (1, 30), (0, 4), (29, 0)], [(49, 3), (51, 40)]])
+def test_answers_past_64_sequences(fmt, D, groups):
+    """Single tokens of more sequences than a wavefront has lanes: shared pages by 128 rows, own pages by 16 or 32, in launches
+    of their own."""
+    log(f"case shared plan answers {fmt} D={D} groups={groups}")
+    n = sum(k for k, _ in groups)
+    _check(Shared(950 + D, groups, [1 + 37 * i % 400 for i in range(n)], [1] * n, 2, D, fmt), 2 * 7)
+
+
+@pytest.mark.parametrize("fmt,D", [("e4m3", 128), ("int8", 64), ("int8", 256)])
+@pytest.mark.parametrize("groups", [[(3, 12), (67, 2)], [(70, 0)], [(35, 25), (35, 1)]])
+def test_prompts_past_64_sequences(fmt, D, groups):
+    """Some of the sequences are prompts: shared and own pages both by 128 rows."""
+    log(f"case shared plan prompts {fmt} D={D} groups={groups}")
+    rows = [(40, 1, 7, 0, 33)[i % 5] for i in range(70)]
+    _check(Shared(960 + D, groups, [r + 90 * i % 1000 for i, r in enumerate(rows)], rows, 1, D, fmt), 4)
+
+
+@pytest.mark.parametrize("rows", [[1], [30, 1, 2]])
+def test_more_than_64_groups(rows):
+    """Groups whose units are cut by the work alone, by 128 rows; single tokens and prompts behind them."""
+    log(f"case shared plan groups rows={rows}")
+    g = np.random.default_rng(971)
+    sizes = [int(v) for v in g.integers(0, 4, 80)]
+    sizes[11] = 30
+    groups = [(n, int(b)) for n, b in zip(sizes, g.integers(0, 30, 80))]
+    n = sum(sizes)
+    r = [rows[i % len(rows)] for i in range(n)]
+    _check(Shared(970, groups, [a + int(b) for a, b in zip(r, g.integers(0, 200, n))], r, 1, 64, "e4m3"), 8)
+
+
+@pytest.mark.parametrize("rows", [1, 30])
+@pytest.mark.parametrize("cu,blocks,max_rows", [([0, 3, 2, 90], [3, 3, 3], None), ([0, 50, 91], [3, 3], None), ([0, 50, 90], [3, 99], None),
+                                                ([0, 50, 90], [3, -1], None), ([0, 60, 90], [3, 3], 40)])
+def test_broken_groups_past_64_sequences(cu, blocks, max_rows, rows):
+    """The sequences of a group whose numbers break a bound get their own pages, beside those of one that does not."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log(f"case shared plan broken groups {cu} {blocks} {max_rows} rows={rows}")
+    sh = Shared(980, [(90, 3)], [rows + 5 * i % 150 for i in range(90)], [rows] * 90, 1, 64, "int8")
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    g = msi.KvGroups(i32(cu), i32(blocks), max_rows=max_rows * rows if max_rows else sh.s.cu[-1], max_blocks=3)
+    _check(sh, 8, groups=g, status=4)
+
+
+@pytest.mark.parametrize("n,rows", [(6, 1), (6, 40), (80, 1), (80, 40)])
+def test_captured_as_sequences_grow_leave_and_come_back(n, rows):
+    """Two captured calls with workspaces of their own, replayed in turn with eager calls between: sequences grow past the end
+    of a page, the second half leaves for a group of its own, the first sequence falls back within the shared pages (its table its own), the
+    shared pages become fewer, and all of it comes back.  Every replay has the eager call's bits, and those are right."""
+    import torch
+    import paper_2608_23805_amd as msi
+    log(f"case shared captured n={n} rows={rows}")
+    sh = Shared(990 + n + rows, [(n, 3)], [rows + 61 + i % 5 for i in range(n)], [rows] * n, 2, 64, "e4m3")
+    s = sh.s
+    dev = lambda v: torch.tensor(np.asarray(v), dtype=torch.int32).cuda()  # noqa: E731
+    table, lens, cu_seqs = dev(s.table), dev(s.lens), dev([0, n, n])
+    blocks = dev([3, 2])
+    seqs = msi.KvSeqs(table, lens, s.seqs.cu_rows, n_rows=s.cu[-1], max_rows=rows, max_len=s.table.shape[1] * 64)
+    groups = msi.KvGroups(cu_seqs, blocks, max_rows=s.cu[-1], max_blocks=3)
+    q = bf16(s.g.standard_normal((s.cu[-1], 8, 64)))
+    ws = [msi.kv_attention_shared_workspace(s.cache, seqs, groups, 8) for _ in range(3)]
+    outs = [torch.zeros_like(q[0]) for _ in range(3)]
+    stream = torch.cuda.Stream()
+    graphs = []
+    for w, o in zip(ws[:2], outs):
+        g = torch.cuda.CUDAGraph()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(g, stream=stream):
+            msi.kv_attention_shared(s.cache, seqs, groups, q[0], o, 0.125, workspace=w, stream=torch.cuda.current_stream())
+        graphs.append(g)
+    start = list(s.lens)
+    inside = [rows + 20 if i == 0 else x for i, x in enumerate(start)]
+    own = s.table.copy()
+    own[0, :3] = -1
+    own[0, :2] = s.table[0, 3:5] if s.table.shape[1] > 4 else s.table[0, 3]
+    steps = [(start, s.table, [0, n, n], 3), ([x + 2 for x in start], s.table, [0, n, n], 3), ([x + 2 for x in start], s.table, [0, n // 2, n], 3),
+             (inside, own, [0, n, n], 3), (start, s.table, [0, n, n], 1), (start, s.table, [0, n, n], 3)]
+    first = None
+    for now, tab, cu, nb in steps:
+        for t, v in ((lens, now), (table, tab), (cu_seqs, cu), (blocks, [nb, 2])):
+            t.copy_(dev(v))
+        for o in outs:
+            o.fill_(5.0)
+        msi.kv_attention_shared(s.cache, seqs, groups, q[0], outs[2], 0.125, workspace=ws[2], stream=torch.cuda.current_stream())
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
+        want, tol, _ = attention(s.host, tab, now, s.cu, q[1], 0.125, 4)
+        assert np.all(np.abs(outs[2].double().cpu().numpy() - want) <= tol + 2.0 ** -86 * max(now))
+        first = outs[2].clone() if first is None else first
+    assert torch.equal(first, outs[2])
