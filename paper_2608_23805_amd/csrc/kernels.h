@@ -10,7 +10,7 @@
 #include <utility>
 
 #include "common.h"
-#include "kv_common.h"
+#include "kv_units.h"
 
 namespace msi {
 
@@ -379,33 +379,6 @@ hipError_t launch_kv_rest(const KvSeqs &s, uint16_t *out, int64_t out_stride, in
 hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c, hipStream_t st);
 
 // ---- the same for batches whose sequences share their first pages
-struct KvGroups {
-    const int32_t *cu;           // [n + 1] first sequence of every group
-    const int32_t *blocks;       // [n] shared blocks
-    int n, max_rows, max_blocks;
-    int usable;                  // blocks that rows can stand behind (max_len / 64): groups with more serve nobody
-};
-// What units are cut from: the shared pages of a group with the rows of its sequences, or the other pages of a sequence
-// with its rows.
-struct alignas(16) KvOwner {
-    int row0, n, len, seq;       // rows, tokens up to the last of these pages, sequence whose table is read
-    int b0, blocks;              // pages
-    int units, tiles;            // row tiles of a unit
-    int64_t part;                // first partial result; a unit's are [H, n * G]
-    int group;                   // of a sequence: its group, -1 if it shares nothing
-    int all;                     // every row sees every token
-};
-struct SharedCut {
-    bool few_p, few_s;           // form of the shared pages' units, of the sequences'
-    bool both;                   // one launch for both
-    int tile_p, tile_s;          // packed rows of a workgroup
-    int items_p, items_s;        // bounds of units times row tiles
-    int most_p, most_s;          // workgroups that units are cut for, at most
-    bool small;                  // every wavefront lays out the units by itself
-    int64_t parts;               // bound of the partial results (rows)
-    size_t first, part_ml, part_o, bytes;   // workspace offsets and size (the owners come first)
-};
-SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D);
 struct SharedLaunch : AttentionLaunch {
     KvGroups g;
     SharedCut cut;

@@ -111,24 +111,6 @@ struct Unit {
     int seq, split, n, first;        // the split-th of the n units of sequence seq, which start at number `first`
 };
 
-// Blocks of a unit for `work` blocks in all (times heads and row tiles): one
-// workgroup per CU as long as each has at most 16 blocks, four a wavefront;
-// then units of 16, which hide their start and their partial results' way
-// through memory, until there are 2048 of them (131072 tokens of one sequence, 2 heads
-// of 256: 36 us with 16 blocks, 46 with 4; 48 sequences of up to 16384, 8 heads of 128:
-// 246, 233, 223 and 219 us with 256, 512, 1024 and 2048 workgroups).
-// Sequences of up to 8 blocks are not cut (4 to 16 sequences of 500 tokens: 9.3 and 10.1 us,
-// 11.6 and 13.5 cut; of 1000 tokens with heads of 256 17.0, 14.1 cut).
-constexpr int DIRECT_BLOCKS = 8, LEAST_BLOCKS = 4, ENOUGH_BLOCKS = 16, FILL_WORKGROUPS = 256, MOST_WORKGROUPS = 2048;
-
-__device__ __forceinline__ int unit_chunk(int64_t work)
-{
-    const int64_t fill = (work + FILL_WORKGROUPS - 1) / FILL_WORKGROUPS;
-    if (fill <= ENOUGH_BLOCKS)
-        return max(int(fill), LEAST_BLOCKS);
-    return int(max(int64_t(ENOUGH_BLOCKS), (work + MOST_WORKGROUPS - 1) / MOST_WORKGROUPS));
-}
-
 // The unit numbered `at` (seq = -1: there are not so many).
 __device__ __forceinline__ Unit find_unit(const AttentionLaunch &A, int at)
 {
@@ -268,18 +250,6 @@ using LaunchOf = std::conditional_t<FORM == SHARED, SharedLaunch, AttentionLaunc
 // from a prompt of 192 tokens: 22.6 us with it, 12.8 without; 64 rows of 32768 shared
 // tokens: 105.7 and 94).
 constexpr int PLAN_THREADS = 1024;
-constexpr int LEAST_MANY = 8;                // blocks of a 128-row unit: below, its partial results outweigh the codes
-constexpr int SMALL_OWNERS = 64;
-constexpr int64_t SMALL_PARTS = 1 << 23;     // sums over the lanes stay in 32 bits
-
-__device__ __forceinline__ int log2_of(int power) { return __builtin_ctz(unsigned(power)); }
-
-// Row tiles of n rows (n G <= 2^29), tiles being powers of two.
-__device__ __forceinline__ int tiles_of(int n, int G, int tile_rows)
-{
-    return int((unsigned(n) * unsigned(G) + unsigned(tile_rows - 1)) >> log2_of(tile_rows));
-}
-
 constexpr int NO_SEQ = 0x7fffffff;
 
 // Group with the sequences [a, z) and `blocks` shared blocks, whose rows are [row0, row1); ok: its offsets are in order.
@@ -312,11 +282,6 @@ __device__ __forceinline__ KvOwner seq_owner(const SharedLaunch &A, const KvSeq 
         o.tiles = tiles_of(q.n, A.G, A.cut.tile_s);
     }
     return o;
-}
-
-__device__ __forceinline__ int shared_chunk(int64_t work, bool few, int most)
-{
-    return few ? unit_chunk(work) : int(max(int64_t(LEAST_MANY), (work + most - 1) >> log2_of(most)));
 }
 
 // Blocks of a 128-row unit for up to 64 owners, one a lane (blocks, row tiles):
@@ -1943,8 +1908,6 @@ void with_shape(int fmt, int D, F f)
         by_d(std::integral_constant<int, KV_E4M3>{});
 }
 
-size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
-
 // The kernel of units for tiles of 16, 32 or 128 packed rows.
 template <int FMT, int D, int FORM>
 hipError_t launch_units(const LaunchOf<FORM> &A, int tile_rows, unsigned grid, hipStream_t st)
@@ -2030,50 +1993,6 @@ hipError_t launch_kv_attention(AttentionLaunch A, int fmt, const AttentionCut &c
         e = hipGetLastError();
     }
     return e;
-}
-
-// How a call with shared pages is cut, by its host-side bounds alone.  Units are cut on the device so that at most `most`
-// workgroups (times heads and row tiles) come of them, besides one for every owner's row tile; that bounds the items and
-// the rows of partial results.
-SharedCut shared_cut(const KvSeqs &s, const KvGroups &g, int H, int G, int D)
-{
-    SharedCut c{};
-    // Up to three tiles of 32 rows read the pages as often, mostly from L2, in less time than a tile of 128 rows takes, which
-    // converts and multiplies for all of them (tokens of its own, 12 rows of 8 heads behind 200 shared blocks: heads of 64,
-    // 128, 256 42, 52, 59 us by 128 rows, 38, 47, 49; shared blocks, 72 rows: 26, 30, 42 and 28, 32, 31).
-    auto tile = [](int64_t rows, int most) { return rows <= 16 ? 16 : rows <= most ? 32 : 128; };
-    c.tile_p = tile(int64_t(g.max_rows) * G, D == 256 ? 96 : 64);
-    c.tile_s = tile(int64_t(s.max_rows) * G, 96);
-    c.few_p = c.tile_p != 128;
-    c.few_s = c.tile_s != 128;
-    c.both = c.few_p && c.few_s;
-    if (c.both)
-        c.tile_p = c.tile_s = std::max(c.tile_p, c.tile_s);
-    const int rounds = 4 * (D == 256 ? 256 : 512);          // four times the 128-row workgroups that the card holds at once
-    c.most_p = c.few_p ? MOST_WORKGROUPS : rounds;
-    c.most_s = c.few_s ? MOST_WORKGROUPS : rounds;
-    const int64_t packed = int64_t(s.n_rows) * G;
-    auto bound = [&](int64_t owners, int64_t blocks, int tile_rows, int most, bool few, int64_t &parts) {
-        const int64_t tiles = packed / tile_rows + owners, units = (blocks + (few ? LEAST_BLOCKS : LEAST_MANY) - 1) / (few ? LEAST_BLOCKS : LEAST_MANY);
-        const int64_t items = std::min(most / H + tiles, units * tiles);
-        parts += std::min(units * packed, items * tile_rows) * H;
-        return int(std::min<int64_t>(items, 0x7fffffff));
-    };
-    const bool any = g.n && g.max_rows && g.usable;
-    c.items_p = any ? bound(g.n, g.usable, c.tile_p, c.most_p, c.few_p, c.parts) : 0;
-    c.items_s = bound(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s, c.most_s, c.few_s, c.parts);
-    auto work = [&](int64_t owners, int64_t blocks, int tile_rows) { return (packed / tile_rows + owners) * blocks * H; };
-    c.small = g.n <= SMALL_OWNERS && s.S <= SMALL_OWNERS && c.parts < SMALL_PARTS && int64_t(c.items_p) + c.items_s < SMALL_PARTS &&
-              work(g.n, g.usable, c.tile_p) + work(s.S, (s.max_len + KV_BLOCK - 1) / KV_BLOCK, c.tile_s) < int64_t(1) << 30;
-    size_t off = up256(size_t(g.n + s.S) * sizeof(KvOwner));
-    c.first = off;
-    off += up256(size_t(g.n + s.S + 1) * sizeof(int32_t));
-    c.part_ml = off;
-    off += up256(size_t(c.parts) * 2 * sizeof(float));
-    c.part_o = off;
-    off += up256(size_t(c.parts) * D * sizeof(float));
-    c.bytes = off;
-    return c;
 }
 
 hipError_t launch_kv_attention_shared(SharedLaunch A, int fmt, hipStream_t st)
