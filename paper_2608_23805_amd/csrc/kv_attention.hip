@@ -343,13 +343,13 @@ __device__ __forceinline__ WavePlan plan_wave(const SharedLaunch &A, uint32_t &s
         g_blocks = in ? __builtin_amdgcn_readlane(p.g.blocks, g) : g_blocks;
     }
     p.s = seq_owner(A, q, lane, mine, g_row0, g_n, g_blocks);
-    for (int g = 0; g < A.g.n && !none; ++g) {
-        const uint64_t behind = __ballot(p.s.group == g);
-        if (lane == g && behind)
-            p.g.seq = __ffsll((unsigned long long)behind) - 1;
+    // the first sequence from `a` on that shares pages, if it is one of the group's
+    const uint64_t behind = __ballot(p.s.group >= 0) >> (a & 63);
+    if (p.g.seq == NO_SEQ) {
+        p.g.seq = behind ? a + __ffsll((unsigned long long)behind) - 1 : z;
+        if (p.g.seq >= z)
+            p.g.n = p.g.blocks = p.g.tiles = 0;
     }
-    if (p.g.seq == NO_SEQ)
-        p.g.n = p.g.blocks = p.g.tiles = 0;
     // (small batches' sums are under 2^30)
     const int work_p = __builtin_amdgcn_readlane(wave_scan_incl(p.g.blocks * p.g.tiles * H), 63);
     const int work_s = __builtin_amdgcn_readlane(wave_scan_incl(p.s.blocks * p.s.tiles * H), 63);
