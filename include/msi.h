@@ -713,7 +713,7 @@ msi_status msi_debug_set_device_gen(msi_plan *plan, uint32_t layer, uint32_t slo
  * features of a workgroup, workgroups that share a CU).  Errors: MSI_E_INVALID_ARG. */
 msi_status msi_debug_linear_tile(uint32_t M, uint32_t N, uint32_t *rows, uint32_t *features, uint32_t *per_cu);
 
-/* The same of msi_linear_q4; rows 0: the kernel of up to 16 rows. */
+/* The same of msi_linear_q4; rows 0: the kernel of up to 32 rows. */
 msi_status msi_debug_linear_q4_tile(uint32_t M, uint32_t N, uint32_t K, uint32_t *rows, uint32_t *features, uint32_t *per_cu);
 
 /* Expert-path selector of a forward, for tests: tokens-per-expert at or below

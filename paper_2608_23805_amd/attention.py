@@ -155,7 +155,8 @@ def linear_q4(x, w, scales, out, bias=None, act: str = "none", residual=None, st
     """out = act(x W^T + bias) + residual with 4-bit weights W[n, k] = scales[n, k / group] * q[n, k] (msi_linear_q4).
 
     w [N, K / 2] uint8: the codes q = -8 .. 7, element 2j in the low nibble of byte j; scales [N, K / group] float16 (or
-    its bits in int16), group 32, 64 or 128; the others as ``linear``'s."""
+    its bits in int16), group 32, 64 or 128; the others as ``linear``'s.  It takes less time than ``linear`` up to some 256
+    rows (half of it for single tokens), more from 512 on."""
     dev, xshape, sshape = x.device, x.shape, scales.shape
     if len(xshape) != 2 or len(sshape) != 2 or w.dim() != 2:
         _refuse("x, w and scales must be matrices")
@@ -517,10 +518,10 @@ class AttentionBlock:
     4-bit weights as ``linear_q4`` takes them; bias float32 or None.  With ``rotary`` (KvRotary) queries and keys turn by the
     ``positions`` of the step's rows on their way into the cache.  With ``groups`` (KvGroups) the step's sequences share their
     first pages.  ``step`` runs it whole; ``project`` and ``attend`` are its halves, for a model that normalises (or rotates
-    in another way) queries and keys between them.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the attention's workspace, unless one is handed
-    in.  Steps allocate nothing and can be captured; those of one block share its buffers, so they must not overlap.  Rows
-    below n_rows that no sequence brings, and those of a sequence that breaks a bound or has more rows than tokens, get
-    nothing added to h."""
+    in another way) queries and keys between them.  Holds the buffers for up to max_rows rows and, from ``reserve`` on, the
+    attention's workspace, unless one is handed in.  Steps allocate nothing and can be captured; those of one block share its
+    buffers, so they must not overlap.  Rows below n_rows that no sequence brings, and those of a sequence that breaks a
+    bound or has more rows than tokens, get nothing added to h."""
 
     def __init__(self, wqkv, wo, cache: KvCache, n_q_heads: int, max_rows: int, bias=None, scale: Optional[float] = None,
                  rotary: Optional[KvRotary] = None):

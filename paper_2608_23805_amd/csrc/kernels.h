@@ -317,7 +317,7 @@ struct LinearQ4Args {
     int group;                   // 32, 64 or 128, K a multiple
 };
 hipError_t launch_linear_q4(const LinearQ4Args &A, int act, hipStream_t st);
-LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K);   // likewise; rows 0: the kernel of up to 16 rows
+LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K);   // likewise; rows 0: the kernel of up to 32 rows
 
 // ---- paged 8-bit cache of keys and values (kv_cache.hip); strides in elements, fmt KV_E4M3 or KV_INT8
 hipError_t launch_kv_append(const KvCache &c, int fmt, const KvSeqs &s, const uint16_t *k, const uint16_t *v,

@@ -866,9 +866,13 @@ __global__ void __launch_bounds__(256, D * RT >= 512 ? 1 : 2) kv_few_rows_kernel
 // everything in the vector registers, where the rescaling needs the outputs (in
 // the accumulation registers every block would move all of them there and back:
 // 753 us for 640).  4096 rows on top of 4096 tokens, two sequences, 16 query heads
-// of 256: 890 us, 926 TFLOP/s; 32 of 128: 795 us, 1038 TFLOP/s.  The conversions
-// bound it: with heads of 256 and eight wavefronts of 16 rows, two a SIMD, every
-// wavefront converts the whole block, 928 us for 890.
+// of 256: 890 us, 926 TFLOP/s; 32 of 128: 795 us, 1038 TFLOP/s.  Neither unit is
+// full: a block's conversions, products and exponentials follow one another in a
+// wavefront, and one (heads of 256) or two a SIMD overlap little of them (2048 rows
+// of 8 sequences on 16384 shared tokens, heads of 128: vector unit 52 % of the time,
+// matrix cores 34 %; 240 rows, heads of 256: 26 and 18).  More wavefronts convert
+// more: with heads of 256 and eight of 16 rows, two a SIMD, every wavefront converts
+// the whole block, 928 us for 890.
 //
 // int8 codes take the vector unit twice as long as e4m3 to convert.  The four
 // wavefronts convert a quarter of a block each and leave it in LDS as the fragments

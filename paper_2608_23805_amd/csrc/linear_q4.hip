@@ -29,7 +29,8 @@ namespace {
 // another row than its neighbour, cost four times the L1's cycles: 16 rows, K 4096,
 // N 2048 7.9 us for 5.9.)  A lane's outputs are four rows of one feature, so it
 // applies that feature's scales.  Weights from HBM, one row: 2048 x 5120 5.0 us,
-// 4096 x 8199 8.9 us (1.9 TB/s), 8192 x 8192 11.5 us (3.0 TB/s).
+// 4096 x 8199 8.9 us (1.9 TB/s), 8192 x 8192 11.5 us (3.0 TB/s), whose wavefronts
+// wait for 60 % of their cycles and issue in 20 %: the chunks' chains.
 constexpr int ROWS_WAVES = 8, CHUNK = 8;      // blocks of 32 elements in a chunk
 
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
@@ -245,9 +246,10 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES, R * MB == 1 ? 4 : 2) q4_rows_
 // so that a lane reads its four features' at once.
 //
 // Up to a few hundred rows a stage is one chain of LDS reads, conversion, MFMAs
-// and scaling with little beside it, 0.6 to 1 us; large calls are bound by the
-// vector unit, whose conversions and scaling take as long as the MFMAs: 2000 x
-// 8192 of K 2048 85 us, 790 TFLOP/s.
+// and scaling with little beside it, 0.6 to 1 us.  In large calls a block's
+// conversion, MFMAs and scaling follow one another as well, in two wavefronts a
+// SIMD, and overlap little: the vector unit is busy for 50 % of the time, the matrix
+// cores for 27 % (2000 x 8192 of K 2048 85 us, 790 TFLOP/s).
 template <int BM_, int TN_, int WR_, int WC_, int KG_, int NBUF_, int WPC_>
 struct Q4Shape {
     static constexpr int BM = BM_, TN = TN_, WR = WR_, WC = WC_, KG = KG_, NBUF = NBUF_, WPC = WPC_;
@@ -513,7 +515,10 @@ hipError_t launch_act(const LinearQ4Args &A, const LinearTile &t, hipStream_t st
 // rows, 4096, 8199 10.0 and 10.5; 16 rows, 4096, 2048 5.8 and 7.5; 4096, 5120 9.0 and
 // 7.8; 8192, 8192 16.1 and 14.0].  Up to 32 rows likewise, while that makes no more than
 // 256 workgroups [20, 8192, 2048 11.3 for 16.9 in tiles; 24, 4096, 2048 7.3 for 8.5; 32,
-// 4096, 5120 9.9 for 11.7; 32, 2048, 16384 13.7 for 11.1].  Above, the smallest
+// 4096, 5120 9.9 for 11.7; 32, 2048, 16384 13.7 for 11.1].  Past 2^22 features tiles take
+// over for few rows, too: up to there a long K is better off without them, a short one with
+// them [1 row, N 2^22 and 64 more, K 2048 1376 and 1495, K 256 921 and 333; 16 rows 1261
+// and 1534, 1013 and 362; 131072, K 4096 78, 3.7 TB/s].  Above, the smallest
 // tiles that give one to every CU at most, since one wave of workgroups lasts as
 // long as a tile does, and that is the latency of its stages.  [16 x 32, 32 x 32,
 // 32 x 64, 64 x 64, 64 x 128, 128 x 128: 61 rows, K 4096, N 2048 8.8 / 10.3 / 14.3 /
@@ -534,7 +539,7 @@ LinearTile linear_q4_tile(int64_t M, int64_t N, int64_t K)
 {
     constexpr int64_t CUS = 256;
     auto tiles = [&](int64_t m, int64_t n) { return (M + m - 1) / m * ((N + n - 1) / n); };
-    if (M <= 16 && N <= 1 << 22)              // (a grid holds under 2^32 threads)
+    if (M <= 16 && N <= 1 << 22)
         return LinearTile{0, tiles(16, 16) > CUS && M > 8 ? 32 : 16, 1};
     if (M <= 32 && tiles(32, 32) <= CUS)
         return LinearTile{0, tiles(32, 16) > CUS ? 32 : 16, 1};
